@@ -15,7 +15,7 @@ own = False
 
 D = 128
 DEV = "cuda"
-SCALE = 1.0 / math.sqrt(D)
+SCALE = float(np.float32(1.0 / math.sqrt(D)))  # as a call's 32-bit argument has it
 
 # Four-bit pages.  A row of 128 elements is 64 bytes of codes (two per byte, the even element in the low half) and four
 # scale bytes, one per 32 elements: value = level(code) * 2^(scale - 127).  Where the bytes of a row sit:
@@ -220,7 +220,9 @@ def prepare(case, seed):
                   c_pages=c, clog_pages=torch.log(deg.sum(2).float()),
                   selected=torch.full((len(lens), H, case["select"]), -7, dtype=torch.int32, device=DEV))
     q = torch.randn((len(lens), H * case["group"], D), generator=g, device=DEV, dtype=torch.bfloat16)
-    st.update(q=q, out=torch.zeros_like(q), workspace=torch.empty(64 << 20, dtype=torch.uint8, device=DEV))
+    st.update(q=q, out=torch.zeros_like(q))
+    if kind == "quantized":
+        st["workspace"] = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
     return st
 
 
@@ -313,10 +315,9 @@ def _run_sparse(st):
     page, H, G = case["page"], case["heads"], case["group"]
     if own:
         from paper_2506_11418_b200 import binding as b
-        b.pages_select(st["views"], st["c_pages"], st["clog_pages"], page, G, st["q"], SCALE, st["longest"], st["selected"], st["workspace"],
-                       case["first"], case["last"])
-        b.decode_attn_selected(st["views"], st["k_pages"], st["v_pages"], st["logdeg_pages"], st["selected"], H, G, st["q"], st["out"], SCALE,
-                               st["workspace"])
+        b.pages_select(st["views"], st["c_pages"], st["clog_pages"], page, G, st["q"], SCALE, st["longest"], st["selected"], case["first"],
+                       case["last"])
+        b.decode_attn_selected(st["views"], st["k_pages"], st["v_pages"], st["logdeg_pages"], st["selected"], H, G, st["q"], st["out"], SCALE)
         return dict(selected=st["selected"], out=st["out"])
     lens, q = st["lens"], st["q"].view(-1, H, G, D)
     n = (lens + page - 1) // page
