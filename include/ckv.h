@@ -246,6 +246,126 @@ int ckv_compress_paged(const ckv_page_pool* pools, int32_t L, int32_t H, int32_t
                        int64_t scratch_pages, const ckv_params* params, void* workspace, size_t workspace_bytes,
                        void* cuda_stream, int64_t* out_len, int32_t* result_in_scratch);
 
+/* ---- Block tables and slot maps on the GPU ---------------------------------------------------------------------------
+ * A serving engine's step turns a batch's lengths into pages: sequences that grow take pages from a free list, sequences
+ * that were compressed or have finished give theirs back, and every new token gets the slot that its keys and values
+ * go to.  ckv_pages_resize does this in one launch from lengths that live on the device, without the host knowing them, so
+ * it can be captured into a graph.
+ *
+ * lens, new_lens [Bz]: tokens of every sequence before and after the step.  block_tables [Bz, table_stride]: row b holds
+ * sequence b's pages, of which the first ceil(lens[b] / page_tokens) are valid on entry.  ring [n_pages]: a queue of free
+ * pages, `count` of them from position `head`, wrapping; ring_state [2] = head, count.  With have = ceil(lens[b] /
+ * page_tokens) and want = ceil(new_lens[b] / page_tokens) the call
+ *  - appends the pages have > i >= want of every shrinking sequence to the back of the queue, sequences in order, pages in
+ *    order (rows are not cleared: entries behind a sequence's last page stay as they are);
+ *  - writes pages from the front of the queue, pages given in the same call last, to entries have <= i < want of every
+ *    growing sequence's row, in the same order;
+ *  - lists the slots page * page_tokens + offset of the new tokens (positions lens[b] .. new_lens[b] - 1 of every sequence,
+ *    sequences in order) in slots [n_slots], -1 behind the last; slot_begin [Bz + 1] says where each sequence's start;
+ *  - writes new_lens to lens_out [Bz], the queue's new head and count to ring_state_out [2], and, if views_dev is not NULL,
+ *    the views [Bz] that the attention and clustering calls take (row of the table, new length);
+ *  - sets *status (device) to 0.
+ * If the step cannot be done, *status says why (ckv_resize_status), tables and ring are untouched, lens_out, ring_state_out
+ * and the views repeat the state before the call, and every slot is -1, so that writes through the map do nothing.
+ * lens_out must not overlap lens or new_lens, nor ring_state_out ring_state; because of that, and because rows and queue only
+ * change where nothing is valid, repeating a call with the same lengths and ring_state repeats its results.
+ * Every page belongs to one sequence or to the queue.  Bz <= 8192. */
+typedef enum {
+  CKV_RESIZE_OK = 0,
+  CKV_RESIZE_NO_PAGES = 1,     /* the queue and the pages given in this call are fewer than the pages to be taken */
+  CKV_RESIZE_TABLE_FULL = 2,   /* some new length needs more than table_stride pages */
+  CKV_RESIZE_SLOTS_FULL = 3,   /* more new tokens than n_slots */
+  CKV_RESIZE_INCONSISTENT = 4  /* a negative length, a length that its row cannot hold, or a queue outside its ring */
+} ckv_resize_status;
+
+int ckv_pages_resize(const int64_t* lens, const int64_t* new_lens, int32_t Bz, int32_t page_tokens, int32_t* block_tables, int64_t table_stride,
+                     int32_t* ring, int64_t n_pages, const int64_t* ring_state, int64_t* slots, int64_t n_slots, int64_t* slot_begin,
+                     int64_t* lens_out, int64_t* ring_state_out, int32_t* status, ckv_paged_view* views_dev, void* cuda_stream);
+
+/* n tokens' keys, values and degrees on their way into pages.  Element d of token i and head h is at
+ * k[i * token_stride + h * head_stride + d] (elements; v alike), so a step's [n, H, D], slices of a fused projection and a
+ * slab [H, cap, D] all fit.  Rows must be 16-byte aligned: k, v, and both strides in bytes. */
+typedef struct ckv_token_rows {
+  const void* k;
+  const void* v;
+  const int32_t* deg; /* deg[i * deg_token_stride + h * deg_head_stride], or NULL: all ones */
+  int64_t token_stride, head_stride, deg_token_stride, deg_head_stride;
+  int32_t H, D, dtype;
+} ckv_token_rows;
+
+/* Writes token i to slot slots[i] (device, as ckv_pages_resize lists them) of one layer's pool [n_pages, H, page_tokens, D]
+ * in the rows' type, its degree to deg_pages and the degree's logarithm to logdeg_pages (either may be NULL).  Slots below 0
+ * or past the pool are skipped.  A slot must not be listed twice (the row would be a mixture of both tokens). */
+int ckv_pages_write(const ckv_token_rows* rows, const int64_t* slots, int64_t n, void* k_pages, void* v_pages, int32_t* deg_pages,
+                    float* logdeg_pages, int64_t n_pages, int32_t page_tokens, void* cuda_stream);
+
+/* ---- Attention over selected pages -----------------------------------------------------------------------------------
+ * For a long cache each query reads only the pages that matter to it.  A page is summarised as one cluster in the sense of
+ * Eq. 5: its degree-weighted mean key and its tokens' degrees summed; log N + q c * scale is then, by Jensen's inequality, a
+ * lower bound of the logarithm of the page's share of Eq. 3's denominator.
+ *
+ * ckv_pages_summarize: for the blocks of every sequence from the one that holds token from_lens[b] on (from_lens NULL: from
+ * the first; a step that appended tokens passes the lengths before it), c_pages [n_pages, H, D] (bf16) = sum n_t k_t / sum n_t
+ * and clog_pages [n_pages, H] (fp32) = log(sum n_t) over the block's tokens that the sequence holds.  deg_pages NULL = all
+ * ones.  max_blocks (host): an upper bound on the blocks that any sequence has from there on; blocks past it are not
+ * summarised.  bf16 pages. */
+int ckv_pages_summarize(const ckv_paged_view* views_dev, const int64_t* from_lens, int32_t Bz, const void* k_pages, const int32_t* deg_pages,
+                        int32_t page_tokens, int32_t H, int32_t D, int32_t dtype, int64_t max_blocks, void* c_pages, float* clog_pages,
+                        void* cuda_stream);
+
+/* For every sequence and KV head the n_select blocks with the largest score
+ *   max over the G query heads of (q c * scale) + clog,
+ * computed in 64 bits, equal scores in the order of the blocks, NaN last; the first n_first and the last n_last blocks are
+ * always chosen (n_first + n_last <= n_select).  selected [Bz, H, n_select]: block numbers in ascending order, -1 behind the
+ * last when the sequence has fewer.  q: [Bz, H*G, D]; clog_pages NULL = zeros.  max_len (host): an upper bound on every
+ * views_dev[b].len, at most 24576 pages (CKV_ERR_UNSUPPORTED above); blocks past it are not considered. */
+int ckv_pages_select(const ckv_paged_view* views_dev, const void* c_pages, const float* clog_pages, int32_t page_tokens, int32_t Bz, int32_t H,
+                     int32_t G, int32_t D, int32_t dtype, const void* q, float scale, int64_t max_len, int32_t n_first, int32_t n_last,
+                     int32_t n_select, int32_t* selected, void* cuda_stream);
+
+/* Eq. 3 over the listed blocks only: as ckv_decode_attn_paged, for each (sequence, KV head) over the tokens of the blocks
+ * selected[b, h, :] (device, [Bz, H, n_select]).  Entries below 0 or past the sequence's last block hold no tokens; a block
+ * that is listed twice counts twice; a list without tokens gives zeros.  One launch, no workspace. */
+int ckv_decode_attn_selected(const ckv_paged_view* views_dev, const void* k_pages, const void* v_pages, const float* logdeg_pages,
+                             int32_t page_tokens, const int32_t* selected, int32_t n_select, int32_t Bz, int32_t H, int32_t G, int32_t D,
+                             int32_t dtype, const void* q, void* out, float scale, void* cuda_stream);
+
+/* ---- Four-bit pages --------------------------------------------------------------------------------------------------
+ * Keys and values as four-bit floating point (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) in groups of 32 elements
+ * of a row that share a power of two, one byte e8m0 per group (value = level * 2^(byte - 127), 255 = NaN): the MXFP4 format of
+ * the OCP microscaling specification.  140 bytes per token and head with the log-degree, 516 in bf16.
+ * One layer's pool: codes [n_pages, H, page_tokens, 64], scales [n_pages, H, page_tokens, 4] (byte j: elements 32 j .. 32 j + 31).
+ * Two elements per byte, the even one in the low half; a row's bytes are in the order of the lanes that multiply them:
+ *   keys    byte 16 t + 4 j + i holds elements 32 j + 8 t + 2 i and + 1   (t, j, i < 4)
+ *   values  byte  8 g + 2 j + i holds elements 32 j + 4 g + 2 i and + 1   (g < 8, j < 4, i < 2) */
+typedef struct ckv_quant_pool {
+  uint8_t* k_codes;    /* 16-byte aligned, as the next three */
+  uint8_t* v_codes;
+  uint8_t* k_scales;
+  uint8_t* v_scales;
+  int32_t* deg_pages;  /* [n_pages, H, page_tokens]; NULL = all ones */
+  float* logdeg_pages; /* [n_pages, H, page_tokens]; NULL = all degrees one */
+} ckv_quant_pool;
+
+/* As ckv_pages_write, into four-bit pages.  A group's power of two is 2^(floor(log2 of its largest magnitude) - 2), no less
+ * than 2^-127; elements round to the nearest code, ties to the even one, and end at 6 times the power of two.  A group with an
+ * infinity or a NaN becomes NaN.  Rows: bf16 or fp32. */
+int ckv_pages_quantize(const ckv_token_rows* rows, const int64_t* slots, int64_t n, const ckv_quant_pool* pool, int64_t n_pages, int32_t page_tokens,
+                       void* cuda_stream);
+
+/* As ckv_pages_gather, from four-bit pages: the values that the codes stand for, exactly, as a slab k, v [H, cap, D] of `dtype`
+ * (to run ckv_compress_* on it), with deg and logdeg [H, cap] (either may be NULL; all ones where the pool has no degrees). */
+int ckv_pages_dequantize(const int32_t* block_table, int64_t len, const ckv_quant_pool* pool, int32_t page_tokens, int32_t H, int32_t D,
+                         int32_t dtype, void* k, void* v, int32_t* deg, float* logdeg, int64_t cap, void* cuda_stream);
+
+/* Host-only: workspace bytes of ckv_decode_attn_quantized (split partials). */
+size_t ckv_decode_quantized_workspace_bytes(int32_t Bz, int32_t H, int32_t G, int32_t D, int64_t max_len);
+
+/* Eq. 3 over four-bit pages: as ckv_decode_attn_paged with the keys and values that the codes stand for.  q, out: bf16. */
+int ckv_decode_attn_quantized(const ckv_paged_view* views_dev, const ckv_quant_pool* pool, int32_t page_tokens, int32_t Bz, int32_t H, int32_t G,
+                              int32_t D, int32_t dtype, const void* q, void* out, float scale, int64_t max_len, void* workspace,
+                              size_t workspace_bytes, void* cuda_stream);
+
 /* ckv_decode_attn for callers that cannot hand over a workspace because they cannot allocate device
  * memory at the point of the call: code running inside a serving engine's steady-state loop whose memory
  * pool is frozen after start-up, a plug-in that is given only its input and output tensors, or a host

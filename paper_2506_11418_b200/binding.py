@@ -22,7 +22,11 @@ EXPORTS = ["ckv_compress_plan", "ckv_workspace_bytes", "ckv_compress_prefill", "
            "ckv_decode_workspace_bytes", "ckv_decode_attn", "ckv_status_string", "ckv_workspace_status",
            "ckv_decode_attn_static", "ckv_compress_append_recluster", "ckv_decode_attn_paged", "ckv_pages_gather",
            "ckv_pages_scatter", "ckv_pages_plan", "ckv_paged_workspace_bytes", "ckv_compress_paged",
-           "ckv_decode_append_attn_paged"]
+           "ckv_decode_append_attn_paged", "ckv_pages_resize", "ckv_pages_write", "ckv_pages_summarize", "ckv_pages_select",
+           "ckv_decode_attn_selected", "ckv_pages_quantize", "ckv_pages_dequantize", "ckv_decode_quantized_workspace_bytes",
+           "ckv_decode_attn_quantized"]
+
+RESIZE_OK, RESIZE_NO_PAGES, RESIZE_TABLE_FULL, RESIZE_SLOTS_FULL, RESIZE_INCONSISTENT = range(5)   # device status of pages_resize
 
 
 class CkvPagePool(C.Structure):
@@ -39,6 +43,17 @@ class CkvParams(C.Structure):
     _fields_ = [("chunk", C.c_int32), ("n_sink", C.c_int32), ("n_recent", C.c_int32), ("n_rounds_max", C.c_int32),
                 ("r_init", C.c_float), ("r_decay", C.c_float), ("r_min", C.c_float), ("select", C.c_int32),
                 ("budget", C.c_int64)]
+
+
+class CkvTokenRows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("deg", C.c_void_p),
+                ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("deg_token_stride", C.c_int64), ("deg_head_stride", C.c_int64),
+                ("H", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32)]
+
+
+class CkvQuantPool(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("deg_pages", C.c_void_p), ("logdeg_pages", C.c_void_p)]
 
 
 class CkvLayerView(C.Structure):
@@ -103,6 +118,20 @@ def _load():
     lib.ckv_decode_attn_static.restype = C.c_int
     lib.ckv_decode_attn_static.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                            C.c_void_p, C.c_float, C.c_int64, C.c_void_p]
+    p, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+    for name, args in {
+            "ckv_pages_resize": [p, p, i32, i32, p, i64, p, i64, p, p, i64, p, p, p, p, p, p],
+            "ckv_pages_write": [p, p, i64, p, p, p, p, i64, i32, p],
+            "ckv_pages_summarize": [p, p, i32, p, p, i32, i32, i32, i32, i64, p, p, p],
+            "ckv_pages_select": [p, p, p, i32, i32, i32, i32, i32, i32, p, f32, i64, i32, i32, i32, p, p],
+            "ckv_decode_attn_selected": [p, p, p, p, i32, p, i32, i32, i32, i32, i32, i32, p, p, f32, p],
+            "ckv_pages_quantize": [p, p, i64, p, i64, i32, p],
+            "ckv_pages_dequantize": [p, i64, p, i32, i32, i32, i32, p, p, p, p, i64, p],
+            "ckv_decode_attn_quantized": [p, p, i32, i32, i32, i32, i32, i32, p, p, f32, i64, p, C.c_size_t, p]}.items():
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = args
+    lib.ckv_decode_quantized_workspace_bytes.restype = C.c_size_t
+    lib.ckv_decode_quantized_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
     return lib
 
 
@@ -387,3 +416,159 @@ def pages_scatter(block_table, length, k, v, deg, k_pages, v_pages, deg_pages, l
                                  dtype_code(k_pages.dtype), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(deg_pages),
                                  _ptr(logdeg_pages), _stream_ptr()))
 
+
+
+# ---- block tables and slot maps, attention over selected pages, four-bit pages
+
+def _stream_for(t: torch.Tensor):
+    """The current stream, for tensors on the current device (the library launches there; another device's are refused)."""
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return _stream_ptr()
+
+
+def _is(t: torch.Tensor, dtype: torch.dtype, *shape) -> bool:
+    return t.dtype == dtype and t.is_contiguous() and (not shape or t.shape == shape)
+
+
+def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_tables: torch.Tensor, ring: torch.Tensor, ring_state: torch.Tensor,
+                 slots: torch.Tensor, slot_begin: torch.Tensor, lens_out: torch.Tensor, ring_state_out: torch.Tensor, status: torch.Tensor,
+                 page_tokens: int, views: torch.Tensor | None = None):
+    """ckv_pages_resize on the current stream: one step of a batch's block tables, free list, slot map and views, from lengths
+    on the device.  lens, new_lens, lens_out int64 [Bz]; block_tables int32 [Bz, row]; ring int32 [n_pages]; ring_state,
+    ring_state_out int64 [2] (head, count); slots int64 [n]; slot_begin int64 [Bz + 1]; status int32 [1] (RESIZE_*);
+    views int64 [Bz, 2] (paged_views' layout)."""
+    Bz, row = block_tables.shape
+    i64, i32 = torch.int64, torch.int32
+    assert _is(lens, i64, Bz) and _is(new_lens, i64, Bz) and _is(lens_out, i64, Bz) and _is(slot_begin, i64, Bz + 1) and _is(slots, i64)
+    assert _is(ring_state, i64, 2) and _is(ring_state_out, i64, 2) and _is(ring, i32) and _is(status, i32) and block_tables.dtype == i32
+    assert block_tables.stride(1) == 1 and block_tables.stride(0) >= row and (views is None or _is(views, i64, Bz, 2))
+    assert block_tables.stride(0) == row or Bz == 1, "rows of the block tables follow one another"
+    _check(lib.ckv_pages_resize(lens.data_ptr(), new_lens.data_ptr(), Bz, page_tokens, block_tables.data_ptr(), row, ring.data_ptr(),
+                                ring.numel(), ring_state.data_ptr(), slots.data_ptr(), slots.numel(), slot_begin.data_ptr(),
+                                lens_out.data_ptr(), ring_state_out.data_ptr(), status.data_ptr(), _ptr(views), _stream_for(lens)))
+
+
+def _token_rows(k: torch.Tensor, v: torch.Tensor, deg: torch.Tensor | None) -> CkvTokenRows:
+    """k, v [n, H, D] with any strides but contiguous rows (a slab [H, cap, D] is passed transposed); deg int32 [n, H]."""
+    n, H, D = k.shape
+    ts, hs, one = k.stride()
+    assert k.dtype == v.dtype and v.shape == k.shape and v.stride() == (ts, hs, one) and one == 1
+    assert deg is None or (deg.dtype == torch.int32 and deg.shape == (n, H))
+    dt, dh = deg.stride() if deg is not None else (0, 0)
+    return CkvTokenRows(k.data_ptr(), v.data_ptr(), _ptr(deg), ts, hs, dt, dh, H, D, dtype_code(k.dtype))
+
+
+def pages_write(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                deg_pages: torch.Tensor | None = None, logdeg_pages: torch.Tensor | None = None, deg: torch.Tensor | None = None):
+    """ckv_pages_write on the current stream: k, v [n, H, D] to the slots of one layer's pool, degrees with them."""
+    n_pages, H, P, D = k_pages.shape
+    rows = _token_rows(k, v, deg)
+    assert _is(slots, torch.int64, k.shape[0]) and k.shape[1:] == (H, D) and _is(k_pages, k.dtype) and _is(v_pages, k.dtype, n_pages, H, P, D)
+    assert deg_pages is None or _is(deg_pages, torch.int32, n_pages, H, P)
+    assert logdeg_pages is None or _is(logdeg_pages, torch.float32, n_pages, H, P)
+    _check(lib.ckv_pages_write(C.byref(rows), slots.data_ptr(), k.shape[0], k_pages.data_ptr(), v_pages.data_ptr(), _ptr(deg_pages),
+                               _ptr(logdeg_pages), n_pages, P, _stream_for(slots)))
+
+
+def pages_summarize(views: torch.Tensor, k_pages: torch.Tensor, deg_pages: torch.Tensor | None, c_pages: torch.Tensor, clog_pages: torch.Tensor,
+                    max_blocks: int, from_lens: torch.Tensor | None = None):
+    """ckv_pages_summarize on the current stream: mean keys c_pages [n_pages, H, D] and log-degrees clog_pages [n_pages, H] of
+    the batch's pages, from the one that holds token from_lens[b] on."""
+    n_pages, H, P, D = k_pages.shape
+    Bz = views.shape[0]
+    assert _is(views, torch.int64, Bz, 2) and _is(k_pages, k_pages.dtype) and _is(c_pages, k_pages.dtype, n_pages, H, D)
+    assert _is(clog_pages, torch.float32, n_pages, H) and (deg_pages is None or _is(deg_pages, torch.int32, n_pages, H, P))
+    assert from_lens is None or _is(from_lens, torch.int64, Bz)
+    _check(lib.ckv_pages_summarize(views.data_ptr(), _ptr(from_lens), Bz, k_pages.data_ptr(), _ptr(deg_pages), P, H, D, dtype_code(k_pages.dtype),
+                                   max_blocks, c_pages.data_ptr(), clog_pages.data_ptr(), _stream_for(views)))
+
+
+def pages_select(views: torch.Tensor, c_pages: torch.Tensor, clog_pages: torch.Tensor | None, page_tokens: int, G: int, q: torch.Tensor,
+                 scale: float, max_len: int, selected: torch.Tensor, n_first: int = 0, n_last: int = 0):
+    """ckv_pages_select on the current stream: the best blocks of every (sequence, KV head) into selected int32 [Bz, H, n_select]."""
+    n_pages, H, D = c_pages.shape
+    Bz = views.shape[0]
+    assert _is(views, torch.int64, Bz, 2) and _is(q, c_pages.dtype, Bz, H * G, D) and c_pages.is_contiguous()
+    assert _is(selected, torch.int32) and selected.shape[:2] == (Bz, H) and (clog_pages is None or _is(clog_pages, torch.float32, n_pages, H))
+    _check(lib.ckv_pages_select(views.data_ptr(), c_pages.data_ptr(), _ptr(clog_pages), page_tokens, Bz, H, G, D, dtype_code(q.dtype), q.data_ptr(),
+                                scale, max_len, n_first, n_last, selected.shape[2], selected.data_ptr(), _stream_for(views)))
+
+
+def decode_attn_selected(views: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, logdeg_pages: torch.Tensor | None,
+                         selected: torch.Tensor, H: int, G: int, q: torch.Tensor, out: torch.Tensor, scale: float):
+    """ckv_decode_attn_selected on the current stream: Eq. 3 over the blocks that selected [Bz, H, n_select] lists."""
+    Bz, HG, D = q.shape
+    n_pages, _, P, _ = k_pages.shape
+    assert HG == H * G and _is(q, k_pages.dtype) and _is(out, q.dtype, Bz, HG, D) and _is(views, torch.int64, Bz, 2)
+    assert _is(k_pages, q.dtype, n_pages, H, P, D) and _is(v_pages, q.dtype, n_pages, H, P, D)
+    assert _is(selected, torch.int32) and selected.shape[:2] == (Bz, H) and (logdeg_pages is None or _is(logdeg_pages, torch.float32, n_pages, H, P))
+    _check(lib.ckv_decode_attn_selected(views.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(logdeg_pages), P, selected.data_ptr(),
+                                        selected.shape[2], Bz, H, G, D, dtype_code(q.dtype), q.data_ptr(), out.data_ptr(), scale,
+                                        _stream_for(views)))
+
+
+@dataclass
+class QuantPool:
+    """One layer's four-bit pool: codes uint8 [n_pages, H, page_tokens, 64], scales uint8 [n_pages, H, page_tokens, 4], degrees
+    int32 and log-degrees fp32 [n_pages, H, page_tokens] (either may be None: all ones)."""
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_scales: torch.Tensor
+    deg_pages: torch.Tensor | None = None
+    logdeg_pages: torch.Tensor | None = None
+
+    def __post_init__(self):
+        n, H, P, _ = self.k_codes.shape
+        assert _is(self.k_codes, torch.uint8, n, H, P, 64) and _is(self.v_codes, torch.uint8, n, H, P, 64)
+        assert _is(self.k_scales, torch.uint8, n, H, P, 4) and _is(self.v_scales, torch.uint8, n, H, P, 4)
+        assert self.deg_pages is None or _is(self.deg_pages, torch.int32, n, H, P)
+        assert self.logdeg_pages is None or _is(self.logdeg_pages, torch.float32, n, H, P)
+
+    @classmethod
+    def empty(cls, n_pages: int, H: int, page_tokens: int, device="cuda"):
+        u8 = dict(dtype=torch.uint8, device=device)
+        return cls(torch.zeros((n_pages, H, page_tokens, 64), **u8), torch.zeros((n_pages, H, page_tokens, 64), **u8),
+                   torch.zeros((n_pages, H, page_tokens, 4), **u8), torch.zeros((n_pages, H, page_tokens, 4), **u8),
+                   torch.zeros((n_pages, H, page_tokens), dtype=torch.int32, device=device),
+                   torch.zeros((n_pages, H, page_tokens), dtype=torch.float32, device=device))
+
+    def c(self) -> CkvQuantPool:
+        return CkvQuantPool(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(), self.v_scales.data_ptr(),
+                            _ptr(self.deg_pages), _ptr(self.logdeg_pages))
+
+
+def pages_quantize(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pool: QuantPool, deg: torch.Tensor | None = None):
+    """ckv_pages_quantize on the current stream: k, v [n, H, D] (bf16 or fp32) to the slots of a four-bit pool."""
+    n_pages, H, P, _ = pool.k_codes.shape
+    rows, cp = _token_rows(k, v, deg), pool.c()
+    assert _is(slots, torch.int64, k.shape[0]) and k.shape[1] == H
+    _check(lib.ckv_pages_quantize(C.byref(rows), slots.data_ptr(), k.shape[0], C.byref(cp), n_pages, P, _stream_for(slots)))
+
+
+def pages_dequantize(block_table: torch.Tensor, length: int, pool: QuantPool, k: torch.Tensor, v: torch.Tensor,
+                     deg: torch.Tensor | None = None, logdeg: torch.Tensor | None = None):
+    """ckv_pages_dequantize on the current stream: one sequence's four-bit pages to a slab k, v [H, cap, D], deg, logdeg [H, cap]."""
+    _, H, P, _ = pool.k_codes.shape
+    cap, cp = k.shape[1], pool.c()
+    assert _is(block_table, torch.int32) and block_table.numel() * P >= length
+    assert _is(k, k.dtype) and k.shape[0] == H and _is(v, k.dtype, *k.shape)
+    assert (deg is None or _is(deg, torch.int32, H, cap)) and (logdeg is None or _is(logdeg, torch.float32, H, cap))
+    _check(lib.ckv_pages_dequantize(block_table.data_ptr(), length, C.byref(cp), P, H, k.shape[2], dtype_code(k.dtype), k.data_ptr(), v.data_ptr(),
+                                    _ptr(deg), _ptr(logdeg), cap, _stream_for(block_table)))
+
+
+def decode_quantized_workspace_bytes(Bz, H, G, D, max_len) -> int:
+    return lib.ckv_decode_quantized_workspace_bytes(Bz, H, G, D, max_len)
+
+
+def decode_attn_quantized(views: torch.Tensor, pool: QuantPool, H: int, G: int, q: torch.Tensor, out: torch.Tensor, scale: float, max_len: int,
+                          workspace: torch.Tensor):
+    """ckv_decode_attn_quantized on the current stream: Eq. 3 over four-bit pages; q, out bf16 [Bz, H*G, D]."""
+    Bz, HG, D = q.shape
+    cp = pool.c()
+    assert HG == H * G and pool.k_codes.shape[1] == H and _is(q, q.dtype) and _is(out, q.dtype, Bz, HG, D) and _is(views, torch.int64, Bz, 2)
+    _check(lib.ckv_decode_attn_quantized(views.data_ptr(), C.byref(cp), pool.k_codes.shape[2], Bz, H, G, D, dtype_code(q.dtype), q.data_ptr(),
+                                         out.data_ptr(), scale, max_len, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                         _stream_for(views)))

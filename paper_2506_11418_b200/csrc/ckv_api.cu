@@ -150,13 +150,6 @@ int check_cache_shape(const ckv_cache* c, bool with_len = true) {
   return CKV_OK;
 }
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-inline bool overlaps(const void* a, size_t an, const void* b, size_t bn) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return an && bn && x < y + bn && y < x + an;
-}
-
 struct Buf {  // one cache buffer a round reads or writes
   void* k;
   void* v;

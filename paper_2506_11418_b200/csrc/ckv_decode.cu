@@ -8,6 +8,7 @@
 
 #include "../../include/ckv.h"
 #include "ckv_common.cuh"
+#include "ckv_decode.cuh"
 #include "ckv_internal.h"
 #include "ckv_ptx.cuh"
 
@@ -19,7 +20,6 @@ constexpr int kDecThreads = 128;
 constexpr int kDecWarps = kDecThreads / 32;
 constexpr int kTile = 32;
 constexpr int kMaxG = 8;
-constexpr float kLog2e = 1.4426950408889634f;
 
 template <typename T, int D>
 struct DecodeSmem {
@@ -310,36 +310,18 @@ constexpr int kCWarps = 4;
 constexpr int kCStages = 3;
 constexpr size_t kCSmemBytes = (size_t)kCWarps * kCStages * (2 * kCT * 256 + kCT * 4);
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t src_bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, uint32_t src_bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 using ptx::ldsm_x4;
 using ptx::ldsm_x4_trans;
-
-__device__ __forceinline__ void cluster_sync_all() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// a float of the shared memory of CTA `rank` of this cluster, at the offset `local_addr` has in this CTA's window
-__device__ __forceinline__ float ld_cluster_f32(uint32_t local_addr, uint32_t rank) {
-  uint32_t ra;
-  float v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(local_addr), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(ra) : "memory");
-  return v;
-}
 
 // PAGED: the cache lives in fixed-size pages, [n_pages, H, page_tokens, D], and a per-sequence block table maps
 // logical block i (tokens i * page_tokens ...) to its page; page_tokens is a multiple of the tile, so a tile never
 // straddles pages.  Each lane keeps one entry of the table (32 blocks per refill), handed out by shuffle.
-template <bool PAGED, int CL, int TT, int NW, int ST>
+// SEL (paged, cluster form only): the sequence is the pages that the pair's list of blocks names, `a.n_sel` entries in any
+// order, -1 = none.  Block i of the loop is block sel[i] of the sequence; its tiles past the sequence's end are empty.
+template <bool PAGED, int CL, int TT, int NW, int ST, bool SEL = false>
 __global__ void __launch_bounds__(NW * 32, 1) decode_fast_kernel(const DecodeArgs a) {
+  static_assert(!SEL || (PAGED && CL > 0), "selected blocks are pages, combined in the cluster");
+  __shared__ int sel_nt[SEL ? NW * ST : 1];  // tokens of each staged tile that exist
   constexpr int D = 128;
   constexpr int kTileBytes = TT * 256;                  // one bf16 tile of K or V
   constexpr int kStageBytes = 2 * kTileBytes + TT * 4;  // K tile, V tile, log-degrees
@@ -364,10 +346,24 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_fast_kernel(const DecodeArg
   const int64_t new_pos = (PAGED && a.k_new) ? len - 1 : -1;
   const __nv_bfloat16* knew = PAGED ? reinterpret_cast<const __nv_bfloat16*>(a.k_new) + ((int64_t)b * a.H + h) * 128 : nullptr;
   const __nv_bfloat16* vnew = PAGED ? reinterpret_cast<const __nv_bfloat16*>(a.v_new) + ((int64_t)b * a.H + h) * 128 : nullptr;
+  const int32_t* sel = nullptr;
+  int64_t span = len;  // what the loop walks: the sequence, or its listed blocks end to end
+  int64_t held_blocks = 0;
+  if constexpr (SEL) {
+    sel = a.sel + ((int64_t)b * a.H + h) * a.n_sel;
+    held_blocks = (len + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift;
+    int n_listed = 0;
+    for (int base = 0; base < a.n_sel; base += 32) {
+      const int e = base + lane < a.n_sel ? sel[base + lane] : -1;
+      const uint32_t ok = __ballot_sync(0xffffffffu, e >= 0 && e < held_blocks);
+      if (ok) n_listed = base + 32 - __clz((int)ok);
+    }
+    span = (int64_t)n_listed << a.page_shift;
+  }
   // the sequence's own tiles are dealt evenly to the splits (a ragged batch stays balanced)
-  const int64_t seq_tiles = (len + TT - 1) / TT;
+  const int64_t seq_tiles = (span + TT - 1) / TT;
   const int64_t t_begin = TT * (seq_tiles * split / a.n_splits);
-  const int64_t t_end = min(len, TT * (seq_tiles * (split + 1) / a.n_splits));
+  const int64_t t_end = min(span, TT * (seq_tiles * (split + 1) / a.n_splits));
   const int ntiles = (int)((t_end - t_begin + TT - 1) / TT);
   const __nv_bfloat16* kbase = PAGED ? reinterpret_cast<const __nv_bfloat16*>(a.k_pages)
                                      : reinterpret_cast<const __nv_bfloat16*>(view.k) + (int64_t)h * view.cap * D;
@@ -375,9 +371,16 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_fast_kernel(const DecodeArg
                                      : reinterpret_cast<const __nv_bfloat16*>(view.v) + (int64_t)h * view.cap * D;
   const float* ldbase = PAGED ? a.logdeg_pages : (view.logdeg ? view.logdeg + (int64_t)h * view.cap : nullptr);
   // paged: block table entries [blk0, blk0 + 32) of this sequence, one per lane
-  const int64_t n_blocks = PAGED ? (len + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift : 0;
+  const int64_t n_blocks = PAGED ? (span + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift : 0;
   int64_t blk0 = PAGED ? t_begin >> a.page_shift : 0;
-  int my_page = (PAGED && ntiles > 0 && blk0 + lane < n_blocks) ? table[blk0 + lane] : 0;
+  int my_blk = -1;  // SEL: the listed block behind my_page
+  auto table_entry = [&](int64_t i) -> int {
+    if (!SEL) return i < n_blocks ? table[i] : 0;
+    const int e = i < n_blocks ? sel[i] : -1;
+    my_blk = e < held_blocks ? e : -1;
+    return my_blk >= 0 ? table[my_blk] : 0;
+  };
+  int my_page = (PAGED && ntiles > 0) ? table_entry(blk0 + lane) : 0;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem_raw) + (uint32_t)warp * ST * kStageBytes;
   const float* ring_ld = reinterpret_cast<const float*>(smem_raw + (size_t)warp * ST * kStageBytes);
 
@@ -399,20 +402,25 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_fast_kernel(const DecodeArg
     const uint32_t st = ring + (uint32_t)(tile % ST) * kStageBytes;
     const int c = lane & 15;
     // row0: where the tile's first token sits in the K / V / log-degree arrays; rows of a tile are contiguous
-    int64_t row0 = t0;
+    int64_t row0 = t0, left = t_end - t0;  // left: tokens from t0 on
     if (PAGED) {
       const int64_t blk = t0 >> a.page_shift;
       if (blk >= blk0 + 32) {  // next 32 entries of the table (tiles are issued in order)
         blk0 = blk;
-        my_page = blk0 + lane < n_blocks ? table[blk0 + lane] : 0;
+        my_page = table_entry(blk0 + lane);
       }
       const int page = __shfl_sync(0xffffffffu, my_page, (int)(blk - blk0));
       row0 = (((int64_t)page * a.H + h) << a.page_shift) + (t0 & (((int64_t)1 << a.page_shift) - 1));
+      if constexpr (SEL) {
+        const int listed = __shfl_sync(0xffffffffu, my_blk, (int)(blk - blk0));
+        left = listed < 0 ? 0 : len - ((int64_t)listed << a.page_shift) - (t0 & (((int64_t)1 << a.page_shift) - 1));
+        if (lane == 0) sel_nt[warp * ST + tile % ST] = (int)max((int64_t)0, min(left, (int64_t)TT));
+      }
     }
 #pragma unroll
     for (int i = 0; i < TT / 2; ++i) {
       const int r = (lane >> 4) + 2 * i;
-      const bool ok = t0 + r < t_end;
+      const bool ok = SEL ? r < left : t0 + r < t_end;
       const int64_t row = ok ? row0 + r : row0;  // clamped address, zero-filled when out of range
       const uint32_t off = (uint32_t)r * 256u + (uint32_t)((c ^ (r & 7)) << 4);
       const bool fresh = PAGED && t0 + r == new_pos;  // the appended token is read from where the caller put it
@@ -421,7 +429,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_fast_kernel(const DecodeArg
     }
     if (ldbase) {  // one log-degree per lane; 4-byte copies have no alignment demands on the slab
       // (the appended token has degree 1: its log-degree is the zero fill)
-      const bool ok = lane < TT && t0 + lane < t_end && t0 + lane != new_pos;
+      const bool ok = SEL ? lane < left : lane < TT && t0 + lane < t_end && t0 + lane != new_pos;
       if (TT == 32 || lane < TT) cp_async4(st + 2 * kTileBytes + lane * 4, ldbase + (ok ? row0 + lane : row0), ok ? 4u : 0u);
     }
   };
@@ -455,7 +463,7 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_fast_kernel(const DecodeArg
     const int stage = tile % ST;
     const uint32_t ks_ = ring + (uint32_t)stage * kStageBytes, vs_ = ks_ + kTileBytes;
     const float* lds = ring_ld + (size_t)stage * (kStageBytes / 4) + 2 * kTileBytes / 4;
-    const int nt = (int)min((int64_t)TT, t_end - (t_begin + (int64_t)tile * TT));
+    const int nt = SEL ? sel_nt[warp * ST + stage] : (int)min((int64_t)TT, t_end - (t_begin + (int64_t)tile * TT));
 
     // ---- S = Q K^T for 32 tokens: n tile j covers tokens 8j .. 8j+7
     constexpr int NT = TT / 8;  // n tiles of 8 tokens
@@ -490,9 +498,11 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_fast_kernel(const DecodeArg
     }
     tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, 1));
     tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, 2));
-    const float m_new = fmaxf(m_run, tmax);
+    float m_new = fmaxf(m_run, tmax);
+    const float m_all = m_new;
+    if (SEL && m_new == -INFINITY) m_new = 0.f;  // no token so far: every weight below is zero, not inf - inf
     const float corr = exp2f(m_run - m_new);
-    m_run = m_new;
+    m_run = SEL ? m_all : m_new;
     float psum = 0.f;
     uint32_t pb[NT];
 #pragma unroll
@@ -528,65 +538,21 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_fast_kernel(const DecodeArg
   l_run += __shfl_xor_sync(0xffffffffu, l_run, 1);
   l_run += __shfl_xor_sync(0xffffffffu, l_run, 2);
   if constexpr (CL > 0) {
-    // ND output columns per combining CTA (a divisor of 32); with 10 CTAs the first 8 combine 16 columns each
-    constexpr int P = D + 4, NP = NW * CL, ND = (D % CL == 0 && 32 % (D / CL) == 0) ? D / CL : 16, NPG = 32 / ND, PER = NP / NPG;
-    __syncthreads();  // every warp of the CTA is done with its ring: the partials take its place
-    float* part = reinterpret_cast<float*>(smem_raw);  // [warp][8 heads][P]
-    float* scl = part + NW * 8 * P;               // [warp][NP] weights 2^(m_p - m)
-    if (t == 0) {
-      part[(warp * 8 + g) * P + D] = m_run;
-      part[(warp * 8 + g) * P + D + 1] = l_run;
-    }
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float* dst = part + (warp * 8 + 2 * t + e) * P;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        dst[16 * i + g] = oacc[i][e];
-        dst[16 * i + 8 + g] = oacc[i][2 + e];
-      }
-    }
-    cluster_sync_all();
-    const uint32_t part_s = (uint32_t)__cvta_generic_to_shared(smem_raw);
-    const int d = lane % ND, pg = lane / ND, d0 = (int)blockIdx.x * ND;  // this CTA's columns d0 .. d0 + ND - 1
-    for (int head = warp; head < G && (int)blockIdx.x * ND < D; head += NW) {
-      constexpr int NK = (NP + 31) / 32;
-      static_assert(NP % NPG == 0, "the partials split evenly over the lane groups");
-      float mp[NK], lp[NK], mm = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < NK; ++k) {
-        const int pi = lane + 32 * k;  // partial of warp (pi % NW) of CTA (pi / NW)
-        const uint32_t addr = part_s + (uint32_t)((((pi % NW) * 8 + head) * P + D) * 4);
-        mp[k] = pi < NP ? ld_cluster_f32(addr, (uint32_t)(pi / NW)) : -INFINITY;
-        lp[k] = pi < NP ? ld_cluster_f32(addr + 4u, (uint32_t)(pi / NW)) : 0.f;
-        mm = fmaxf(mm, mp[k]);
-      }
-      mm = warp_max(mm);
-      float ll = 0.f;
-#pragma unroll
-      for (int k = 0; k < NK; ++k) {
-        const float f = mp[k] == -INFINITY ? 0.f : exp2f(mp[k] - mm);
-        if (lane + 32 * k < NP) scl[warp * NP + lane + 32 * k] = f;
-        ll = fmaf(f, lp[k], ll);
-      }
-      ll = warp_sum(ll);
-      __syncwarp();
-      float acc = 0.f;
-#pragma unroll 4
-      for (int j = 0; j < PER; ++j) {
-        const int pi = pg * PER + j;
-        acc = fmaf(scl[warp * NP + pi], ld_cluster_f32(part_s + (uint32_t)((((pi % NW) * 8 + head) * P + d0 + d) * 4), (uint32_t)(pi / NW)),
-                   acc);
+    cluster_combine<CL, NW>(smem_raw, warp, lane, G, reinterpret_cast<__nv_bfloat16*>(a.out) + ((int64_t)b * a.H + h) * G * D, [&](float* part) {
+      if (t == 0) {
+        part[g * kPartial + D] = m_run;
+        part[g * kPartial + D + 1] = l_run;
       }
 #pragma unroll
-      for (int sft = ND; sft < 32; sft <<= 1) acc += __shfl_xor_sync(0xffffffffu, acc, sft);
-      if (pg == 0) {
-        const float inv = ll > 0.f ? 1.f / ll : 0.f;
-        reinterpret_cast<__nv_bfloat16*>(a.out)[(((int64_t)b * a.H + h) * G + head) * D + d0 + d] = __float2bfloat16_rn(acc * inv);
+      for (int e = 0; e < 2; ++e) {
+        float* dst = part + (2 * t + e) * kPartial;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          dst[16 * i + g] = oacc[i][e];
+          dst[16 * i + 8 + g] = oacc[i][2 + e];
+        }
       }
-      __syncwarp();
-    }
-    cluster_sync_all();  // nobody leaves while its shared memory may still be read
+    });
     return;
   }
   float* pbase = a.partial + ((((int64_t)b * a.H + h) * G) * a.n_splits + split) * (D + 4);
@@ -609,10 +575,10 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_fast_kernel(const DecodeArg
   }
 }
 
-template <bool PAGED, int CL>
+template <bool PAGED, int CL, bool SEL = false>
 cudaError_t launch_decode_cluster(DecodeArgs a, cudaStream_t st) {
   // (the kernel's attributes were set by max_active_clusters, which every caller asks first)
-  auto kern = decode_fast_kernel<PAGED, CL, kCT, kCWarps, kCStages>;
+  auto kern = decode_fast_kernel<PAGED, CL, kCT, kCWarps, kCStages, SEL>;
   a.n_splits = kCWarps * CL;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(CL, (unsigned)a.H, (unsigned)a.Bz);
@@ -633,14 +599,14 @@ cudaError_t launch_decode_cluster(DecodeArgs a, cudaStream_t st) {
 
 // How many clusters of CL CTAs of the decode kernel the device can hold at once (0: this cluster size cannot be
 // scheduled here); asked once per device and kernel.
-template <bool PAGED, int CL>
+template <bool PAGED, int CL, bool SEL = false>
 int max_active_clusters() {
   constexpr int kMaxDev = 64;
   static int cached[kMaxDev];  // 0 = not asked yet, else the answer + 1
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDev) return 0;
   if (cached[dev] == 0) {
-    auto kern = decode_fast_kernel<PAGED, CL, kCT, kCWarps, kCStages>;
+    auto kern = decode_fast_kernel<PAGED, CL, kCT, kCWarps, kCStages, SEL>;
     int n = 0;
     bool ok = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kCSmemBytes) == cudaSuccess;
     if (ok && CL > 8) ok = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
@@ -689,8 +655,7 @@ cudaError_t launch_decode_fast(const DecodeArgs& a, cudaStream_t st) {
   }
   const dim3 grid((unsigned)((a.n_splits + kFWarps - 1) / kFWarps), (unsigned)a.H, (unsigned)a.Bz);
   if ((e = launch_dependent(decode_fast_kernel<PAGED, 0, kFT, kFWarps, kFStages>, grid, dim3(kFWarps * 32), kFSmemBytes, st, a)) != cudaSuccess) return e;
-  return launch_dependent(decode_combine_kernel<__nv_bfloat16, 128>, dim3((unsigned)(a.Bz * a.H * a.G)), dim3(kCombThreads), 0,
-                          st, a);
+  return launch_decode_combine(a, st);
 }
 
 }  // namespace
@@ -749,6 +714,22 @@ cudaError_t launch_decode(const DecodeArgs& a, int dtype, int D, cudaStream_t st
 }
 
 cudaError_t launch_decode_paged(const DecodeArgs& a, cudaStream_t st) { return launch_decode_fast<true>(a, st); }
+
+cudaError_t launch_decode_combine(const DecodeArgs& a, cudaStream_t st) {
+  return launch_dependent(decode_combine_kernel<__nv_bfloat16, 128>, dim3((unsigned)(a.Bz * a.H * a.G)), dim3(kCombThreads), 0, st, a);
+}
+
+cudaError_t launch_decode_selected(const DecodeArgs& a, cudaStream_t st) {
+  // The largest cluster of which all pairs are resident at once, while its warps have two tiles or more each; a larger
+  // batch takes one CTA per pair (its lists are alike in length, so the CTAs balance by themselves).
+  const int64_t pairs = (int64_t)a.Bz * a.H, tiles = a.max_len / kCT;
+  if (tiles >= 2 * 16 * kCWarps && max_active_clusters<true, 16, true>() >= pairs) return launch_decode_cluster<true, 16, true>(a, st);
+  if (tiles >= 2 * 8 * kCWarps && max_active_clusters<true, 8, true>() >= pairs) return launch_decode_cluster<true, 8, true>(a, st);
+  if (tiles >= 2 * 4 * kCWarps && max_active_clusters<true, 4, true>() >= pairs) return launch_decode_cluster<true, 4, true>(a, st);
+  if (tiles >= 2 * 2 * kCWarps && max_active_clusters<true, 2, true>() >= pairs) return launch_decode_cluster<true, 2, true>(a, st);
+  if (max_active_clusters<true, 1, true>() < 1) return cudaErrorInvalidConfiguration;
+  return launch_decode_cluster<true, 1, true>(a, st);
+}
 
 }  // namespace ckv
 

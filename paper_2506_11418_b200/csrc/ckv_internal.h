@@ -150,6 +150,9 @@ struct DecodeArgs {
   void* v_pages_w;
   int32_t* deg_pages_w;
   float* logdeg_pages_w;      // may be null
+  // paged, selected blocks: [Bz, H, n_sel] (max_len is then n_sel pages of tokens)
+  const int32_t* sel;
+  int32_t n_sel;
 };
 
 // Streaming multiprocessors of the current device, asked once per device (the grids are sized from it).
@@ -163,6 +166,13 @@ inline int sm_count() {
   if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 148;
   if (slot) cached[dev].store(n, std::memory_order_relaxed);
   return n;
+}
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+inline bool overlaps(const void* a, size_t an, const void* b, size_t bn) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return an && bn && x < y + bn && y < x + an;
 }
 
 // Launch with programmatic stream serialization: the kernel may become resident while the kernel ahead of it
@@ -202,6 +212,8 @@ cudaError_t launch_compose_assign(int32_t* total, const int32_t* step, int64_t n
                                   cudaStream_t st);
 cudaError_t launch_decode(const DecodeArgs& a, int dtype, int D, cudaStream_t st);
 cudaError_t launch_decode_paged(const DecodeArgs& a, cudaStream_t st);
+cudaError_t launch_decode_selected(const DecodeArgs& a, cudaStream_t st);
+cudaError_t launch_decode_combine(const DecodeArgs& a, cudaStream_t st);  // bf16: partials of a split launch -> out
 void decode_plan(int32_t Bz, int32_t H, int dtype, int64_t max_len, int64_t max_partial_floats, int32_t G, int32_t D,
                  int32_t* n_splits, int64_t* span);
 size_t decode_partial_floats(int32_t Bz, int32_t H, int32_t G, int32_t D, int64_t max_len);

@@ -119,8 +119,6 @@ int page_copy(bool to_pages, const PageCopyArgs& a, cudaStream_t st) {
   return cudaGetLastError() == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 }  // namespace
 
 cudaError_t launch_rows_copy(const RowsCopyArgs& a, const PagedArgs& pools, cudaStream_t st) {
@@ -221,6 +219,24 @@ int ckv_decode_append_attn_paged(const ckv_paged_view* views_dev, void* k_pages,
   a.k_new = k_new; a.v_new = v_new;
   a.k_pages_w = k_pages; a.v_pages_w = v_pages; a.deg_pages_w = deg_pages; a.logdeg_pages_w = logdeg_pages;
   return launch_decode_paged(a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
+}
+
+int ckv_decode_attn_selected(const ckv_paged_view* views_dev, const void* k_pages, const void* v_pages, const float* logdeg_pages,
+                             int32_t page_tokens, const int32_t* selected, int32_t n_select, int32_t Bz, int32_t H, int32_t G, int32_t D,
+                             int32_t dtype, const void* q, void* out, float scale, void* cuda_stream) {
+  if (!views_dev || !k_pages || !v_pages || !selected || !q || !out || n_select <= 0 || Bz <= 0 || H <= 0 || G <= 0) return CKV_ERR_INVALID_ARG;
+  if (dtype != CKV_F32 && dtype != CKV_BF16) return CKV_ERR_INVALID_ARG;
+  const int shift = page_shift_of(page_tokens);
+  if (dtype != CKV_BF16 || shift < 0 || D != 128 || G > 8 || H > 65535 || Bz > 65535) return CKV_ERR_UNSUPPORTED;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(k_pages) || !aligned16(v_pages)) return CKV_ERR_ALIGNMENT;
+  DecodeArgs a{};
+  a.views = views_dev; a.q = q; a.out = out;
+  a.Bz = Bz; a.H = H; a.G = G;
+  a.max_len = (int64_t)n_select << shift;
+  a.scale = scale;
+  a.k_pages = k_pages; a.v_pages = v_pages; a.logdeg_pages = logdeg_pages; a.page_shift = shift;
+  a.sel = selected; a.n_sel = n_select;
+  return launch_decode_selected(a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
 }  // extern "C"
