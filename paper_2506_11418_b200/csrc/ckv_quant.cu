@@ -182,26 +182,35 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
 // As the bf16 kernel: every warp walks its own span of a sequence in tiles of 32 tokens through a ring of cp.async copies,
 // scores and outputs on mma.sync (fp16 inputs: e2m1 levels are exact in fp16, and so are the query's elements after the
 // row is scaled by a power of two), softmax online in the exp2 domain, and partials that are joined in the cluster or by
-// the combine kernel.  With four bits per element the tensor cores and the copies are no longer what counts: unpacking
-// and scaling are, so both are arranged to cost as little as they can:
+// a second kernel.  With four bits per element the issue slots are what counts (a tile's 4480 bytes take 192 cycles of an
+// SM's share of the measured bandwidth), so unpacking and scaling are arranged to cost as few instructions as they can:
 //   S   a group's 32 elements are two k steps of the product; their sum is multiplied by the token's scale of that group
-//       (one FFMA per token, head and group in place of 32 products with the scale)
+//       (one multiply-add per token, head and group in place of 32 products with the scale), two tokens per instruction
 //   O   V's scale belongs to a token and a group, as the weight p belongs to a token: the weight of token t in group j is
-//       p_t 2^e_tj, one B operand per group.  It goes to fp16 relative to the largest one so far (a running power of two
-//       per head and group, with its own rescaling of the accumulators), so that whatever the scales are the tokens that
-//       matter keep 11 bits and only weights below 2^-28 of the largest lose any.
+//       p_t 2^e_tj, one B operand per group.  It goes to fp16 times a power of two F that is the head's and the group's own
+//       and follows the largest such weight so far, so that whatever the scales are the tokens that matter keep 11 bits:
+//       weights from 2^-21 of the largest on, and below that 2^-32 of the largest.
+//   m   the softmax's reference and F move only when a tile needs it (an exponent above 6, a weight that would pass 2^15):
+//       after a sequence's first tiles that is rare, and the accumulators are left alone.
+//   e   the lanes of a head read the same scales: each tile's 256 are converted once, one token per lane, and read back
+//       as fp32 pairs of neighbouring tokens
 //   V   two tokens' codes are interleaved by nibble before they are unpacked, which gives the operand's pairs of
 //       neighbouring tokens without permuting fp16 values.
 constexpr int kQT = 32;  // tokens per tile
 constexpr int kQWarps = 4;
 constexpr int kQStages = 3;
+constexpr int kQCtasPerSm = 3;
 constexpr int kQCodes = kQT * kCodeBytes;
 constexpr int kQStageBytes = 2 * kQCodes + 2 * kQT * kScaleBytes + kQT * 4;  // codes of K, V; scales of K, V; log-degrees
-constexpr size_t kQRingBytes = (size_t)kQWarps * kQStages * kQStageBytes;
-static_assert(kQRingBytes >= (size_t)kQWarps * 8 * kPartial * 4 + (size_t)kQWarps * kQWarps * 16 * 4, "cluster_combine's rows and weights fit");
+constexpr int kQScaleOut = 2 * kQT * 16;                                     // a tile's scales of K, V as fp32
+constexpr int kQWarpBytes = kQStages * kQStageBytes + kQScaleOut;
+constexpr size_t kQSmemBytes = (size_t)kQWarps * kQWarpBytes;
+static_assert(kQSmemBytes >= (size_t)kQWarps * 8 * kPartial * 4 + (size_t)kQWarps * kQWarps * 16 * 4, "the partials and their weights fit");
+constexpr float kQLazy = 6.f;           // exponents up to this above the reference are let through
+constexpr uint32_t kQFactor = 7u;       // F puts the largest weight at 2^7 .. 2^8 when it is set; it may grow to 2^15
 
 struct QuantArgs {
-  DecodeArgs d;  // views, q, out, partial, shapes, n_splits, page_shift
+  DecodeArgs d;  // views, q, out, partial, shapes, n_splits (CTAs per pair at max_len), span (tiles per CTA), page_shift
   ckv_quant_pool pool;
 };
 
@@ -210,8 +219,34 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// a row's four scale bytes as fp32: 2^(byte - 127), 255 NaN (bf16 holds them all exactly)
-__device__ __forceinline__ void scales_f32(uint32_t w, float (&s)[4]) {
+__device__ __forceinline__ float ex2(float x) {  // 2^x, results below 2^-126 are 0
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+
+// pairs of fp32 in one register pair: two products or multiply-adds per instruction, each rounded as the scalar one
+struct f32x2 {
+  uint64_t v;
+  __device__ __forceinline__ f32x2() {}
+  __device__ __forceinline__ f32x2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
+}
+
+// four scale bytes as fp32: 2^(byte - 127), 255 NaN (bf16 holds them all exactly)
+__device__ __forceinline__ float4 scales_f32(uint32_t w) {
   uint32_t lo, hi;
   asm("{\n\t.reg .b16 a, b;\n\t"
       "mov.b32 {a, b}, %2;\n\t"
@@ -219,10 +254,7 @@ __device__ __forceinline__ void scales_f32(uint32_t w, float (&s)[4]) {
       "cvt.rn.bf16x2.ue8m0x2 %1, b;\n\t}"
       : "=r"(lo), "=r"(hi)
       : "r"(w));
-  s[0] = __uint_as_float(lo << 16);
-  s[1] = __uint_as_float(lo & 0xffff0000u);
-  s[2] = __uint_as_float(hi << 16);
-  s[3] = __uint_as_float(hi & 0xffff0000u);
+  return make_float4(__uint_as_float(lo << 16), __uint_as_float(lo & 0xffff0000u), __uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u));
 }
 
 // Where row r of a tile of V codes sits, and its 16-byte piece c: even rows first, pieces exchanged every other row pair, so
@@ -233,29 +265,41 @@ __device__ __forceinline__ uint32_t v_off(int r, int c) {
 }
 
 template <int CL>
-__global__ void __launch_bounds__(kQWarps * 32, 4) decode_quant_kernel(const QuantArgs qa_) {
+__global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel(const QuantArgs qa_) {
   constexpr int TT = kQT, NW = kQWarps, ST = kQStages;
   const DecodeArgs& a = qa_.d;
   extern __shared__ __align__(128) unsigned char smem_raw[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t = lane & 3;
-  const int split = blockIdx.x * NW + warp;
   griddep_wait();
   griddep_launch();
-  if (CL == 0 && split >= a.n_splits) return;
   const int h = blockIdx.y, b = blockIdx.z, G = a.G;
   const ckv_paged_view view = reinterpret_cast<const ckv_paged_view*>(a.views)[b];
   const int64_t len = view.len;
   const int64_t seq_tiles = (len + TT - 1) / TT;
-  const int64_t t_begin = TT * (seq_tiles * split / a.n_splits);
-  const int64_t t_end = min(len, TT * (seq_tiles * (split + 1) / a.n_splits));
-  const int ntiles = (int)((t_end - t_begin + TT - 1) / TT);
+  int64_t tile0, tile1;  // this warp's tiles
+  if (CL > 0) {          // the cluster's warps share the sequence's tiles evenly
+    const int split = blockIdx.x * NW + warp;
+    tile0 = seq_tiles * split / (CL * NW);
+    tile1 = seq_tiles * (split + 1) / (CL * NW);
+  } else {               // every CTA has a span of the same length, so a ragged batch's CTAs are alike
+    const int64_t c0 = (int64_t)blockIdx.x * a.span, c1 = min(seq_tiles, c0 + a.span);
+    if (c0 >= seq_tiles) return;
+    tile0 = c0 + (c1 - c0) * warp / NW;
+    tile1 = c0 + (c1 - c0) * (warp + 1) / NW;
+  }
+  const int64_t t_begin = tile0 * TT, t_end = min(len, tile1 * TT);
+  const int ntiles = (int)(tile1 - tile0);
   const int64_t n_blocks = (len + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift;
   int64_t blk0 = t_begin >> a.page_shift;
   int my_page = (ntiles > 0 && blk0 + lane < n_blocks) ? view.block_table[blk0 + lane] : 0;
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem_raw) + (uint32_t)warp * ST * kQStageBytes;
+  unsigned char* const mine = smem_raw + (size_t)warp * kQWarpBytes;
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(mine);
+  float4* const sc_out = reinterpret_cast<float4*>(mine + ST * kQStageBytes);  // [K, V][pair of tokens][groups 0 1, groups 2 3]
   const float* logdeg = qa_.pool.logdeg_pages;
 
+  // piece i of a tile of codes is row 8 i + lane / 4, 16 bytes lane % 4: 512 bytes on in memory, 256 in the tile of V
+  const uint32_t v_dst = kQCodes + v_off(lane >> 2, lane & 3);
   auto issue = [&](int tile) {
     const int64_t t0 = t_begin + (int64_t)tile * TT;
     const uint32_t st = ring + (uint32_t)(tile % ST) * kQStageBytes;
@@ -267,23 +311,30 @@ __global__ void __launch_bounds__(kQWarps * 32, 4) decode_quant_kernel(const Qua
     const int page = __shfl_sync(0xffffffffu, my_page, (int)(blk - blk0));
     const int64_t row0 = (((int64_t)page * a.H + h) << a.page_shift) + (t0 & (((int64_t)1 << a.page_shift) - 1));
     const int nt = (int)min((int64_t)TT, t_end - t0);
-    const unsigned char* kc = qa_.pool.k_codes + row0 * kCodeBytes;
-    const unsigned char* vc = qa_.pool.v_codes + row0 * kCodeBytes;
+    const unsigned char* kc = qa_.pool.k_codes + row0 * kCodeBytes + lane * 16;
+    const unsigned char* vc = qa_.pool.v_codes + row0 * kCodeBytes + lane * 16;
+    const unsigned char* s = (lane < 8 ? qa_.pool.k_scales : qa_.pool.v_scales) + row0 * kScaleBytes + (lane & 7) * 16;
+    const uint32_t s_dst = st + 2 * kQCodes + (uint32_t)lane * 16;  // lanes 0 .. 7: K's scales, 8 .. 15: V's
+    const uint32_t l_dst = st + 2 * kQCodes + 2 * TT * kScaleBytes + (uint32_t)lane * 4;
+    if (nt == TT) {
 #pragma unroll
-    for (int i = 0; i < TT / 8; ++i) {
-      const int r = 8 * i + (lane >> 2), c = lane & 3;
-      const uint32_t ok = r < nt ? 16u : 0u;
-      const int off = r < nt ? r * kCodeBytes + c * 16 : 0;  // clamped address, zero-filled when out of range
-      cp_async16(st + (uint32_t)(r * kCodeBytes + c * 16), kc + off, ok);
-      cp_async16(st + kQCodes + v_off(r, c), vc + off, ok);
+      for (int i = 0; i < TT / 8; ++i) {
+        cp_async16(st + (uint32_t)(lane * 16 + i * 512), kc + i * 512, 16u);
+        cp_async16(st + v_dst + (uint32_t)(i * 256), vc + i * 512, 16u);
+      }
+      if (lane < 16) cp_async16(s_dst, s, 16u);
+      if (logdeg) cp_async4(l_dst, logdeg + row0 + lane, 4u);
+    } else {  // the sequence's last tile: rows past its end are zero-filled, from addresses inside the tile's first row
+#pragma unroll
+      for (int i = 0; i < TT / 8; ++i) {
+        const bool ok = 8 * i + (lane >> 2) < nt;
+        cp_async16(st + (uint32_t)(lane * 16 + i * 512), ok ? kc + i * 512 : kc - lane * 16, ok ? 16u : 0u);
+        cp_async16(st + v_dst + (uint32_t)(i * 256), ok ? vc + i * 512 : vc - lane * 16, ok ? 16u : 0u);
+      }
+      const int bytes = max(0, min(16, (nt - 4 * (lane & 7)) * kScaleBytes));
+      if (lane < 16) cp_async16(s_dst, bytes > 0 ? s : s - (lane & 7) * 16, (uint32_t)bytes);
+      if (logdeg) cp_async4(l_dst, logdeg + (lane < nt ? row0 + lane : row0), lane < nt ? 4u : 0u);
     }
-    if (lane < 16) {  // scales: eight pieces of four rows each, for K and for V
-      const int c = lane & 7;
-      const int bytes = max(0, min(16, (nt - 4 * c) * kScaleBytes));
-      const unsigned char* s = (lane < 8 ? qa_.pool.k_scales : qa_.pool.v_scales) + row0 * kScaleBytes;
-      cp_async16(st + 2 * kQCodes + (uint32_t)((lane < 8 ? 0 : TT * kScaleBytes) + c * 16), s + (bytes > 0 ? c * 16 : 0), (uint32_t)bytes);
-    }
-    if (logdeg) cp_async4(st + 2 * kQCodes + 2 * TT * kScaleBytes + lane * 4, logdeg + (lane < nt ? row0 + lane : row0), lane < nt ? 4u : 0u);
   };
 
   // query fragments: head g's elements 32 j + 8 t .. + 7, scaled by a power of two that puts the row's largest at 2^14
@@ -318,9 +369,11 @@ __global__ void __launch_bounds__(kQWarps * 32, 4) decode_quant_kernel(const Qua
   float oacc[8][4];
 #pragma unroll
   for (int i = 0; i < 8; ++i) oacc[i][0] = oacc[i][1] = oacc[i][2] = oacc[i][3] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;            // for head g (this thread's share of the tokens)
-  float wmax[4] = {0.f, 0.f, 0.f, 0.f};            // largest weight p 2^e of head g in each group
-  uint32_t fref[4] = {253u << 23, 253u << 23, 253u << 23, 253u << 23};  // bits of the power of two that the weights are multiplied by
+  float m_ref = 0.f, l_run = 0.f;  // head g: the exponents' reference, and this thread's share of the sum
+  bool seen = false;               // head g has had a score above -inf
+  float wmax[4] = {0.f, 0.f, 0.f, 0.f};                                 // head g, this thread's tokens: largest p 2^e of each group
+  uint32_t fbits[4] = {253u << 23, 253u << 23, 253u << 23, 253u << 23}; // F of head g and each group
+  const f32x2 sc2(sc, sc), log2e2(kLog2e, kLog2e);
 
 #pragma unroll
   for (int i = 0; i < ST - 1; ++i) {
@@ -332,20 +385,29 @@ __global__ void __launch_bounds__(kQWarps * 32, 4) decode_quant_kernel(const Qua
     __syncwarp();
     if (tile + ST - 1 < ntiles) issue(tile + ST - 1);
     cp_async_commit();
-    const unsigned char* st = smem_raw + (size_t)(warp * ST + tile % ST) * kQStageBytes;
+    const unsigned char* st = mine + (size_t)(tile % ST) * kQStageBytes;
     const int nt = (int)min((int64_t)TT, t_end - (t_begin + (int64_t)tile * TT));
 
-    // ---- scores of tokens 8 n + 2 t, + 1 with head g
-    float p[4][2];
-    float tmax = -INFINITY;
+    // ---- scales: lanes 2 i and 2 i + 1 have the bytes of these tokens; the first takes groups 0 and 1 of both, the second 2 and 3
+    {
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(st + 2 * kQCodes);
+      const uint32_t sel = (lane & 1) ? 0x3726u : 0x5140u;
+      const uint32_t wk = w[lane], wv = w[TT + lane];
+      sc_out[lane] = scales_f32(__byte_perm(wk, __shfl_xor_sync(0xffffffffu, wk, 1), sel));
+      sc_out[TT + lane] = scales_f32(__byte_perm(wv, __shfl_xor_sync(0xffffffffu, wv, 1), sel));
+      __syncwarp();
+    }
+    // ---- exponents of tokens 8 n + 2 t, + 1 with head g, relative to the reference
+    float x[4][2];
+    float top = -INFINITY;
+    const f32x2 minus_m(-m_ref, -m_ref);
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const uint4 kw = *reinterpret_cast<const uint4*>(st + (8 * n + g) * kCodeBytes + 16 * t);
-      const uint2 ks = *reinterpret_cast<const uint2*>(st + 2 * kQCodes + (8 * n + 2 * t) * kScaleBytes);
-      float s0 = 0.f, s1 = 0.f, k0[4], k1[4];
-      scales_f32(ks.x, k0);
-      scales_f32(ks.y, k1);
       const uint32_t kj[4] = {kw.x, kw.y, kw.z, kw.w};
+      const float4 s01 = sc_out[2 * (4 * n + t)], s23 = sc_out[2 * (4 * n + t) + 1];
+      const f32x2 ks[4] = {f32x2(s01.x, s01.y), f32x2(s01.z, s01.w), f32x2(s23.x, s23.y), f32x2(s23.z, s23.w)};
+      f32x2 s(0.f, 0.f);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         uint32_t e[4];
@@ -353,66 +415,89 @@ __global__ void __launch_bounds__(kQWarps * 32, 4) decode_quant_kernel(const Qua
         float c[4];
         ptx::mma_f16_first(c, qa[j][0], 0u, qa[j][1], 0u, e[0], e[1]);
         ptx::mma_f16(c, qa[j][2], 0u, qa[j][3], 0u, e[2], e[3]);
-        s0 = fmaf(c[0], k0[j], s0);
-        s1 = fmaf(c[1], k1[j], s1);
+        s = j == 0 ? mul2(f32x2(c[0], c[1]), ks[j]) : fma2(f32x2(c[0], c[1]), ks[j], s);
       }
-      float2 bias = make_float2(0.f, 0.f);
-      if (logdeg) bias = *reinterpret_cast<const float2*>(st + 2 * kQCodes + 2 * TT * kScaleBytes + (8 * n + 2 * t) * 4);
-      s0 = 8 * n + 2 * t < nt ? fmaf(s0, sc, bias.x * kLog2e) : -INFINITY;
-      s1 = 8 * n + 2 * t + 1 < nt ? fmaf(s1, sc, bias.y * kLog2e) : -INFINITY;
-      p[n][0] = s0;
-      p[n][1] = s1;
-      tmax = fmaxf(tmax, fmaxf(s0, s1));
+      f32x2 base = minus_m;
+      if (logdeg) {
+        const float2 bias = *reinterpret_cast<const float2*>(st + 2 * kQCodes + 2 * TT * kScaleBytes + (8 * n + 2 * t) * 4);
+        base = fma2(f32x2(bias.x, bias.y), log2e2, minus_m);
+      }
+      fma2(s, sc2, base).get(x[n][0], x[n][1]);
     }
-    // ---- online softmax
-    tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, 1));
-    tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, 2));
-    const float m_new = fmaxf(m_run, tmax);
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;  // nothing but -inf so far: weights of zero, not inf - inf
-    const float corr = exp2f(m_run - m_use);
-    m_run = m_new;
-    float psum = 0.f;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      p[n][0] = exp2f(p[n][0] - m_use);
-      p[n][1] = exp2f(p[n][1] - m_use);
-      psum += p[n][0] + p[n][1];
-    }
-    l_run = l_run * corr + psum;
-    // ---- weights p 2^e of every group in fp16, relative to the largest so far
-    float vs[4][2][4];
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const uint2 w = *reinterpret_cast<const uint2*>(st + 2 * kQCodes + TT * kScaleBytes + (8 * n + 2 * t) * kScaleBytes);
-      scales_f32(w.x, vs[n][0]);
-      scales_f32(w.y, vs[n][1]);
-    }
-    uint32_t pb[4][4];  // [group][n]: tokens 8 n + 2 t, + 1
-    float ratio[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float w[4][2], top = 0.f;
+    if (nt < TT) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
-        w[n][0] = p[n][0] * vs[n][0][j];
-        w[n][1] = p[n][1] * vs[n][1][j];
-        top = fmaxf(top, fmaxf(w[n][0], w[n][1]));
+        if (8 * n + 2 * t >= nt) x[n][0] = -INFINITY;
+        if (8 * n + 2 * t + 1 >= nt) x[n][1] = -INFINITY;
       }
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n) top = max3(top, x[n][0], x[n][1]);
+    float corr = 1.f;
+    const bool move = __any_sync(0xffffffffu, top > kQLazy || !seen);
+    if (move) {  // the reference goes to the largest score so far
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      wmax[j] = fmaxf(wmax[j] * corr, top);
-      // f = 2^(14 - floor(log2 wmax)), 2^126 at most
-      const uint32_t f = (268u << 23) - max(__float_as_uint(wmax[j]) & 0x7f800000u, 15u << 23);
-      ratio[j] = corr * __uint_as_float(f) * __uint_as_float((254u << 23) - fref[j]);
-      fref[j] = f;
+      if (top > -INFINITY) {
+        const float up = seen ? fmaxf(top, 0.f) : top;
+        corr = seen ? ex2(-up) : 0.f;
+        seen = true;
+        m_ref += up;
 #pragma unroll
-      for (int n = 0; n < 4; ++n) pb[j][n] = pack_f16x2(w[n][0] * __uint_as_float(f), w[n][1] * __uint_as_float(f));
+        for (int n = 0; n < 4; ++n) {
+          x[n][0] -= up;
+          x[n][1] -= up;
+        }
+        l_run *= corr;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) wmax[j] *= corr;
+      }
     }
-    if (__any_sync(0xffffffffu, ratio[0] != 1.f || ratio[1] != 1.f || ratio[2] != 1.f || ratio[3] != 1.f)) {
-      // the accumulators hold heads 2 t and 2 t + 1: their factors are in quads 2 t and 2 t + 1
+    f32x2 p[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const float p0 = ex2(x[n][0]), p1 = ex2(x[n][1]);
+      l_run += p0 + p1;
+      p[n] = f32x2(p0, p1);
+    }
+    // ---- weights p 2^e of every group, times F in fp16; if F has to move (rarely), once more
+    uint32_t pb[4][4];  // [group][n]: tokens 8 n + 2 t, + 1
+    bool over = move;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+      f32x2 f2[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f2[j] = f32x2(__uint_as_float(fbits[j]), __uint_as_float(fbits[j]));
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const float4 s01 = sc_out[TT + 2 * (4 * n + t)], s23 = sc_out[TT + 2 * (4 * n + t) + 1];
+        const f32x2 vs[4] = {f32x2(s01.x, s01.y), f32x2(s01.z, s01.w), f32x2(s23.x, s23.y), f32x2(s23.z, s23.w)};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x2 w = mul2(p[n], vs[j]);
+          float w0, w1;
+          w.get(w0, w1);
+          wmax[j] = max3(wmax[j], w0, w1);
+          mul2(w, f2[j]).get(w0, w1);
+          pb[j][n] = pack_f16x2(w0, w1);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)  // wmax F > 2^15, in exponents (an infinity counts)
+        over |= (__float_as_uint(wmax[j]) & 0x7f800000u) + fbits[j] > (127u + 14u + 127u) << 23;
+      if (!__any_sync(0xffffffffu, over)) break;
+      over = false;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float r0 = __shfl_sync(0xffffffffu, ratio[j], 8 * t), r1 = __shfl_sync(0xffffffffu, ratio[j], 8 * t + 4);
+        float q = wmax[j];
+        q = fmaxf(q, __shfl_xor_sync(0xffffffffu, q, 1));
+        q = fmaxf(q, __shfl_xor_sync(0xffffffffu, q, 2));
+        // F = 2^(7 - floor(log2 q)), 2^126 at most
+        const uint32_t f = ((254u + kQFactor) << 23) - max(__float_as_uint(q) & 0x7f800000u, (kQFactor + 1u) << 23);
+        const float ratio = corr * __uint_as_float(f) * __uint_as_float((254u << 23) - fbits[j]);
+        fbits[j] = f;
+        // the accumulators hold heads 2 t and 2 t + 1: their factors are in quads 2 t and 2 t + 1
+        const float r0 = __shfl_sync(0xffffffffu, ratio, 8 * t), r1 = __shfl_sync(0xffffffffu, ratio, 8 * t + 4);
 #pragma unroll
         for (int i = 2 * j; i < 2 * j + 2; ++i) {
           oacc[i][0] *= r0; oacc[i][1] *= r1; oacc[i][2] *= r0; oacc[i][3] *= r1;
@@ -439,9 +524,9 @@ __global__ void __launch_bounds__(kQWarps * 32, 4) decode_quant_kernel(const Qua
         ptx::unpack_e2m1x8((a1 & lo) | ((b1 << 4) & hi), e1);
         ptx::unpack_e2m1x8(((a1 >> 4) & lo) | (b1 & hi), o1);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int j = 2 * u + (x >> 1);
-          ptx::mma_f16(oacc[4 * u + x], e0[x], o0[x], e1[x], o1[x], pb[j][2 * s], pb[j][2 * s + 1]);
+        for (int i = 0; i < 4; ++i) {
+          const int j = 2 * u + (i >> 1);
+          ptx::mma_f16(oacc[4 * u + i], e0[i], o0[i], e1[i], o1[i], pb[j][2 * s], pb[j][2 * s + 1]);
         }
       }
     }
@@ -450,59 +535,128 @@ __global__ void __launch_bounds__(kQWarps * 32, 4) decode_quant_kernel(const Qua
 
   l_run += __shfl_xor_sync(0xffffffffu, l_run, 1);
   l_run += __shfl_xor_sync(0xffffffffu, l_run, 2);
+  const float m_out = l_run == 0.f ? -INFINITY : m_ref;
   // back from each group's own power of two
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float inv = __uint_as_float((254u << 23) - fref[j]);
+    const float inv = __uint_as_float((254u << 23) - fbits[j]);
     const float r0 = __shfl_sync(0xffffffffu, inv, 8 * t), r1 = __shfl_sync(0xffffffffu, inv, 8 * t + 4);
 #pragma unroll
     for (int i = 2 * j; i < 2 * j + 2; ++i) {
       oacc[i][0] *= r0; oacc[i][1] *= r1; oacc[i][2] *= r0; oacc[i][3] *= r1;
     }
   }
-  auto park = [&](float* dst, int64_t hstride, int heads) {
-    if (t == 0 && g < heads) {
-      dst[g * hstride + kD] = m_run;
-      dst[g * hstride + kD + 1] = l_run;
+  auto park = [&](float* part) {
+    if (t == 0) {
+      part[g * kPartial + kD] = m_out;
+      part[g * kPartial + kD + 1] = l_run;
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      if (2 * t + e >= heads) continue;
-      float* o = dst + (2 * t + e) * hstride + 4 * g;
+      float* o = part + (2 * t + e) * kPartial + 4 * g;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         *reinterpret_cast<float4*>(o + 32 * j) = make_float4(oacc[2 * j][e], oacc[2 * j][2 + e], oacc[2 * j + 1][e], oacc[2 * j + 1][2 + e]);
     }
   };
   if constexpr (CL > 0) {
-    cluster_combine<CL, NW>(smem_raw, warp, lane, G, reinterpret_cast<__nv_bfloat16*>(a.out) + ((int64_t)b * a.H + h) * G * kD,
-                            [&](float* part) { park(part, kPartial, 8); });
+    cluster_combine<CL, NW>(smem_raw, warp, lane, G, reinterpret_cast<__nv_bfloat16*>(a.out) + ((int64_t)b * a.H + h) * G * kD, park);
   } else {
-    park(a.partial + ((((int64_t)b * a.H + h) * G) * a.n_splits + split) * kPartial, (int64_t)a.n_splits * kPartial, G);
+    // the CTA's four partials become one: a quarter of the traffic to and from the workspace
+    __syncthreads();
+    float* part = reinterpret_cast<float*>(smem_raw);
+    park(part + warp * 8 * kPartial);
+    __syncthreads();
+    for (int head = warp; head < G; head += NW) {
+      const float* r = part + head * kPartial;
+      float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) mm = fmaxf(mm, r[w * 8 * kPartial + kD]);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float* x = r + w * 8 * kPartial;
+        const float f = x[kD] == -INFINITY ? 0.f : exp2f(x[kD] - mm);
+        const float4 y = *reinterpret_cast<const float4*>(x + lane * 4);
+        o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
+        ll = fmaf(f, x[kD + 1], ll);
+      }
+      float* dst = a.partial + ((((int64_t)b * a.H + h) * G + head) * a.n_splits + blockIdx.x) * kPartial;
+      *reinterpret_cast<float4*>(dst + lane * 4) = o;
+      if (lane == 0) *reinterpret_cast<float2*>(dst + kD) = make_float2(mm, ll);
+    }
   }
 }
 
+// One warp per (sequence, query head) joins the partials of the spans that the sequence has: a lane owns four columns.
+constexpr int kQCombThreads = 128;
+
+__global__ void __launch_bounds__(kQCombThreads) quant_combine_kernel(const DecodeArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * (kQCombThreads / 32) + (threadIdx.x >> 5);
+  griddep_wait();
+  griddep_launch();
+  if (row >= (int64_t)a.Bz * a.H * a.G) return;
+  const int64_t len = reinterpret_cast<const ckv_paged_view*>(a.views)[row / (a.H * a.G)].len;
+  const int n = (int)min((int64_t)a.n_splits, ((len + kQT - 1) / kQT + a.span - 1) / a.span);
+  const float* p = a.partial + row * a.n_splits * kPartial;
+  float mm = -INFINITY;
+  for (int s = lane; s < n; s += 32) mm = fmaxf(mm, p[(int64_t)s * kPartial + kD]);
+  mm = warp_max(mm);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float ll = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < n; ++s) {
+    const float* r = p + (int64_t)s * kPartial;
+    const float2 ml = *reinterpret_cast<const float2*>(r + kD);
+    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mm);
+    const float4 y = *reinterpret_cast<const float4*>(r + lane * 4);
+    o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
+    ll = fmaf(f, ml.y, ll);
+  }
+  const float inv = ll == 0.f ? 0.f : 1.f / ll;
+  store4(reinterpret_cast<__nv_bfloat16*>(a.out) + row * kD + lane * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+}
+
+// Sets the kernel's shared memory (and a cluster size above 8) once per device; how many clusters fit at once, 0: none
 template <int CL>
-bool quant_ready() {  // sets the kernel's shared memory once per device
+int quant_clusters() {
   constexpr int kMaxDev = 64;
-  static std::atomic<bool> done[kMaxDev];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return false;
-  if (dev >= 0 && dev < kMaxDev && done[dev].load(std::memory_order_relaxed)) return true;
-  if (cudaFuncSetAttribute(decode_quant_kernel<CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kQRingBytes) != cudaSuccess) return false;
-  if (dev >= 0 && dev < kMaxDev) done[dev].store(true, std::memory_order_relaxed);
-  return true;
+  static std::atomic<int> cached[kMaxDev];  // 0 = not asked yet, else the answer + 1
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDev) return 0;
+  if ((n = cached[dev].load(std::memory_order_relaxed)) > 0) return n - 1;
+  bool ok = cudaFuncSetAttribute(decode_quant_kernel<CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kQSmemBytes) == cudaSuccess;
+  if (ok && CL > 8) ok = cudaFuncSetAttribute(decode_quant_kernel<CL>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+  if (ok && CL == 0) n = 1;
+  if (ok && CL > 0) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(CL, 1, 1);
+    cfg.blockDim = dim3(kQWarps * 32);
+    cfg.dynamicSmemBytes = kQSmemBytes;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CL;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, decode_quant_kernel<CL>, &cfg) != cudaSuccess) {
+      n = 0;
+      cudaGetLastError();  // a refusal here only means "not this cluster size"
+    }
+  }
+  cached[dev].store(n + 1, std::memory_order_relaxed);
+  return n;
 }
 
 template <int CL>
-cudaError_t launch_quant(QuantArgs a, cudaStream_t st) {
-  if (!quant_ready<CL>()) return cudaErrorInvalidValue;
+cudaError_t launch_quant(const QuantArgs& a, cudaStream_t st) {
+  if (quant_clusters<CL>() < 1) return cudaErrorInvalidConfiguration;
   cudaLaunchConfig_t cfg{};
-  const int ctas = CL > 0 ? CL : (a.d.n_splits + kQWarps - 1) / kQWarps;
-  if (CL > 0) a.d.n_splits = CL * kQWarps;
-  cfg.gridDim = dim3((unsigned)ctas, (unsigned)a.d.H, (unsigned)a.d.Bz);
+  cfg.gridDim = dim3((unsigned)(CL > 0 ? CL : a.d.n_splits), (unsigned)a.d.H, (unsigned)a.d.Bz);
   cfg.blockDim = dim3(kQWarps * 32);
-  cfg.dynamicSmemBytes = kQRingBytes;
+  cfg.dynamicSmemBytes = kQSmemBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -513,26 +667,23 @@ cudaError_t launch_quant(QuantArgs a, cudaStream_t st) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CL > 0 ? 2 : 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, decode_quant_kernel<CL>, a);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, decode_quant_kernel<CL>, a);
   if (e != cudaSuccess || CL > 0) return e;
-  return launch_decode_combine(a.d, st);
+  const int64_t rows = (int64_t)a.d.Bz * a.d.H * a.d.G, per = kQCombThreads / 32;
+  return launch_dependent(quant_combine_kernel, dim3((unsigned)((rows + per - 1) / per)), dim3(kQCombThreads), 0, st, a.d);
 }
 
-// Splits of a launch that joins its partials in a second kernel: four CTAs per SM, four splits per CTA; the count that
-// minimises waves x (tiles per warp + a fixed cost of two tiles), with at least two tiles per warp.
-int32_t quant_splits(int32_t Bz, int32_t H, int64_t max_len) {
-  const int64_t pairs = (int64_t)Bz * H, slots = 4ll * sm_count();
-  const int64_t tiles = std::max<int64_t>(1, (max_len + kQT - 1) / kQT);
-  const int64_t most = std::min<int64_t>(64, std::max<int64_t>(1, tiles / (2 * kQWarps)));
-  int64_t best = 1, best_cost = INT64_MAX;
-  for (int64_t c = 1; c <= most; ++c) {
-    const int64_t cost = ((pairs * c + slots - 1) / slots) * ((tiles + c * kQWarps - 1) / (c * kQWarps) + 2);
-    if (cost < best_cost) {
-      best_cost = cost;
-      best = c;
-    }
-  }
-  return (int32_t)(best * kQWarps);
+// Tiles per CTA of a launch that joins its partials in a second kernel: four waves of CTAs if all sequences were max_len
+// long, eight tiles per warp at least, and no more than 65535 spans.
+int64_t quant_span(int32_t Bz, int32_t H, int64_t max_len) {
+  const int64_t pairs = (int64_t)Bz * H, slots = (int64_t)kQCtasPerSm * sm_count();
+  const int64_t tiles = (max_len + kQT - 1) / kQT;
+  return std::max({(pairs * tiles + 4 * slots - 1) / (4 * slots), (int64_t)8 * kQWarps, (tiles + 65534) / 65535});
+}
+
+int64_t quant_splits(int32_t Bz, int32_t H, int64_t max_len) {
+  const int64_t span = quant_span(Bz, H, max_len);
+  return std::max<int64_t>(1, ((max_len + kQT - 1) / kQT + span - 1) / span);
 }
 
 int check_pool(const ckv_quant_pool* p) {
@@ -612,14 +763,19 @@ int ckv_decode_attn_quantized(const ckv_paged_view* views_dev, const ckv_quant_p
   a.d.views = views_dev; a.d.q = q; a.d.out = out;
   a.d.partial = static_cast<float*>(workspace);
   a.d.Bz = Bz; a.d.H = H; a.d.G = G;
-  a.d.n_splits = quant_splits(Bz, H, max_len);
+  a.d.n_splits = (int32_t)quant_splits(Bz, H, max_len);
+  a.d.span = quant_span(Bz, H, max_len);
   a.d.max_len = max_len;
   a.d.scale = scale;
   a.d.page_shift = shift;
   a.pool = *pool;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  // few pairs: one cluster of eight CTAs each, joined on the chip, while all are resident at once (four CTAs per SM)
-  const cudaError_t e = (int64_t)Bz * H * 8 <= 4ll * sm_count() ? launch_quant<8>(a, stream) : launch_quant<0>(a, stream);
+  // Few pairs: one cluster each, joined on the chip, the largest of which all are resident at once.  More: spans of equal
+  // length and a second kernel.
+  const int64_t pairs = (int64_t)Bz * H;
+  const cudaError_t e = quant_clusters<16>() >= pairs ? launch_quant<16>(a, stream)
+                        : quant_clusters<8>() >= pairs ? launch_quant<8>(a, stream)
+                                                       : launch_quant<0>(a, stream);
   return e == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
