@@ -184,16 +184,17 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
 // row is scaled by a power of two), softmax online in the exp2 domain, and partials that are joined in the cluster or by
 // a second kernel.  With four bits per element the issue slots are what counts (a tile's 4480 bytes take 192 cycles of an
 // SM's share of the measured bandwidth), so unpacking and scaling are arranged to cost as few instructions as they can:
-//   S   a group's 32 elements are two k steps of the product; their sum is multiplied by the token's scale of that group
-//       (one multiply-add per token, head and group in place of 32 products with the scale), two tokens per instruction
+//   S   S^T = K Q^T: tokens fill the 16 rows of the A operand and up to eight heads the columns of B, so no row is padding.  A
+//       group's 32 elements are two k steps; their sum is multiplied by the token's scale of that group (one multiply-add
+//       per token, head and group in place of 32 products with the scale), two heads per instruction
 //   O   V's scale belongs to a token and a group, as the weight p belongs to a token: the weight of token t in group j is
-//       p_t 2^e_tj, one B operand per group.  It goes to fp16 times a power of two F that is the head's and the group's own
-//       and follows the largest such weight so far, so that whatever the scales are the tokens that matter keep 11 bits:
-//       weights from 2^-21 of the largest on, and below that 2^-32 of the largest.
+//       p_t 2^e_tj, one B operand per group, turned from S^T's layout by movmatrix.  It goes to fp16 times a power of two F
+//       that is the head's and the group's own and follows the largest such weight so far, so that whatever the scales are
+//       the tokens that matter keep 11 bits: weights from 2^-21 of the largest on, and below that 2^-32 of the largest.
 //   m   the softmax's reference and F move only when a tile needs it (an exponent above 6, a weight that would pass 2^15):
 //       after a sequence's first tiles that is rare, and the accumulators are left alone.
-//   e   the lanes of a head read the same scales: each tile's 256 are converted once, one token per lane, and read back
-//       as fp32 pairs of neighbouring tokens
+//   e   lanes share tokens: each tile's 256 scales are converted once, one token per lane, and read back as fp32, each twice in
+//       a row, ready to multiply two heads
 //   V   two tokens' codes are interleaved by nibble before they are unpacked, which gives the operand's pairs of
 //       neighbouring tokens without permuting fp16 values.
 constexpr int kQT = 32;  // tokens per tile
@@ -202,7 +203,7 @@ constexpr int kQStages = 3;
 constexpr int kQCtasPerSm = 3;
 constexpr int kQCodes = kQT * kCodeBytes;
 constexpr int kQStageBytes = 2 * kQCodes + 2 * kQT * kScaleBytes + kQT * 4;  // codes of K, V; scales of K, V; log-degrees
-constexpr int kQScaleOut = 2 * kQT * 16;                                     // a tile's scales of K, V as fp32
+constexpr int kQScaleOut = 2 * kQT * 32;                                     // a tile's scales of K, V as fp32, twice each
 constexpr int kQWarpBytes = kQStages * kQStageBytes + kQScaleOut;
 constexpr size_t kQSmemBytes = (size_t)kQWarps * kQWarpBytes;
 static_assert(kQSmemBytes >= (size_t)kQWarps * 8 * kPartial * 4 + (size_t)kQWarps * kQWarps * 16 * 4, "the partials and their weights fit");
@@ -225,8 +226,6 @@ __device__ __forceinline__ float ex2(float x) {  // 2^x, results below 2^-126 ar
   return y;
 }
 
-__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
-
 // pairs of fp32 in one register pair: two products or multiply-adds per instruction, each rounded as the scalar one
 struct f32x2 {
   uint64_t v;
@@ -245,8 +244,25 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
   return d;
 }
 
-// four scale bytes as fp32: 2^(byte - 127), 255 NaN (bf16 holds them all exactly)
-__device__ __forceinline__ float4 scales_f32(uint32_t w) {
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
+}
+
+__device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+
+// four scale bytes as fp32, each twice: 2^(byte - 127), 255 NaN (bf16 holds them all exactly)
+__device__ __forceinline__ void scales_f32(uint32_t w, float4* out) {
   uint32_t lo, hi;
   asm("{\n\t.reg .b16 a, b;\n\t"
       "mov.b32 {a, b}, %2;\n\t"
@@ -254,7 +270,10 @@ __device__ __forceinline__ float4 scales_f32(uint32_t w) {
       "cvt.rn.bf16x2.ue8m0x2 %1, b;\n\t}"
       : "=r"(lo), "=r"(hi)
       : "r"(w));
-  return make_float4(__uint_as_float(lo << 16), __uint_as_float(lo & 0xffff0000u), __uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u));
+  const float s0 = __uint_as_float(lo << 16), s1 = __uint_as_float(lo & 0xffff0000u);
+  const float s2 = __uint_as_float(hi << 16), s3 = __uint_as_float(hi & 0xffff0000u);
+  out[0] = make_float4(s0, s0, s1, s1);
+  out[1] = make_float4(s2, s2, s3, s3);
 }
 
 // Where row r of a tile of V codes sits, and its 16-byte piece c: even rows first, pieces exchanged every other row pair, so
@@ -278,11 +297,11 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
   const int64_t len = view.len;
   const int64_t seq_tiles = (len + TT - 1) / TT;
   int64_t tile0, tile1;  // this warp's tiles
-  if (CL > 0) {          // the cluster's warps share the sequence's tiles evenly
+  if constexpr (CL > 0) {  // the cluster's warps share the sequence's tiles evenly
     const int split = blockIdx.x * NW + warp;
     tile0 = seq_tiles * split / (CL * NW);
     tile1 = seq_tiles * (split + 1) / (CL * NW);
-  } else {               // every CTA has a span of the same length, so a ragged batch's CTAs are alike
+  } else {                 // every CTA has a span of the same length, so a ragged batch's CTAs are alike
     const int64_t c0 = (int64_t)blockIdx.x * a.span, c1 = min(seq_tiles, c0 + a.span);
     if (c0 >= seq_tiles) return;
     tile0 = c0 + (c1 - c0) * warp / NW;
@@ -295,7 +314,7 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
   int my_page = (ntiles > 0 && blk0 + lane < n_blocks) ? view.block_table[blk0 + lane] : 0;
   unsigned char* const mine = smem_raw + (size_t)warp * kQWarpBytes;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(mine);
-  float4* const sc_out = reinterpret_cast<float4*>(mine + ST * kQStageBytes);  // [K, V][pair of tokens][groups 0 1, groups 2 3]
+  float4* const sc_out = reinterpret_cast<float4*>(mine + ST * kQStageBytes);  // [K, V][token][groups 0 0 1 1, 2 2 3 3]
   const float* logdeg = qa_.pool.logdeg_pages;
 
   // piece i of a tile of codes is row 8 i + lane / 4, 16 bytes lane % 4: 512 bytes on in memory, 256 in the tile of V
@@ -369,11 +388,15 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
   float oacc[8][4];
 #pragma unroll
   for (int i = 0; i < 8; ++i) oacc[i][0] = oacc[i][1] = oacc[i][2] = oacc[i][3] = 0.f;
-  float m_ref = 0.f, l_run = 0.f;  // head g: the exponents' reference, and this thread's share of the sum
-  bool seen = false;               // head g has had a score above -inf
-  float wmax[4] = {0.f, 0.f, 0.f, 0.f};                                 // head g, this thread's tokens: largest p 2^e of each group
-  uint32_t fbits[4] = {253u << 23, 253u << 23, 253u << 23, 253u << 23}; // F of head g and each group
-  const f32x2 sc2(sc, sc), log2e2(kLog2e, kLog2e);
+  // this thread's two heads, 2 t and 2 t + 1: the columns of S^T and O^T that it holds
+  const f32x2 sc2(__shfl_sync(0xffffffffu, sc, 8 * t), __shfl_sync(0xffffffffu, sc, 8 * t + 4));
+  float m_ref[2] = {0.f, 0.f};          // the exponents' reference
+  bool seen[2] = {false, false};        // a score above -inf has been met
+  f32x2 l_run(0.f, 0.f);                // this thread's share of the sum
+  f32x2 fac[4];                         // F of each group
+  uint32_t wtop[4] = {0u, 0u, 0u, 0u};  // this thread's largest weight of each group, times F, in fp16
+#pragma unroll
+  for (int j = 0; j < 4; ++j) fac[j] = f32x2(__uint_as_float(253u << 23), __uint_as_float(253u << 23));
 
 #pragma unroll
   for (int i = 0; i < ST - 1; ++i) {
@@ -388,122 +411,155 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
     const unsigned char* st = mine + (size_t)(tile % ST) * kQStageBytes;
     const int nt = (int)min((int64_t)TT, t_end - (t_begin + (int64_t)tile * TT));
 
-    // ---- scales: lanes 2 i and 2 i + 1 have the bytes of these tokens; the first takes groups 0 and 1 of both, the second 2 and 3
+    // ---- scales: one token per lane
     {
       const uint32_t* w = reinterpret_cast<const uint32_t*>(st + 2 * kQCodes);
-      const uint32_t sel = (lane & 1) ? 0x3726u : 0x5140u;
-      const uint32_t wk = w[lane], wv = w[TT + lane];
-      sc_out[lane] = scales_f32(__byte_perm(wk, __shfl_xor_sync(0xffffffffu, wk, 1), sel));
-      sc_out[TT + lane] = scales_f32(__byte_perm(wv, __shfl_xor_sync(0xffffffffu, wv, 1), sel));
+      scales_f32(w[lane], sc_out + 2 * lane);
+      scales_f32(w[TT + lane], sc_out + 2 * (TT + lane));
       __syncwarp();
     }
-    // ---- exponents of tokens 8 n + 2 t, + 1 with head g, relative to the reference
-    float x[4][2];
-    float top = -INFINITY;
-    const f32x2 minus_m(-m_ref, -m_ref);
+    // ---- exponents of tokens 8 n + g with heads 2 t, 2 t + 1, relative to the reference
+    f32x2 x[4];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const uint4 kw = *reinterpret_cast<const uint4*>(st + (8 * n + g) * kCodeBytes + 16 * t);
-      const uint32_t kj[4] = {kw.x, kw.y, kw.z, kw.w};
-      const float4 s01 = sc_out[2 * (4 * n + t)], s23 = sc_out[2 * (4 * n + t) + 1];
-      const f32x2 ks[4] = {f32x2(s01.x, s01.y), f32x2(s01.z, s01.w), f32x2(s23.x, s23.y), f32x2(s23.z, s23.w)};
-      f32x2 s(0.f, 0.f);
+    for (int s = 0; s < 2; ++s) {
+      const uint4 ka = *reinterpret_cast<const uint4*>(st + (16 * s + g) * kCodeBytes + 16 * t);
+      const uint4 kb = *reinterpret_cast<const uint4*>(st + (16 * s + 8 + g) * kCodeBytes + 16 * t);
+      const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+      const float4 a01 = sc_out[2 * (16 * s + g)], a23 = sc_out[2 * (16 * s + g) + 1];
+      const float4 b01 = sc_out[2 * (16 * s + 8 + g)], b23 = sc_out[2 * (16 * s + 8 + g) + 1];
+      const f32x2 sa[4] = {f32x2(a01.x, a01.y), f32x2(a01.z, a01.w), f32x2(a23.x, a23.y), f32x2(a23.z, a23.w)};
+      const f32x2 sb[4] = {f32x2(b01.x, b01.y), f32x2(b01.z, b01.w), f32x2(b23.x, b23.y), f32x2(b23.z, b23.w)};
+      f32x2 xa, xb;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        uint32_t e[4];
-        ptx::unpack_e2m1x8(kj[j], e);
+        uint32_t ea[4], eb[4];
+        ptx::unpack_e2m1x8(wa[j], ea);
+        ptx::unpack_e2m1x8(wb[j], eb);
         float c[4];
-        ptx::mma_f16_first(c, qa[j][0], 0u, qa[j][1], 0u, e[0], e[1]);
-        ptx::mma_f16(c, qa[j][2], 0u, qa[j][3], 0u, e[2], e[3]);
-        s = j == 0 ? mul2(f32x2(c[0], c[1]), ks[j]) : fma2(f32x2(c[0], c[1]), ks[j], s);
+        ptx::mma_f16_first(c, ea[0], eb[0], ea[1], eb[1], qa[j][0], qa[j][1]);
+        ptx::mma_f16(c, ea[2], eb[2], ea[3], eb[3], qa[j][2], qa[j][3]);
+        xa = j == 0 ? mul2(f32x2(c[0], c[1]), sa[j]) : fma2(f32x2(c[0], c[1]), sa[j], xa);
+        xb = j == 0 ? mul2(f32x2(c[2], c[3]), sb[j]) : fma2(f32x2(c[2], c[3]), sb[j], xb);
       }
-      f32x2 base = minus_m;
+      float ba = 0.f, bb = 0.f;
       if (logdeg) {
-        const float2 bias = *reinterpret_cast<const float2*>(st + 2 * kQCodes + 2 * TT * kScaleBytes + (8 * n + 2 * t) * 4);
-        base = fma2(f32x2(bias.x, bias.y), log2e2, minus_m);
+        const float* ld = reinterpret_cast<const float*>(st + 2 * kQCodes + 2 * TT * kScaleBytes) + 16 * s + g;
+        ba = ld[0];
+        bb = ld[8];
       }
-      fma2(s, sc2, base).get(x[n][0], x[n][1]);
+      x[2 * s] = fma2(xa, sc2, f32x2(fmaf(ba, kLog2e, -m_ref[0]), fmaf(ba, kLog2e, -m_ref[1])));
+      x[2 * s + 1] = fma2(xb, sc2, f32x2(fmaf(bb, kLog2e, -m_ref[0]), fmaf(bb, kLog2e, -m_ref[1])));
     }
     if (nt < TT) {
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        if (8 * n + 2 * t >= nt) x[n][0] = -INFINITY;
-        if (8 * n + 2 * t + 1 >= nt) x[n][1] = -INFINITY;
-      }
+      for (int n = 0; n < 4; ++n)
+        if (8 * n + g >= nt) x[n] = f32x2(-INFINITY, -INFINITY);
     }
+    float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-    for (int n = 0; n < 4; ++n) top = max3(top, x[n][0], x[n][1]);
-    float corr = 1.f;
-    const bool move = __any_sync(0xffffffffu, top > kQLazy || !seen);
+    for (int n = 0; n < 4; ++n) {
+      float x0, x1;
+      x[n].get(x0, x1);
+      top[0] = fmaxf(top[0], x0);
+      top[1] = fmaxf(top[1], x1);
+    }
+    float corr[2] = {1.f, 1.f};
+    const bool move = __any_sync(0xffffffffu, fmaxf(top[0], top[1]) > kQLazy || !(seen[0] && seen[1]));
     if (move) {  // the reference goes to the largest score so far
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      if (top > -INFINITY) {
-        const float up = seen ? fmaxf(top, 0.f) : top;
-        corr = seen ? ex2(-up) : 0.f;
-        seen = true;
-        m_ref += up;
+      float up[2] = {0.f, 0.f};
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          x[n][0] -= up;
-          x[n][1] -= up;
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], o));
+        if (top[e] > -INFINITY) {
+          up[e] = seen[e] ? fmaxf(top[e], 0.f) : top[e];
+          corr[e] = seen[e] ? ex2(-up[e]) : 0.f;
+          seen[e] = true;
+          m_ref[e] += up[e];
         }
-        l_run *= corr;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) wmax[j] *= corr;
       }
+      const f32x2 down(-up[0], -up[1]);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) x[n] = add2(x[n], down);
+      l_run = mul2(l_run, f32x2(corr[0], corr[1]));
     }
     f32x2 p[4];
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      const float p0 = ex2(x[n][0]), p1 = ex2(x[n][1]);
-      l_run += p0 + p1;
-      p[n] = f32x2(p0, p1);
+      float x0, x1;
+      x[n].get(x0, x1);
+      p[n] = f32x2(ex2(x0), ex2(x1));
+      l_run = add2(l_run, p[n]);
     }
     // ---- weights p 2^e of every group, times F in fp16; if F has to move (rarely), once more
-    uint32_t pb[4][4];  // [group][n]: tokens 8 n + 2 t, + 1
+    uint32_t pk[4][4];  // [group][n]: token 8 n + g, heads 2 t, 2 t + 1
     bool over = move;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
-      f32x2 f2[4];
+      uint32_t high[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f2[j] = f32x2(__uint_as_float(fbits[j]), __uint_as_float(fbits[j]));
+      for (int j = 0; j < 4; ++j) high[j] = wtop[j];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
-        const float4 s01 = sc_out[TT + 2 * (4 * n + t)], s23 = sc_out[TT + 2 * (4 * n + t) + 1];
+        const float4 s01 = sc_out[2 * (TT + 8 * n + g)], s23 = sc_out[2 * (TT + 8 * n + g) + 1];
         const f32x2 vs[4] = {f32x2(s01.x, s01.y), f32x2(s01.z, s01.w), f32x2(s23.x, s23.y), f32x2(s23.z, s23.w)};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const f32x2 w = mul2(p[n], vs[j]);
           float w0, w1;
-          w.get(w0, w1);
-          wmax[j] = max3(wmax[j], w0, w1);
-          mul2(w, f2[j]).get(w0, w1);
-          pb[j][n] = pack_f16x2(w0, w1);
+          mul2(mul2(p[n], vs[j]), fac[j]).get(w0, w1);
+          pk[j][n] = pack_f16x2(w0, w1);
+          high[j] = max_f16x2(high[j], pk[j][n]);
         }
       }
+      const uint32_t all = max_f16x2(max_f16x2(high[0], high[1]), max_f16x2(high[2], high[3]));
+      over |= (all & 0x7fffu) > 0x7800u || all > 0x78000000u + 0xffffu;  // above 2^15 (the weights are not negative)
+      if (pass == 1 || !__any_sync(0xffffffffu, over)) {  // (still over after F has moved: NaN)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)  // wmax F > 2^15, in exponents (an infinity counts)
-        over |= (__float_as_uint(wmax[j]) & 0x7f800000u) + fbits[j] > (127u + 14u + 127u) << 23;
-      if (!__any_sync(0xffffffffu, over)) break;
-      over = false;
+        for (int j = 0; j < 4; ++j) wtop[j] = high[j];
+        break;
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        float q = wmax[j];
-        q = fmaxf(q, __shfl_xor_sync(0xffffffffu, q, 1));
-        q = fmaxf(q, __shfl_xor_sync(0xffffffffu, q, 2));
-        // F = 2^(7 - floor(log2 q)), 2^126 at most
-        const uint32_t f = ((254u + kQFactor) << 23) - max(__float_as_uint(q) & 0x7f800000u, (kQFactor + 1u) << 23);
-        const float ratio = corr * __uint_as_float(f) * __uint_as_float((254u << 23) - fbits[j]);
-        fbits[j] = f;
-        // the accumulators hold heads 2 t and 2 t + 1: their factors are in quads 2 t and 2 t + 1
-        const float r0 = __shfl_sync(0xffffffffu, ratio, 8 * t), r1 = __shfl_sync(0xffffffffu, ratio, 8 * t + 4);
+        float f[2], q[2];
+        fac[j].get(f[0], f[1]);
+        const float2 past = __half22float2(*reinterpret_cast<const __half2*>(&wtop[j]));
+        float old[2] = {past.x * corr[0], past.y * corr[1]};  // largest weight before this tile, times the old F
+        float now[2] = {0.f, 0.f};
 #pragma unroll
-        for (int i = 2 * j; i < 2 * j + 2; ++i) {
-          oacc[i][0] *= r0; oacc[i][1] *= r1; oacc[i][2] *= r0; oacc[i][3] *= r1;
+        for (int n = 0; n < 4; ++n) {
+          const float v = reinterpret_cast<const float*>(sc_out + 2 * (TT + 8 * n + g))[2 * j];
+          float p0, p1;
+          p[n].get(p0, p1);
+          now[0] = fmaxf(now[0], p0 * v);
+          now[1] = fmaxf(now[1], p1 * v);
         }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t fb = __float_as_uint(f[e]);
+          const float inv = __uint_as_float((254u << 23) - fb);
+          q[e] = fmaxf(old[e] * inv, now[e]);
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) q[e] = fmaxf(q[e], __shfl_xor_sync(0xffffffffu, q[e], o));
+          // F = 2^(7 - floor(log2 q)), 2^126 at most
+          f[e] = __uint_as_float(((254u + kQFactor) << 23) - max(__float_as_uint(q[e]) & 0x7f800000u, (kQFactor + 1u) << 23));
+          const float ratio = corr[e] * f[e] * inv;
+          old[e] = old[e] * inv * f[e];
+#pragma unroll
+          for (int i = 2 * j; i < 2 * j + 2; ++i) {
+            oacc[i][e] *= ratio;
+            oacc[i][2 + e] *= ratio;
+          }
+        }
+        fac[j] = f32x2(f[0], f[1]);
+        wtop[j] = pack_f16x2(old[0], old[1]);
       }
+      corr[0] = corr[1] = 1.f;
     }
+    uint32_t pb[4][4];  // [group][n]: tokens 8 n + 2 t, + 1, head g
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) pb[j][n] = transpose8x8(pk[j][n]);
     // ---- O^T += V^T P: step s covers tokens 16 s .. 16 s + 15; m tile 2 j + i holds elements 32 j + 4 g + 2 i (row g), + 1 (row g + 8)
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -533,23 +589,29 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
   }
   cp_async_wait<0>();
 
-  l_run += __shfl_xor_sync(0xffffffffu, l_run, 1);
-  l_run += __shfl_xor_sync(0xffffffffu, l_run, 2);
-  const float m_out = l_run == 0.f ? -INFINITY : m_ref;
+  float l[2], m_out[2];
+  l_run.get(l[0], l[1]);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) l[e] += __shfl_xor_sync(0xffffffffu, l[e], o);
+    m_out[e] = l[e] == 0.f ? -INFINITY : m_ref[e];
+  }
   // back from each group's own power of two
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float inv = __uint_as_float((254u << 23) - fbits[j]);
-    const float r0 = __shfl_sync(0xffffffffu, inv, 8 * t), r1 = __shfl_sync(0xffffffffu, inv, 8 * t + 4);
+    float f0, f1;
+    fac[j].get(f0, f1);
+    const float r0 = __uint_as_float((254u << 23) - __float_as_uint(f0)), r1 = __uint_as_float((254u << 23) - __float_as_uint(f1));
 #pragma unroll
     for (int i = 2 * j; i < 2 * j + 2; ++i) {
       oacc[i][0] *= r0; oacc[i][1] *= r1; oacc[i][2] *= r0; oacc[i][3] *= r1;
     }
   }
   auto park = [&](float* part) {
-    if (t == 0) {
-      part[g * kPartial + kD] = m_out;
-      part[g * kPartial + kD + 1] = l_run;
+    if (g == 0) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) *reinterpret_cast<float2*>(part + (2 * t + e) * kPartial + kD) = make_float2(m_out[e], l[e]);
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
