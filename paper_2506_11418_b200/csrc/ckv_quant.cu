@@ -198,22 +198,26 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
 //   V   two tokens' codes are interleaved by nibble before they are unpacked, which gives the operand's pairs of
 //       neighbouring tokens without permuting fp16 values.
 constexpr int kQT = 32;  // tokens per tile
-constexpr int kQWarps = 4;
 constexpr int kQStages = 3;
-constexpr int kQCtasPerSm = 3;
+constexpr int kQCtaWarps = 4, kQCtasPerSm = 3;  // the persistent launch: twelve warps per SM at 168 registers
+constexpr int kQClusterWarps = 8;               // the cluster launch
+constexpr int kQMinShare = 2;                   // tiles per warp of the persistent launch, at least
 constexpr int kQCodes = kQT * kCodeBytes;
 constexpr int kQStageBytes = 2 * kQCodes + 2 * kQT * kScaleBytes + kQT * 4;  // codes of K, V; scales of K, V; log-degrees
 constexpr int kQScaleOut = 2 * kQT * 32;                                     // a tile's scales of K, V as fp32, twice each
 constexpr int kQWarpBytes = kQStages * kQStageBytes + kQScaleOut;
-constexpr size_t kQSmemBytes = (size_t)kQWarps * kQWarpBytes;
-static_assert(kQSmemBytes >= (size_t)kQWarps * 8 * kPartial * 4 + (size_t)kQWarps * kQWarps * 16 * 4, "the partials and their weights fit");
+static_assert(kQWarpBytes >= 8 * kPartial * 4 + kQClusterWarps * 16 * 4, "cluster_combine's rows and weights take a warp's share or less");
 constexpr float kQLazy = 6.f;           // exponents up to this above the reference are let through
 constexpr uint32_t kQFactor = 7u;       // F puts the largest weight at 2^7 .. 2^8 when it is set; it may grow to 2^15
 
 struct QuantArgs {
-  DecodeArgs d;  // views, q, out, partial, shapes, n_splits (CTAs per pair at max_len), span (tiles per CTA), page_shift
+  DecodeArgs d;        // views, q, out, partial ([warp + pair][G][kPartial], persistent launch), shapes, page_shift
+  int32_t* plan;       // persistent launch, for the combine kernel: tiles of one head before each sequence [Bz + 1], tiles per warp
   ckv_quant_pool pool;
 };
+
+// tiles of a length; a batch's tiles over all heads fit 31 bits (they would be 9 TB of codes)
+__device__ __forceinline__ int tiles_of(int64_t len) { return (int)((max(len, (int64_t)0) + kQT - 1) / kQT); }
 
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
@@ -283,53 +287,109 @@ __device__ __forceinline__ uint32_t v_off(int r, int c) {
   return (uint32_t)(s * kCodeBytes + ((c ^ (s & 2)) << 4));
 }
 
-template <int CL>
-__global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel(const QuantArgs qa_) {
-  constexpr int TT = kQT, NW = kQWarps, ST = kQStages;
+// HALF: at most four query heads.  They stand twice in the columns of S^T, and a lane weighs its two heads for two of the
+// four groups: of the outputs' columns the first four then hold groups 0 and 1, the others 2 and 3.
+//
+// CL > 0: one cluster per (sequence, KV head), its warps share the tiles evenly and join their partials on the chip.
+// CL = 0: as many warps as the GPU holds; each takes an equal share of all tiles of the batch, in the order of the pairs, so a
+// ragged batch is balanced to a tile and every warp runs from start to end.  A share may end in one pair and go on in the
+// next: each stretch leaves a partial at index warp + pair, which no other stretch has.
+template <int CL, bool HALF, int NW>
+__global__ void __launch_bounds__(NW * 32, CL > 0 ? 1 : kQCtasPerSm) decode_quant_kernel(const QuantArgs qa_) {
+  constexpr int TT = kQT, ST = kQStages;
+  constexpr int NU = HALF ? 1 : 2;  // pairs of groups that a lane weighs
   const DecodeArgs& a = qa_.d;
   extern __shared__ __align__(128) unsigned char smem_raw[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t = lane & 3;
+  const int head0 = 2 * (HALF ? t & 1 : t);  // this lane's heads: head0, head0 + 1
   griddep_wait();
   griddep_launch();
-  const int h = blockIdx.y, b = blockIdx.z, G = a.G;
-  const ckv_paged_view view = reinterpret_cast<const ckv_paged_view*>(a.views)[b];
-  const int64_t len = view.len;
-  const int64_t seq_tiles = (len + TT - 1) / TT;
-  int64_t tile0, tile1;  // this warp's tiles
-  if constexpr (CL > 0) {  // the cluster's warps share the sequence's tiles evenly
-    const int split = blockIdx.x * NW + warp;
-    tile0 = seq_tiles * split / (CL * NW);
-    tile1 = seq_tiles * (split + 1) / (CL * NW);
-  } else {                 // every CTA has a span of the same length, so a ragged batch's CTAs are alike
-    const int64_t c0 = (int64_t)blockIdx.x * a.span, c1 = min(seq_tiles, c0 + a.span);
-    if (c0 >= seq_tiles) return;
-    tile0 = c0 + (c1 - c0) * warp / NW;
-    tile1 = c0 + (c1 - c0) * (warp + 1) / NW;
+  const ckv_paged_view* const views = reinterpret_cast<const ckv_paged_view*>(a.views);
+  const int G = a.G;
+  int b, h, tile0;  // where this warp is, and its first tile there
+  int share = 0;    // tiles that it has to do from there (CL = 0)
+  ckv_paged_view view;
+  const int gw = blockIdx.x * NW + warp;
+  if constexpr (CL > 0) {
+    b = blockIdx.z;
+    h = blockIdx.y;
+    view = views[b];
+    tile0 = (int)((int64_t)tiles_of(view.len) * gw / (CL * NW));
+  } else {
+    // tiles of 32 sequences, one per lane, summed up to and with each
+    auto scan = [&](int i, ckv_paged_view& v, int& n) {
+      v = ckv_paged_view{nullptr, 0};
+      if (i + lane < a.Bz) v = views[i + lane];
+      n = tiles_of(v.len);
+      int sum = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += y;
+      }
+      return sum;
+    };
+    ckv_paged_view v;
+    int n, sum = 0, total = 0;  // tiles of one head
+    for (int i = 0; i < a.Bz; i += 32) {
+      sum = scan(i, v, n);
+      if (gw == 0 && i + lane < a.Bz) qa_.plan[i + lane] = total + sum - n;
+      total += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    const uint32_t all = (uint32_t)total * a.H, warps = gridDim.x * NW;
+    share = max((int)((all + warps - 1) / warps), kQMinShare);
+    if (gw == 0 && lane == 0) {
+      qa_.plan[a.Bz] = total;
+      qa_.plan[a.Bz + 1] = share;
+    }
+    const int64_t start64 = (int64_t)gw * share;
+    if (start64 >= all) return;
+    const int start = (int)start64;
+    share = min(share, (int)(all - start));
+    int before = 0;  // tiles of all heads before the 32 sequences
+    for (b = 0;; b += 32) {
+      if (a.Bz > 32) sum = scan(b, v, n);  // (else they are at hand)
+      const uint32_t past = __ballot_sync(0xffffffffu, before + sum * a.H > start);
+      if (past) {
+        const int l = __ffs((int)past) - 1, of_b = __shfl_sync(0xffffffffu, n, l);
+        const int rest = start - before - __shfl_sync(0xffffffffu, sum - n, l) * a.H;
+        b += l;
+        h = rest / of_b;
+        tile0 = rest - h * of_b;
+        view.block_table = reinterpret_cast<const int32_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(v.block_table), l));
+        view.len = __shfl_sync(0xffffffffu, v.len, l);
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, sum, 31) * a.H;
+    }
   }
-  const int64_t t_begin = tile0 * TT, t_end = min(len, tile1 * TT);
-  const int ntiles = (int)(tile1 - tile0);
-  const int64_t n_blocks = (len + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift;
-  int64_t blk0 = t_begin >> a.page_shift;
-  int my_page = (ntiles > 0 && blk0 + lane < n_blocks) ? view.block_table[blk0 + lane] : 0;
   unsigned char* const mine = smem_raw + (size_t)warp * kQWarpBytes;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(mine);
   float4* const sc_out = reinterpret_cast<float4*>(mine + ST * kQStageBytes);  // [K, V][token][groups 0 0 1 1, 2 2 3 3]
   const float* logdeg = qa_.pool.logdeg_pages;
 
+  for (;;) {  // one stretch of tiles of one (sequence, KV head)
+  const int len = (int)view.len, seq_tiles = tiles_of(view.len);
+  const int ntiles = CL > 0 ? (int)((int64_t)seq_tiles * (gw + 1) / (CL * NW)) - tile0 : min(share, seq_tiles - tile0);
+  const int n_tail = len - (seq_tiles - 1) * TT;  // tokens of the sequence's last tile
+  const int tile_shift = a.page_shift - 5;        // tiles per page
+  const int n_blocks = (seq_tiles + (1 << tile_shift) - 1) >> tile_shift;
+  int blk0 = tile0 >> tile_shift;
+  int my_page = (ntiles > 0 && blk0 + lane < n_blocks) ? view.block_table[blk0 + lane] : 0;
+
   // piece i of a tile of codes is row 8 i + lane / 4, 16 bytes lane % 4: 512 bytes on in memory, 256 in the tile of V
   const uint32_t v_dst = kQCodes + v_off(lane >> 2, lane & 3);
   auto issue = [&](int tile) {
-    const int64_t t0 = t_begin + (int64_t)tile * TT;
     const uint32_t st = ring + (uint32_t)(tile % ST) * kQStageBytes;
-    const int64_t blk = t0 >> a.page_shift;
+    const int at = tile0 + tile, blk = at >> tile_shift;
     if (blk >= blk0 + 32) {  // next 32 entries of the table (tiles are issued in order)
       blk0 = blk;
       my_page = blk0 + lane < n_blocks ? view.block_table[blk0 + lane] : 0;
     }
-    const int page = __shfl_sync(0xffffffffu, my_page, (int)(blk - blk0));
-    const int64_t row0 = (((int64_t)page * a.H + h) << a.page_shift) + (t0 & (((int64_t)1 << a.page_shift) - 1));
-    const int nt = (int)min((int64_t)TT, t_end - t0);
+    const int page = __shfl_sync(0xffffffffu, my_page, blk - blk0);
+    const int64_t row0 = (((int64_t)page * a.H + h) << a.page_shift) + (at & ((1 << tile_shift) - 1)) * TT;
+    const int nt = at == seq_tiles - 1 ? n_tail : TT;
     const unsigned char* kc = qa_.pool.k_codes + row0 * kCodeBytes + lane * 16;
     const unsigned char* vc = qa_.pool.v_codes + row0 * kCodeBytes + lane * 16;
     const unsigned char* s = (lane < 8 ? qa_.pool.k_scales : qa_.pool.v_scales) + row0 * kScaleBytes + (lane & 7) * 16;
@@ -365,7 +425,8 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       uint4 u = make_uint4(0u, 0u, 0u, 0u);
-      if (g < G) u = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + (((int64_t)b * a.H + h) * G + g) * kD)[4 * j + t];
+      const int head = HALF ? g & 3 : g;
+      if (head < G) u = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + (((int64_t)b * a.H + h) * G + head) * kD)[4 * j + t];
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -388,15 +449,17 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
   float oacc[8][4];
 #pragma unroll
   for (int i = 0; i < 8; ++i) oacc[i][0] = oacc[i][1] = oacc[i][2] = oacc[i][3] = 0.f;
-  // this thread's two heads, 2 t and 2 t + 1: the columns of S^T and O^T that it holds
-  const f32x2 sc2(__shfl_sync(0xffffffffu, sc, 8 * t), __shfl_sync(0xffffffffu, sc, 8 * t + 4));
+  const f32x2 sc2(__shfl_sync(0xffffffffu, sc, 4 * head0), __shfl_sync(0xffffffffu, sc, 4 * head0 + 4));
   float m_ref[2] = {0.f, 0.f};          // the exponents' reference
   bool seen[2] = {false, false};        // a score above -inf has been met
   f32x2 l_run(0.f, 0.f);                // this thread's share of the sum
-  f32x2 fac[4];                         // F of each group
-  uint32_t wtop[4] = {0u, 0u, 0u, 0u};  // this thread's largest weight of each group, times F, in fp16
+  f32x2 fac[2 * NU];                    // F of each group
+  uint32_t wtop[2 * NU];                // this thread's largest weight of each group, times F, in fp16
 #pragma unroll
-  for (int j = 0; j < 4; ++j) fac[j] = f32x2(__uint_as_float(253u << 23), __uint_as_float(253u << 23));
+  for (int j = 0; j < 2 * NU; ++j) {
+    fac[j] = f32x2(__uint_as_float(253u << 23), __uint_as_float(253u << 23));
+    wtop[j] = 0u;
+  }
 
 #pragma unroll
   for (int i = 0; i < ST - 1; ++i) {
@@ -409,7 +472,7 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
     if (tile + ST - 1 < ntiles) issue(tile + ST - 1);
     cp_async_commit();
     const unsigned char* st = mine + (size_t)(tile % ST) * kQStageBytes;
-    const int nt = (int)min((int64_t)TT, t_end - (t_begin + (int64_t)tile * TT));
+    const int nt = tile0 + tile == seq_tiles - 1 ? n_tail : TT;
 
     // ---- scales: one token per lane
     {
@@ -418,7 +481,7 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
       scales_f32(w[TT + lane], sc_out + 2 * (TT + lane));
       __syncwarp();
     }
-    // ---- exponents of tokens 8 n + g with heads 2 t, 2 t + 1, relative to the reference
+    // ---- exponents of tokens 8 n + g with this lane's heads, relative to the reference
     f32x2 x[4];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -491,98 +554,103 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
       p[n] = f32x2(ex2(x0), ex2(x1));
       l_run = add2(l_run, p[n]);
     }
-    // ---- weights p 2^e of every group, times F in fp16; if F has to move (rarely), once more
-    uint32_t pk[4][4];  // [group][n]: token 8 n + g, heads 2 t, 2 t + 1
-    bool over = move;
+    // ---- weights p 2^e of two groups times F in fp16, then their O^T += V^T P
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const float4* const v_scales = sc_out + 2 * (TT + g) + (HALF ? t >> 1 : u);
+      uint32_t pk[2][4];  // [group][n]: token 8 n + g, this lane's heads
+      bool over = move;
 #pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-      uint32_t high[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) high[j] = wtop[j];
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const float4 s01 = sc_out[2 * (TT + 8 * n + g)], s23 = sc_out[2 * (TT + 8 * n + g) + 1];
-        const f32x2 vs[4] = {f32x2(s01.x, s01.y), f32x2(s01.z, s01.w), f32x2(s23.x, s23.y), f32x2(s23.z, s23.w)};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float w0, w1;
-          mul2(mul2(p[n], vs[j]), fac[j]).get(w0, w1);
-          pk[j][n] = pack_f16x2(w0, w1);
-          high[j] = max_f16x2(high[j], pk[j][n]);
-        }
-      }
-      const uint32_t all = max_f16x2(max_f16x2(high[0], high[1]), max_f16x2(high[2], high[3]));
-      over |= (all & 0x7fffu) > 0x7800u || all > 0x78000000u + 0xffffu;  // above 2^15 (the weights are not negative)
-      if (pass == 1 || !__any_sync(0xffffffffu, over)) {  // (still over after F has moved: NaN)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) wtop[j] = high[j];
-        break;
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float f[2], q[2];
-        fac[j].get(f[0], f[1]);
-        const float2 past = __half22float2(*reinterpret_cast<const __half2*>(&wtop[j]));
-        float old[2] = {past.x * corr[0], past.y * corr[1]};  // largest weight before this tile, times the old F
-        float now[2] = {0.f, 0.f};
+      for (int pass = 0; pass < 2; ++pass) {  // (once more if F has to move, which is rare)
+        uint32_t high[2] = {wtop[2 * u], wtop[2 * u + 1]};
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-          const float v = reinterpret_cast<const float*>(sc_out + 2 * (TT + 8 * n + g))[2 * j];
-          float p0, p1;
-          p[n].get(p0, p1);
-          now[0] = fmaxf(now[0], p0 * v);
-          now[1] = fmaxf(now[1], p1 * v);
-        }
+          const float4 s01 = v_scales[16 * n];
+          const f32x2 vs[2] = {f32x2(s01.x, s01.y), f32x2(s01.z, s01.w)};
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t fb = __float_as_uint(f[e]);
-          const float inv = __uint_as_float((254u << 23) - fb);
-          q[e] = fmaxf(old[e] * inv, now[e]);
-#pragma unroll
-          for (int o = 4; o < 32; o <<= 1) q[e] = fmaxf(q[e], __shfl_xor_sync(0xffffffffu, q[e], o));
-          // F = 2^(7 - floor(log2 q)), 2^126 at most
-          f[e] = __uint_as_float(((254u + kQFactor) << 23) - max(__float_as_uint(q[e]) & 0x7f800000u, (kQFactor + 1u) << 23));
-          const float ratio = corr[e] * f[e] * inv;
-          old[e] = old[e] * inv * f[e];
-#pragma unroll
-          for (int i = 2 * j; i < 2 * j + 2; ++i) {
-            oacc[i][e] *= ratio;
-            oacc[i][2 + e] *= ratio;
+          for (int j = 0; j < 2; ++j) {
+            float w0, w1;
+            mul2(mul2(p[n], vs[j]), fac[2 * u + j]).get(w0, w1);
+            pk[j][n] = pack_f16x2(w0, w1);
+            high[j] = max_f16x2(high[j], pk[j][n]);
           }
         }
-        fac[j] = f32x2(f[0], f[1]);
-        wtop[j] = pack_f16x2(old[0], old[1]);
+        const uint32_t all = max_f16x2(high[0], high[1]);
+        over |= (all & 0x7fffu) > 0x7800u || all > 0x7800ffffu;  // above 2^15 (the weights are not negative)
+        if (pass == 1 || !__any_sync(0xffffffffu, over)) {  // (still over after F has moved: NaN)
+          wtop[2 * u] = high[0];
+          wtop[2 * u + 1] = high[1];
+          break;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float f[2], q[2];
+          fac[2 * u + j].get(f[0], f[1]);
+          const float2 past = __half22float2(*reinterpret_cast<const __half2*>(&wtop[2 * u + j]));
+          float old[2] = {past.x * corr[0], past.y * corr[1]};  // largest weight before this tile, times the old F
+          float now[2] = {0.f, 0.f};
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            const float v = reinterpret_cast<const float*>(v_scales + 16 * n)[2 * j];
+            float p0, p1;
+            p[n].get(p0, p1);
+            now[0] = fmaxf(now[0], p0 * v);
+            now[1] = fmaxf(now[1], p1 * v);
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float inv = __uint_as_float((254u << 23) - __float_as_uint(f[e]));
+            q[e] = fmaxf(old[e] * inv, now[e]);
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) q[e] = fmaxf(q[e], __shfl_xor_sync(0xffffffffu, q[e], o));
+            // F = 2^(7 - floor(log2 q)), 2^126 at most
+            f[e] = __uint_as_float(((254u + kQFactor) << 23) - max(__float_as_uint(q[e]) & 0x7f800000u, (kQFactor + 1u) << 23));
+            const float ratio = corr[e] * f[e] * inv;
+            old[e] = old[e] * inv * f[e];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              oacc[2 * (2 * u + j) + i][e] *= ratio;
+              oacc[2 * (2 * u + j) + i][2 + e] *= ratio;
+              if (HALF) {
+                oacc[2 * (2 + j) + i][e] *= ratio;
+                oacc[2 * (2 + j) + i][2 + e] *= ratio;
+              }
+            }
+          }
+          fac[2 * u + j] = f32x2(f[0], f[1]);
+          wtop[2 * u + j] = pack_f16x2(old[0], old[1]);
+        }
       }
-      corr[0] = corr[1] = 1.f;
-    }
-    uint32_t pb[4][4];  // [group][n]: tokens 8 n + 2 t, + 1, head g
+      // step s covers tokens 16 s .. 16 s + 15; m tile 2 j + i holds elements 32 j + 4 g + 2 i (row g), + 1 (row g + 8)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int s = 0; s < 2; ++s) {
+        uint32_t v[4][3 - NU], pb[2][2];
 #pragma unroll
-      for (int n = 0; n < 4; ++n) pb[j][n] = transpose8x8(pk[j][n]);
-    // ---- O^T += V^T P: step s covers tokens 16 s .. 16 s + 15; m tile 2 j + i holds elements 32 j + 4 g + 2 i (row g), + 1 (row g + 8)
+        for (int e = 0; e < 4; ++e) {  // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+          const int r = 16 * s + 2 * t + (e & 1) + 8 * (e >> 1);
+          const unsigned char* at = st + kQCodes + v_off(r, g >> 1) + (g & 1) * 8;
+          if constexpr (HALF) {
+            const uint2 x = *reinterpret_cast<const uint2*>(at);
+            v[e][0] = x.x;
+            v[e][1] = x.y;
+          } else {
+            v[e][0] = *reinterpret_cast<const uint32_t*>(at + 4 * u);
+          }
+        }
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const unsigned char* vt = st + kQCodes;
-      uint2 v4[4];
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {  // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-        const int r = 16 * s + 2 * t + (e & 1) + 8 * (e >> 1);
-        v4[e] = *reinterpret_cast<const uint2*>(vt + v_off(r, g >> 1) + (g & 1) * 8);
-      }
+          for (int i = 0; i < 2; ++i) pb[j][i] = transpose8x8(pk[j][2 * s + i]);  // tokens 8 n + 2 t, + 1, column g
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {  // groups 2 u and 2 u + 1
-        const uint32_t a0 = u ? v4[0].y : v4[0].x, b0 = u ? v4[1].y : v4[1].x, a1 = u ? v4[2].y : v4[2].x, b1 = u ? v4[3].y : v4[3].x;
-        constexpr uint32_t lo = 0x0f0f0f0fu, hi = 0xf0f0f0f0u;
-        uint32_t e0[4], o0[4], e1[4], o1[4];  // even / odd elements of tokens (2 t, + 1) and (2 t + 8, + 9)
-        ptx::unpack_e2m1x8((a0 & lo) | ((b0 << 4) & hi), e0);
-        ptx::unpack_e2m1x8(((a0 >> 4) & lo) | (b0 & hi), o0);
-        ptx::unpack_e2m1x8((a1 & lo) | ((b1 << 4) & hi), e1);
-        ptx::unpack_e2m1x8(((a1 >> 4) & lo) | (b1 & hi), o1);
+        for (int y = 0; y < 3 - NU; ++y) {
+          constexpr uint32_t lo = 0x0f0f0f0fu, hi = 0xf0f0f0f0u;
+          uint32_t e0[4], o0[4], e1[4], o1[4];  // even / odd elements of tokens (2 t, + 1) and (2 t + 8, + 9)
+          ptx::unpack_e2m1x8((v[0][y] & lo) | ((v[1][y] << 4) & hi), e0);
+          ptx::unpack_e2m1x8(((v[0][y] >> 4) & lo) | (v[1][y] & hi), o0);
+          ptx::unpack_e2m1x8((v[2][y] & lo) | ((v[3][y] << 4) & hi), e1);
+          ptx::unpack_e2m1x8(((v[2][y] >> 4) & lo) | (v[3][y] & hi), o1);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int j = 2 * u + (i >> 1);
-          ptx::mma_f16(oacc[4 * u + i], e0[i], o0[i], e1[i], o1[i], pb[j][2 * s], pb[j][2 * s + 1]);
+          for (int i = 0; i < 4; ++i) ptx::mma_f16(oacc[4 * (u + y) + i], e0[i], o0[i], e1[i], o1[i], pb[i >> 1][0], pb[i >> 1][1]);
         }
       }
     }
@@ -601,7 +669,7 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     float f0, f1;
-    fac[j].get(f0, f1);
+    fac[HALF ? j & 1 : j].get(f0, f1);
     const float r0 = __uint_as_float((254u << 23) - __float_as_uint(f0)), r1 = __uint_as_float((254u << 23) - __float_as_uint(f1));
 #pragma unroll
     for (int i = 2 * j; i < 2 * j + 2; ++i) {
@@ -609,93 +677,110 @@ __global__ void __launch_bounds__(kQWarps * 32, kQCtasPerSm) decode_quant_kernel
     }
   }
   auto park = [&](float* part) {
-    if (g == 0) {
+    if (g == 0 && (!HALF || t < 2)) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) *reinterpret_cast<float2*>(part + (2 * t + e) * kPartial + kD) = make_float2(m_out[e], l[e]);
+      for (int e = 0; e < 2; ++e) *reinterpret_cast<float2*>(part + (head0 + e) * kPartial + kD) = make_float2(m_out[e], l[e]);
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      float* o = part + (2 * t + e) * kPartial + 4 * g;
+      float* o = part + (head0 + e) * kPartial + 4 * g;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<float4*>(o + 32 * j) = make_float4(oacc[2 * j][e], oacc[2 * j][2 + e], oacc[2 * j + 1][e], oacc[2 * j + 1][2 + e]);
+        if (!HALF || (j >> 1) == (t >> 1))
+          *reinterpret_cast<float4*>(o + 32 * j) = make_float4(oacc[2 * j][e], oacc[2 * j][2 + e], oacc[2 * j + 1][e], oacc[2 * j + 1][2 + e]);
     }
   };
   if constexpr (CL > 0) {
     cluster_combine<CL, NW>(smem_raw, warp, lane, G, reinterpret_cast<__nv_bfloat16*>(a.out) + ((int64_t)b * a.H + h) * G * kD, park);
-  } else {
-    // the CTA's four partials become one: a quarter of the traffic to and from the workspace
-    __syncthreads();
-    float* part = reinterpret_cast<float*>(smem_raw);
-    park(part + warp * 8 * kPartial);
-    __syncthreads();
-    for (int head = warp; head < G; head += NW) {
-      const float* r = part + head * kPartial;
-      float mm = -INFINITY, ll = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) mm = fmaxf(mm, r[w * 8 * kPartial + kD]);
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float* x = r + w * 8 * kPartial;
-        const float f = x[kD] == -INFINITY ? 0.f : exp2f(x[kD] - mm);
-        const float4 y = *reinterpret_cast<const float4*>(x + lane * 4);
-        o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
-        ll = fmaf(f, x[kD + 1], ll);
-      }
-      float* dst = a.partial + ((((int64_t)b * a.H + h) * G + head) * a.n_splits + blockIdx.x) * kPartial;
-      *reinterpret_cast<float4*>(dst + lane * 4) = o;
-      if (lane == 0) *reinterpret_cast<float2*>(dst + kD) = make_float2(mm, ll);
-    }
+    return;
+  }
+  __syncwarp();  // the ring is read: the partial takes its place, and leaves in whole rows
+  float* const part = reinterpret_cast<float*>(mine);
+  park(part);
+  __syncwarp();
+  float4* const dst = reinterpret_cast<float4*>(a.partial + (gw + (int64_t)b * a.H + h) * G * kPartial);
+  for (int i = lane; i < G * (kPartial / 4); i += 32) dst[i] = reinterpret_cast<const float4*>(part)[i];
+  share -= ntiles;
+  if (share <= 0) return;
+  __syncwarp();
+  tile0 = 0;
+  if (++h == a.H) {
+    h = 0;
+    do view = views[++b];
+    while (view.len <= 0);  // (tiles are left, so a later sequence has some)
+  }
   }
 }
 
-// One warp per (sequence, query head) joins the partials of the spans that the sequence has: a lane owns four columns.
+// One CTA per (sequence, query head) joins the partials of the stretches that cover its pair: its warps take every fourth, a
+// lane owns four columns.
 constexpr int kQCombThreads = 128;
 
-__global__ void __launch_bounds__(kQCombThreads) quant_combine_kernel(const DecodeArgs a) {
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * (kQCombThreads / 32) + (threadIdx.x >> 5);
+__global__ void __launch_bounds__(kQCombThreads) quant_combine_kernel(const QuantArgs qa_) {
+  constexpr int W = kQCombThreads / 32;
+  __shared__ float s_max[W], s_sum[W];
+  __shared__ float4 s_out[W][32];
+  const DecodeArgs& a = qa_.d;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int row = blockIdx.x, pair = row / a.G, b = pair / a.H, h = pair - b * a.H;
   griddep_wait();
   griddep_launch();
-  if (row >= (int64_t)a.Bz * a.H * a.G) return;
-  const int64_t len = reinterpret_cast<const ckv_paged_view*>(a.views)[row / (a.H * a.G)].len;
-  const int n = (int)min((int64_t)a.n_splits, ((len + kQT - 1) / kQT + a.span - 1) / a.span);
-  const float* p = a.partial + row * a.n_splits * kPartial;
+  const int t0 = qa_.plan[b], tiles = qa_.plan[b + 1] - t0, share = qa_.plan[a.Bz + 1];
+  const int first = t0 * a.H + h * tiles;                // of all tiles, in the order of the pairs
+  const int w0 = first / share, w1 = tiles > 0 ? (first + tiles - 1) / share : w0 - 1;
+  const int64_t step = (int64_t)a.G * kPartial;
+  const float* p = a.partial + ((int64_t)(w0 + pair) * a.G + (row - pair * a.G)) * kPartial;
+  const int n = w1 - w0 + 1;
   float mm = -INFINITY;
-  for (int s = lane; s < n; s += 32) mm = fmaxf(mm, p[(int64_t)s * kPartial + kD]);
+  for (int s = tid; s < n; s += kQCombThreads) mm = fmaxf(mm, p[s * step + kD]);
   mm = warp_max(mm);
+  if (lane == 0) s_max[warp] = mm;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < W; ++w) mm = fmaxf(mm, s_max[w]);
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   float ll = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < n; ++s) {
-    const float* r = p + (int64_t)s * kPartial;
+#pragma unroll 8
+  for (int s = warp; s < n; s += W) {
+    const float* r = p + s * step;
     const float2 ml = *reinterpret_cast<const float2*>(r + kD);
     const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mm);
     const float4 y = *reinterpret_cast<const float4*>(r + lane * 4);
     o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
     ll = fmaf(f, ml.y, ll);
   }
-  const float inv = ll == 0.f ? 0.f : 1.f / ll;
-  store4(reinterpret_cast<__nv_bfloat16*>(a.out) + row * kD + lane * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  s_out[warp][lane] = o;
+  if (lane == 0) s_sum[warp] = ll;
+  __syncthreads();
+  if (warp == 0) {
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+      const float4 y = s_out[w][lane];
+      o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
+      ll += s_sum[w];
+    }
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+    store4(reinterpret_cast<__nv_bfloat16*>(a.out) + (int64_t)row * kD + lane * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  }
 }
 
 // Sets the kernel's shared memory (and a cluster size above 8) once per device; how many clusters fit at once, 0: none
-template <int CL>
+template <int CL, bool HALF, int NW>
 int quant_clusters() {
   constexpr int kMaxDev = 64;
   static std::atomic<int> cached[kMaxDev];  // 0 = not asked yet, else the answer + 1
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDev) return 0;
   if ((n = cached[dev].load(std::memory_order_relaxed)) > 0) return n - 1;
-  bool ok = cudaFuncSetAttribute(decode_quant_kernel<CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kQSmemBytes) == cudaSuccess;
-  if (ok && CL > 8) ok = cudaFuncSetAttribute(decode_quant_kernel<CL>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+  auto kern = decode_quant_kernel<CL, HALF, NW>;
+  bool ok = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NW * kQWarpBytes) == cudaSuccess;
+  if (ok && CL > 8) ok = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
   if (ok && CL == 0) n = 1;
   if (ok && CL > 0) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(CL, 1, 1);
-    cfg.blockDim = dim3(kQWarps * 32);
-    cfg.dynamicSmemBytes = kQSmemBytes;
+    cfg.blockDim = dim3(NW * 32);
+    cfg.dynamicSmemBytes = NW * kQWarpBytes;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = CL;
@@ -703,7 +788,7 @@ int quant_clusters() {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, decode_quant_kernel<CL>, &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) {
       n = 0;
       cudaGetLastError();  // a refusal here only means "not this cluster size"
     }
@@ -712,13 +797,21 @@ int quant_clusters() {
   return n;
 }
 
-template <int CL>
+// CTAs of the persistent launch: what the GPU holds, or less where max_len says that there is less to do
+int64_t quant_ctas(int32_t Bz, int32_t H, int64_t max_len) {
+  const int64_t tiles = (int64_t)Bz * H * ((max_len + kQT - 1) / kQT), per = kQCtaWarps * kQMinShare;
+  return std::min<int64_t>((int64_t)kQCtasPerSm * sm_count(), std::max<int64_t>(1, (tiles + per - 1) / per));
+}
+
+inline size_t quant_plan_bytes(int32_t Bz) { return ((size_t)(Bz + 2) * 4 + 255) / 256 * 256; }
+
+template <int CL, bool HALF, int NW>
 cudaError_t launch_quant(const QuantArgs& a, cudaStream_t st) {
-  if (quant_clusters<CL>() < 1) return cudaErrorInvalidConfiguration;
+  if (quant_clusters<CL, HALF, NW>() < 1) return cudaErrorInvalidConfiguration;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(CL > 0 ? CL : a.d.n_splits), (unsigned)a.d.H, (unsigned)a.d.Bz);
-  cfg.blockDim = dim3(kQWarps * 32);
-  cfg.dynamicSmemBytes = kQSmemBytes;
+  cfg.gridDim = CL > 0 ? dim3(CL, (unsigned)a.d.H, (unsigned)a.d.Bz) : dim3((unsigned)quant_ctas(a.d.Bz, a.d.H, a.d.max_len));
+  cfg.blockDim = dim3(NW * 32);
+  cfg.dynamicSmemBytes = NW * kQWarpBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -729,23 +822,19 @@ cudaError_t launch_quant(const QuantArgs& a, cudaStream_t st) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CL > 0 ? 2 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, decode_quant_kernel<CL>, a);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, decode_quant_kernel<CL, HALF, NW>, a);
   if (e != cudaSuccess || CL > 0) return e;
-  const int64_t rows = (int64_t)a.d.Bz * a.d.H * a.d.G, per = kQCombThreads / 32;
-  return launch_dependent(quant_combine_kernel, dim3((unsigned)((rows + per - 1) / per)), dim3(kQCombThreads), 0, st, a.d);
+  return launch_dependent(quant_combine_kernel, dim3((unsigned)(a.d.Bz * a.d.H * a.d.G)), dim3(kQCombThreads), 0, st, a);
 }
 
-// Tiles per CTA of a launch that joins its partials in a second kernel: four waves of CTAs if all sequences were max_len
-// long, eight tiles per warp at least, and no more than 65535 spans.
-int64_t quant_span(int32_t Bz, int32_t H, int64_t max_len) {
-  const int64_t pairs = (int64_t)Bz * H, slots = (int64_t)kQCtasPerSm * sm_count();
-  const int64_t tiles = (max_len + kQT - 1) / kQT;
-  return std::max({(pairs * tiles + 4 * slots - 1) / (4 * slots), (int64_t)8 * kQWarps, (tiles + 65534) / 65535});
-}
-
-int64_t quant_splits(int32_t Bz, int32_t H, int64_t max_len) {
-  const int64_t span = quant_span(Bz, H, max_len);
-  return std::max<int64_t>(1, ((max_len + kQT - 1) / kQT + span - 1) / span);
+template <bool HALF>
+cudaError_t launch_quant_heads(const QuantArgs& a, cudaStream_t st) {
+  // few pairs: one cluster each, the largest of which all are resident at once
+  const int64_t pairs = (int64_t)a.d.Bz * a.d.H;
+  if (quant_clusters<16, HALF, kQClusterWarps>() >= pairs) return launch_quant<16, HALF, kQClusterWarps>(a, st);
+  if (quant_clusters<10, HALF, kQClusterWarps>() >= pairs) return launch_quant<10, HALF, kQClusterWarps>(a, st);
+  if (quant_clusters<8, HALF, kQClusterWarps>() >= pairs) return launch_quant<8, HALF, kQClusterWarps>(a, st);
+  return launch_quant<0, HALF, kQCtaWarps>(a, st);
 }
 
 int check_pool(const ckv_quant_pool* p) {
@@ -806,7 +895,8 @@ int ckv_pages_dequantize(const int32_t* block_table, int64_t len, const ckv_quan
 
 size_t ckv_decode_quantized_workspace_bytes(int32_t Bz, int32_t H, int32_t G, int32_t D, int64_t max_len) {
   if (Bz <= 0 || H <= 0 || G <= 0 || D <= 0 || max_len < 0) return 0;
-  return ((size_t)Bz * H * G * quant_splits(Bz, H, max_len) * kPartial * sizeof(float) + 255) / 256 * 256;
+  const size_t stretches = (size_t)quant_ctas(Bz, H, max_len) * kQCtaWarps + (size_t)Bz * H;
+  return quant_plan_bytes(Bz) + (stretches * G * kPartial * sizeof(float) + 255) / 256 * 256;
 }
 
 int ckv_decode_attn_quantized(const ckv_paged_view* views_dev, const ckv_quant_pool* pool, int32_t page_tokens, int32_t Bz, int32_t H, int32_t G,
@@ -823,21 +913,15 @@ int ckv_decode_attn_quantized(const ckv_paged_view* views_dev, const ckv_quant_p
   if (!workspace || workspace_bytes < need || !aligned16(workspace)) return CKV_ERR_WORKSPACE;
   QuantArgs a{};
   a.d.views = views_dev; a.d.q = q; a.d.out = out;
-  a.d.partial = static_cast<float*>(workspace);
+  a.plan = static_cast<int32_t*>(workspace);
+  a.d.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + quant_plan_bytes(Bz));
   a.d.Bz = Bz; a.d.H = H; a.d.G = G;
-  a.d.n_splits = (int32_t)quant_splits(Bz, H, max_len);
-  a.d.span = quant_span(Bz, H, max_len);
   a.d.max_len = max_len;
   a.d.scale = scale;
   a.d.page_shift = shift;
   a.pool = *pool;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  // Few pairs: one cluster each, joined on the chip, the largest of which all are resident at once.  More: spans of equal
-  // length and a second kernel.
-  const int64_t pairs = (int64_t)Bz * H;
-  const cudaError_t e = quant_clusters<16>() >= pairs ? launch_quant<16>(a, stream)
-                        : quant_clusters<8>() >= pairs ? launch_quant<8>(a, stream)
-                                                       : launch_quant<0>(a, stream);
+  const cudaError_t e = G <= 4 ? launch_quant_heads<true>(a, stream) : launch_quant_heads<false>(a, stream);
   return e == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
