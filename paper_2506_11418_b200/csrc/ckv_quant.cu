@@ -712,54 +712,54 @@ __global__ void __launch_bounds__(NW * 32, CL > 0 ? 1 : kQCtasPerSm) decode_quan
   }
 }
 
-// One CTA per (sequence, query head) joins the partials of the stretches that cover its pair: its warps take every fourth, a
-// lane owns four columns.
+// One CTA per (sequence, query head) joins the partials of the stretches that cover its pair: every warp takes every fourth, a
+// lane owns four columns, and the loads of four partials are in flight at once.
 constexpr int kQCombThreads = 128;
 
 __global__ void __launch_bounds__(kQCombThreads) quant_combine_kernel(const QuantArgs qa_) {
   constexpr int W = kQCombThreads / 32;
-  __shared__ float s_max[W], s_sum[W];
+  __shared__ float2 s_ml[W];
   __shared__ float4 s_out[W][32];
   const DecodeArgs& a = qa_.d;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row = blockIdx.x, pair = row / a.G, b = pair / a.H, h = pair - b * a.H;
   griddep_wait();
   griddep_launch();
   const int t0 = qa_.plan[b], tiles = qa_.plan[b + 1] - t0, share = qa_.plan[a.Bz + 1];
   const int first = t0 * a.H + h * tiles;                // of all tiles, in the order of the pairs
-  const int w0 = first / share, w1 = tiles > 0 ? (first + tiles - 1) / share : w0 - 1;
+  const int w0 = first / share, n = tiles > 0 ? (first + tiles - 1) / share - w0 + 1 : 0;
   const int64_t step = (int64_t)a.G * kPartial;
   const float* p = a.partial + ((int64_t)(w0 + pair) * a.G + (row - pair * a.G)) * kPartial;
-  const int n = w1 - w0 + 1;
-  float mm = -INFINITY;
-  for (int s = tid; s < n; s += kQCombThreads) mm = fmaxf(mm, p[s * step + kD]);
-  mm = warp_max(mm);
-  if (lane == 0) s_max[warp] = mm;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < W; ++w) mm = fmaxf(mm, s_max[w]);
+  float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  float ll = 0.f;
-#pragma unroll 8
-  for (int s = warp; s < n; s += W) {
-    const float* r = p + s * step;
-    const float2 ml = *reinterpret_cast<const float2*>(r + kD);
-    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mm);
-    const float4 y = *reinterpret_cast<const float4*>(r + lane * 4);
-    o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
-    ll = fmaf(f, ml.y, ll);
+  auto add = [&](float2 ml, float4 y) {  // out, max and sum of one more partial
+    const float mm = fmaxf(m, ml.x);
+    if (mm == -INFINITY && !(ml.y != 0.f)) return;  // (no tokens, or only tokens of weight zero)
+    const float c = m == -INFINITY ? 0.f : exp2f(m - mm), f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mm);
+    o.x = fmaf(f, y.x, o.x * c); o.y = fmaf(f, y.y, o.y * c); o.z = fmaf(f, y.z, o.z * c); o.w = fmaf(f, y.w, o.w * c);
+    l = fmaf(f, ml.y, l * c);
+    m = mm;
+  };
+  for (int s = warp; s < n; s += 4 * W) {
+    float2 ml[4];
+    float4 y[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const bool ok = s + u * W < n;
+      const float* r = p + (s + u * W) * step;
+      ml[u] = ok ? *reinterpret_cast<const float2*>(r + kD) : make_float2(-INFINITY, 0.f);
+      y[u] = ok ? *reinterpret_cast<const float4*>(r + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) add(ml[u], y[u]);
   }
   s_out[warp][lane] = o;
-  if (lane == 0) s_sum[warp] = ll;
+  if (lane == 0) s_ml[warp] = make_float2(m, l);
   __syncthreads();
   if (warp == 0) {
 #pragma unroll
-    for (int w = 1; w < W; ++w) {
-      const float4 y = s_out[w][lane];
-      o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
-      ll += s_sum[w];
-    }
-    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+    for (int w = 1; w < W; ++w) add(s_ml[w], s_out[w][lane]);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     store4(reinterpret_cast<__nv_bfloat16*>(a.out) + (int64_t)row * kD + lane * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
   }
 }
@@ -829,11 +829,14 @@ cudaError_t launch_quant(const QuantArgs& a, cudaStream_t st) {
 
 template <bool HALF>
 cudaError_t launch_quant_heads(const QuantArgs& a, cudaStream_t st) {
-  // few pairs: one cluster each, the largest of which all are resident at once
-  const int64_t pairs = (int64_t)a.d.Bz * a.d.H;
-  if (quant_clusters<16, HALF, kQClusterWarps>() >= pairs) return launch_quant<16, HALF, kQClusterWarps>(a, st);
-  if (quant_clusters<10, HALF, kQClusterWarps>() >= pairs) return launch_quant<10, HALF, kQClusterWarps>(a, st);
-  if (quant_clusters<8, HALF, kQClusterWarps>() >= pairs) return launch_quant<8, HALF, kQClusterWarps>(a, st);
+  // Few pairs: one cluster each, the largest of which all are resident at once, unless the sequences are so long that the
+  // SMs a cluster cannot use (all but 80 of 148 for 8 pairs) count for more than the second kernel (about 5 us).  8 pairs
+  // of 16416 tokens: 15.1 us by clusters, 16.9 by shares; of 131072 tokens: 67 and 47.
+  const int64_t pairs = (int64_t)a.d.Bz * a.d.H, tiles = (a.d.max_len + kQT - 1) / kQT;
+  auto fits = [&](int clusters, int cl) { return clusters >= pairs && tiles <= (int64_t)16 * cl * kQClusterWarps; };
+  if (fits(quant_clusters<16, HALF, kQClusterWarps>(), 16)) return launch_quant<16, HALF, kQClusterWarps>(a, st);
+  if (fits(quant_clusters<10, HALF, kQClusterWarps>(), 10)) return launch_quant<10, HALF, kQClusterWarps>(a, st);
+  if (fits(quant_clusters<8, HALF, kQClusterWarps>(), 8)) return launch_quant<8, HALF, kQClusterWarps>(a, st);
   return launch_quant<0, HALF, kQCtaWarps>(a, st);
 }
 
