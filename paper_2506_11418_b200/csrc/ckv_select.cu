@@ -29,7 +29,7 @@ struct SummarizeArgs {
 };
 
 __global__ void __launch_bounds__(kSumThreads) pages_summarize_kernel(const SummarizeArgs a) {
-  __shared__ float s_acc[4][128];
+  __shared__ __align__(16) float s_acc[4][128];
   __shared__ long long s_n[4];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = lane & 15, r0 = warp * 2 + (lane >> 4);
   const int h = blockIdx.y, b = blockIdx.z;
@@ -75,15 +75,23 @@ __global__ void __launch_bounds__(kSumThreads) pages_summarize_kernel(const Summ
 }
 
 // ---- ckv_pages_select --------------------------------------------------------------------------------------------
-// One thread-block cluster of CL CTAs per (sequence, KV head).  Scores are exact to the last bits of 64: products of
-// bf16 are exact in it, and a choice between near pages then does not hang on the order of a 32-bit sum (with 32 bits
-// about one selection in a thousand would).  A summary row is read once by half a warp, eight elements per lane, for
-// all G query heads; the scores of all CTAs land as order-preserving 64-bit keys in the first CTA's shared memory,
-// which finds the k-th largest by counting digits of eight bits, from the top of the range that the keys span, and
-// writes the chosen blocks in ascending order.
+// The result is that of scores computed in 64 bits: a choice between near pages must not hang on the order of a 32-bit sum
+// (it would for about one selection in a thousand).  Few pages are near the border, so only those are scored in 64 bits:
+//  1. All scores in fp32 on the tensor cores, with a bound on how far they may be off: bf16 products are exact in fp32, 128
+//     additions lose at most 2^-23 of sum |q c| each.  A summary row is read once, straight into the lanes that multiply it,
+//     for all G heads.  The CTAs of a thread-block cluster share the pages; scores land in the first CTA's shared memory.
+//  2. That CTA finds a narrow interval that holds the k-th largest: a histogram over the scores' range, the bin that holds
+//     it, a histogram over that bin if it is still full.
+//  3. Pages above the interval by more than twice the error are chosen, those below by as much are not; the others (a few)
+//     are scored in 64 bits and ranked.  If they are many (equal pages, or scores that are not finite), all pages are scored
+//     in 64 bits and the k-th is found digit by digit.
+//  4. The chosen blocks are written in ascending order.
+// A serving batch is bound by the latency of these steps, a long prompt by reading the summaries.
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
-constexpr int kSelHalves = 2 * kSelWarps;      // summary rows in work at once per CTA
+constexpr int kSelBins = 1024;
+constexpr int kSelNear = 512;                  // pages near the border that are ranked against each other
+constexpr int kSelZoom = 4;                    // histograms at most
 constexpr uint64_t kForced = ~0ull;            // key of a block that is always chosen; no score maps to it
 constexpr int kSelMaxBlocks = 24576;           // 192 KB of keys
 
@@ -95,7 +103,7 @@ struct SelectPagesArgs {
   int32_t* selected;
   int64_t max_blocks;
   float scale;
-  int32_t H, shift, n_first, n_last, n_select;
+  int32_t H, G, shift, n_first, n_last, n_select;
 };
 
 // ascending in the score; NaN lowest, the two zeros equal
@@ -105,113 +113,51 @@ __device__ __forceinline__ uint64_t score_key(double s) {
   return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
 
-__device__ __forceinline__ void st_cluster_u64(uint32_t local_addr, uint32_t rank, uint64_t v) {
+__device__ __forceinline__ void st_cluster_f32(uint32_t local_addr, uint32_t rank, float v) {
   uint32_t ra;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(local_addr), "r"(rank));
-  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(ra), "l"(v) : "memory");
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(ra), "f"(v) : "memory");
 }
 
-template <int G, int CL>
-__global__ void __launch_bounds__(kSelThreads, 1) pages_select_kernel(const SelectPagesArgs a) {
-  extern __shared__ __align__(16) uint64_t keys[];
-  __shared__ uint32_t s_hist[256];
-  __shared__ uint64_t s_lo[kSelWarps], s_hi[kSelWarps];
-  __shared__ int s_gt[kSelWarps], s_eq[kSelWarps], s_bin, s_above, s_count;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rank = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-  griddep_wait();
-  griddep_launch();
-  const ckv_paged_view view = a.views[b];
-  const int64_t mask = ((int64_t)1 << a.shift) - 1;
-  const int n = (int)max((int64_t)0, min((view.len + mask) >> a.shift, a.max_blocks));
-  int32_t* out = a.selected + ((int64_t)b * a.H + h) * a.n_select;
-  if (n <= a.n_select) {  // every block is chosen
-    if (rank == 0)
-      for (int i = tid; i < a.n_select; i += kSelThreads) out[i] = i < n ? i : -1;
-    return;  // (the whole cluster leaves: the condition is the sequence's)
-  }
-  if (CL > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-  // ---- scores
-  {
-    const int c = lane & 15, half = 2 * warp + (lane >> 4);
-    double q[G][8];
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const uint4 u = reinterpret_cast<const uint4*>(a.q + (((int64_t)b * a.H + h) * G + g) * 128)[c];
-      const uint32_t p[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        q[g][2 * i] = (double)__uint_as_float(p[i] << 16);
-        q[g][2 * i + 1] = (double)__uint_as_float(p[i] & 0xffff0000u);
-      }
-    }
-    const uint32_t keys_s = (uint32_t)__cvta_generic_to_shared(keys);
-    if (CL > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // the first CTA has started: its keys can be written
-    constexpr int kStep = kSelHalves * CL;
-    const int i0 = rank * kSelHalves + half;
-    // sixteen blocks at a time: lane c holds the page of the c-th
-    for (int base = 0; base < n; base += 16 * kStep) {
-      const int mine = base + i0 + c * kStep;
-      const int page = mine < n ? view.block_table[mine] : 0;
-      for (int u0 = 0; u0 < 16 && base + u0 * kStep < n; u0 += 4) {
-        uint4 rows[4];
-        int64_t ph[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          ph[u] = (int64_t)__shfl_sync(0xffffffffu, page, u0 + u, 16) * a.H + h;
-          rows[u] = a.c_pages[ph[u] * 16 + c];  // (a block past the end reads page 0's row and is dropped below)
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const uint32_t p[4] = {rows[u].x, rows[u].y, rows[u].z, rows[u].w};
-          double acc[G];
-#pragma unroll
-          for (int g = 0; g < G; ++g) acc[g] = 0.0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const double x = (double)__uint_as_float(p[i] << 16), y = (double)__uint_as_float(p[i] & 0xffff0000u);
-#pragma unroll
-            for (int g = 0; g < G; ++g) acc[g] = fma(x, q[g][2 * i], fma(y, q[g][2 * i + 1], acc[g]));
-          }
-#pragma unroll
-          for (int o = 8; o > 0; o >>= 1)
-#pragma unroll
-            for (int g = 0; g < G; ++g) acc[g] += __shfl_xor_sync(0xffffffffu, acc[g], o);
-          const int i = base + i0 + (u0 + u) * kStep;
-          if (c == 0 && i < n) {
-            double best = acc[0] * (double)a.scale;
-#pragma unroll
-            for (int g = 1; g < G; ++g) {
-              const double s = acc[g] * (double)a.scale;
-              if (s > best || isnan(s)) best = s;  // (a NaN stays)
-            }
-            if (a.clog_pages) best += (double)a.clog_pages[ph[u]];
-            const bool always = i < a.n_first || i >= n - a.n_last;
-            const uint64_t key = always ? kForced : score_key(best);
-            if (CL == 1)
-              keys[i] = key;
-            else
-              st_cluster_u64(keys_s + 8u * (uint32_t)i, 0, key);
-          }
-        }
-      }
-    }
-  }
-  if (CL > 1) {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    if (rank != 0) return;
-  } else {
-    __syncthreads();
-  }
+__device__ __forceinline__ double bf16_lo(uint32_t u) { return (double)__uint_as_float(u << 16); }
+__device__ __forceinline__ double bf16_hi(uint32_t u) { return (double)__uint_as_float(u & 0xffff0000u); }
 
-  // ---- the range of the scores, and how many are to be found among them
+// score of one block in 64 bits, by one warp: a lane has four elements of the row; q: the heads' rows in shared memory
+__device__ __forceinline__ uint64_t exact_key(const SelectPagesArgs& a, const uint2* q, int64_t ph, int lane) {
+  const uint2 u = reinterpret_cast<const uint2*>(a.c_pages)[ph * 32 + lane];
+  const double c0 = bf16_lo(u.x), c1 = bf16_hi(u.x), c2 = bf16_lo(u.y), c3 = bf16_hi(u.y);
+  double best = 0.0;
+  for (int g = 0; g < a.G; ++g) {
+    const uint2 w = q[g * 32 + lane];
+    double s = fma(c0, bf16_lo(w.x), fma(c1, bf16_hi(w.x), fma(c2, bf16_lo(w.y), c3 * bf16_hi(w.y))));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    s *= (double)a.scale;
+    if (g == 0 || s > best || isnan(s)) best = s;  // (a NaN stays)
+  }
+  return score_key(best + (a.clog_pages ? (double)a.clog_pages[ph] : 0.0));
+}
+
+struct SelectShared {
+  alignas(16) uint2 q[8 * 32];  // the query heads' rows, filled in pieces of sixteen bytes
+  uint32_t hist[kSelBins + 2];
+  uint64_t near_key[kSelNear];
+  int32_t near_id[kSelNear];
+  float err[8 * kSelWarps];  // each scoring warp's bound on its scores' error, the whole cluster's
+  float lo[kSelWarps], hi[kSelWarps];
+  uint64_t key_lo[kSelWarps], key_hi[kSelWarps];
+  int gt[kSelWarps], eq[kSelWarps];
+  int bin, above, count, n_near;
+};
+
+// The k-th largest of keys[0, n) without the forced ones, k = need > 0 and fewer than all: chosen are keys above `edge` and the
+// first `ties` of those equal to it.  Digits of eight bits from the top of the range that the keys span.
+__device__ void radix_select(const uint64_t* keys, int n, int need, SelectShared& sh, uint64_t& edge, int& ties) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   uint64_t lo = kForced, hi = 0;
-  int forced = 0;
   for (int i = tid; i < n; i += kSelThreads) {
     const uint64_t k = keys[i];
-    if (k == kForced) {
-      ++forced;
-    } else {
+    if (k != kForced) {
       lo = min(lo, k);
       hi = max(hi, k);
     }
@@ -220,85 +166,302 @@ __global__ void __launch_bounds__(kSelThreads, 1) pages_select_kernel(const Sele
   for (int o = 16; o > 0; o >>= 1) {
     lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
     hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    forced += __shfl_xor_sync(0xffffffffu, forced, o);
   }
   if (lane == 0) {
-    s_lo[warp] = lo;
-    s_hi[warp] = hi;
-    s_gt[warp] = forced;
+    sh.key_lo[warp] = lo;
+    sh.key_hi[warp] = hi;
   }
   __syncthreads();
-  forced = 0;
 #pragma unroll
   for (int w = 0; w < kSelWarps; ++w) {
-    lo = min(lo, s_lo[w]);
-    hi = max(hi, s_hi[w]);
-    forced += s_gt[w];
+    lo = min(lo, sh.key_lo[w]);
+    hi = max(hi, sh.key_hi[w]);
   }
-  // chosen: keys above `edge`, and the first `ties` of those equal to it
-  int need = a.n_select - forced, ties = 0;
-  uint64_t edge = hi;  // need == 0: only the forced ones
-  if (need > 0) {
-    // digits of (key - lo), eight bits at a time from the top bit of the span
-    uint64_t prefix = 0;
-    int bits = hi > lo ? 64 - __clzll((long long)(hi - lo)) : 0;  // bits still open below the prefix
-    bool all = false;
-    while (bits > 0 && !all) {
-      const int take = min(bits, 8), low = bits - take;
-      s_hist[tid] = 0;
-      __syncthreads();
-      for (int i = tid; i < n; i += kSelThreads) {
-        const uint64_t k = keys[i];
-        if (k == kForced) continue;
-        const uint64_t d = k - lo;
-        if (bits == 64 || (d >> bits) == prefix) atomicAdd(&s_hist[(uint32_t)(d >> low) & ((1u << take) - 1u)], 1u);
+  uint64_t prefix = 0;
+  int bits = hi > lo ? 64 - __clzll((long long)(hi - lo)) : 0;  // bits still open below the prefix
+  bool all = false;
+  while (bits > 0 && !all) {
+    const int take = min(bits, 8), low = bits - take;
+    sh.hist[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += kSelThreads) {
+      const uint64_t k = keys[i];
+      if (k == kForced) continue;
+      const uint64_t d = k - lo;
+      if (bits == 64 || (d >> bits) == prefix) atomicAdd(&sh.hist[(uint32_t)(d >> low) & ((1u << take) - 1u)], 1u);
+    }
+    __syncthreads();
+    if (warp == 0) {  // lane l sums digits 8 l .. 8 l + 7; suffix sums from the top digit down
+      uint32_t cnt[8], sum = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += cnt[j] = sh.hist[8 * lane + j];
+      uint32_t above = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_down_sync(0xffffffffu, above, o);
+        if (lane + o < 32) above += y;
       }
-      __syncthreads();
-      if (warp == 0) {  // lane l sums digits 8 l .. 8 l + 7; suffix sums from the top digit down
-        uint32_t cnt[8], sum = 0;
+      above -= sum;  // keys in the digits of higher lanes
+      if ((int)above < need && (int)(above + sum) >= need) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum += cnt[j] = s_hist[8 * lane + j];
-        uint32_t above = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t y = __shfl_down_sync(0xffffffffu, above, o);
-          if (lane + o < 32) above += y;
-        }
-        above -= sum;  // keys in the digits of higher lanes
-        if ((int)above < need && (int)(above + sum) >= need) {
-#pragma unroll
-          for (int j = 7; j >= 0; --j) {
-            if ((int)above < need && (int)(above + cnt[j]) >= need) {
-              s_bin = 8 * lane + j;
-              s_above = (int)above;
-              s_count = (int)cnt[j];
-            }
-            above += cnt[j];
+        for (int j = 7; j >= 0; --j) {
+          if ((int)above < need && (int)(above + cnt[j]) >= need) {
+            sh.bin = 8 * lane + j;
+            sh.above = (int)above;
+            sh.count = (int)cnt[j];
           }
+          above += cnt[j];
         }
       }
-      __syncthreads();
-      prefix = (prefix << take) | (uint64_t)s_bin;
-      need -= s_above;
-      bits = low;
-      all = s_count == need;  // the whole digit is chosen: no need to open it further
-      __syncthreads();
     }
-    const uint64_t least = lo + (bits > 0 ? prefix << bits : prefix);  // the smallest key of the digit
-    if (all) {
-      edge = least - 1;  // (fewer than all are chosen, so some key lies below: least is not 0)
-    } else {
-      edge = least;
-      ties = need;
+    __syncthreads();
+    prefix = (prefix << take) | (uint64_t)sh.bin;
+    need -= sh.above;
+    bits = low;
+    all = sh.count == need;  // the whole digit is chosen: no need to open it further
+    __syncthreads();
+  }
+  const uint64_t least = lo + (bits > 0 ? prefix << bits : prefix);  // the smallest key of the digit
+  edge = all ? least - 1 : least;  // (fewer than all are chosen, so some key lies below a digit that is: least is not 0)
+  ties = all ? 0 : need;
+}
+
+template <int CL>
+__global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const SelectPagesArgs a) {
+  extern __shared__ __align__(16) unsigned char dyn[];
+  __shared__ SelectShared sh;
+  float* const score = reinterpret_cast<float*>(dyn);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int rank = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  griddep_wait();
+  griddep_launch();
+  const ckv_paged_view view = a.views[b];
+  const int64_t mask = ((int64_t)1 << a.shift) - 1;
+  const int n = (int)max((int64_t)0, min((view.len + mask) >> a.shift, a.max_blocks));
+  int32_t* const out = a.selected + ((int64_t)b * a.H + h) * a.n_select;
+  if (n <= a.n_select) {  // every block is chosen
+    if (rank == 0)
+      for (int i = tid; i < a.n_select; i += kSelThreads) out[i] = i < n ? i : -1;
+    return;  // (the whole cluster leaves: the condition is the sequence's)
+  }
+  if (CL > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+  const uint4* const q_rows = reinterpret_cast<const uint4*>(a.q + ((int64_t)b * a.H + h) * a.G * 128);
+  if (rank == 0)
+    for (int i = tid; i < a.G * 16; i += kSelThreads) reinterpret_cast<uint4*>(sh.q)[i] = q_rows[i];
+
+  // ---- 1. scores in fp32.  Lane (g, t) has elements 8 (t + 4 i) .. + 7 (i < 4) of rows g and g + 8 of a block of sixteen, and
+  // of query head g: the same elements in the same k steps, which is all that a product needs.
+  {
+    uint4 qf[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) qf[i] = g < a.G ? q_rows[g * 16 + t + 4 * i] : make_uint4(0u, 0u, 0u, 0u);
+    if (CL > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");  // the first CTA has started: its scores can be written
+    const uint32_t score_s = (uint32_t)__cvta_generic_to_shared(score);
+    const bool h0 = 2 * t < a.G, h1 = 2 * t + 1 < a.G;
+    float err = 0.f;
+    constexpr int kStep = 16 * kSelWarps * CL;
+    int base = 16 * (rank * kSelWarps + warp);
+    int page = base + (lane & 15) < n ? view.block_table[base + (lane & 15)] : 0;
+    for (; base < n; base += kStep) {
+      const int64_t pa = (int64_t)__shfl_sync(0xffffffffu, page, g) * a.H + h, pb = (int64_t)__shfl_sync(0xffffffffu, page, g + 8) * a.H + h;
+      uint4 ra[4], rb[4];  // (rows past the end are page 0's, and dropped below)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        ra[i] = a.c_pages[pa * 16 + t + 4 * i];
+        rb[i] = a.c_pages[pb * 16 + t + 4 * i];
+      }
+      const float la = a.clog_pages ? a.clog_pages[pa] : 0.f, lb = a.clog_pages ? a.clog_pages[pb] : 0.f;
+      const int next = base + kStep + (lane & 15);
+      page = next < n ? view.block_table[next] : 0;
+      float c[4] = {0.f, 0.f, 0.f, 0.f}, m[4] = {0.f, 0.f, 0.f, 0.f};  // q c, and |q| |c|
+      constexpr uint32_t kAbs = 0x7fff7fffu;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        ptx::mma_bf16(c, ra[i].x, rb[i].x, ra[i].y, rb[i].y, qf[i].x, qf[i].y);
+        ptx::mma_bf16(c, ra[i].z, rb[i].z, ra[i].w, rb[i].w, qf[i].z, qf[i].w);
+        ptx::mma_bf16(m, ra[i].x & kAbs, rb[i].x & kAbs, ra[i].y & kAbs, rb[i].y & kAbs, qf[i].x & kAbs, qf[i].y & kAbs);
+        ptx::mma_bf16(m, ra[i].z & kAbs, rb[i].z & kAbs, ra[i].w & kAbs, rb[i].w & kAbs, qf[i].z & kAbs, qf[i].w & kAbs);
+      }
+      // heads 2 t and 2 t + 1 of rows g and g + 8, then all heads over the four lanes of a row
+      float sa = fmaxf(h0 ? c[0] * a.scale : -INFINITY, h1 ? c[1] * a.scale : -INFINITY);
+      float sb = fmaxf(h0 ? c[2] * a.scale : -INFINITY, h1 ? c[3] * a.scale : -INFINITY);
+      // (a sum, not a maximum: it keeps infinities and NaN)
+      float ea = (m[0] + m[1]), eb = (m[2] + m[3]);
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        sa = fmaxf(sa, __shfl_xor_sync(0xffffffffu, sa, o));
+        sb = fmaxf(sb, __shfl_xor_sync(0xffffffffu, sb, o));
+        ea += __shfl_xor_sync(0xffffffffu, ea, o);
+        eb += __shfl_xor_sync(0xffffffffu, eb, o);
+      }
+      if (t < 2) {  // lanes 4 g: row g; 4 g + 1: row g + 8
+        const int i = base + g + 8 * t;
+        const float s = (t ? sb : sa) + (t ? lb : la);
+        // |q c| scale 2^-16, and the roundings after the sum
+        const float e = (t ? eb : ea) * fabsf(a.scale) * 0x1p-16f + fabsf(t ? lb : la) * 0x1p-20f + 0x1p-120f;
+        if (i < n) {
+          err = fmaxf(err, e < 1e30f ? e : INFINITY);  // (NaN becomes infinite)
+          if (CL == 1)
+            score[i] = s;
+          else
+            st_cluster_f32(score_s + 4u * (uint32_t)i, 0, s);
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) err = fmaxf(err, __shfl_xor_sync(0xffffffffu, err, o));
+    if (lane == 0) {
+      if (CL == 1)
+        sh.err[warp] = err;
+      else
+        st_cluster_f32((uint32_t)__cvta_generic_to_shared(&sh.err[rank * kSelWarps + warp]), 0, err);
     }
   }
-  // ---- the chosen blocks in ascending order: every thread takes a run of consecutive blocks
+  if (CL > 1) {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    if (rank != 0) return;
+  }
+
+  // ---- 2. an interval that holds the k-th largest of the blocks that are not always chosen: f0 <= i < f1
+  const int f0 = a.n_first, f1 = n - a.n_last, need = a.n_select - a.n_first - a.n_last;
+  float lo = INFINITY, hi = -INFINITY, err = 0.f;
+  if (CL == 1) __syncthreads();
+  for (int i = f0 + tid; i < f1; i += kSelThreads) {
+    lo = fminf(lo, score[i]);
+    hi = fmaxf(hi, score[i]);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+  }
+  if (lane == 0) {
+    sh.lo[warp] = lo;
+    sh.hi[warp] = hi;
+  }
+  if (tid == 0) sh.n_near = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kSelWarps; ++w) {
+    lo = fminf(lo, sh.lo[w]);
+    hi = fmaxf(hi, sh.hi[w]);
+  }
+  bool fine = true;  // every score is finite and its error known
+#pragma unroll
+  for (int w = 0; w < kSelWarps * CL; ++w) {
+    const float y = sh.err[w];
+    fine &= y < 1e30f;
+    err = fmaxf(err, y);
+  }
+  fine &= lo > -1e30f && hi < 1e30f;
+  uint64_t edge = 0;
+  int ties = 0;
+  float top = INFINITY, bottom = INFINITY;  // chosen above `top`, not chosen below `bottom`, to be seen in between
+  if (need > 0 && fine) {
+    for (int zoom = 0; zoom < kSelZoom; ++zoom) {
+      const float width = (hi - lo) * (1.f / kSelBins), inv = 1.f / width;
+      if (!(width > 1e-30f) || !(inv > 0.f)) break;
+      for (int i = tid; i < kSelBins + 2; i += kSelThreads) sh.hist[i] = 0;
+      __syncthreads();
+      for (int i = f0 + tid; i < f1; i += kSelThreads) {
+        const float s = score[i];
+        const int bin = s < lo ? 0 : s > hi ? kSelBins + 1 : 1 + min(kSelBins - 1, (int)((s - lo) * inv));
+        atomicAdd(&sh.hist[bin], 1u);
+      }
+      __syncthreads();
+      // thread x sums bins 4 x + 1 .. 4 x + 4, from the top down
+      const int x = tid;
+      int cnt[4], sum = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += cnt[j] = (int)sh.hist[4 * x + 1 + j];
+      int above = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_down_sync(0xffffffffu, above, o);
+        if (lane + o < 32) above += y;
+      }
+      if (lane == 0) sh.gt[warp] = above;
+      __syncthreads();
+      above += (int)sh.hist[kSelBins + 1] - sum;
+      for (int w = warp + 1; w < kSelWarps; ++w) above += sh.gt[w];
+#pragma unroll
+      for (int j = 3; j >= 0; --j) {
+        if (above < need && above + cnt[j] >= need) {
+          sh.bin = 4 * x + j;
+          sh.count = cnt[j];
+        }
+        above += cnt[j];
+      }
+      __syncthreads();
+      // the bin's range, and room for the rounding of its borders
+      const float at = lo + width * (float)sh.bin, room = 0.125f * width + 0x1p-21f * fmaxf(fabsf(lo), fabsf(hi));
+      const int count = sh.count;
+      lo = at - room;
+      hi = at + width + room;
+      if (count <= 32 || width <= err) break;
+      __syncthreads();  // (the counters are read)
+    }
+    top = hi + 2.f * err;
+    bottom = lo - 2.f * err;
+  }
+
+  // ---- 3. the blocks in between
   const int per = (n + kSelThreads - 1) / kSelThreads, c0 = min(n, tid * per), c1 = min(n, c0 + per);
+  int above = 0;
+  if (need > 0 && fine) {
+    for (int i = f0 + tid; i < f1; i += kSelThreads) {
+      const float s = score[i];
+      if (s > top) {
+        ++above;
+      } else if (s >= bottom) {
+        const int at = atomicAdd(&sh.n_near, 1);
+        if (at < kSelNear) sh.near_id[at] = i;
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
+    if (lane == 0) sh.eq[warp] = above;
+  }
+  __syncthreads();
+  const int n_near = sh.n_near;
+  uint64_t* const keys = reinterpret_cast<uint64_t*>(dyn);  // (in the scores' place)
+  const bool few = need == 0 || (fine && n_near <= kSelNear);
+  if (need > 0 && few) {
+    above = 0;
+#pragma unroll
+    for (int w = 0; w < kSelWarps; ++w) above += sh.eq[w];
+    for (int j = warp; j < n_near; j += kSelWarps) {
+      const uint64_t k = exact_key(a, sh.q, (int64_t)view.block_table[sh.near_id[j]] * a.H + h, lane);
+      if (lane == 0) sh.near_key[j] = k;
+    }
+    __syncthreads();
+    // ranked by key, then by number: the best need - above of them are chosen (their scores become infinite)
+    for (int j = tid; j < n_near; j += kSelThreads) {
+      const uint64_t k = sh.near_key[j];
+      const int id = sh.near_id[j];
+      int better = 0;
+      for (int x = 0; x < n_near; ++x) better += sh.near_key[x] > k || (sh.near_key[x] == k && sh.near_id[x] < id);
+      score[id] = better < need - above ? INFINITY : -INFINITY;
+    }
+    __syncthreads();
+  } else if (need > 0) {
+    for (int i = warp; i < n; i += kSelWarps) {
+      const uint64_t k = i < f0 || i >= f1 ? kForced : exact_key(a, sh.q, (int64_t)view.block_table[i] * a.H + h, lane);
+      if (lane == 0) keys[i] = k;
+    }
+    __syncthreads();
+    radix_select(keys, n, need, sh, edge, ties);
+  }
+
+  // ---- 4. in ascending order: every thread takes a run of consecutive blocks
   int gt = 0, eq = 0;
   for (int i = c0; i < c1; ++i) {
-    const uint64_t k = keys[i];
-    gt += k > edge;
-    eq += k == edge;
+    if (few) {
+      gt += i < f0 || i >= f1 || (need > 0 && score[i] > top);
+    } else {
+      gt += keys[i] > edge;
+      eq += keys[i] == edge;
+    }
   }
   int gt_at = gt, eq_at = eq;
 #pragma unroll
@@ -309,39 +472,52 @@ __global__ void __launch_bounds__(kSelThreads, 1) pages_select_kernel(const Sele
       eq_at += y;
     }
   }
-  __syncthreads();  // (s_gt was read above)
+  __syncthreads();  // (sh.gt and sh.eq were read above)
   if (lane == 31) {
-    s_gt[warp] = gt_at;
-    s_eq[warp] = eq_at;
+    sh.gt[warp] = gt_at;
+    sh.eq[warp] = eq_at;
   }
   __syncthreads();
   gt_at -= gt;
   eq_at -= eq;
   for (int w = 0; w < warp; ++w) {
-    gt_at += s_gt[w];
-    eq_at += s_eq[w];
+    gt_at += sh.gt[w];
+    eq_at += sh.eq[w];
   }
+  auto put = [&](int at, int i) {
+    if (at < a.n_select) out[at] = i;
+  };
   for (int i = c0; i < c1; ++i) {
-    const uint64_t k = keys[i];
-    if (k > edge) {
-      out[gt_at + min(eq_at, ties)] = i;
-      ++gt_at;
-    } else if (k == edge) {
-      if (eq_at < ties) out[gt_at + eq_at] = i;
-      ++eq_at;
+    if (few) {
+      if (i < f0 || i >= f1 || (need > 0 && score[i] > top)) put(gt_at++, i);
+    } else {
+      const uint64_t k = keys[i];
+      if (k > edge) {
+        put(gt_at + min(eq_at, ties), i);
+        ++gt_at;
+      } else if (k == edge) {
+        if (eq_at < ties) put(gt_at + eq_at, i);
+        ++eq_at;
+      }
     }
   }
 }
 
-template <int G, int CL>
+template <int CL>
 cudaError_t launch_pages_select(const SelectPagesArgs& a, int32_t Bz, cudaStream_t st) {
-  const size_t smem = (size_t)a.max_blocks * 8;
-  cudaError_t e = cudaFuncSetAttribute(pages_select_kernel<G, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelMaxBlocks * 8);
+  static std::atomic<bool> ready[64];  // per device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64 || !ready[dev].load(std::memory_order_relaxed)) {
+    e = cudaFuncSetAttribute(pages_select_kernel<CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelMaxBlocks * 8);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) ready[dev].store(true, std::memory_order_relaxed);
+  }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(CL, (unsigned)a.H, (unsigned)Bz);
   cfg.blockDim = dim3(kSelThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = (size_t)a.max_blocks * 8;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -352,16 +528,16 @@ cudaError_t launch_pages_select(const SelectPagesArgs& a, int32_t Bz, cudaStream
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, pages_select_kernel<G, CL>, a);
+  return cudaLaunchKernelEx(&cfg, pages_select_kernel<CL>, a);
 }
 
-template <int G>
-cudaError_t launch_pages_select_g(const SelectPagesArgs& a, int32_t Bz, cudaStream_t st) {
-  // the scores are split over a cluster while that leaves every CTA 64 blocks to score and the SMs are not all taken
+cudaError_t launch_pages_select_any(const SelectPagesArgs& a, int32_t Bz, cudaStream_t st) {
+  // the scores are split over a cluster while that leaves every warp a block of sixteen or more and the SMs are not all taken
   const int64_t pairs = (int64_t)Bz * a.H, sms = sm_count();
-  if (a.max_blocks >= 512 && pairs * 8 <= 2 * sms) return launch_pages_select<G, 8>(a, Bz, st);
-  if (a.max_blocks >= 128 && pairs * 2 <= 2 * sms) return launch_pages_select<G, 2>(a, Bz, st);
-  return launch_pages_select<G, 1>(a, Bz, st);
+  if (a.max_blocks >= 1024 && pairs * 8 <= sms) return launch_pages_select<8>(a, Bz, st);
+  if (a.max_blocks >= 512 && pairs * 4 <= 2 * sms) return launch_pages_select<4>(a, Bz, st);
+  if (a.max_blocks >= 256 && pairs * 2 <= 2 * sms) return launch_pages_select<2>(a, Bz, st);
+  return launch_pages_select<1>(a, Bz, st);
 }
 
 }  // namespace
@@ -404,21 +580,9 @@ int ckv_pages_select(const ckv_paged_view* views_dev, const void* c_pages, const
   SelectPagesArgs a{};
   a.views = views_dev; a.c_pages = static_cast<const uint4*>(c_pages); a.clog_pages = clog_pages;
   a.q = static_cast<const __nv_bfloat16*>(q); a.selected = selected;
-  a.max_blocks = max_blocks; a.scale = scale; a.H = H; a.shift = shift;
+  a.max_blocks = max_blocks; a.scale = scale; a.H = H; a.G = G; a.shift = shift;
   a.n_first = n_first; a.n_last = n_last; a.n_select = n_select;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  cudaError_t e = cudaErrorInvalidValue;
-  switch (G) {
-    case 1: e = launch_pages_select_g<1>(a, Bz, st); break;
-    case 2: e = launch_pages_select_g<2>(a, Bz, st); break;
-    case 3: e = launch_pages_select_g<3>(a, Bz, st); break;
-    case 4: e = launch_pages_select_g<4>(a, Bz, st); break;
-    case 5: e = launch_pages_select_g<5>(a, Bz, st); break;
-    case 6: e = launch_pages_select_g<6>(a, Bz, st); break;
-    case 7: e = launch_pages_select_g<7>(a, Bz, st); break;
-    case 8: e = launch_pages_select_g<8>(a, Bz, st); break;
-  }
-  return e == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
+  return launch_pages_select_any(a, Bz, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
 }  // extern "C"

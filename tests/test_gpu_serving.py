@@ -366,6 +366,27 @@ def test_select_values_that_are_not_finite():
     select_case([64 * 100], 2, 4, 64, 25, 1, 2, seed=7, change=all_nan)
 
 
+def test_select_scores_far_from_zero_and_outliers():
+    def offset(cp, cl, q, tables):                            # scores near 1000 that differ by less than a 32-bit step
+        cl.add_(1000.0)
+        cp.mul_(1e-4)
+    select_case([64 * 700, 64 * 90], 2, 4, 64, 30, 1, 1, seed=11, change=offset)
+    select_case([64 * 700], 2, 4, 64, 1, 0, 0, seed=12, change=offset)
+
+    def outliers(cp, cl, q, tables):                          # a few pages far above and below all others
+        cp[::97] *= 3000.0
+        cp[5::131] *= -1e6
+    select_case([64 * 1500, 64 * 700], 2, 4, 64, 40, 1, 1, seed=13, change=outliers)
+    select_case([64 * 1500, 64 * 700], 2, 4, 64, 3, 0, 0, seed=14, change=outliers)
+
+    def channel(cp, cl, q, tables):                           # one large channel: products that cancel
+        cp[..., 7] = 200.0
+        q[..., 7] = 50.0
+        cp[..., 8] = 200.0
+        q[..., 8] = -50.0
+    select_case([64 * 1500, 64 * 700], 2, 4, 64, 40, 1, 1, seed=15, change=channel)
+
+
 def test_select_scale_and_missing_log_degrees():
     select_case([6400, 640], 2, 4, 64, 12, 1, 1, seed=8, scale=-0.25)
     select_case([6400, 640], 2, 4, 64, 12, 1, 1, seed=9, scale=0.0)
