@@ -575,15 +575,15 @@ __global__ void __launch_bounds__(NW * 32, 1) decode_fast_kernel(const DecodeArg
   }
 }
 
-template <bool PAGED, int CL, bool SEL = false>
+template <bool PAGED, int CL, bool SEL = false, int NW = kCWarps>
 cudaError_t launch_decode_cluster(DecodeArgs a, cudaStream_t st) {
   // (the kernel's attributes were set by max_active_clusters, which every caller asks first)
-  auto kern = decode_fast_kernel<PAGED, CL, kCT, kCWarps, kCStages, SEL>;
-  a.n_splits = kCWarps * CL;
+  auto kern = decode_fast_kernel<PAGED, CL, kCT, NW, kCStages, SEL>;
+  a.n_splits = NW * CL;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(CL, (unsigned)a.H, (unsigned)a.Bz);
-  cfg.blockDim = dim3(kCWarps * 32);
-  cfg.dynamicSmemBytes = kCSmemBytes;
+  cfg.blockDim = dim3(NW * 32);
+  cfg.dynamicSmemBytes = kCSmemBytes / kCWarps * NW;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -599,22 +599,23 @@ cudaError_t launch_decode_cluster(DecodeArgs a, cudaStream_t st) {
 
 // How many clusters of CL CTAs of the decode kernel the device can hold at once (0: this cluster size cannot be
 // scheduled here); asked once per device and kernel.
-template <bool PAGED, int CL, bool SEL = false>
+template <bool PAGED, int CL, bool SEL = false, int NW = kCWarps>
 int max_active_clusters() {
   constexpr int kMaxDev = 64;
   static int cached[kMaxDev];  // 0 = not asked yet, else the answer + 1
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDev) return 0;
   if (cached[dev] == 0) {
-    auto kern = decode_fast_kernel<PAGED, CL, kCT, kCWarps, kCStages, SEL>;
+    auto kern = decode_fast_kernel<PAGED, CL, kCT, NW, kCStages, SEL>;
+    constexpr size_t kSmem = kCSmemBytes / kCWarps * NW;
     int n = 0;
-    bool ok = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kCSmemBytes) == cudaSuccess;
+    bool ok = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) == cudaSuccess;
     if (ok && CL > 8) ok = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
     if (ok) {
       cudaLaunchConfig_t cfg{};
       cfg.gridDim = dim3(CL, 1, 1);
-      cfg.blockDim = dim3(kCWarps * 32);
-      cfg.dynamicSmemBytes = kCSmemBytes;
+      cfg.blockDim = dim3(NW * 32);
+      cfg.dynamicSmemBytes = kSmem;
       cudaLaunchAttribute attr[1];
       attr[0].id = cudaLaunchAttributeClusterDimension;
       attr[0].val.clusterDim.x = CL;
@@ -720,15 +721,20 @@ cudaError_t launch_decode_combine(const DecodeArgs& a, cudaStream_t st) {
 }
 
 cudaError_t launch_decode_selected(const DecodeArgs& a, cudaStream_t st) {
-  // The largest cluster of which all pairs are resident at once, while its warps have two tiles or more each; a larger
-  // batch takes one CTA per pair (its lists are alike in length, so the CTAs balance by themselves).
+  // The most warps per pair of which all pairs are resident at once (an SM holds four warps and their rings), while each has
+  // two tiles or more.  A larger batch takes two warps per pair, two CTAs per SM: up to 296 pairs then stream in one wave.
+  // Pairs of 2048 tokens, 256 of them: 47 us, with one four-warp CTA per SM 51 us; 128 of them with two warps each 37 us, with
+  // two CTAs of two 27 us.
   const int64_t pairs = (int64_t)a.Bz * a.H, tiles = a.max_len / kCT;
-  if (tiles >= 2 * 16 * kCWarps && max_active_clusters<true, 16, true>() >= pairs) return launch_decode_cluster<true, 16, true>(a, st);
-  if (tiles >= 2 * 8 * kCWarps && max_active_clusters<true, 8, true>() >= pairs) return launch_decode_cluster<true, 8, true>(a, st);
-  if (tiles >= 2 * 4 * kCWarps && max_active_clusters<true, 4, true>() >= pairs) return launch_decode_cluster<true, 4, true>(a, st);
-  if (tiles >= 2 * 2 * kCWarps && max_active_clusters<true, 2, true>() >= pairs) return launch_decode_cluster<true, 2, true>(a, st);
-  if (max_active_clusters<true, 1, true>() < 1) return cudaErrorInvalidConfiguration;
-  return launch_decode_cluster<true, 1, true>(a, st);
+  auto fits = [&](int clusters, int warps) { return clusters >= pairs && tiles >= 2 * warps; };
+  if (fits(max_active_clusters<true, 16, true>(), 64)) return launch_decode_cluster<true, 16, true>(a, st);
+  if (fits(max_active_clusters<true, 10, true>(), 40)) return launch_decode_cluster<true, 10, true>(a, st);
+  if (fits(max_active_clusters<true, 8, true>(), 32)) return launch_decode_cluster<true, 8, true>(a, st);
+  if (fits(max_active_clusters<true, 4, true>(), 16)) return launch_decode_cluster<true, 4, true>(a, st);
+  if (fits(max_active_clusters<true, 2, true>(), 8)) return launch_decode_cluster<true, 2, true>(a, st);
+  if (fits(max_active_clusters<true, 2, true, 2>(), 4)) return launch_decode_cluster<true, 2, true, 2>(a, st);
+  if (max_active_clusters<true, 1, true, 2>() < 1) return cudaErrorInvalidConfiguration;
+  return launch_decode_cluster<true, 1, true, 2>(a, st);
 }
 
 }  // namespace ckv

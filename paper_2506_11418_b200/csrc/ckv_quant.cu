@@ -29,40 +29,59 @@ constexpr int kCodeBytes = 64, kScaleBytes = 4;  // per row
 // magnitude) - 2, so that the largest element lies in [4, 8) steps and codes end at 6; elements round to the nearest even
 // code.  A group with an element that is not finite becomes NaN as a whole (scale 255, codes 0).
 
-__device__ __forceinline__ void load8(const void* p, int64_t vec, int lane16, bool f32, float (&x)[8]) {
-  if (f32) {
-    const float4* f = reinterpret_cast<const float4*>(p) + vec + 2 * lane16;
-    const float4 a = f[0], b = f[1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+// a lane's eight elements as they lie in memory
+template <bool F32>
+struct Eight {
+  uint4 u[F32 ? 2 : 1];
+};
+
+template <bool F32>
+__device__ __forceinline__ Eight<F32> load8(const void* p, int64_t vec, int lane16) {
+  Eight<F32> r;
+  if constexpr (F32) {
+    r.u[0] = reinterpret_cast<const uint4*>(p)[vec + 2 * lane16];
+    r.u[1] = reinterpret_cast<const uint4*>(p)[vec + 2 * lane16 + 1];
   } else {
-    const uint4 u = reinterpret_cast<const uint4*>(p)[vec + lane16];
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    r.u[0] = reinterpret_cast<const uint4*>(p)[vec + lane16];
   }
+  return r;
 }
 
-// codes of a lane's eight elements, and the row's four scale bytes (every lane of the half warp has them)
-__device__ __forceinline__ uint32_t encode8(const float (&x)[8], int lane16, uint32_t& scales) {
-  uint32_t top = 0;
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+
+// codes of a lane's eight elements, and its group's scale byte.  Magnitudes compare as their bits do, NaN above infinity.
+template <bool F32>
+__device__ __forceinline__ uint32_t encode8(const Eight<F32>& v, uint32_t& byte) {
+  const uint32_t w[8] = {v.u[0].x, v.u[0].y, v.u[0].z, v.u[0].w, v.u[F32].x, v.u[F32].y, v.u[F32].z, v.u[F32].w};
+  uint32_t field;  // exponent field of the group's largest magnitude; 255: infinity or NaN
+  if constexpr (F32) {
+    uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  const int field = (int)(top >> 23);  // exponent field of the largest magnitude; 255: infinity or NaN
+    for (int i = 0; i < 8; ++i) top = max(top, w[i] & 0x7fffffffu);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    field = top >> 23;
+  } else {
+    constexpr uint32_t kAbs = 0x7fff7fffu;
+    uint32_t top = max_u16x2(max_u16x2(w[0] & kAbs, w[1] & kAbs), max_u16x2(w[2] & kAbs, w[3] & kAbs));
+    top = max_u16x2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max_u16x2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    field = max(top >> 16, top & 0xffffu) >> 7;
+  }
   const bool finite = field != 255;
-  const int byte = finite ? max(field - 2, 0) : 255;
-  const float f = finite ? __uint_as_float((uint32_t)(254 - byte) << 23) : 0.f;  // 2^(127 - byte), byte <= 252
-  float y[8];
+  byte = finite ? (uint32_t)max((int)field - 2, 0) : 255u;
+  const float f = __uint_as_float((254u - byte) << 23);  // 2^(127 - byte), byte <= 252: products are exact
+  float x[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = finite ? x[i] * f : 0.f;  // exact
-  scales = (uint32_t)byte << (8 * (lane16 >> 2));
-  scales |= __shfl_xor_sync(0xffffffffu, scales, 4);
-  scales |= __shfl_xor_sync(0xffffffffu, scales, 8);
-  return ptx::pack_e2m1x8(y);
+  for (int i = 0; i < 8; ++i) {
+    const float y = F32 ? __uint_as_float(w[i]) : __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+    x[i] = y * f;
+  }
+  return finite ? ptx::pack_e2m1x8(x) : 0u;
 }
 
 constexpr int kQuantThreads = 256;
@@ -76,32 +95,31 @@ __global__ void __launch_bounds__(kQuantThreads) pages_quantize_kernel(const Row
   griddep_wait();
   griddep_launch();
   int64_t row[U];
-  float k[U][8], v[U][8];
+  Eight<F32> k[U] = {}, v[U] = {};
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t i = i0 + u * kRows + r0;
     const int64_t s = i < n ? slots[i] : -1;
     row[u] = (s >= 0 && s < n_rows) ? (((s >> shift) * r.H + h) << shift) + (s & mask) : -1;
     if (row[u] >= 0) {
-      load8(r.k, i * r.token_vecs + h * r.head_vecs, lane16, F32, k[u]);
-      load8(r.v, i * r.token_vecs + h * r.head_vecs, lane16, F32, v[u]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) k[u][e] = v[u][e] = 0.f;
+      k[u] = load8<F32>(r.k, i * r.token_vecs + h * r.head_vecs, lane16);
+      v[u] = load8<F32>(r.v, i * r.token_vecs + h * r.head_vecs, lane16);
     }
   }
   const int j = lane16 >> 2, t = lane16 & 3;  // this lane's elements: 32 j + 8 t ..
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     uint32_t ks, vs;
-    const uint32_t kc = encode8(k[u], lane16, ks), vc = encode8(v[u], lane16, vs);
+    const uint32_t kc = encode8<F32>(k[u], ks), vc = encode8<F32>(v[u], vs);
     if (row[u] < 0) continue;
     reinterpret_cast<uint32_t*>(pool.k_codes)[row[u] * 16 + 4 * t + j] = kc;
     uint16_t* vd = reinterpret_cast<uint16_t*>(pool.v_codes) + row[u] * 32 + 8 * t + j;  // g = 2 t and 2 t + 1
     vd[0] = (uint16_t)vc;
     vd[4] = (uint16_t)(vc >> 16);
-    if (lane16 == 0) reinterpret_cast<uint32_t*>(pool.k_scales)[row[u]] = ks;
-    if (lane16 == 1) reinterpret_cast<uint32_t*>(pool.v_scales)[row[u]] = vs;
+    if (t == 0) {
+      pool.k_scales[row[u] * 4 + j] = (uint8_t)ks;
+      pool.v_scales[row[u] * 4 + j] = (uint8_t)vs;
+    }
   }
   if (pool.deg_pages || pool.logdeg_pages) write_degrees(r, slots, n, i0, kRows * U, h, pool.deg_pages, pool.logdeg_pages, n_rows, shift);
 }
@@ -866,9 +884,9 @@ int ckv_pages_quantize(const ckv_token_rows* rows, const int64_t* slots, int64_t
     const dim3 grid((unsigned)((n + rows_per_cta - 1) / rows_per_cta), (unsigned)rows->H);
     return launch_dependent(kernel, grid, dim3(kQuantThreads), 0, stream, r, slots, n, *pool, n_rows, (int32_t)shift);
   };
-  const bool many = n * rows->H >= (int64_t)32 * sm_count();  // two rows per half warp once that fills the SMs
-  const cudaError_t e = rows->dtype == CKV_F32 ? (many ? go(pages_quantize_kernel<true, 2>, 32) : go(pages_quantize_kernel<true, 1>, 16))
-                                               : (many ? go(pages_quantize_kernel<false, 2>, 32) : go(pages_quantize_kernel<false, 1>, 16));
+  const bool many = n * rows->H >= (int64_t)64 * sm_count();  // four rows per half warp once that fills the SMs
+  const cudaError_t e = rows->dtype == CKV_F32 ? (many ? go(pages_quantize_kernel<true, 4>, 64) : go(pages_quantize_kernel<true, 1>, 16))
+                                               : (many ? go(pages_quantize_kernel<false, 4>, 64) : go(pages_quantize_kernel<false, 1>, 16));
   return e == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 

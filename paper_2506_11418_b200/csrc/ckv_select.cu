@@ -13,9 +13,11 @@ namespace ckv {
 namespace {
 
 // ---- ckv_pages_summarize -----------------------------------------------------------------------------------------
-// One CTA of four warps per (page, head); half a warp takes a key row (16 bytes per lane), so eight rows are in flight
-// per step, and the partial sums meet in shared memory.  Bound by reading the keys once.
-constexpr int kSumThreads = 128;
+// WPH warps per (page, head): one for a prompt's many pages (the eight warps of a CTA take neighbouring heads, and none waits
+// for another), four for a step's few (the page's rows are in flight at once; the partial sums meet
+// in shared memory).  Half a warp takes a key row, 16 bytes per lane, eight rows in flight per lane.  Bound by reading the
+// keys once.
+constexpr int kSumThreads = 256;
 
 struct SummarizeArgs {
   const ckv_paged_view* views;
@@ -28,49 +30,72 @@ struct SummarizeArgs {
   int32_t H, shift;
 };
 
+template <int WPH>
 __global__ void __launch_bounds__(kSumThreads) pages_summarize_kernel(const SummarizeArgs a) {
-  __shared__ __align__(16) float s_acc[4][128];
-  __shared__ long long s_n[4];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = lane & 15, r0 = warp * 2 + (lane >> 4);
-  const int h = blockIdx.y, b = blockIdx.z;
+  constexpr int kHeads = kSumThreads / 32 / WPH, kRows = 8;
+  __shared__ __align__(16) float s_acc[WPH > 1 ? kSumThreads / 32 : 1][128];
+  __shared__ long long s_n[kSumThreads / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane & 15, part = warp % WPH;
+  const int64_t unit = (int64_t)blockIdx.x * kHeads + warp / WPH, x = unit / a.H;  // (block, head) of the sequence
+  const int h = (int)(unit - x * a.H), b = blockIdx.y;
   griddep_wait();
   griddep_launch();
   const ckv_paged_view view = a.views[b];
-  const int64_t first = a.from_lens ? max(a.from_lens[b], (int64_t)0) >> a.shift : 0;
-  for (int64_t x = blockIdx.x; x < a.max_blocks; x += gridDim.x) {
-    const int64_t blk = first + x, left = view.len - (blk << a.shift);
-    if (left <= 0) break;
-    const int rows = (int)min(left, (int64_t)1 << a.shift);
-    const int64_t ph = (int64_t)view.block_table[blk] * a.H + h, row = ph << a.shift;
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    long long total = 0;
-#pragma unroll 8
-    for (int r = r0; r < rows; r += 8) {
-      const uint4 u = a.k_pages[(row + r) * 16 + c];
-      const int dg = a.deg_pages ? a.deg_pages[row + r] : 1;
-      const float w = (float)dg;
-      total += dg;
-      const uint32_t p[4] = {u.x, u.y, u.z, u.w};
+  const int64_t blk = (a.from_lens ? max(a.from_lens[b], (int64_t)0) >> a.shift : 0) + x, left = view.len - (blk << a.shift);
+  const int rows = x < a.max_blocks && left > 0 ? (int)min(left, (int64_t)1 << a.shift) : 0;
+  if (WPH == 1 && rows == 0) return;
+  const int64_t ph = rows > 0 ? (int64_t)view.block_table[blk] * a.H + h : 0, row = ph << a.shift;
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  long long total = 0;
+  for (int r0 = 2 * part + (lane >> 4); r0 < rows; r0 += 2 * WPH * kRows) {
+    uint4 u[kRows];
+    int dg[kRows];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        acc[2 * i] = fmaf(w, __uint_as_float(p[i] << 16), acc[2 * i]);
-        acc[2 * i + 1] = fmaf(w, __uint_as_float(p[i] & 0xffff0000u), acc[2 * i + 1]);
-      }
+    for (int i = 0; i < kRows; ++i) {
+      const int r = r0 + 2 * WPH * i;
+      const bool ok = r < rows;
+      u[i] = ok ? a.k_pages[(row + r) * 16 + c] : make_uint4(0u, 0u, 0u, 0u);
+      dg[i] = ok ? (a.deg_pages ? a.deg_pages[row + r] : 1) : 0;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 16);
-    total += __shfl_xor_sync(0xffffffffu, total, 16);
+    for (int i = 0; i < kRows; ++i) {
+      const float w = (float)dg[i];
+      total += dg[i];
+      const uint32_t p[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[2 * j] = fmaf(w, __uint_as_float(p[j] << 16), acc[2 * j]);
+        acc[2 * j + 1] = fmaf(w, __uint_as_float(p[j] & 0xffff0000u), acc[2 * j + 1]);
+      }
+    }
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 16);
+  total += __shfl_xor_sync(0xffffffffu, total, 16);
+  if constexpr (WPH == 1) {
+    if (rows > 0 && lane < 16) {
+      const float n = (float)total;
+      reinterpret_cast<uint4*>(a.c_pages)[ph * 16 + c] =
+          make_uint4(pack_bf16x2(acc[0] / n, acc[1] / n), pack_bf16x2(acc[2] / n, acc[3] / n), pack_bf16x2(acc[4] / n, acc[5] / n),
+                     pack_bf16x2(acc[6] / n, acc[7] / n));
+      if (lane == 0) a.clog_pages[ph] = logf(n);
+    }
+  } else {
     if (lane < 16) {
       *reinterpret_cast<float4*>(&s_acc[warp][c * 8]) = make_float4(acc[0], acc[1], acc[2], acc[3]);
       *reinterpret_cast<float4*>(&s_acc[warp][c * 8 + 4]) = make_float4(acc[4], acc[5], acc[6], acc[7]);
       if (lane == 0) s_n[warp] = total;
     }
     __syncthreads();
-    const float n = (float)(s_n[0] + s_n[1] + s_n[2] + s_n[3]);
-    const float s = (s_acc[0][tid] + s_acc[1][tid]) + (s_acc[2][tid] + s_acc[3][tid]);
-    a.c_pages[ph * 128 + tid] = __float2bfloat16_rn(s / n);
-    if (tid == 0) a.clog_pages[ph] = logf(n);
-    __syncthreads();  // the sums are read before the next block's overwrite them
+    if (rows > 0) {
+      const int w0 = warp - part, d = part * 32 + lane;
+      static_assert(WPH == 1 || WPH == 4, "a warp finishes 32 of the 128 columns");
+      const float n = (float)(s_n[w0] + s_n[w0 + 1] + s_n[w0 + 2] + s_n[w0 + 3]);
+      const float s = (s_acc[w0][d] + s_acc[w0 + 1][d]) + (s_acc[w0 + 2][d] + s_acc[w0 + 3][d]);
+      a.c_pages[ph * 128 + d] = __float2bfloat16_rn(s / n);
+      if (d == 0) a.clog_pages[ph] = logf(n);
+    }
   }
 }
 
@@ -119,32 +144,50 @@ __device__ __forceinline__ void st_cluster_f32(uint32_t local_addr, uint32_t ran
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(ra), "f"(v) : "memory");
 }
 
-__device__ __forceinline__ double bf16_lo(uint32_t u) { return (double)__uint_as_float(u << 16); }
-__device__ __forceinline__ double bf16_hi(uint32_t u) { return (double)__uint_as_float(u & 0xffff0000u); }
-
-// score of one block in 64 bits, by one warp: a lane has four elements of the row; q: the heads' rows in shared memory
-__device__ __forceinline__ uint64_t exact_key(const SelectPagesArgs& a, const uint2* q, int64_t ph, int lane) {
-  const uint2 u = reinterpret_cast<const uint2*>(a.c_pages)[ph * 32 + lane];
-  const double c0 = bf16_lo(u.x), c1 = bf16_hi(u.x), c2 = bf16_lo(u.y), c3 = bf16_hi(u.y);
-  double best = 0.0;
-  for (int g = 0; g < a.G; ++g) {
-    const uint2 w = q[g * 32 + lane];
-    double s = fma(c0, bf16_lo(w.x), fma(c1, bf16_hi(w.x), fma(c2, bf16_lo(w.y), c3 * bf16_hi(w.y))));
+// score of one block in 64 bits, by eight lanes (x = 0 .. 7) that have sixteen elements each: pieces x and x + 8 of the row;
+// q: the heads' rows in shared memory.  All 32 lanes call; lanes with ok = false read nothing.
+__device__ __forceinline__ uint64_t exact_key(const SelectPagesArgs& a, const uint4* q, int64_t ph, int x, bool ok) {
+  double c[16];
+  auto unpack = [](const uint4& u, double* d) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    for (int i = 0; i < 4; ++i) {
+      d[2 * i] = (double)__uint_as_float(w[i] << 16);
+      d[2 * i + 1] = (double)__uint_as_float(w[i] & 0xffff0000u);
+    }
+  };
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  unpack(ok ? a.c_pages[ph * 16 + x] : zero, c);
+  unpack(ok ? a.c_pages[ph * 16 + 8 + x] : zero, c + 8);
+  const double lg = ok && a.clog_pages ? (double)a.clog_pages[ph] : 0.0;
+  double best = 0.0;
+#pragma unroll 2
+  for (int g = 0; g < a.G; ++g) {
+    double w[16], s = 0.0, r = 0.0;
+    unpack(q[g * 16 + x], w);
+    unpack(q[g * 16 + 8 + x], w + 8);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      s = fma(c[i], w[i], s);
+      r = fma(c[8 + i], w[8 + i], r);
+    }
+    s += r;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     s *= (double)a.scale;
     if (g == 0 || s > best || isnan(s)) best = s;  // (a NaN stays)
   }
-  return score_key(best + (a.clog_pages ? (double)a.clog_pages[ph] : 0.0));
+  return score_key(best + lg);
 }
 
 struct SelectShared {
-  alignas(16) uint2 q[8 * 32];  // the query heads' rows, filled in pieces of sixteen bytes
+  uint4 q[8 * 16];           // the query heads' rows
   uint32_t hist[kSelBins + 2];
   uint64_t near_key[kSelNear];
   int32_t near_id[kSelNear];
-  float err[8 * kSelWarps];  // each scoring warp's bound on its scores' error, the whole cluster's
-  float lo[kSelWarps], hi[kSelWarps];
+  float err[8 * kSelWarps];  // of each scoring warp of the cluster: the bound on its scores' error,
+  float lo[8 * kSelWarps];   // its lowest score and its highest, without the blocks that are always chosen
+  float hi[8 * kSelWarps];
   uint64_t key_lo[kSelWarps], key_hi[kSelWarps];
   int gt[kSelWarps], eq[kSelWarps];
   int bin, above, count, n_near;
@@ -245,9 +288,10 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
     return;  // (the whole cluster leaves: the condition is the sequence's)
   }
   if (CL > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+  const int f0 = a.n_first, f1 = n - a.n_last, need = a.n_select - a.n_first - a.n_last;  // the others are f0 <= i < f1
   const uint4* const q_rows = reinterpret_cast<const uint4*>(a.q + ((int64_t)b * a.H + h) * a.G * 128);
   if (rank == 0)
-    for (int i = tid; i < a.G * 16; i += kSelThreads) reinterpret_cast<uint4*>(sh.q)[i] = q_rows[i];
+    for (int i = tid; i < a.G * 16; i += kSelThreads) sh.q[i] = q_rows[i];
 
   // ---- 1. scores in fp32.  Lane (g, t) has elements 8 (t + 4 i) .. + 7 (i < 4) of rows g and g + 8 of a block of sixteen, and
   // of query head g: the same elements in the same k steps, which is all that a product needs.
@@ -258,7 +302,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
     if (CL > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");  // the first CTA has started: its scores can be written
     const uint32_t score_s = (uint32_t)__cvta_generic_to_shared(score);
     const bool h0 = 2 * t < a.G, h1 = 2 * t + 1 < a.G;
-    float err = 0.f;
+    float err = 0.f, lo = INFINITY, hi = -INFINITY;
     constexpr int kStep = 16 * kSelWarps * CL;
     int base = 16 * (rank * kSelWarps + warp);
     int page = base + (lane & 15) < n ? view.block_table[base + (lane & 15)] : 0;
@@ -301,6 +345,10 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
         const float e = (t ? eb : ea) * fabsf(a.scale) * 0x1p-16f + fabsf(t ? lb : la) * 0x1p-20f + 0x1p-120f;
         if (i < n) {
           err = fmaxf(err, e < 1e30f ? e : INFINITY);  // (NaN becomes infinite)
+          if (i >= f0 && i < f1) {
+            lo = fminf(lo, s);
+            hi = fmaxf(hi, s);
+          }
           if (CL == 1)
             score[i] = s;
           else
@@ -309,12 +357,18 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
       }
     }
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) err = fmaxf(err, __shfl_xor_sync(0xffffffffu, err, o));
-    if (lane == 0) {
+    for (int o = 1; o < 32; o <<= 1) {
+      err = fmaxf(err, __shfl_xor_sync(0xffffffffu, err, o));
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    }
+    if (lane < 3) {
+      float* const to = (lane == 0 ? sh.err : lane == 1 ? sh.lo : sh.hi) + rank * kSelWarps + warp;
+      const float v = lane == 0 ? err : lane == 1 ? lo : hi;
       if (CL == 1)
-        sh.err[warp] = err;
+        *to = v;
       else
-        st_cluster_f32((uint32_t)__cvta_generic_to_shared(&sh.err[rank * kSelWarps + warp]), 0, err);
+        st_cluster_f32((uint32_t)__cvta_generic_to_shared(to), 0, v);
     }
   }
   if (CL > 1) {
@@ -322,37 +376,17 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
     if (rank != 0) return;
   }
 
-  // ---- 2. an interval that holds the k-th largest of the blocks that are not always chosen: f0 <= i < f1
-  const int f0 = a.n_first, f1 = n - a.n_last, need = a.n_select - a.n_first - a.n_last;
+  // ---- 2. an interval that holds the k-th largest of the blocks that are not always chosen
   float lo = INFINITY, hi = -INFINITY, err = 0.f;
-  if (CL == 1) __syncthreads();
-  for (int i = f0 + tid; i < f1; i += kSelThreads) {
-    lo = fminf(lo, score[i]);
-    hi = fmaxf(hi, score[i]);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-  }
-  if (lane == 0) {
-    sh.lo[warp] = lo;
-    sh.hi[warp] = hi;
-  }
   if (tid == 0) sh.n_near = 0;
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kSelWarps; ++w) {
+#pragma unroll 8
+  for (int w = 0; w < kSelWarps * CL; ++w) {
     lo = fminf(lo, sh.lo[w]);
     hi = fmaxf(hi, sh.hi[w]);
+    err = fmaxf(err, sh.err[w]);
   }
-  bool fine = true;  // every score is finite and its error known
-#pragma unroll
-  for (int w = 0; w < kSelWarps * CL; ++w) {
-    const float y = sh.err[w];
-    fine &= y < 1e30f;
-    err = fmaxf(err, y);
-  }
+  bool fine = err < 1e30f;  // every score is finite and its error known
   fine &= lo > -1e30f && hi < 1e30f;
   uint64_t edge = 0;
   int ties = 0;
@@ -406,7 +440,6 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
   }
 
   // ---- 3. the blocks in between
-  const int per = (n + kSelThreads - 1) / kSelThreads, c0 = min(n, tid * per), c1 = min(n, c0 + per);
   int above = 0;
   if (need > 0 && fine) {
     for (int i = f0 + tid; i < f1; i += kSelThreads) {
@@ -430,9 +463,11 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
     above = 0;
 #pragma unroll
     for (int w = 0; w < kSelWarps; ++w) above += sh.eq[w];
-    for (int j = warp; j < n_near; j += kSelWarps) {
-      const uint64_t k = exact_key(a, sh.q, (int64_t)view.block_table[sh.near_id[j]] * a.H + h, lane);
-      if (lane == 0) sh.near_key[j] = k;
+    for (int j0 = 4 * warp; j0 < n_near; j0 += 4 * kSelWarps) {
+      const int j = j0 + (lane >> 3);
+      const bool ok = j < n_near;
+      const uint64_t k = exact_key(a, sh.q, ok ? (int64_t)view.block_table[sh.near_id[j]] * a.H + h : 0, lane & 7, ok);
+      if (ok && (lane & 7) == 0) sh.near_key[j] = k;
     }
     __syncthreads();
     // ranked by key, then by number: the best need - above of them are chosen (their scores become infinite)
@@ -445,61 +480,56 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
     }
     __syncthreads();
   } else if (need > 0) {
-    for (int i = warp; i < n; i += kSelWarps) {
-      const uint64_t k = i < f0 || i >= f1 ? kForced : exact_key(a, sh.q, (int64_t)view.block_table[i] * a.H + h, lane);
-      if (lane == 0) keys[i] = k;
+    for (int i0 = 4 * warp; i0 < n; i0 += 4 * kSelWarps) {
+      const int i = i0 + (lane >> 3);
+      const bool ok = i >= f0 && i < f1;
+      const uint64_t k = exact_key(a, sh.q, ok ? (int64_t)view.block_table[i] * a.H + h : 0, lane & 7, ok);
+      if (i < n && (lane & 7) == 0) keys[i] = ok ? k : kForced;
     }
     __syncthreads();
     radix_select(keys, n, need, sh, edge, ties);
   }
 
-  // ---- 4. in ascending order: every thread takes a run of consecutive blocks
-  int gt = 0, eq = 0;
-  for (int i = c0; i < c1; ++i) {
+  // ---- 4. in ascending order: every warp takes a run of consecutive blocks, 32 at a time
+  const int per = ((n + kSelThreads - 1) / kSelThreads) * 32, c0 = min(n, warp * per), c1 = min(n, c0 + per);
+  auto look = [&](int i, bool& more, bool& same) {
+    more = same = false;
+    if (i >= c1) return;
     if (few) {
-      gt += i < f0 || i >= f1 || (need > 0 && score[i] > top);
-    } else {
-      gt += keys[i] > edge;
-      eq += keys[i] == edge;
-    }
-  }
-  int gt_at = gt, eq_at = eq;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, gt_at, o), y = __shfl_up_sync(0xffffffffu, eq_at, o);
-    if (lane >= o) {
-      gt_at += x;
-      eq_at += y;
-    }
-  }
-  __syncthreads();  // (sh.gt and sh.eq were read above)
-  if (lane == 31) {
-    sh.gt[warp] = gt_at;
-    sh.eq[warp] = eq_at;
-  }
-  __syncthreads();
-  gt_at -= gt;
-  eq_at -= eq;
-  for (int w = 0; w < warp; ++w) {
-    gt_at += sh.gt[w];
-    eq_at += sh.eq[w];
-  }
-  auto put = [&](int at, int i) {
-    if (at < a.n_select) out[at] = i;
-  };
-  for (int i = c0; i < c1; ++i) {
-    if (few) {
-      if (i < f0 || i >= f1 || (need > 0 && score[i] > top)) put(gt_at++, i);
+      more = i < f0 || i >= f1 || (need > 0 && score[i] > top);
     } else {
       const uint64_t k = keys[i];
-      if (k > edge) {
-        put(gt_at + min(eq_at, ties), i);
-        ++gt_at;
-      } else if (k == edge) {
-        if (eq_at < ties) put(gt_at + eq_at, i);
-        ++eq_at;
-      }
+      more = k > edge;
+      same = k == edge;
     }
+  };
+  int gt = 0, eq = 0;
+  for (int i = c0; i < c1; i += 32) {
+    bool more, same;
+    look(i + lane, more, same);
+    gt += __popc(__ballot_sync(0xffffffffu, more));
+    eq += __popc(__ballot_sync(0xffffffffu, same));
+  }
+  __syncthreads();  // (sh.gt and sh.eq were read above)
+  if (lane == 0) {
+    sh.gt[warp] = gt;
+    sh.eq[warp] = eq;
+  }
+  __syncthreads();
+  gt = eq = 0;  // chosen and equal blocks before this warp's
+  for (int w = 0; w < warp; ++w) {
+    gt += sh.gt[w];
+    eq += sh.eq[w];
+  }
+  const uint32_t below = (1u << lane) - 1u;
+  for (int i = c0; i < c1; i += 32) {
+    bool more, same;
+    look(i + lane, more, same);
+    const uint32_t bm = __ballot_sync(0xffffffffu, more), bs = __ballot_sync(0xffffffffu, same);
+    const int eq_at = eq + __popc(bs & below), at = gt + __popc(bm & below) + min(eq_at, ties);
+    if ((more || (same && eq_at < ties)) && at < a.n_select) out[at] = i + lane;
+    gt += __popc(bm);
+    eq += __popc(bs);
   }
 }
 
@@ -560,9 +590,15 @@ int ckv_pages_summarize(const ckv_paged_view* views_dev, const int64_t* from_len
   a.views = views_dev; a.from_lens = from_lens; a.k_pages = static_cast<const uint4*>(k_pages); a.deg_pages = deg_pages;
   a.c_pages = static_cast<__nv_bfloat16*>(c_pages); a.clog_pages = clog_pages;
   a.max_blocks = max_blocks; a.H = H; a.shift = shift;
-  const dim3 grid((unsigned)std::min<int64_t>(max_blocks, 65535), (unsigned)H, (unsigned)Bz);
-  return launch_dependent(pages_summarize_kernel, grid, dim3(kSumThreads), 0, static_cast<cudaStream_t>(cuda_stream), a) == cudaSuccess
-             ? CKV_OK : CKV_ERR_CUDA;
+  // one warp per (page, head) once that gives every SM's warp slots something to do
+  const bool many = max_blocks * H * Bz >= (int64_t)32 * sm_count();
+  const int64_t units = many ? 8 : 2, ctas = (max_blocks * H + units - 1) / units;
+  if (max_blocks > INT32_MAX || ctas > INT32_MAX) return CKV_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)ctas, (unsigned)Bz);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = many ? launch_dependent(pages_summarize_kernel<1>, grid, dim3(kSumThreads), 0, st, a)
+                             : launch_dependent(pages_summarize_kernel<4>, grid, dim3(kSumThreads), 0, st, a);
+  return e == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
 int ckv_pages_select(const ckv_paged_view* views_dev, const void* c_pages, const float* clog_pages, int32_t page_tokens, int32_t Bz, int32_t H,
