@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -149,8 +150,11 @@ def _check(status: int):
         raise CkvError(status)
 
 
+_DTYPE_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 def dtype_code(t: torch.dtype) -> int:
-    return {torch.float32: F32, torch.bfloat16: BF16}[t]
+    return _DTYPE_CODES[t]
 
 
 @dataclass
@@ -419,16 +423,29 @@ def pages_scatter(block_table, length, k, v, deg, k_pages, v_pages, deg_pages, l
 
 
 # ---- block tables and slot maps, attention over selected pages, four-bit pages
+# (Calls of a few microseconds on the GPU: the checks are kept to what a wrong pointer could come from.)
+
+_raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_i32, _i64, _f32, _u8 = torch.int32, torch.int64, torch.float32, torch.uint8
+_ROWS = struct.Struct("@PPPqqqqiii4x")     # ckv_token_rows
+_POOL = struct.Struct("@PPPPPP")           # ckv_quant_pool
+
 
 def _stream_for(t: torch.Tensor):
     """The current stream, for tensors on the current device (the library launches there; another device's are refused)."""
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return _stream_ptr()
+    dev = t.get_device()
+    if dev < 0 or dev != _raw_device():
+        raise ValueError(f"tensors are on {t.device}, which is not the current CUDA device")
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
-def _is(t: torch.Tensor, dtype: torch.dtype, *shape) -> bool:
-    return t.dtype == dtype and t.is_contiguous() and (not shape or t.shape == shape)
+def _vec(t: torch.Tensor, dtype: torch.dtype, n: int) -> bool:
+    return t.dtype is dtype and t.numel() == n and t.is_contiguous()
+
+
+def _like(t: torch.Tensor | None, dtype: torch.dtype, shape) -> bool:
+    """None, or a contiguous tensor of that type and shape."""
+    return t is None or (t.dtype is dtype and t.shape == shape and t.is_contiguous())
 
 
 def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_tables: torch.Tensor, ring: torch.Tensor, ring_state: torch.Tensor,
@@ -439,35 +456,38 @@ def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_tables: torch
     ring_state_out int64 [2] (head, count); slots int64 [n]; slot_begin int64 [Bz + 1]; status int32 [1] (RESIZE_*);
     views int64 [Bz, 2] (paged_views' layout)."""
     Bz, row = block_tables.shape
-    i64, i32 = torch.int64, torch.int32
-    assert _is(lens, i64, Bz) and _is(new_lens, i64, Bz) and _is(lens_out, i64, Bz) and _is(slot_begin, i64, Bz + 1) and _is(slots, i64)
-    assert _is(ring_state, i64, 2) and _is(ring_state_out, i64, 2) and _is(ring, i32) and _is(status, i32) and block_tables.dtype == i32
-    assert block_tables.stride(1) == 1 and block_tables.stride(0) >= row and (views is None or _is(views, i64, Bz, 2))
-    assert block_tables.stride(0) == row or Bz == 1, "rows of the block tables follow one another"
+    n_pages, n_slots = ring.numel(), slots.numel()
+    assert _vec(lens, _i64, Bz) and _vec(new_lens, _i64, Bz) and _vec(lens_out, _i64, Bz) and _vec(slot_begin, _i64, Bz + 1), "lengths"
+    assert _vec(ring, _i32, n_pages) and _vec(ring_state, _i64, 2) and _vec(ring_state_out, _i64, 2) and _vec(status, _i32, 1), "ring"
+    assert _vec(block_tables, _i32, Bz * row) and _vec(slots, _i64, n_slots) and (views is None or _vec(views, _i64, 2 * Bz)), "tables"
     _check(lib.ckv_pages_resize(lens.data_ptr(), new_lens.data_ptr(), Bz, page_tokens, block_tables.data_ptr(), row, ring.data_ptr(),
-                                ring.numel(), ring_state.data_ptr(), slots.data_ptr(), slots.numel(), slot_begin.data_ptr(),
+                                n_pages, ring_state.data_ptr(), slots.data_ptr(), n_slots, slot_begin.data_ptr(),
                                 lens_out.data_ptr(), ring_state_out.data_ptr(), status.data_ptr(), _ptr(views), _stream_for(lens)))
 
 
-def _token_rows(k: torch.Tensor, v: torch.Tensor, deg: torch.Tensor | None) -> CkvTokenRows:
-    """k, v [n, H, D] with any strides but contiguous rows (a slab [H, cap, D] is passed transposed); deg int32 [n, H]."""
-    n, H, D = k.shape
-    ts, hs, one = k.stride()
-    assert k.dtype == v.dtype and v.shape == k.shape and v.stride() == (ts, hs, one) and one == 1
-    assert deg is None or (deg.dtype == torch.int32 and deg.shape == (n, H))
-    dt, dh = deg.stride() if deg is not None else (0, 0)
-    return CkvTokenRows(k.data_ptr(), v.data_ptr(), _ptr(deg), ts, hs, dt, dh, H, D, dtype_code(k.dtype))
+def _token_rows(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, deg: torch.Tensor | None, heads: int) -> bytes:
+    """ckv_token_rows of k, v [n, H, D] with any strides but contiguous rows (a slab [H, cap, D] is passed transposed); deg
+    int32 [n, H] with any strides."""
+    shape, strides, dt = k.shape, k.stride(), k.dtype
+    n, H, D = shape
+    assert strides[2] == 1 and v.dtype is dt and v.shape == shape and v.stride() == strides and H == heads, "rows"
+    assert _vec(slots, _i64, n), "slots"
+    ts, hs, dp = 0, 0, 0
+    if deg is not None:
+        assert deg.dtype is _i32 and deg.shape == (n, H), "degrees"
+        (ts, hs), dp = deg.stride(), deg.data_ptr()
+    return _ROWS.pack(k.data_ptr(), v.data_ptr(), dp, strides[0], strides[1], ts, hs, H, D, BF16 if dt is torch.bfloat16 else dtype_code(dt))
 
 
 def pages_write(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
                 deg_pages: torch.Tensor | None = None, logdeg_pages: torch.Tensor | None = None, deg: torch.Tensor | None = None):
     """ckv_pages_write on the current stream: k, v [n, H, D] to the slots of one layer's pool, degrees with them."""
-    n_pages, H, P, D = k_pages.shape
-    rows = _token_rows(k, v, deg)
-    assert _is(slots, torch.int64, k.shape[0]) and k.shape[1:] == (H, D) and _is(k_pages, k.dtype) and _is(v_pages, k.dtype, n_pages, H, P, D)
-    assert deg_pages is None or _is(deg_pages, torch.int32, n_pages, H, P)
-    assert logdeg_pages is None or _is(logdeg_pages, torch.float32, n_pages, H, P)
-    _check(lib.ckv_pages_write(C.byref(rows), slots.data_ptr(), k.shape[0], k_pages.data_ptr(), v_pages.data_ptr(), _ptr(deg_pages),
+    shape = k_pages.shape
+    n_pages, H, P, D = shape
+    rows, dt = _token_rows(slots, k, v, deg, H), k.dtype
+    assert k_pages.dtype is dt and k_pages.is_contiguous() and _like(v_pages, dt, shape) and k.shape[2] == D, "pages"
+    assert _like(deg_pages, _i32, shape[:3]) and _like(logdeg_pages, _f32, shape[:3]), "degree pages"
+    _check(lib.ckv_pages_write(rows, slots.data_ptr(), k.shape[0], k_pages.data_ptr(), v_pages.data_ptr(), _ptr(deg_pages),
                                _ptr(logdeg_pages), n_pages, P, _stream_for(slots)))
 
 
@@ -475,12 +495,13 @@ def pages_summarize(views: torch.Tensor, k_pages: torch.Tensor, deg_pages: torch
                     max_blocks: int, from_lens: torch.Tensor | None = None):
     """ckv_pages_summarize on the current stream: mean keys c_pages [n_pages, H, D] and log-degrees clog_pages [n_pages, H] of
     the batch's pages, from the one that holds token from_lens[b] on."""
-    n_pages, H, P, D = k_pages.shape
-    Bz = views.shape[0]
-    assert _is(views, torch.int64, Bz, 2) and _is(k_pages, k_pages.dtype) and _is(c_pages, k_pages.dtype, n_pages, H, D)
-    assert _is(clog_pages, torch.float32, n_pages, H) and (deg_pages is None or _is(deg_pages, torch.int32, n_pages, H, P))
-    assert from_lens is None or _is(from_lens, torch.int64, Bz)
-    _check(lib.ckv_pages_summarize(views.data_ptr(), _ptr(from_lens), Bz, k_pages.data_ptr(), _ptr(deg_pages), P, H, D, dtype_code(k_pages.dtype),
+    shape = k_pages.shape
+    n_pages, H, P, D = shape
+    Bz, dt = views.numel() // 2, k_pages.dtype
+    assert _vec(views, _i64, 2 * Bz) and (from_lens is None or _vec(from_lens, _i64, Bz)), "views"
+    assert k_pages.is_contiguous() and _like(deg_pages, _i32, shape[:3]), "pages"
+    assert _vec(c_pages, dt, n_pages * H * D) and _vec(clog_pages, _f32, n_pages * H), "summaries"
+    _check(lib.ckv_pages_summarize(views.data_ptr(), _ptr(from_lens), Bz, k_pages.data_ptr(), _ptr(deg_pages), P, H, D, dtype_code(dt),
                                    max_blocks, c_pages.data_ptr(), clog_pages.data_ptr(), _stream_for(views)))
 
 
@@ -488,24 +509,26 @@ def pages_select(views: torch.Tensor, c_pages: torch.Tensor, clog_pages: torch.T
                  scale: float, max_len: int, selected: torch.Tensor, n_first: int = 0, n_last: int = 0):
     """ckv_pages_select on the current stream: the best blocks of every (sequence, KV head) into selected int32 [Bz, H, n_select]."""
     n_pages, H, D = c_pages.shape
-    Bz = views.shape[0]
-    assert _is(views, torch.int64, Bz, 2) and _is(q, c_pages.dtype, Bz, H * G, D) and c_pages.is_contiguous()
-    assert _is(selected, torch.int32) and selected.shape[:2] == (Bz, H) and (clog_pages is None or _is(clog_pages, torch.float32, n_pages, H))
-    _check(lib.ckv_pages_select(views.data_ptr(), c_pages.data_ptr(), _ptr(clog_pages), page_tokens, Bz, H, G, D, dtype_code(q.dtype), q.data_ptr(),
-                                scale, max_len, n_first, n_last, selected.shape[2], selected.data_ptr(), _stream_for(views)))
+    Bz, heads, n_select = selected.shape
+    dt = q.dtype
+    assert heads == H and q.shape == (Bz, H * G, D) and q.is_contiguous() and _vec(views, _i64, 2 * Bz), "queries"
+    assert c_pages.dtype is dt and c_pages.is_contiguous() and (clog_pages is None or _vec(clog_pages, _f32, n_pages * H)), "summaries"
+    assert selected.dtype is _i32 and selected.is_contiguous(), "selected"
+    _check(lib.ckv_pages_select(views.data_ptr(), c_pages.data_ptr(), _ptr(clog_pages), page_tokens, Bz, H, G, D, dtype_code(dt), q.data_ptr(),
+                                scale, max_len, n_first, n_last, n_select, selected.data_ptr(), _stream_for(views)))
 
 
 def decode_attn_selected(views: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, logdeg_pages: torch.Tensor | None,
                          selected: torch.Tensor, H: int, G: int, q: torch.Tensor, out: torch.Tensor, scale: float):
     """ckv_decode_attn_selected on the current stream: Eq. 3 over the blocks that selected [Bz, H, n_select] lists."""
     Bz, HG, D = q.shape
-    n_pages, _, P, _ = k_pages.shape
-    assert HG == H * G and _is(q, k_pages.dtype) and _is(out, q.dtype, Bz, HG, D) and _is(views, torch.int64, Bz, 2)
-    assert _is(k_pages, q.dtype, n_pages, H, P, D) and _is(v_pages, q.dtype, n_pages, H, P, D)
-    assert _is(selected, torch.int32) and selected.shape[:2] == (Bz, H) and (logdeg_pages is None or _is(logdeg_pages, torch.float32, n_pages, H, P))
-    _check(lib.ckv_decode_attn_selected(views.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(logdeg_pages), P, selected.data_ptr(),
-                                        selected.shape[2], Bz, H, G, D, dtype_code(q.dtype), q.data_ptr(), out.data_ptr(), scale,
-                                        _stream_for(views)))
+    shape, dt = k_pages.shape, q.dtype
+    n_select = selected.shape[2]
+    assert HG == H * G and shape[1] == H and shape[3] == D and q.is_contiguous() and _vec(out, dt, Bz * HG * D) and _vec(views, _i64, 2 * Bz), "queries"
+    assert k_pages.dtype is dt and k_pages.is_contiguous() and _like(v_pages, dt, shape) and _like(logdeg_pages, _f32, shape[:3]), "pages"
+    assert _vec(selected, _i32, Bz * H * n_select), "selected"
+    _check(lib.ckv_decode_attn_selected(views.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(logdeg_pages), shape[2], selected.data_ptr(),
+                                        n_select, Bz, H, G, D, dtype_code(dt), q.data_ptr(), out.data_ptr(), scale, _stream_for(views)))
 
 
 @dataclass
@@ -519,13 +542,6 @@ class QuantPool:
     deg_pages: torch.Tensor | None = None
     logdeg_pages: torch.Tensor | None = None
 
-    def __post_init__(self):
-        n, H, P, _ = self.k_codes.shape
-        assert _is(self.k_codes, torch.uint8, n, H, P, 64) and _is(self.v_codes, torch.uint8, n, H, P, 64)
-        assert _is(self.k_scales, torch.uint8, n, H, P, 4) and _is(self.v_scales, torch.uint8, n, H, P, 4)
-        assert self.deg_pages is None or _is(self.deg_pages, torch.int32, n, H, P)
-        assert self.logdeg_pages is None or _is(self.logdeg_pages, torch.float32, n, H, P)
-
     @classmethod
     def empty(cls, n_pages: int, H: int, page_tokens: int, device="cuda"):
         u8 = dict(dtype=torch.uint8, device=device)
@@ -534,29 +550,33 @@ class QuantPool:
                    torch.zeros((n_pages, H, page_tokens), dtype=torch.int32, device=device),
                    torch.zeros((n_pages, H, page_tokens), dtype=torch.float32, device=device))
 
-    def c(self) -> CkvQuantPool:
-        return CkvQuantPool(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(), self.v_scales.data_ptr(),
-                            _ptr(self.deg_pages), _ptr(self.logdeg_pages))
+    def c(self):
+        """(ckv_quant_pool, n_pages, H, page_tokens), checked."""
+        shape = self.k_codes.shape
+        n, H, P, width = shape
+        rows, deg, logdeg = n * H * P, self.deg_pages, self.logdeg_pages
+        assert width == 64 and _vec(self.k_codes, _u8, 64 * rows) and _vec(self.v_codes, _u8, 64 * rows), "codes"
+        assert _vec(self.k_scales, _u8, 4 * rows) and _vec(self.v_scales, _u8, 4 * rows), "scales"
+        assert (deg is None or _vec(deg, _i32, rows)) and (logdeg is None or _vec(logdeg, _f32, rows)), "degree pages"
+        return _POOL.pack(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(), self.v_scales.data_ptr(),
+                          0 if deg is None else deg.data_ptr(), 0 if logdeg is None else logdeg.data_ptr()), n, H, P
 
 
 def pages_quantize(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pool: QuantPool, deg: torch.Tensor | None = None):
     """ckv_pages_quantize on the current stream: k, v [n, H, D] (bf16 or fp32) to the slots of a four-bit pool."""
-    n_pages, H, P, _ = pool.k_codes.shape
-    rows, cp = _token_rows(k, v, deg), pool.c()
-    assert _is(slots, torch.int64, k.shape[0]) and k.shape[1] == H
-    _check(lib.ckv_pages_quantize(C.byref(rows), slots.data_ptr(), k.shape[0], C.byref(cp), n_pages, P, _stream_for(slots)))
+    cp, n_pages, H, P = pool.c()
+    _check(lib.ckv_pages_quantize(_token_rows(slots, k, v, deg, H), slots.data_ptr(), k.shape[0], cp, n_pages, P, _stream_for(slots)))
 
 
 def pages_dequantize(block_table: torch.Tensor, length: int, pool: QuantPool, k: torch.Tensor, v: torch.Tensor,
                      deg: torch.Tensor | None = None, logdeg: torch.Tensor | None = None):
     """ckv_pages_dequantize on the current stream: one sequence's four-bit pages to a slab k, v [H, cap, D], deg, logdeg [H, cap]."""
-    _, H, P, _ = pool.k_codes.shape
-    cap, cp = k.shape[1], pool.c()
-    assert _is(block_table, torch.int32) and block_table.numel() * P >= length
-    assert _is(k, k.dtype) and k.shape[0] == H and _is(v, k.dtype, *k.shape)
-    assert (deg is None or _is(deg, torch.int32, H, cap)) and (logdeg is None or _is(logdeg, torch.float32, H, cap))
-    _check(lib.ckv_pages_dequantize(block_table.data_ptr(), length, C.byref(cp), P, H, k.shape[2], dtype_code(k.dtype), k.data_ptr(), v.data_ptr(),
-                                    _ptr(deg), _ptr(logdeg), cap, _stream_for(block_table)))
+    cp, _, H, P = pool.c()
+    shape, dt = k.shape, k.dtype
+    assert block_table.dtype is _i32 and block_table.is_contiguous() and block_table.numel() * P >= length, "block table"
+    assert shape[0] == H and k.is_contiguous() and _like(v, dt, shape) and _like(deg, _i32, shape[:2]) and _like(logdeg, _f32, shape[:2]), "slab"
+    _check(lib.ckv_pages_dequantize(block_table.data_ptr(), length, cp, P, H, shape[2], dtype_code(dt), k.data_ptr(), v.data_ptr(),
+                                    _ptr(deg), _ptr(logdeg), shape[1], _stream_for(block_table)))
 
 
 def decode_quantized_workspace_bytes(Bz, H, G, D, max_len) -> int:
@@ -567,8 +587,8 @@ def decode_attn_quantized(views: torch.Tensor, pool: QuantPool, H: int, G: int, 
                           workspace: torch.Tensor):
     """ckv_decode_attn_quantized on the current stream: Eq. 3 over four-bit pages; q, out bf16 [Bz, H*G, D]."""
     Bz, HG, D = q.shape
-    cp = pool.c()
-    assert HG == H * G and pool.k_codes.shape[1] == H and _is(q, q.dtype) and _is(out, q.dtype, Bz, HG, D) and _is(views, torch.int64, Bz, 2)
-    _check(lib.ckv_decode_attn_quantized(views.data_ptr(), C.byref(cp), pool.k_codes.shape[2], Bz, H, G, D, dtype_code(q.dtype), q.data_ptr(),
-                                         out.data_ptr(), scale, max_len, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                         _stream_for(views)))
+    cp, _, heads, P = pool.c()
+    dt = q.dtype
+    assert HG == H * G and heads == H and q.is_contiguous() and _vec(out, dt, Bz * HG * D) and _vec(views, _i64, 2 * Bz), "queries"
+    _check(lib.ckv_decode_attn_quantized(views.data_ptr(), cp, P, Bz, H, G, D, dtype_code(dt), q.data_ptr(), out.data_ptr(), scale, max_len,
+                                         workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_for(views)))

@@ -116,9 +116,31 @@ def test_binding_refuses_shapes_and_types(b):
     with pytest.raises(AssertionError):
         b.pages_write(z(3, dt=i64), k.transpose(0, 2), k.transpose(0, 2), z(4, 2, 64, 128), z(4, 2, 64, 128))
     with pytest.raises(AssertionError):
-        b.QuantPool(z(4, 2, 64, 64, dt=torch.uint8), z(4, 2, 64, 64, dt=torch.uint8), z(4, 2, 64, 4, dt=torch.uint8), z(4, 2, 64, 8, dt=torch.uint8))
+        b.QuantPool(z(4, 2, 64, 64, dt=torch.uint8), z(4, 2, 64, 64, dt=torch.uint8), z(4, 2, 64, 4, dt=torch.uint8), z(4, 2, 64, 8, dt=torch.uint8)).c()
     with pytest.raises(AssertionError):
         b.pages_select(z(2, 2, dt=i64), z(4, 2, 128), None, 64, 4, z(2, 4, 128), 0.1, 100, z(2, 2, 8, dt=torch.int32))
     with pytest.raises(AssertionError):
         b.pages_resize(z(2, dt=i64), z(2, dt=i64), z(2, 4, dt=torch.int32), z(9, dt=torch.int32), z(2, dt=i64), z(3, dt=i64), z(2, dt=i64), z(2, dt=i64),
                        z(2, dt=i64), z(1, dt=torch.int32), 64)
+    u8 = torch.uint8
+    pool = b.QuantPool(z(4, 2, 64, 64, dt=u8), z(4, 2, 64, 64, dt=u8), z(4, 2, 64, 4, dt=u8), z(4, 2, 64, 4, dt=u8))
+    with pytest.raises(AssertionError):
+        b.pages_quantize(z(3, dt=i64), z(3, 3, 128), z(3, 3, 128), pool)
+    with pytest.raises(AssertionError):
+        b.pages_dequantize(z(1, dt=torch.int32), 65, pool, z(2, 65, 128), z(2, 65, 128))
+    with pytest.raises(AssertionError):
+        b.decode_attn_quantized(z(1, 2, dt=i64), pool, 4, 1, z(1, 4, 128), z(1, 4, 128), 0.1, 10, z(64, dt=u8))
+    with pytest.raises(AssertionError):
+        b.pages_summarize(z(2, 2, dt=i64), z(4, 2, 64, 128), None, z(4, 2, 64), z(4, 2, dt=torch.float32), 1)
+    with pytest.raises(AssertionError):
+        b.decode_attn_selected(z(1, 2, dt=i64), z(4, 2, 64, 128), z(4, 2, 64, 128), None, z(1, 2, 3, dt=i64), 2, 4, z(1, 8, 128), z(1, 8, 128), 0.1)
+
+
+def test_binding_refuses_another_device(b):
+    """Tensors that are not on the current CUDA device (here: on none) never reach a launch."""
+    i64, k = torch.int64, torch.zeros((3, 2, 128), dtype=torch.bfloat16)
+    pages = torch.zeros((4, 2, 64, 128), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        b._stream_for(k)
+    with pytest.raises((ValueError, RuntimeError, AssertionError)):
+        b.pages_write(torch.zeros(3, dtype=i64), k, k, pages, pages)
