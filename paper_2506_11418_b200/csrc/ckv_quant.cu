@@ -579,7 +579,47 @@ __global__ void __launch_bounds__(NW * 32, CL > 0 ? 1 : kQCtasPerSm) decode_quan
       uint32_t pk[2][4];  // [group][n]: token 8 n + g, this lane's heads
       bool over = move;
 #pragma unroll 1
-      for (int pass = 0; pass < 2; ++pass) {  // (once more if F has to move, which is rare)
+      for (;;) {
+        if (over) {  // F moves (rarely)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float f[2], q[2];
+            fac[2 * u + j].get(f[0], f[1]);
+            const float2 past = __half22float2(*reinterpret_cast<const __half2*>(&wtop[2 * u + j]));
+            float old[2] = {past.x * corr[0], past.y * corr[1]};  // largest weight before this tile, times the old F
+            float now[2] = {0.f, 0.f};
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+              const float v = reinterpret_cast<const float*>(v_scales + 16 * n)[2 * j];
+              float p0, p1;
+              p[n].get(p0, p1);
+              now[0] = fmaxf(now[0], p0 * v);
+              now[1] = fmaxf(now[1], p1 * v);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float inv = __uint_as_float((254u << 23) - __float_as_uint(f[e]));
+              q[e] = fmaxf(old[e] * inv, now[e]);
+#pragma unroll
+              for (int o = 4; o < 32; o <<= 1) q[e] = fmaxf(q[e], __shfl_xor_sync(0xffffffffu, q[e], o));
+              // F = 2^(7 - floor(log2 q)), 2^126 at most
+              f[e] = __uint_as_float(((254u + kQFactor) << 23) - max(__float_as_uint(q[e]) & 0x7f800000u, (kQFactor + 1u) << 23));
+              const float ratio = corr[e] * f[e] * inv;
+              old[e] = old[e] * inv * f[e];
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                oacc[2 * (2 * u + j) + i][e] *= ratio;
+                oacc[2 * (2 * u + j) + i][2 + e] *= ratio;
+                if (HALF) {
+                  oacc[2 * (2 + j) + i][e] *= ratio;
+                  oacc[2 * (2 + j) + i][2 + e] *= ratio;
+                }
+              }
+            }
+            fac[2 * u + j] = f32x2(f[0], f[1]);
+            wtop[2 * u + j] = pack_f16x2(old[0], old[1]);
+          }
+        }
         uint32_t high[2] = {wtop[2 * u], wtop[2 * u + 1]};
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
@@ -594,50 +634,13 @@ __global__ void __launch_bounds__(NW * 32, CL > 0 ? 1 : kQCtasPerSm) decode_quan
           }
         }
         const uint32_t all = max_f16x2(high[0], high[1]);
-        over |= (all & 0x7fffu) > 0x7800u || all > 0x7800ffffu;  // above 2^15 (the weights are not negative)
-        if (pass == 1 || !__any_sync(0xffffffffu, over)) {  // (still over after F has moved: NaN)
+        const bool too_large = (all & 0x7fffu) > 0x7800u || all > 0x7800ffffu;  // above 2^15 (the weights are not negative)
+        if (over || !__any_sync(0xffffffffu, too_large)) {  // (still too large after F has moved: NaN)
           wtop[2 * u] = high[0];
           wtop[2 * u + 1] = high[1];
           break;
         }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float f[2], q[2];
-          fac[2 * u + j].get(f[0], f[1]);
-          const float2 past = __half22float2(*reinterpret_cast<const __half2*>(&wtop[2 * u + j]));
-          float old[2] = {past.x * corr[0], past.y * corr[1]};  // largest weight before this tile, times the old F
-          float now[2] = {0.f, 0.f};
-#pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            const float v = reinterpret_cast<const float*>(v_scales + 16 * n)[2 * j];
-            float p0, p1;
-            p[n].get(p0, p1);
-            now[0] = fmaxf(now[0], p0 * v);
-            now[1] = fmaxf(now[1], p1 * v);
-          }
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float inv = __uint_as_float((254u << 23) - __float_as_uint(f[e]));
-            q[e] = fmaxf(old[e] * inv, now[e]);
-#pragma unroll
-            for (int o = 4; o < 32; o <<= 1) q[e] = fmaxf(q[e], __shfl_xor_sync(0xffffffffu, q[e], o));
-            // F = 2^(7 - floor(log2 q)), 2^126 at most
-            f[e] = __uint_as_float(((254u + kQFactor) << 23) - max(__float_as_uint(q[e]) & 0x7f800000u, (kQFactor + 1u) << 23));
-            const float ratio = corr[e] * f[e] * inv;
-            old[e] = old[e] * inv * f[e];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              oacc[2 * (2 * u + j) + i][e] *= ratio;
-              oacc[2 * (2 * u + j) + i][2 + e] *= ratio;
-              if (HALF) {
-                oacc[2 * (2 + j) + i][e] *= ratio;
-                oacc[2 * (2 + j) + i][2 + e] *= ratio;
-              }
-            }
-          }
-          fac[2 * u + j] = f32x2(f[0], f[1]);
-          wtop[2 * u + j] = pack_f16x2(old[0], old[1]);
-        }
+        over = true;
       }
       // step s covers tokens 16 s .. 16 s + 15; m tile 2 j + i holds elements 32 j + 4 g + 2 i (row g), + 1 (row g + 8)
 #pragma unroll
@@ -730,14 +733,15 @@ __global__ void __launch_bounds__(NW * 32, CL > 0 ? 1 : kQCtasPerSm) decode_quan
   }
 }
 
-// One CTA per (sequence, query head) joins the partials of the stretches that cover its pair: every warp takes every fourth, a
-// lane owns four columns, and the loads of four partials are in flight at once.
-constexpr int kQCombThreads = 128;
+// One CTA per (sequence, query head) joins the partials of the stretches that cover its pair: its W warps take every W-th, a
+// lane owns four columns, and the loads of four partials are in flight at once.  Eight warps for few rows (their pairs are
+// spread over many stretches), four for a batch.
+constexpr int kQCombThreads = 256;
 
 __global__ void __launch_bounds__(kQCombThreads) quant_combine_kernel(const QuantArgs qa_) {
-  constexpr int W = kQCombThreads / 32;
-  __shared__ float2 s_ml[W];
-  __shared__ float4 s_out[W][32];
+  const int W = blockDim.x / 32;
+  __shared__ float2 s_ml[kQCombThreads / 32];
+  __shared__ float4 s_out[kQCombThreads / 32][32];
   const DecodeArgs& a = qa_.d;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row = blockIdx.x, pair = row / a.G, b = pair / a.H, h = pair - b * a.H;
@@ -775,7 +779,6 @@ __global__ void __launch_bounds__(kQCombThreads) quant_combine_kernel(const Quan
   if (lane == 0) s_ml[warp] = make_float2(m, l);
   __syncthreads();
   if (warp == 0) {
-#pragma unroll
     for (int w = 1; w < W; ++w) add(s_ml[w], s_out[w][lane]);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     store4(reinterpret_cast<__nv_bfloat16*>(a.out) + (int64_t)row * kD + lane * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
@@ -842,7 +845,8 @@ cudaError_t launch_quant(const QuantArgs& a, cudaStream_t st) {
   cfg.numAttrs = CL > 0 ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, decode_quant_kernel<CL, HALF, NW>, a);
   if (e != cudaSuccess || CL > 0) return e;
-  return launch_dependent(quant_combine_kernel, dim3((unsigned)(a.d.Bz * a.d.H * a.d.G)), dim3(kQCombThreads), 0, st, a);
+  const int64_t rows = (int64_t)a.d.Bz * a.d.H * a.d.G;
+  return launch_dependent(quant_combine_kernel, dim3((unsigned)rows), dim3(rows < 512 ? kQCombThreads : kQCombThreads / 2), 0, st, a);
 }
 
 template <bool HALF>
