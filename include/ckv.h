@@ -283,13 +283,13 @@ int ckv_pages_resize(const int64_t* lens, const int64_t* new_lens, int32_t Bz, i
                      int64_t* lens_out, int64_t* ring_state_out, int32_t* status, ckv_paged_view* views_dev, void* cuda_stream);
 
 /* n tokens' keys, values and degrees on their way into pages.  Element d of token i and head h is at
- * k[i * token_stride + h * head_stride + d] (elements; v alike), so a step's [n, H, D], slices of a fused projection and a
- * slab [H, cap, D] all fit.  Rows must be 16-byte aligned: k, v, and both strides in bytes. */
+ * k[i * k_token_stride + h * k_head_stride + d] (in elements; v alike), so a step's [n, H, D], slices of a fused projection
+ * and a slab [H, cap, D] all fit.  Rows must be 16-byte aligned: k, v, and the strides in bytes. */
 typedef struct ckv_token_rows {
   const void* k;
   const void* v;
   const int32_t* deg; /* deg[i * deg_token_stride + h * deg_head_stride], or NULL: all ones */
-  int64_t token_stride, head_stride, deg_token_stride, deg_head_stride;
+  int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride, deg_token_stride, deg_head_stride;
   int32_t H, D, dtype;
 } ckv_token_rows;
 

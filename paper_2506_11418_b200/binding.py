@@ -48,7 +48,8 @@ class CkvParams(C.Structure):
 
 class CkvTokenRows(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("deg", C.c_void_p),
-                ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("deg_token_stride", C.c_int64), ("deg_head_stride", C.c_int64),
+                ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64),
+                ("deg_token_stride", C.c_int64), ("deg_head_stride", C.c_int64),
                 ("H", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32)]
 
 
@@ -427,7 +428,7 @@ def pages_scatter(block_table, length, k, v, deg, k_pages, v_pages, deg_pages, l
 
 _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _i32, _i64, _f32, _u8 = torch.int32, torch.int64, torch.float32, torch.uint8
-_ROWS = struct.Struct("@PPPqqqqiii4x")     # ckv_token_rows
+_ROWS = struct.Struct("@PPPqqqqqqiii4x")     # ckv_token_rows
 _POOL = struct.Struct("@PPPPPP")           # ckv_quant_pool
 
 
@@ -468,15 +469,15 @@ def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_tables: torch
 def _token_rows(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, deg: torch.Tensor | None, heads: int) -> bytes:
     """ckv_token_rows of k, v [n, H, D] with any strides but contiguous rows (a slab [H, cap, D] is passed transposed); deg
     int32 [n, H] with any strides."""
-    shape, strides, dt = k.shape, k.stride(), k.dtype
+    shape, (kt, kh, k1), (vt, vh, v1), dt = k.shape, k.stride(), v.stride(), k.dtype
     n, H, D = shape
-    assert strides[2] == 1 and v.dtype is dt and v.shape == shape and v.stride() == strides and H == heads, "rows"
+    assert k1 == v1 == 1 and v.dtype is dt and v.shape == shape and H == heads, "rows"
     assert _vec(slots, _i64, n), "slots"
     ts, hs, dp = 0, 0, 0
     if deg is not None:
         assert deg.dtype is _i32 and deg.shape == (n, H), "degrees"
         (ts, hs), dp = deg.stride(), deg.data_ptr()
-    return _ROWS.pack(k.data_ptr(), v.data_ptr(), dp, strides[0], strides[1], ts, hs, H, D, BF16 if dt is torch.bfloat16 else dtype_code(dt))
+    return _ROWS.pack(k.data_ptr(), v.data_ptr(), dp, kt, kh, vt, vh, ts, hs, H, D, BF16 if dt is torch.bfloat16 else dtype_code(dt))
 
 
 def pages_write(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,

@@ -102,8 +102,8 @@ __global__ void __launch_bounds__(kQuantThreads) pages_quantize_kernel(const Row
     const int64_t s = i < n ? slots[i] : -1;
     row[u] = (s >= 0 && s < n_rows) ? (((s >> shift) * r.H + h) << shift) + (s & mask) : -1;
     if (row[u] >= 0) {
-      k[u] = load8<F32>(r.k, i * r.token_vecs + h * r.head_vecs, lane16);
-      v[u] = load8<F32>(r.v, i * r.token_vecs + h * r.head_vecs, lane16);
+      k[u] = load8<F32>(r.k, i * r.k_token + h * r.k_head, lane16);
+      v[u] = load8<F32>(r.v, i * r.v_token + h * r.v_head, lane16);
     }
   }
   const int j = lane16 >> 2, t = lane16 & 3;  // this lane's elements: 32 j + 8 t ..

@@ -102,8 +102,8 @@ __global__ void __launch_bounds__(kSumThreads) pages_summarize_kernel(const Summ
 // ---- ckv_pages_select --------------------------------------------------------------------------------------------
 // The result is that of scores computed in 64 bits: a choice between near pages must not hang on the order of a 32-bit sum
 // (it would for about one selection in a thousand).  Few pages are near the border, so only those are scored in 64 bits:
-//  1. All scores in fp32 on the tensor cores, with a bound on how far they may be off: bf16 products are exact in fp32, 128
-//     additions lose at most 2^-23 of sum |q c| each.  A summary row is read once, straight into the lanes that multiply it,
+//  1. All scores in fp32 on the tensor cores, with a bound on how far they may be off: bf16 products are exact in fp32, and
+//     128 additions, cut off rather than rounded, lose at most 2^-23 of sum |q c| each: 2^-15 has a factor of two to spare.  A summary row is read once, straight into the lanes that multiply it,
 //     for all G heads.  The CTAs of a thread-block cluster share the pages; scores land in the first CTA's shared memory.
 //  2. That CTA finds a narrow interval that holds the k-th largest: a histogram over the scores' range, the bin that holds
 //     it, a histogram over that bin if it is still full.
@@ -341,8 +341,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
       if (t < 2) {  // lanes 4 g: row g; 4 g + 1: row g + 8
         const int i = base + g + 8 * t;
         const float s = (t ? sb : sa) + (t ? lb : la);
-        // |q c| scale 2^-16, and the roundings after the sum
-        const float e = (t ? eb : ea) * fabsf(a.scale) * 0x1p-16f + fabsf(t ? lb : la) * 0x1p-20f + 0x1p-120f;
+        // |q| |c| scale 2^-15, and the roundings after the sum
+        const float e = (t ? eb : ea) * fabsf(a.scale) * 0x1p-15f + fabsf(t ? lb : la) * 0x1p-20f + 0x1p-120f;
         if (i < n) {
           err = fmaxf(err, e < 1e30f ? e : INFINITY);  // (NaN becomes infinite)
           if (i >= f0 && i < f1) {

@@ -249,9 +249,8 @@ __global__ void __launch_bounds__(kWriteThreads) pages_write_kernel(const RowsIn
     const int64_t s = i < n ? slots[i] : -1;
     dst[u] = (s >= 0 && s < n_rows) ? ((((s >> shift) * r.H + h) << shift) + (s & mask)) * VEC + c : -1;
     if (dst[u] >= 0) {
-      const int64_t src = i * r.token_vecs + h * r.head_vecs + c;
-      k[u] = reinterpret_cast<const uint4*>(r.k)[src];
-      v[u] = reinterpret_cast<const uint4*>(r.v)[src];
+      k[u] = reinterpret_cast<const uint4*>(r.k)[i * r.k_token + h * r.k_head + c];
+      v[u] = reinterpret_cast<const uint4*>(r.v)[i * r.v_token + h * r.v_head + c];
     }
   }
 #pragma unroll

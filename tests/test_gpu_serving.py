@@ -152,6 +152,11 @@ def token_rows(n, H, dt, layout, seed):
     g = torch.Generator(DEV).manual_seed(seed)
     if layout == "step":
         return tuple(torch.randn((n, H, D), generator=g, device=DEV).to(dt) for _ in range(2))
+    if layout == "mixed":  # keys of a step, values of a slab
+        return (torch.randn((n, H, D), generator=g, device=DEV).to(dt),
+                torch.randn((H, n + 3, D), generator=g, device=DEV).to(dt)[:, :n].transpose(0, 1))
+    if layout == "broadcast":  # one row for all heads
+        return tuple(torch.randn((n, 1, D), generator=g, device=DEV).to(dt).expand(n, H, D) for _ in range(2))
     if layout == "fused":  # slices of a projection's rows
         x = torch.randn((n, 6 * H + 1, D), generator=g, device=DEV).to(dt)
         return x[:, H:2 * H], x[:, 3 * H:4 * H]
@@ -170,7 +175,8 @@ def slot_list(n, n_pages, P, seed):
 
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("n,H,P,layout,with_deg", [(1, 1, 32, "step", False), (17, 3, 64, "fused", True), (1500, 8, 64, "slab", True), (333, 2, 128, "fused", False),
-                                                   (2000, 8, 32, "step", True)])
+                                                   (2000, 8, 32, "step", True), (99, 4, 64, "mixed", True), (40, 8, 32, "broadcast", False),
+                                                   (1, 3, 32, "slab", True), (70, 1, 32, "fused", False)])
 def test_write(dt, n, H, P, layout, with_deg):
     b = lib()
     n_pages = n // P + 4
@@ -515,7 +521,8 @@ def odd_rows(k):
 
 
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("n,H,P,layout", [(1, 1, 32, "step"), (65, 3, 64, "fused"), (2047, 8, 64, "slab"), (300, 2, 256, "step")])
+@pytest.mark.parametrize("n,H,P,layout", [(1, 1, 32, "step"), (65, 3, 64, "fused"), (2047, 8, 64, "slab"), (300, 2, 256, "step"), (77, 4, 32, "mixed"),
+                                          (3, 1, 64, "fused")])
 def test_quantize_and_back(dt, n, H, P, layout):
     b = lib()
     k, v = token_rows(n, H, dt, layout, n)

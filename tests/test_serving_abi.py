@@ -32,7 +32,7 @@ def test_resize_refusals(b, status, kw):
 
 
 def rows(b, **kw):
-    a = dict(k=A, v=2 * A, deg=None, token_stride=1024, head_stride=128, deg_token_stride=0, deg_head_stride=0, H=8, D=128, dtype=b.BF16)
+    a = dict(k=A, v=2 * A, deg=None, kt=1024, kh=128, vt=2048, vh=256, dt=0, dh=0, H=8, D=128, dtype=b.BF16)
     a.update(kw)
     return b.CkvTokenRows(*a.values())
 
@@ -44,8 +44,8 @@ def pool(b, **kw):
 
 
 @pytest.mark.parametrize("status,kw", [
-    (1, dict(k=None)), (1, dict(v=None)), (1, dict(H=0)), (1, dict(dtype=7)), (1, dict(token_stride=-1024)), (1, dict(head_stride=-128)),
-    (2, dict(k=A + 8)), (2, dict(v=A + 4)), (2, dict(token_stride=1028)), (2, dict(head_stride=132)), (6, dict(D=64)), (6, dict(H=65536))])
+    (1, dict(k=None)), (1, dict(v=None)), (1, dict(H=0)), (1, dict(dtype=7)), (1, dict(kt=-1024)), (1, dict(kh=-128)), (1, dict(vt=-8)), (1, dict(vh=-8)), (1, dict(dt=-1)),
+    (2, dict(k=A + 8)), (2, dict(v=A + 4)), (2, dict(kt=1028)), (2, dict(kh=132)), (2, dict(vt=1028)), (2, dict(vh=132)), (6, dict(D=64)), (6, dict(H=65536))])
 def test_token_rows_refusals(b, status, kw):
     r = rows(b, **kw)
     assert b.lib.ckv_pages_write(C.byref(r), 5 * A, 3, 6 * A, 7 * A, None, None, 4, 64, None) == status
