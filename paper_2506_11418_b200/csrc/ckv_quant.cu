@@ -216,21 +216,20 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
 //   V   two tokens' codes are interleaved by nibble before they are unpacked, which gives the operand's pairs of
 //       neighbouring tokens without permuting fp16 values.
 constexpr int kQT = 32;  // tokens per tile
-constexpr int kQStages = 3;
-constexpr int kQCtaWarps = 4, kQCtasPerSm = 3;  // the persistent launch: twelve warps per SM at 168 registers
-constexpr int kQClusterWarps = 8;               // the cluster launch
-constexpr int kQMinShare = 2;                   // tiles per warp of the persistent launch, at least
+constexpr int kQShareWarps = 16, kQShareStages = 2;      // the launch by shares: one CTA per SM, 128 registers per thread
+constexpr int kQClusterWarps = 8, kQClusterStages = 3;   // the launch by clusters
 constexpr int kQCodes = kQT * kCodeBytes;
 constexpr int kQStageBytes = 2 * kQCodes + 2 * kQT * kScaleBytes + kQT * 4;  // codes of K, V; scales of K, V; log-degrees
 constexpr int kQScaleOut = 2 * kQT * 32;                                     // a tile's scales of K, V as fp32, twice each
-constexpr int kQWarpBytes = kQStages * kQStageBytes + kQScaleOut;
-static_assert(kQWarpBytes >= 8 * kPartial * 4 + kQClusterWarps * 16 * 4, "cluster_combine's rows and weights take a warp's share or less");
+constexpr int quant_warp_bytes(int stages) { return stages * kQStageBytes + kQScaleOut; }
+static_assert(quant_warp_bytes(kQClusterStages) >= 8 * kPartial * 4 + kQClusterWarps * 16 * 4, "cluster_combine's rows and weights take a warp's part or less");
+static_assert(quant_warp_bytes(kQShareStages) >= 8 * kPartial * 4, "a warp's partial takes its ring's place");
 constexpr float kQLazy = 6.f;           // exponents up to this above the reference are let through
 constexpr uint32_t kQFactor = 7u;       // F puts the largest weight at 2^7 .. 2^8 when it is set; it may grow to 2^15
 
 struct QuantArgs {
-  DecodeArgs d;        // views, q, out, partial ([warp + pair][G][kPartial], persistent launch), shapes, page_shift
-  int32_t* plan;       // persistent launch, for the combine kernel: tiles of one head before each sequence [Bz + 1], tiles per warp
+  DecodeArgs d;        // views, q, out, partial ([warp + pair][G][kPartial], launch by shares), shapes, page_shift
+  int32_t* plan;       // launch by shares, for the combine kernel: tiles of one head before each sequence [Bz + 1], tiles per warp
   ckv_quant_pool pool;
 };
 
@@ -312,9 +311,10 @@ __device__ __forceinline__ uint32_t v_off(int r, int c) {
 // CL = 0: as many warps as the GPU holds; each takes an equal share of all tiles of the batch, in the order of the pairs, so a
 // ragged batch is balanced to a tile and every warp runs from start to end.  A share may end in one pair and go on in the
 // next: each stretch leaves a partial at index warp + pair, which no other stretch has.
-template <int CL, bool HALF, int NW>
-__global__ void __launch_bounds__(NW * 32, CL > 0 ? 1 : kQCtasPerSm) decode_quant_kernel(const QuantArgs qa_) {
-  constexpr int TT = kQT, ST = kQStages;
+template <int CL, bool HALF>
+__global__ void __launch_bounds__((CL > 0 ? kQClusterWarps : kQShareWarps) * 32, 1) decode_quant_kernel(const QuantArgs qa_) {
+  constexpr int TT = kQT, NW = CL > 0 ? kQClusterWarps : kQShareWarps, ST = CL > 0 ? kQClusterStages : kQShareStages;
+  constexpr int kQWarpBytes = ST * kQStageBytes + kQScaleOut;
   constexpr int NU = HALF ? 1 : 2;  // pairs of groups that a lane weighs
   const DecodeArgs& a = qa_.d;
   extern __shared__ __align__(128) unsigned char smem_raw[];
@@ -328,7 +328,8 @@ __global__ void __launch_bounds__(NW * 32, CL > 0 ? 1 : kQCtasPerSm) decode_quan
   int b, h, tile0;  // where this warp is, and its first tile there
   int share = 0;    // tiles that it has to do from there (CL = 0)
   ckv_paged_view view;
-  const int gw = blockIdx.x * NW + warp;
+  // (shares go round the SMs first, so that a small batch is spread over all of them)
+  const int gw = CL > 0 ? (int)blockIdx.x * NW + warp : warp * (int)gridDim.x + (int)blockIdx.x;
   if constexpr (CL > 0) {
     b = blockIdx.z;
     h = blockIdx.y;
@@ -356,7 +357,7 @@ __global__ void __launch_bounds__(NW * 32, CL > 0 ? 1 : kQCtasPerSm) decode_quan
       total += __shfl_sync(0xffffffffu, sum, 31);
     }
     const uint32_t all = (uint32_t)total * a.H, warps = gridDim.x * NW;
-    share = max((int)((all + warps - 1) / warps), kQMinShare);
+    share = max((int)((all + warps - 1) / warps), 1);
     if (gw == 0 && lane == 0) {
       qa_.plan[a.Bz] = total;
       qa_.plan[a.Bz + 1] = share;
@@ -786,22 +787,23 @@ __global__ void __launch_bounds__(kQCombThreads) quant_combine_kernel(const Quan
 }
 
 // Sets the kernel's shared memory (and a cluster size above 8) once per device; how many clusters fit at once, 0: none
-template <int CL, bool HALF, int NW>
+template <int CL, bool HALF>
 int quant_clusters() {
+  constexpr int NW = CL > 0 ? kQClusterWarps : kQShareWarps, kSmem = NW * quant_warp_bytes(CL > 0 ? kQClusterStages : kQShareStages);
   constexpr int kMaxDev = 64;
   static std::atomic<int> cached[kMaxDev];  // 0 = not asked yet, else the answer + 1
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDev) return 0;
   if ((n = cached[dev].load(std::memory_order_relaxed)) > 0) return n - 1;
-  auto kern = decode_quant_kernel<CL, HALF, NW>;
-  bool ok = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NW * kQWarpBytes) == cudaSuccess;
+  auto kern = decode_quant_kernel<CL, HALF>;
+  bool ok = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) == cudaSuccess;
   if (ok && CL > 8) ok = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
   if (ok && CL == 0) n = 1;
   if (ok && CL > 0) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(CL, 1, 1);
     cfg.blockDim = dim3(NW * 32);
-    cfg.dynamicSmemBytes = NW * kQWarpBytes;
+    cfg.dynamicSmemBytes = kSmem;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = CL;
@@ -818,21 +820,21 @@ int quant_clusters() {
   return n;
 }
 
-// CTAs of the persistent launch: what the GPU holds, or less where max_len says that there is less to do
+// CTAs of the launch by shares: one per SM, or one per tile where max_len says that there are fewer
 int64_t quant_ctas(int32_t Bz, int32_t H, int64_t max_len) {
-  const int64_t tiles = (int64_t)Bz * H * ((max_len + kQT - 1) / kQT), per = kQCtaWarps * kQMinShare;
-  return std::min<int64_t>((int64_t)kQCtasPerSm * sm_count(), std::max<int64_t>(1, (tiles + per - 1) / per));
+  return std::min<int64_t>(sm_count(), std::max<int64_t>(1, (int64_t)Bz * H * ((max_len + kQT - 1) / kQT)));
 }
 
 inline size_t quant_plan_bytes(int32_t Bz) { return ((size_t)(Bz + 2) * 4 + 255) / 256 * 256; }
 
-template <int CL, bool HALF, int NW>
+template <int CL, bool HALF>
 cudaError_t launch_quant(const QuantArgs& a, cudaStream_t st) {
-  if (quant_clusters<CL, HALF, NW>() < 1) return cudaErrorInvalidConfiguration;
+  constexpr int NW = CL > 0 ? kQClusterWarps : kQShareWarps;
+  if (quant_clusters<CL, HALF>() < 1) return cudaErrorInvalidConfiguration;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = CL > 0 ? dim3(CL, (unsigned)a.d.H, (unsigned)a.d.Bz) : dim3((unsigned)quant_ctas(a.d.Bz, a.d.H, a.d.max_len));
   cfg.blockDim = dim3(NW * 32);
-  cfg.dynamicSmemBytes = NW * kQWarpBytes;
+  cfg.dynamicSmemBytes = NW * quant_warp_bytes(CL > 0 ? kQClusterStages : kQShareStages);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -843,7 +845,7 @@ cudaError_t launch_quant(const QuantArgs& a, cudaStream_t st) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CL > 0 ? 2 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, decode_quant_kernel<CL, HALF, NW>, a);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, decode_quant_kernel<CL, HALF>, a);
   if (e != cudaSuccess || CL > 0) return e;
   const int64_t rows = (int64_t)a.d.Bz * a.d.H * a.d.G;
   return launch_dependent(quant_combine_kernel, dim3((unsigned)rows), dim3(rows < 512 ? kQCombThreads : kQCombThreads / 2), 0, st, a);
@@ -856,10 +858,10 @@ cudaError_t launch_quant_heads(const QuantArgs& a, cudaStream_t st) {
   // of 16416 tokens: 15.1 us by clusters, 16.9 by shares; of 131072 tokens: 67 and 47.
   const int64_t pairs = (int64_t)a.d.Bz * a.d.H, tiles = (a.d.max_len + kQT - 1) / kQT;
   auto fits = [&](int clusters, int cl) { return clusters >= pairs && tiles <= (int64_t)16 * cl * kQClusterWarps; };
-  if (fits(quant_clusters<16, HALF, kQClusterWarps>(), 16)) return launch_quant<16, HALF, kQClusterWarps>(a, st);
-  if (fits(quant_clusters<10, HALF, kQClusterWarps>(), 10)) return launch_quant<10, HALF, kQClusterWarps>(a, st);
-  if (fits(quant_clusters<8, HALF, kQClusterWarps>(), 8)) return launch_quant<8, HALF, kQClusterWarps>(a, st);
-  return launch_quant<0, HALF, kQCtaWarps>(a, st);
+  if (fits(quant_clusters<16, HALF>(), 16)) return launch_quant<16, HALF>(a, st);
+  if (fits(quant_clusters<10, HALF>(), 10)) return launch_quant<10, HALF>(a, st);
+  if (fits(quant_clusters<8, HALF>(), 8)) return launch_quant<8, HALF>(a, st);
+  return launch_quant<0, HALF>(a, st);
 }
 
 int check_pool(const ckv_quant_pool* p) {
@@ -920,7 +922,7 @@ int ckv_pages_dequantize(const int32_t* block_table, int64_t len, const ckv_quan
 
 size_t ckv_decode_quantized_workspace_bytes(int32_t Bz, int32_t H, int32_t G, int32_t D, int64_t max_len) {
   if (Bz <= 0 || H <= 0 || G <= 0 || D <= 0 || max_len < 0) return 0;
-  const size_t stretches = (size_t)quant_ctas(Bz, H, max_len) * kQCtaWarps + (size_t)Bz * H;
+  const size_t stretches = (size_t)quant_ctas(Bz, H, max_len) * kQShareWarps + (size_t)Bz * H;
   return quant_plan_bytes(Bz) + (stretches * G * kPartial * sizeof(float) + 255) / 256 * 256;
 }
 
