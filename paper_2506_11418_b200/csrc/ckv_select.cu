@@ -191,7 +191,25 @@ struct SelectShared {
   uint64_t key_lo[kSelWarps], key_hi[kSelWarps];
   int gt[kSelWarps], eq[kSelWarps];
   int bin, above, count, n_near;
+  uint32_t more[kSelMaxBlocks / 32], same[kSelMaxBlocks / 32];  // a bit per block: chosen; equal to the border
 };
+
+// the sum of x over the threads before this one; `part` is scratch for a sum per warp.  All threads call.
+__device__ __forceinline__ int sum_before(int x, int* part) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int y = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int z = __shfl_up_sync(0xffffffffu, y, o);
+    if (lane >= o) y += z;
+  }
+  if (lane == 31) part[warp] = y;
+  __syncthreads();
+  y -= x;
+#pragma unroll
+  for (int w = 0; w < kSelWarps; ++w) y += w < warp ? part[w] : 0;
+  return y;
+}
 
 // The k-th largest of keys[0, n) without the forced ones, k = need > 0 and fewer than all: chosen are keys above `edge` and the
 // first `ties` of those equal to it.  Digits of eight bits from the top of the range that the keys span.
@@ -380,11 +398,16 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
   float lo = INFINITY, hi = -INFINITY, err = 0.f;
   if (tid == 0) sh.n_near = 0;
   __syncthreads();
-#pragma unroll 8
-  for (int w = 0; w < kSelWarps * CL; ++w) {
+  for (int w = lane; w < kSelWarps * CL; w += 32) {
     lo = fminf(lo, sh.lo[w]);
     hi = fmaxf(hi, sh.hi[w]);
     err = fmaxf(err, sh.err[w]);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    err = fmaxf(err, __shfl_xor_sync(0xffffffffu, err, o));
   }
   bool fine = err < 1e30f;  // every score is finite and its error known
   fine &= lo > -1e30f && hi < 1e30f;
@@ -490,46 +513,49 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
     radix_select(keys, n, need, sh, edge, ties);
   }
 
-  // ---- 4. in ascending order: every warp takes a run of consecutive blocks, 32 at a time
-  const int per = ((n + kSelThreads - 1) / kSelThreads) * 32, c0 = min(n, warp * per), c1 = min(n, c0 + per);
-  auto look = [&](int i, bool& more, bool& same) {
-    more = same = false;
-    if (i >= c1) return;
-    if (few) {
-      more = i < f0 || i >= f1 || (need > 0 && score[i] > top);
-    } else {
-      const uint64_t k = keys[i];
-      more = k > edge;
-      same = k == edge;
+  // ---- 4. in ascending order: a bit per block, a place per word of 32 blocks, then a lane per block
+  const int words = (n + 31) / 32;
+#pragma unroll 4
+  for (int w = warp; w < words; w += kSelWarps) {
+    const int i = 32 * w + lane;
+    bool more = false, same = false;
+    if (i < n) {
+      if (few) {
+        more = i < f0 || i >= f1 || (need > 0 && score[i] > top);
+      } else {
+        const uint64_t k = keys[i];
+        more = k > edge;
+        same = k == edge;
+      }
     }
-  };
-  int gt = 0, eq = 0;
-  for (int i = c0; i < c1; i += 32) {
-    bool more, same;
-    look(i + lane, more, same);
-    gt += __popc(__ballot_sync(0xffffffffu, more));
-    eq += __popc(__ballot_sync(0xffffffffu, same));
-  }
-  __syncthreads();  // (sh.gt and sh.eq were read above)
-  if (lane == 0) {
-    sh.gt[warp] = gt;
-    sh.eq[warp] = eq;
+    const uint32_t bm = __ballot_sync(0xffffffffu, more), bs = few ? 0u : __ballot_sync(0xffffffffu, same);
+    if (lane == 0) {
+      sh.more[w] = bm;
+      sh.same[w] = bs;
+    }
   }
   __syncthreads();
-  gt = eq = 0;  // chosen and equal blocks before this warp's
-  for (int w = 0; w < warp; ++w) {
-    gt += sh.gt[w];
-    eq += sh.eq[w];
+  const int per = (words + kSelThreads - 1) / kSelThreads, w0 = min(words, tid * per), w1 = min(words, w0 + per);
+  if (!few) {  // of the equal ones the first `ties`
+    int equal = 0;
+    for (int w = w0; w < w1; ++w) equal += __popc(sh.same[w]);
+    int left = ties - sum_before(equal, sh.eq);
+    for (int w = w0; w < w1; ++w)
+      for (uint32_t bits = sh.same[w]; bits && left > 0; bits &= bits - 1, --left) sh.more[w] |= bits & -bits;
   }
-  const uint32_t below = (1u << lane) - 1u;
-  for (int i = c0; i < c1; i += 32) {
-    bool more, same;
-    look(i + lane, more, same);
-    const uint32_t bm = __ballot_sync(0xffffffffu, more), bs = __ballot_sync(0xffffffffu, same);
-    const int eq_at = eq + __popc(bs & below), at = gt + __popc(bm & below) + min(eq_at, ties);
-    if ((more || (same && eq_at < ties)) && at < a.n_select) out[at] = i + lane;
-    gt += __popc(bm);
-    eq += __popc(bs);
+  int chosen = 0;
+  for (int w = w0; w < w1; ++w) chosen += __popc(sh.more[w]);
+  int at = sum_before(chosen, sh.gt);
+  for (int w = w0; w < w1; ++w) {  // where each word's blocks go
+    sh.same[w] = (uint32_t)at;
+    at += __popc(sh.more[w]);
+  }
+  __syncthreads();
+#pragma unroll 4
+  for (int w = warp; w < words; w += kSelWarps) {
+    const uint32_t bits = sh.more[w];
+    const int to = (int)sh.same[w] + __popc(bits & ((1u << lane) - 1u));
+    if ((bits >> lane & 1u) && to < a.n_select) out[to] = 32 * w + lane;
   }
 }
 
