@@ -53,35 +53,45 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
   return d;
 }
 
-// codes of a lane's eight elements, and its group's scale byte.  Magnitudes compare as their bits do, NaN above infinity.
+// The bits of a lane's largest magnitude, as far as the exponent needs them: the upper 16.  Magnitudes compare as their bits do,
+// NaN above infinity.
 template <bool F32>
-__device__ __forceinline__ uint32_t encode8(const Eight<F32>& v, uint32_t& byte) {
-  const uint32_t w[8] = {v.u[0].x, v.u[0].y, v.u[0].z, v.u[0].w, v.u[F32].x, v.u[F32].y, v.u[F32].z, v.u[F32].w};
-  uint32_t field;  // exponent field of the group's largest magnitude; 255: infinity or NaN
-  if constexpr (F32) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, w[i] & 0x7fffffffu);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    field = top >> 23;
+__device__ __forceinline__ uint32_t top16(const Eight<F32>& v) {
+  constexpr uint32_t kAbs = 0x7fff7fffu;
+  uint32_t w[4];
+  if constexpr (F32) {  // (of two fp32 the upper halves in one register)
+    w[0] = __byte_perm(v.u[0].x, v.u[0].y, 0x7632);
+    w[1] = __byte_perm(v.u[0].z, v.u[0].w, 0x7632);
+    w[2] = __byte_perm(v.u[1].x, v.u[1].y, 0x7632);
+    w[3] = __byte_perm(v.u[1].z, v.u[1].w, 0x7632);
   } else {
-    constexpr uint32_t kAbs = 0x7fff7fffu;
-    uint32_t top = max_u16x2(max_u16x2(w[0] & kAbs, w[1] & kAbs), max_u16x2(w[2] & kAbs, w[3] & kAbs));
-    top = max_u16x2(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max_u16x2(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    field = max(top >> 16, top & 0xffffu) >> 7;
+    w[0] = v.u[0].x; w[1] = v.u[0].y; w[2] = v.u[0].z; w[3] = v.u[0].w;
   }
-  const bool finite = field != 255;
-  byte = finite ? (uint32_t)max((int)field - 2, 0) : 255u;
+  const uint32_t t = max_u16x2(max_u16x2(w[0] & kAbs, w[1] & kAbs), max_u16x2(w[2] & kAbs, w[3] & kAbs));
+  return max(t >> 16, t & 0xffffu);
+}
+
+// codes of a lane's eight elements, and its group's scale byte; top: the group's largest magnitude, its upper 16 bits
+template <bool F32>
+__device__ __forceinline__ uint32_t encode8(const Eight<F32>& v, uint32_t top, uint32_t& byte) {
+  const uint32_t field = top >> 7;  // its exponent field; 255: infinity or NaN
+  byte = field == 255 ? 255u : (uint32_t)max((int)field - 2, 0);
   const float f = __uint_as_float((254u - byte) << 23);  // 2^(127 - byte), byte <= 252: products are exact
   float x[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = F32 ? __uint_as_float(w[i]) : __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
-    x[i] = y * f;
+  for (int i = 0; i < 4; ++i) {
+    float a, b;
+    if constexpr (F32) {
+      a = __uint_as_float((i & 1) ? v.u[i >> 1].z : v.u[i >> 1].x);
+      b = __uint_as_float((i & 1) ? v.u[i >> 1].w : v.u[i >> 1].y);
+    } else {
+      const uint32_t w = i == 0 ? v.u[0].x : i == 1 ? v.u[0].y : i == 2 ? v.u[0].z : v.u[0].w;
+      a = __uint_as_float(w << 16);
+      b = __uint_as_float(w & 0xffff0000u);
+    }
+    ptx::mul_f32x2(x[2 * i], x[2 * i + 1], a, b, f);
   }
-  return finite ? ptx::pack_e2m1x8(x) : 0u;
+  return field == 255 ? 0u : ptx::pack_e2m1x8(x);
 }
 
 constexpr int kQuantThreads = 256;
@@ -94,14 +104,15 @@ __global__ void __launch_bounds__(kQuantThreads) pages_quantize_kernel(const Row
   const int64_t i0 = (int64_t)blockIdx.x * (kRows * U), mask = ((int64_t)1 << shift) - 1;
   griddep_wait();
   griddep_launch();
-  int64_t row[U];
+  uint32_t row[U];  // (the rows of a pool fit 31 bits: the host checks)
   Eight<F32> k[U] = {}, v[U] = {};
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t i = i0 + u * kRows + r0;
-    const int64_t s = i < n ? slots[i] : -1;
-    row[u] = (s >= 0 && s < n_rows) ? (((s >> shift) * r.H + h) << shift) + (s & mask) : -1;
-    if (row[u] >= 0) {
+    const uint64_t s = i < n ? (uint64_t)slots[i] : ~0ull;
+    row[u] = ~0u;
+    if (s < (uint64_t)n_rows) {
+      row[u] = ((((uint32_t)s >> shift) * r.H + h) << shift) + ((uint32_t)s & (uint32_t)mask);
       k[u] = load8<F32>(r.k, i * r.k_token + h * r.k_head, lane16);
       v[u] = load8<F32>(r.v, i * r.v_token + h * r.v_head, lane16);
     }
@@ -109,16 +120,19 @@ __global__ void __launch_bounds__(kQuantThreads) pages_quantize_kernel(const Row
   const int j = lane16 >> 2, t = lane16 & 3;  // this lane's elements: 32 j + 8 t ..
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    uint32_t ks, vs;
-    const uint32_t kc = encode8<F32>(k[u], ks), vc = encode8<F32>(v[u], vs);
-    if (row[u] < 0) continue;
-    reinterpret_cast<uint32_t*>(pool.k_codes)[row[u] * 16 + 4 * t + j] = kc;
-    uint16_t* vd = reinterpret_cast<uint16_t*>(pool.v_codes) + row[u] * 32 + 8 * t + j;  // g = 2 t and 2 t + 1
+    // K's largest in the lower half, V's in the upper: one exchange for both over the group's four lanes
+    uint32_t top = top16<F32>(k[u]) | top16<F32>(v[u]) << 16, ks, vs;
+    top = max_u16x2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max_u16x2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    if (row[u] == ~0u) continue;
+    const uint32_t kc = encode8<F32>(k[u], top & 0xffffu, ks), vc = encode8<F32>(v[u], top >> 16, vs);
+    reinterpret_cast<uint32_t*>(pool.k_codes)[(size_t)row[u] * 16 + 4 * t + j] = kc;
+    uint16_t* vd = reinterpret_cast<uint16_t*>(pool.v_codes) + (size_t)row[u] * 32 + 8 * t + j;  // g = 2 t and 2 t + 1
     vd[0] = (uint16_t)vc;
     vd[4] = (uint16_t)(vc >> 16);
     if (t == 0) {
-      pool.k_scales[row[u] * 4 + j] = (uint8_t)ks;
-      pool.v_scales[row[u] * 4 + j] = (uint8_t)vs;
+      pool.k_scales[(size_t)row[u] * 4 + j] = (uint8_t)ks;
+      pool.v_scales[(size_t)row[u] * 4 + j] = (uint8_t)vs;
     }
   }
   if (pool.deg_pages || pool.logdeg_pages) write_degrees(r, slots, n, i0, kRows * U, h, pool.deg_pages, pool.logdeg_pages, n_rows, shift);
@@ -857,7 +871,7 @@ cudaError_t launch_quant_heads(const QuantArgs& a, cudaStream_t st) {
   // SMs a cluster cannot use (all but 80 of 148 for 8 pairs) count for more than the second kernel (about 5 us).  8 pairs
   // of 16416 tokens: 15.1 us by clusters, 16.9 by shares; of 131072 tokens: 67 and 47.
   const int64_t pairs = (int64_t)a.d.Bz * a.d.H, tiles = (a.d.max_len + kQT - 1) / kQT;
-  auto fits = [&](int clusters, int cl) { return clusters >= pairs && tiles <= (int64_t)16 * cl * kQClusterWarps; };
+  auto fits = [&](int clusters, int cl) { return clusters >= pairs && tiles <= (int64_t)128 * cl; };
   if (fits(quant_clusters<16, HALF>(), 16)) return launch_quant<16, HALF>(a, st);
   if (fits(quant_clusters<10, HALF>(), 10)) return launch_quant<10, HALF>(a, st);
   if (fits(quant_clusters<8, HALF>(), 8)) return launch_quant<8, HALF>(a, st);
@@ -885,6 +899,7 @@ int ckv_pages_quantize(const ckv_token_rows* rows, const int64_t* slots, int64_t
   const RowsIn r = rows_in(*rows);
   const int shift = page_shift(page_tokens);
   const int64_t n_rows = n_pages << shift;
+  if (n_rows > INT32_MAX / rows->H) return CKV_ERR_UNSUPPORTED;  // (2^31 rows of a pool: 290 GB)
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   auto go = [&](auto kernel, int rows_per_cta) {
     const dim3 grid((unsigned)((n + rows_per_cta - 1) / rows_per_cta), (unsigned)rows->H);
