@@ -424,11 +424,12 @@ def pages_scatter(block_table, length, k, v, deg, k_pages, v_pages, deg_pages, l
 
 
 # ---- block tables and slot maps, attention over selected pages, four-bit pages
-# (Calls of a few microseconds on the GPU: the checks are kept to what a wrong pointer could come from.)
+# (Calls of a few microseconds on the GPU: what is checked of a tensor is its size in bytes and that it is contiguous, which is what
+# a wrong read or write could come from, and its type where the library is told one.)
 
 _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-_i32, _i64, _f32, _u8 = torch.int32, torch.int64, torch.float32, torch.uint8
-_ROWS = struct.Struct("@PPPqqqqqqiii4x")     # ckv_token_rows
+_i32, _i64 = torch.int32, torch.int64
+_ROWS = struct.Struct("@PPPqqqqqqiii4x")   # ckv_token_rows
 _POOL = struct.Struct("@PPPPPP")           # ckv_quant_pool
 
 
@@ -440,15 +441,6 @@ def _stream_for(t: torch.Tensor):
     return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
-def _vec(t: torch.Tensor, dtype: torch.dtype, n: int) -> bool:
-    return t.dtype is dtype and t.numel() == n and t.is_contiguous()
-
-
-def _like(t: torch.Tensor | None, dtype: torch.dtype, shape) -> bool:
-    """None, or a contiguous tensor of that type and shape."""
-    return t is None or (t.dtype is dtype and t.shape == shape and t.is_contiguous())
-
-
 def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_tables: torch.Tensor, ring: torch.Tensor, ring_state: torch.Tensor,
                  slots: torch.Tensor, slot_begin: torch.Tensor, lens_out: torch.Tensor, ring_state_out: torch.Tensor, status: torch.Tensor,
                  page_tokens: int, views: torch.Tensor | None = None):
@@ -458,9 +450,12 @@ def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_tables: torch
     views int64 [Bz, 2] (paged_views' layout)."""
     Bz, row = block_tables.shape
     n_pages, n_slots = ring.numel(), slots.numel()
-    assert _vec(lens, _i64, Bz) and _vec(new_lens, _i64, Bz) and _vec(lens_out, _i64, Bz) and _vec(slot_begin, _i64, Bz + 1), "lengths"
-    assert _vec(ring, _i32, n_pages) and _vec(ring_state, _i64, 2) and _vec(ring_state_out, _i64, 2) and _vec(status, _i32, 1), "ring"
-    assert _vec(block_tables, _i32, Bz * row) and _vec(slots, _i64, n_slots) and (views is None or _vec(views, _i64, 2 * Bz)), "tables"
+    assert lens.nbytes == new_lens.nbytes == lens_out.nbytes == slot_begin.nbytes - 8 == 8 * Bz, "lengths"
+    assert lens.is_contiguous() and new_lens.is_contiguous() and lens_out.is_contiguous() and slot_begin.is_contiguous(), "lengths"
+    assert ring_state.nbytes == ring_state_out.nbytes == 16 and ring_state.is_contiguous() and ring_state_out.is_contiguous(), "ring"
+    assert ring.dtype is _i32 and ring.is_contiguous() and status.nbytes == 4, "ring"
+    assert block_tables.dtype is _i32 and block_tables.is_contiguous() and slots.dtype is _i64 and slots.is_contiguous(), "tables"
+    assert views is None or views.nbytes == 16 * Bz and views.is_contiguous(), "views"
     _check(lib.ckv_pages_resize(lens.data_ptr(), new_lens.data_ptr(), Bz, page_tokens, block_tables.data_ptr(), row, ring.data_ptr(),
                                 n_pages, ring_state.data_ptr(), slots.data_ptr(), n_slots, slot_begin.data_ptr(),
                                 lens_out.data_ptr(), ring_state_out.data_ptr(), status.data_ptr(), _ptr(views), _stream_for(lens)))
@@ -469,26 +464,26 @@ def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_tables: torch
 def _token_rows(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, deg: torch.Tensor | None, heads: int) -> bytes:
     """ckv_token_rows of k, v [n, H, D] with any strides but contiguous rows (a slab [H, cap, D] is passed transposed); deg
     int32 [n, H] with any strides."""
-    shape, (kt, kh, k1), (vt, vh, v1), dt = k.shape, k.stride(), v.stride(), k.dtype
-    n, H, D = shape
-    assert k1 == v1 == 1 and v.dtype is dt and v.shape == shape and H == heads, "rows"
-    assert _vec(slots, _i64, n), "slots"
+    (n, H, D), (kt, kh, k1), (vt, vh, v1), dt = k.shape, k.stride(), v.stride(), k.dtype
+    assert k1 == v1 == 1 and v.dtype is dt and v.shape == (n, H, D) and H == heads, "rows"
+    assert slots.nbytes == 8 * n and slots.is_contiguous(), "slots"
     ts, hs, dp = 0, 0, 0
     if deg is not None:
         assert deg.dtype is _i32 and deg.shape == (n, H), "degrees"
         (ts, hs), dp = deg.stride(), deg.data_ptr()
-    return _ROWS.pack(k.data_ptr(), v.data_ptr(), dp, kt, kh, vt, vh, ts, hs, H, D, BF16 if dt is torch.bfloat16 else dtype_code(dt))
+    return _ROWS.pack(k.data_ptr(), v.data_ptr(), dp, kt, kh, vt, vh, ts, hs, H, D, _DTYPE_CODES[dt])
 
 
 def pages_write(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
                 deg_pages: torch.Tensor | None = None, logdeg_pages: torch.Tensor | None = None, deg: torch.Tensor | None = None):
     """ckv_pages_write on the current stream: k, v [n, H, D] to the slots of one layer's pool, degrees with them."""
-    shape = k_pages.shape
-    n_pages, H, P, D = shape
-    rows, dt = _token_rows(slots, k, v, deg, H), k.dtype
-    assert k_pages.dtype is dt and k_pages.is_contiguous() and _like(v_pages, dt, shape) and k.shape[2] == D, "pages"
-    assert _like(deg_pages, _i32, shape[:3]) and _like(logdeg_pages, _f32, shape[:3]), "degree pages"
-    _check(lib.ckv_pages_write(rows, slots.data_ptr(), k.shape[0], k_pages.data_ptr(), v_pages.data_ptr(), _ptr(deg_pages),
+    n_pages, H, P, D = k_pages.shape
+    rows, per_row = _token_rows(slots, k, v, deg, H), 4 * n_pages * H * P
+    assert k_pages.dtype is v_pages.dtype is k.dtype and k_pages.nbytes == v_pages.nbytes and k.shape[2] == D, "pages"
+    assert k_pages.is_contiguous() and v_pages.is_contiguous(), "pages"
+    assert deg_pages is None or deg_pages.nbytes == per_row and deg_pages.is_contiguous(), "degree pages"
+    assert logdeg_pages is None or logdeg_pages.nbytes == per_row and logdeg_pages.is_contiguous(), "log-degree pages"
+    _check(lib.ckv_pages_write(rows, slots.data_ptr(), slots.numel(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(deg_pages),
                                _ptr(logdeg_pages), n_pages, P, _stream_for(slots)))
 
 
@@ -496,13 +491,13 @@ def pages_summarize(views: torch.Tensor, k_pages: torch.Tensor, deg_pages: torch
                     max_blocks: int, from_lens: torch.Tensor | None = None):
     """ckv_pages_summarize on the current stream: mean keys c_pages [n_pages, H, D] and log-degrees clog_pages [n_pages, H] of
     the batch's pages, from the one that holds token from_lens[b] on."""
-    shape = k_pages.shape
-    n_pages, H, P, D = shape
-    Bz, dt = views.numel() // 2, k_pages.dtype
-    assert _vec(views, _i64, 2 * Bz) and (from_lens is None or _vec(from_lens, _i64, Bz)), "views"
-    assert k_pages.is_contiguous() and _like(deg_pages, _i32, shape[:3]), "pages"
-    assert _vec(c_pages, dt, n_pages * H * D) and _vec(clog_pages, _f32, n_pages * H), "summaries"
-    _check(lib.ckv_pages_summarize(views.data_ptr(), _ptr(from_lens), Bz, k_pages.data_ptr(), _ptr(deg_pages), P, H, D, dtype_code(dt),
+    n_pages, H, P, D = k_pages.shape
+    Bz, dt, heads = views.numel() // 2, k_pages.dtype, n_pages * H
+    assert views.dtype is _i64 and views.is_contiguous() and (from_lens is None or from_lens.nbytes == 8 * Bz and from_lens.is_contiguous()), "views"
+    assert k_pages.is_contiguous() and (deg_pages is None or deg_pages.nbytes == 4 * heads * P and deg_pages.is_contiguous()), "pages"
+    assert c_pages.dtype is dt and c_pages.numel() == heads * D and c_pages.is_contiguous(), "summaries"
+    assert clog_pages.nbytes == 4 * heads and clog_pages.is_contiguous(), "summaries"
+    _check(lib.ckv_pages_summarize(views.data_ptr(), _ptr(from_lens), Bz, k_pages.data_ptr(), _ptr(deg_pages), P, H, D, _DTYPE_CODES[dt],
                                    max_blocks, c_pages.data_ptr(), clog_pages.data_ptr(), _stream_for(views)))
 
 
@@ -512,10 +507,11 @@ def pages_select(views: torch.Tensor, c_pages: torch.Tensor, clog_pages: torch.T
     n_pages, H, D = c_pages.shape
     Bz, heads, n_select = selected.shape
     dt = q.dtype
-    assert heads == H and q.shape == (Bz, H * G, D) and q.is_contiguous() and _vec(views, _i64, 2 * Bz), "queries"
-    assert c_pages.dtype is dt and c_pages.is_contiguous() and (clog_pages is None or _vec(clog_pages, _f32, n_pages * H)), "summaries"
+    assert heads == H and q.shape == (Bz, H * G, D) and q.is_contiguous() and views.nbytes == 16 * Bz and views.is_contiguous(), "queries"
+    assert c_pages.dtype is dt and c_pages.is_contiguous(), "summaries"
+    assert clog_pages is None or clog_pages.nbytes == 4 * n_pages * H and clog_pages.is_contiguous(), "summaries"
     assert selected.dtype is _i32 and selected.is_contiguous(), "selected"
-    _check(lib.ckv_pages_select(views.data_ptr(), c_pages.data_ptr(), _ptr(clog_pages), page_tokens, Bz, H, G, D, dtype_code(dt), q.data_ptr(),
+    _check(lib.ckv_pages_select(views.data_ptr(), c_pages.data_ptr(), _ptr(clog_pages), page_tokens, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(),
                                 scale, max_len, n_first, n_last, n_select, selected.data_ptr(), _stream_for(views)))
 
 
@@ -523,13 +519,15 @@ def decode_attn_selected(views: torch.Tensor, k_pages: torch.Tensor, v_pages: to
                          selected: torch.Tensor, H: int, G: int, q: torch.Tensor, out: torch.Tensor, scale: float):
     """ckv_decode_attn_selected on the current stream: Eq. 3 over the blocks that selected [Bz, H, n_select] lists."""
     Bz, HG, D = q.shape
-    shape, dt = k_pages.shape, q.dtype
-    n_select = selected.shape[2]
-    assert HG == H * G and shape[1] == H and shape[3] == D and q.is_contiguous() and _vec(out, dt, Bz * HG * D) and _vec(views, _i64, 2 * Bz), "queries"
-    assert k_pages.dtype is dt and k_pages.is_contiguous() and _like(v_pages, dt, shape) and _like(logdeg_pages, _f32, shape[:3]), "pages"
-    assert _vec(selected, _i32, Bz * H * n_select), "selected"
-    _check(lib.ckv_decode_attn_selected(views.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(logdeg_pages), shape[2], selected.data_ptr(),
-                                        n_select, Bz, H, G, D, dtype_code(dt), q.data_ptr(), out.data_ptr(), scale, _stream_for(views)))
+    n_pages, heads, P, width = k_pages.shape
+    dt, n_select = q.dtype, selected.shape[2]
+    assert HG == H * G and heads == H and width == D and q.is_contiguous() and views.nbytes == 16 * Bz and views.is_contiguous(), "queries"
+    assert out.dtype is dt and out.numel() == Bz * HG * D and out.is_contiguous(), "out"
+    assert k_pages.dtype is v_pages.dtype is dt and k_pages.nbytes == v_pages.nbytes and k_pages.is_contiguous() and v_pages.is_contiguous(), "pages"
+    assert logdeg_pages is None or logdeg_pages.nbytes == 4 * n_pages * H * P and logdeg_pages.is_contiguous(), "log-degree pages"
+    assert selected.dtype is _i32 and selected.numel() == Bz * H * n_select and selected.is_contiguous(), "selected"
+    _check(lib.ckv_decode_attn_selected(views.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(logdeg_pages), P, selected.data_ptr(),
+                                        n_select, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(), out.data_ptr(), scale, _stream_for(views)))
 
 
 @dataclass
@@ -553,31 +551,34 @@ class QuantPool:
 
     def c(self):
         """(ckv_quant_pool, n_pages, H, page_tokens), checked."""
-        shape = self.k_codes.shape
-        n, H, P, width = shape
-        rows, deg, logdeg = n * H * P, self.deg_pages, self.logdeg_pages
-        assert width == 64 and _vec(self.k_codes, _u8, 64 * rows) and _vec(self.v_codes, _u8, 64 * rows), "codes"
-        assert _vec(self.k_scales, _u8, 4 * rows) and _vec(self.v_scales, _u8, 4 * rows), "scales"
-        assert (deg is None or _vec(deg, _i32, rows)) and (logdeg is None or _vec(logdeg, _f32, rows)), "degree pages"
-        return _POOL.pack(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(), self.v_scales.data_ptr(),
-                          0 if deg is None else deg.data_ptr(), 0 if logdeg is None else logdeg.data_ptr()), n, H, P
+        kc, vc, ks, vs, deg, logdeg = self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.deg_pages, self.logdeg_pages
+        n, H, P, width = kc.shape
+        per_row = 4 * n * H * P
+        assert width == 64 and kc.nbytes == vc.nbytes == 16 * per_row and kc.is_contiguous() and vc.is_contiguous(), "codes"
+        assert ks.nbytes == vs.nbytes == per_row and ks.is_contiguous() and vs.is_contiguous(), "scales"
+        assert deg is None or deg.nbytes == per_row and deg.is_contiguous(), "degree pages"
+        assert logdeg is None or logdeg.nbytes == per_row and logdeg.is_contiguous(), "log-degree pages"
+        return _POOL.pack(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), 0 if deg is None else deg.data_ptr(),
+                          0 if logdeg is None else logdeg.data_ptr()), n, H, P
 
 
 def pages_quantize(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pool: QuantPool, deg: torch.Tensor | None = None):
     """ckv_pages_quantize on the current stream: k, v [n, H, D] (bf16 or fp32) to the slots of a four-bit pool."""
     cp, n_pages, H, P = pool.c()
-    _check(lib.ckv_pages_quantize(_token_rows(slots, k, v, deg, H), slots.data_ptr(), k.shape[0], cp, n_pages, P, _stream_for(slots)))
+    _check(lib.ckv_pages_quantize(_token_rows(slots, k, v, deg, H), slots.data_ptr(), slots.numel(), cp, n_pages, P, _stream_for(slots)))
 
 
 def pages_dequantize(block_table: torch.Tensor, length: int, pool: QuantPool, k: torch.Tensor, v: torch.Tensor,
                      deg: torch.Tensor | None = None, logdeg: torch.Tensor | None = None):
     """ckv_pages_dequantize on the current stream: one sequence's four-bit pages to a slab k, v [H, cap, D], deg, logdeg [H, cap]."""
     cp, _, H, P = pool.c()
-    shape, dt = k.shape, k.dtype
+    (heads, cap, D), dt = k.shape, k.dtype
     assert block_table.dtype is _i32 and block_table.is_contiguous() and block_table.numel() * P >= length, "block table"
-    assert shape[0] == H and k.is_contiguous() and _like(v, dt, shape) and _like(deg, _i32, shape[:2]) and _like(logdeg, _f32, shape[:2]), "slab"
-    _check(lib.ckv_pages_dequantize(block_table.data_ptr(), length, cp, P, H, shape[2], dtype_code(dt), k.data_ptr(), v.data_ptr(),
-                                    _ptr(deg), _ptr(logdeg), shape[1], _stream_for(block_table)))
+    assert heads == H and v.dtype is dt and v.nbytes == k.nbytes and k.is_contiguous() and v.is_contiguous(), "slab"
+    assert deg is None or deg.nbytes == 4 * H * cap and deg.is_contiguous(), "degrees"
+    assert logdeg is None or logdeg.nbytes == 4 * H * cap and logdeg.is_contiguous(), "log-degrees"
+    _check(lib.ckv_pages_dequantize(block_table.data_ptr(), length, cp, P, H, D, _DTYPE_CODES[dt], k.data_ptr(), v.data_ptr(),
+                                    _ptr(deg), _ptr(logdeg), cap, _stream_for(block_table)))
 
 
 def decode_quantized_workspace_bytes(Bz, H, G, D, max_len) -> int:
@@ -590,6 +591,7 @@ def decode_attn_quantized(views: torch.Tensor, pool: QuantPool, H: int, G: int, 
     Bz, HG, D = q.shape
     cp, _, heads, P = pool.c()
     dt = q.dtype
-    assert HG == H * G and heads == H and q.is_contiguous() and _vec(out, dt, Bz * HG * D) and _vec(views, _i64, 2 * Bz), "queries"
-    _check(lib.ckv_decode_attn_quantized(views.data_ptr(), cp, P, Bz, H, G, D, dtype_code(dt), q.data_ptr(), out.data_ptr(), scale, max_len,
-                                         workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_for(views)))
+    assert HG == H * G and heads == H and q.is_contiguous() and views.nbytes == 16 * Bz and views.is_contiguous(), "queries"
+    assert out.dtype is dt and out.numel() == Bz * HG * D and out.is_contiguous(), "out"
+    _check(lib.ckv_decode_attn_quantized(views.data_ptr(), cp, P, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(), out.data_ptr(), scale, max_len,
+                                         workspace.data_ptr(), workspace.nbytes, _stream_for(views)))
