@@ -238,26 +238,30 @@ __global__ void __launch_bounds__(kWriteThreads) pages_write_kernel(const RowsIn
                                                                     int32_t* deg_pages, float* logdeg_pages, int64_t n_rows, int32_t shift) {
   constexpr int kRows = kWriteThreads / VEC;
   const int h = blockIdx.y, c = threadIdx.x % VEC, r0 = threadIdx.x / VEC;
-  const int64_t i0 = (int64_t)blockIdx.x * (kRows * U), mask = ((int64_t)1 << shift) - 1;
+  const int64_t i0 = (int64_t)blockIdx.x * (kRows * U);
+  const uint32_t mask = (1u << shift) - 1u;
   griddep_wait();
   griddep_launch();
-  int64_t dst[U];
+  const uint4* const k_from = reinterpret_cast<const uint4*>(r.k) + h * r.k_head + c;
+  const uint4* const v_from = reinterpret_cast<const uint4*>(r.v) + h * r.v_head + c;
+  uint32_t row[U];  // (the rows of a pool fit 31 bits: the host checks)
   uint4 k[U], v[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t i = i0 + u * kRows + r0;
-    const int64_t s = i < n ? slots[i] : -1;
-    dst[u] = (s >= 0 && s < n_rows) ? ((((s >> shift) * r.H + h) << shift) + (s & mask)) * VEC + c : -1;
-    if (dst[u] >= 0) {
-      k[u] = reinterpret_cast<const uint4*>(r.k)[i * r.k_token + h * r.k_head + c];
-      v[u] = reinterpret_cast<const uint4*>(r.v)[i * r.v_token + h * r.v_head + c];
+    const uint64_t s = i < n ? (uint64_t)slots[i] : ~0ull;
+    row[u] = ~0u;
+    if (s < (uint64_t)n_rows) {
+      row[u] = ((((uint32_t)s >> shift) * r.H + h) << shift) + ((uint32_t)s & mask);
+      k[u] = k_from[i * r.k_token];
+      v[u] = v_from[i * r.v_token];
     }
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (dst[u] < 0) continue;
-    k_pages[dst[u]] = k[u];
-    v_pages[dst[u]] = v[u];
+    if (row[u] == ~0u) continue;
+    k_pages[(size_t)row[u] * VEC + c] = k[u];
+    v_pages[(size_t)row[u] * VEC + c] = v[u];
   }
   if (deg_pages || logdeg_pages) write_degrees(r, slots, n, i0, kRows * U, h, deg_pages, logdeg_pages, n_rows, shift);
 }
@@ -303,6 +307,7 @@ int ckv_pages_write(const ckv_token_rows* rows, const int64_t* slots, int64_t n,
   const RowsIn r = rows_in(*rows);
   const int shift = page_shift(page_tokens);
   const int64_t n_rows = n_pages << shift;
+  if (n_rows > INT32_MAX / rows->H) return CKV_ERR_UNSUPPORTED;  // (2^31 rows of a bf16 pool: 1 TB)
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   auto go = [&](auto kernel, int rows_per_cta) {
     const dim3 grid((unsigned)((n + rows_per_cta - 1) / rows_per_cta), (unsigned)rows->H);
