@@ -8,9 +8,10 @@ Tolerances (half a step of a type, relative: bf16 2^-8, fp16 2^-11, fp32 2^-24)
   log-degrees      1e-6 relative (logf).
   mean keys        the result's rounding to bf16, and the fp32 sum's: page + 2 roundings of sum w |k| / sum w.
   attention, bf16  parity_util.check_attention's bound.
-  attention, 4 bit the result's rounding to bf16; each weight's to fp16 (twice that, since weights from 2^-28 of the largest
-                   on lose more, and at most 2^-38 of it each); scores in fp32: 2^-20 of sum |q k| scale + |bias|, as a
-                   relative error of every weight, in the numerator and the denominator.
+  attention, 4 bit the result's rounding to bf16; each weight's to fp16 (2^-11 relative, and twice that for the products before
+                   it); weights below 2^-21 of the group's largest are multiples of 2^-31 of it, off by half of that, times a
+                   level of 6 at most and a token each; scores in fp32: 2^-20 of sum |q k| scale + |bias|, as a relative error
+                   of every weight, in the numerator and the denominator.
 """
 import math
 
@@ -628,10 +629,11 @@ def quant_attention(lens, H, G, P, seed, with_logdeg=True, q_change=None, scale=
         w = np.exp(s - s.max(-1, keepdims=True))
         w /= w.sum(-1, keepdims=True)
         ref = np.einsum("hgn,hnd->hgd", w, V)
-        # every weight: twice half an fp16 step, its score's error, and what lies below 2^-28 of the group's largest weight
+        # every weight: twice half an fp16 step, its score's error, and what lies below 2^-21 of the group's largest weight
+        # (a group's largest level is 4 or 6, so its unit is scale_v / 4, and 6 levels times 2^-32 are 1.5 x 2^-32 of w scale_v)
         rel = 2.0 ** -10 + 2 * err_s.max(-1, keepdims=True)
         scale_v = 2.0 ** np.floor(np.log2(np.maximum(np.abs(V).reshape(H, n, 4, 32).max(-1), 2.0 ** -120)))
-        floor = 2.0 ** -36 * n * (w[..., None] * scale_v[:, None]).max(2)
+        floor = 1.5 * 2.0 ** -32 * n * (w[..., None] * scale_v[:, None]).max(2)
         bound = 2.0 ** -8 * np.abs(ref) + rel * np.einsum("hgn,hnd->hgd", w, np.abs(V)) + np.repeat(floor, 32, -1)
         err = np.abs(got.reshape(H, G, D) - ref)
         assert np.all(err <= bound), f"sequence {i} (len {n}): {np.max(err / bound):.2f} x the bound"
