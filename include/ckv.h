@@ -266,7 +266,8 @@ int ckv_compress_paged(const ckv_page_pool* pools, int32_t L, int32_t H, int32_t
  *    the views [Bz] that the attention and clustering calls take (row of the table, new length);
  *  - sets *status (device) to 0.
  * If the step cannot be done, *status says why (ckv_resize_status), tables and ring are untouched, lens_out, ring_state_out
- * and the views repeat the state before the call, and every slot is -1, so that writes through the map do nothing.
+ * and the views repeat the state before the call (a view's length within 0 and what its row holds), and every slot is -1, so
+ * that writes through the map do nothing.
  * lens_out must not overlap lens or new_lens, nor ring_state_out ring_state; because of that, and because rows and queue only
  * change where nothing is valid, repeating a call with the same lengths and ring_state repeats its results.
  * Every page belongs to one sequence or to the queue.  Bz <= 8192. */
@@ -295,7 +296,8 @@ typedef struct ckv_token_rows {
 
 /* Writes token i to slot slots[i] (device, as ckv_pages_resize lists them) of one layer's pool [n_pages, H, page_tokens, D]
  * in the rows' type, its degree to deg_pages and the degree's logarithm to logdeg_pages (either may be NULL).  Slots below 0
- * or past the pool are skipped.  A slot must not be listed twice (the row would be a mixture of both tokens). */
+ * or past the pool are skipped.  A slot must not be listed twice (the row would be a mixture of both tokens), and the rows must
+ * not lie in the pages. */
 int ckv_pages_write(const ckv_token_rows* rows, const int64_t* slots, int64_t n, void* k_pages, void* v_pages, int32_t* deg_pages,
                     float* logdeg_pages, int64_t n_pages, int32_t page_tokens, void* cuda_stream);
 
@@ -361,7 +363,8 @@ int ckv_pages_dequantize(const int32_t* block_table, int64_t len, const ckv_quan
 /* Host-only: workspace bytes of ckv_decode_attn_quantized (split partials). */
 size_t ckv_decode_quantized_workspace_bytes(int32_t Bz, int32_t H, int32_t G, int32_t D, int64_t max_len);
 
-/* Eq. 3 over four-bit pages: as ckv_decode_attn_paged with the keys and values that the codes stand for.  q, out: bf16. */
+/* Eq. 3 over four-bit pages: as ckv_decode_attn_paged with the keys and values that the codes stand for.  q, out: bf16.
+ * Bz * H * (max_len + 32) < 2^36 (CKV_ERR_UNSUPPORTED above). */
 int ckv_decode_attn_quantized(const ckv_paged_view* views_dev, const ckv_quant_pool* pool, int32_t page_tokens, int32_t Bz, int32_t H, int32_t G,
                               int32_t D, int32_t dtype, const void* q, void* out, float scale, int64_t max_len, void* workspace,
                               size_t workspace_bytes, void* cuda_stream);

@@ -250,7 +250,7 @@ struct QuantArgs {
   ckv_quant_pool pool;
 };
 
-// tiles of a length; a batch's tiles over all heads fit 31 bits (they would be 9 TB of codes)
+// tiles of a length; a batch's tiles over all heads fit 31 bits (the host checks, from max_len)
 __device__ __forceinline__ int tiles_of(int64_t len) { return (int)((max(len, (int64_t)0) + kQT - 1) / kQT); }
 
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
@@ -325,9 +325,10 @@ __device__ __forceinline__ uint32_t v_off(int r, int c) {
 // four groups: of the outputs' columns the first four then hold groups 0 and 1, the others 2 and 3.
 //
 // CL > 0: one cluster per (sequence, KV head), its warps share the tiles evenly and join their partials on the chip.
-// CL = 0: one CTA of sixteen warps per SM (twelve warps without the few spills of 128 registers: 77 us); each warp takes an equal share of all tiles of the batch, in the order of the pairs, so a
-// ragged batch is balanced to a tile and every warp runs from start to end.  A share may end in one pair and go on in the
-// next: each stretch leaves a partial at index warp + pair, which no other stretch has.
+// CL = 0: one CTA of sixteen warps per SM (twelve warps without the few spills of 128 registers: 77 us); each warp takes an
+// equal share of all tiles of the batch, in the order of the pairs, so a ragged batch is balanced to a tile and every warp
+// runs from start to end.  A share may end in one pair and go on in the next: each stretch leaves a partial at index share +
+// pair, which no other stretch has.
 template <int CL, bool HALF>
 __global__ void __launch_bounds__((CL > 0 ? kQClusterWarps : kQShareWarps) * 32, 1) decode_quant_kernel(const QuantArgs qa_) {
   constexpr int TT = kQT, NW = CL > 0 ? kQClusterWarps : kQShareWarps, ST = CL > 0 ? kQClusterStages : kQShareStages;
@@ -839,7 +840,8 @@ int quant_clusters() {
 
 // CTAs of the launch by shares: one per SM, or one per tile where max_len says that there are fewer
 int64_t quant_ctas(int32_t Bz, int32_t H, int64_t max_len) {
-  return std::min<int64_t>(sm_count(), std::max<int64_t>(1, (int64_t)Bz * H * ((max_len + kQT - 1) / kQT)));
+  const int64_t sms = sm_count(), tiles = std::min<int64_t>(max_len / kQT + (max_len % kQT ? 1 : 0), sms);
+  return std::max<int64_t>(1, std::min<int64_t>(sms, std::min<int64_t>((int64_t)Bz * H, sms) * tiles));
 }
 
 inline size_t quant_plan_bytes(int32_t Bz) { return ((size_t)(Bz + 2) * 4 + 255) / 256 * 256; }
@@ -952,7 +954,9 @@ int ckv_decode_attn_quantized(const ckv_paged_view* views_dev, const ckv_quant_p
   int st = check_pool(pool);
   if (st != CKV_OK) return st;
   const int shift = page_shift(page_tokens);
-  if (dtype != CKV_BF16 || shift < 0 || D != kD || G > 8 || H > 65535 || Bz > 65535) return CKV_ERR_UNSUPPORTED;
+  if (dtype != CKV_BF16 || shift < 0 || D != kD || G > 8 || H > 65535 || Bz > 65535 || (int64_t)Bz * H * G > INT32_MAX ||
+      max_len > (((int64_t)1 << 36) - 1) / ((int64_t)Bz * H) - kQT)  // (tiles of all pairs are counted in 31 bits)
+    return CKV_ERR_UNSUPPORTED;
   if (!aligned16(q) || !aligned16(out)) return CKV_ERR_ALIGNMENT;
   const size_t need = ckv_decode_quantized_workspace_bytes(Bz, H, G, D, max_len);
   if (!workspace || workspace_bytes < need || !aligned16(workspace)) return CKV_ERR_WORKSPACE;

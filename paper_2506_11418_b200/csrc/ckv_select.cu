@@ -104,8 +104,9 @@ __global__ void __launch_bounds__(kSumThreads) pages_summarize_kernel(const Summ
 // The result is that of scores computed in 64 bits: a choice between near pages must not hang on the order of a 32-bit sum
 // (it would for about one selection in a thousand).  Few pages are near the border, so only those are scored in 64 bits:
 //  1. All scores in fp32 on the tensor cores, with a bound on how far they may be off: bf16 products are exact in fp32, and
-//     128 additions, cut off rather than rounded, lose at most 2^-23 of sum |q c| each: 2^-15 has a factor of two to spare.  A summary row is read once, straight into the lanes that multiply it,
-//     for all G heads.  The CTAs of a thread-block cluster share the pages; scores land in the first CTA's shared memory.
+//     128 additions, cut off rather than rounded, lose at most 2^-23 of sum |q c| each: 2^-15 has a factor of two to spare.
+//     A summary row is read once, straight into the lanes that multiply it, for all G heads.  The CTAs of a thread-block
+//     cluster share the pages; scores land in the first CTA's shared memory.
 //  2. That CTA finds a narrow interval that holds the k-th largest: a histogram over the scores' range, the bin that holds
 //     it, a histogram over that bin if it is still full.
 //  3. Pages above the interval by more than twice the error are chosen, those below by as much are not; the others (a few)
@@ -611,7 +612,7 @@ int ckv_pages_summarize(const ckv_paged_view* views_dev, const int64_t* from_len
   if (!views_dev || !k_pages || !c_pages || !clog_pages || Bz <= 0 || H <= 0 || max_blocks < 0) return CKV_ERR_INVALID_ARG;
   if (dtype != CKV_F32 && dtype != CKV_BF16) return CKV_ERR_INVALID_ARG;
   const int shift = page_shift(page_tokens);
-  if (dtype != CKV_BF16 || shift < 0 || D != 128 || H > 65535 || Bz > 65535) return CKV_ERR_UNSUPPORTED;
+  if (dtype != CKV_BF16 || shift < 0 || D != 128 || H > 65535 || Bz > 65535 || max_blocks > INT32_MAX) return CKV_ERR_UNSUPPORTED;
   if (!aligned16(k_pages) || !aligned16(c_pages)) return CKV_ERR_ALIGNMENT;
   if (max_blocks == 0) return CKV_OK;
   SummarizeArgs a{};
@@ -621,7 +622,7 @@ int ckv_pages_summarize(const ckv_paged_view* views_dev, const int64_t* from_len
   // one warp per (page, head) once that gives every SM's warp slots something to do
   const bool many = max_blocks * H * Bz >= (int64_t)32 * sm_count();
   const int64_t units = many ? 8 : 2, ctas = (max_blocks * H + units - 1) / units;
-  if (max_blocks > INT32_MAX || ctas > INT32_MAX) return CKV_ERR_UNSUPPORTED;
+  if (ctas > INT32_MAX) return CKV_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)ctas, (unsigned)Bz);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = many ? launch_dependent(pages_summarize_kernel<1>, grid, dim3(kSumThreads), 0, st, a)

@@ -138,14 +138,14 @@ __global__ void __launch_bounds__(kResizeThreads) pages_resize_kernel(const Resi
     status = CKV_RESIZE_NO_PAGES;
 
   const int64_t gid = (int64_t)blockIdx.x * kResizeThreads + tid, gsize = (int64_t)gridDim.x * kResizeThreads;
-  if (status != 0) {  // nothing is assigned: lengths, tables and ring stay as they are, no token has a slot
+  if (status != 0) {  // nothing is assigned: lengths, tables and ring stay as they are, no token has a slot, no view passes its row
     for (int64_t i = gid; i < a.n_slots; i += gsize) a.slots[i] = -1;
     for (int64_t b = gid; b <= n; b += gsize) {
       a.slot_begin[b] = 0;
       if (b < n) {
         const int64_t o = a.lens[b];
         a.lens_out[b] = o;
-        if (a.views) a.views[b] = ckv_paged_view{a.tables + b * a.table_stride, max(o, (int64_t)0)};
+        if (a.views) a.views[b] = ckv_paged_view{a.tables + b * a.table_stride, min(max(o, (int64_t)0), a.table_stride << a.shift)};
       }
     }
     if (gid == 0) {
@@ -155,7 +155,8 @@ __global__ void __launch_bounds__(kResizeThreads) pages_resize_kernel(const Resi
     }
     return;
   }
-  // (the sums fit 32 bits now: grown <= n_slots, taken and given are pages of one pool)
+  // (the sums fit 32 bits now: grown <= n_slots, taken and given are pages of one pool; a sum of tokens that passed 63 bits
+  // would have taken more pages than any pool has)
 #pragma unroll
   for (int k = 0; k < 3; ++k) at[k] += s_warp[k][warp];
   for (int b = b0; b < b1; ++b) {

@@ -14,6 +14,9 @@ Tolerances (half a step of a type, relative: bf16 2^-8, fp16 2^-11, fp32 2^-24)
                    of every weight, in the numerator and the denominator.
 """
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -144,7 +147,7 @@ def test_resize_that_cannot_be_done(status, old, new, row, n_pages, n_slots, sta
     np.testing.assert_array_equal(t["tables"].cpu().numpy(), tables)
     np.testing.assert_array_equal(t["ring"].cpu().numpy(), ring)
     assert t["state_out"].tolist() == state and t["lens_out"].tolist() == old and t["begin"].tolist() == [0, 0, 0]
-    assert t["slots"].tolist() == [-1] * n_slots and t["views"][:, 1].tolist() == [max(n, 0) for n in old]
+    assert t["slots"].tolist() == [-1] * n_slots and t["views"][:, 1].tolist() == held  # (never more than a row holds)
 
 
 # ---------------------------------------------------------------- writes through a slot map
@@ -875,3 +878,130 @@ def test_calls_on_two_streams_do_not_interfere():
     torch.cuda.synchronize()
     for i in range(2):
         assert torch.equal(outs[i][0], outs[2][0]) and torch.equal(outs[i][1], outs[2][1])
+
+
+def test_empty_batches():
+    """Sequences without tokens: nothing is summarised, nothing selected, outputs are zeros; a step in which nothing grows."""
+    b = lib()
+    for Bz in (1, 40):
+        lens, H, G, P = [0] * Bz, 8, 4, 64
+        s = paged_batch(lens, H, P, seed=Bz)
+        pool, views, _, _ = quant_batch(lens, H, P, seed=Bz)
+        cp, cl = torch.full((s["n_pages"], H, D), 9.0, dtype=torch.bfloat16, device=DEV), torch.full((s["n_pages"], H), 9.0, device=DEV)
+        b.pages_summarize(s["views"], s["kp"], None, cp, cl, 3)
+        assert torch.all(cp == 9) and torch.all(cl == 9)
+        q = synth.queries(Bz, H * G, D, seed=1, dtype="bf16", device=DEV)
+        for max_len in (0, 1000):
+            sel, out = torch.full((Bz, H, 4), -9, **I32), torch.full_like(q, 5.0)
+            b.pages_select(s["views"], cp, cl, P, G, q, SCALE, max_len, sel)
+            assert torch.all(sel == -1)
+            b.decode_attn_selected(s["views"], s["kp"], s["vp"], s["lp"], sel, H, G, q, out, SCALE)
+            assert torch.all(out == 0)
+            out.fill_(5.0)
+            ws = torch.empty(b.decode_quantized_workspace_bytes(Bz, H, G, D, max_len), dtype=torch.uint8, device=DEV)
+            b.decode_attn_quantized(views, pool, H, G, q, out, SCALE, max_len, ws)
+            assert torch.all(out == 0)
+    check_resize([70, 5], [3, 5], 64, 4, 9, 2, seed=1, spare=0)          # no slots at all
+
+
+def test_pools_past_32_bits():
+    """Pools whose elements and bytes pass 2^31 and 2^32, with pages at both ends in use."""
+    b = lib()
+    H, G, P, n = 8, 4, 64, 64 * 40 + 9
+    n_pages = 2**32 // (H * P * 64) + 700                                # four-bit codes past 2^32 bytes, keys past 2^33 elements
+    ids = torch.cat([torch.arange(20), torch.arange(n_pages - 21, n_pages)]).to(torch.int32).to(DEV)[torch.randperm(41)]
+    pos = torch.arange(n, device=DEV)
+    slots = ids.long()[pos // P] * P + pos % P
+    K = synth.ar1_keys(1, H, n, D, (0.7, 0.95), 0.5, seed=5, dtype="bf16", device=DEV)[0].transpose(0, 1).contiguous()
+    V = synth.normal_values(1, H, n, D, seed=5, dtype="bf16", device=DEV)[0].transpose(0, 1).contiguous()
+    deg = torch.randint(1, 8, (n, H), **I32)
+    views, scale = b.paged_views([ids], [n], DEV), SCALE
+    q = synth.queries(1, H * G, D, seed=6, dtype="bf16", device=DEV)
+    kp, vp = (torch.empty((n_pages, H, P, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    dp, lp = torch.empty((n_pages, H, P), **I32), torch.empty((n_pages, H, P), device=DEV)
+    b.pages_write(slots, K, V, kp, vp, dp, lp, deg)
+    s = dict(kp=kp, vp=vp, dp=dp, lp=lp, tables=ids[None], views=views, lens=[n], H=H, P=P, n_pages=n_pages)
+    for blk in (0, 17, 40):
+        m = min(P, n - blk * P)
+        assert torch.equal(kp[ids[blk].item(), :, :m], K[blk * P:blk * P + m].transpose(0, 1))
+    cp, cl = torch.empty((n_pages, H, D), dtype=torch.bfloat16, device=DEV), torch.empty((n_pages, H), device=DEV)
+    b.pages_summarize(views, kp, dp, cp, cl, 41)
+    got = PU.to_np64(cp[ids.long()])
+    for j, (c, _, mag) in enumerate(summaries_plain(s, 0, 0, True)):
+        assert np.all(np.abs(got[j] - c) <= 2.0 ** -8 * np.abs(c) + (P + 2) * 2.0 ** -24 * mag)
+    sel, out = torch.full((1, H, 12), -9, **I32), torch.empty_like(q)
+    b.pages_select(views, cp, cl, P, G, q, scale, n, sel, 1, 1)
+    qn, cn, ln = PU.to_np64(q[0]), got, cl[ids.long()].cpu().numpy().astype(np.float64)
+    for h in range(H):
+        assert sel[0, h].tolist() == select_plain(qn[h * G:(h + 1) * G], cn[:, h], ln[:, h], scale, 1, 1, 12)
+    b.decode_attn_selected(views, kp, vp, lp, sel, H, G, q, out, scale)
+    check_selected(s, sel, q, out, G, True, "far pages")
+    del kp, vp, dp, lp, cp, cl, s
+    torch.cuda.empty_cache()
+    pool = b.QuantPool(*(torch.empty((n_pages, H, P, w), dtype=torch.uint8, device=DEV) for w in (64, 64, 4, 4)),
+                       torch.empty((n_pages, H, P), **I32), torch.empty((n_pages, H, P), device=DEV))
+    b.pages_quantize(slots, K, V, pool, deg)
+    ko, vo = (torch.empty((H, n, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    b.pages_dequantize(ids, n, pool, ko, vo)
+    Kq, Vq = quantize_plain(PU.to_np64(K.transpose(0, 1))), quantize_plain(PU.to_np64(V.transpose(0, 1)))
+    np.testing.assert_array_equal(PU.to_np64(ko), Kq)
+    np.testing.assert_array_equal(PU.to_np64(vo), Vq)
+    ws = torch.empty(b.decode_quantized_workspace_bytes(1, H, G, D, n), dtype=torch.uint8, device=DEV)
+    b.decode_attn_quantized(views, pool, H, G, q, out, scale, n, ws)
+    for h in range(H):
+        rows = slice(h * G, (h + 1) * G)
+        PU.check_attention(PU.to_np64(out[0, rows]), qn[rows], Kq[h:h + 1], Vq[h:h + 1], deg.t()[h:h + 1].cpu().numpy().astype(np.int64), scale,
+                           "bf16", f"far four-bit pages, head {h}")
+
+
+def test_first_calls_inside_a_capture():
+    """In a fresh process every call's first run is inside a stream capture; replayed, the graph gives the eager results."""
+    code = """
+import sys
+sys.path[:0] = [{tests!r}, {root!r}]
+import torch
+import test_gpu_serving as T
+from paper_2506_11418_b200 import binding as b
+lens, H, G, P = [700, 64, 1, 300], 2, 4, 64
+g = torch.Generator("cuda").manual_seed(1)
+n_pages = 30
+k, v = (torch.randn((sum(lens), H, 128), generator=g, device="cuda").bfloat16() for _ in range(2))
+old, new = torch.zeros(4, **T.I64), torch.tensor(lens, **T.I64)
+tables, ring = torch.zeros((4, 12), **T.I32), torch.arange(n_pages, **T.I32)
+state, state_out, lens_out = torch.tensor([0, n_pages], **T.I64), torch.zeros(2, **T.I64), torch.zeros(4, **T.I64)
+slots, begin, status, views = torch.zeros(sum(lens), **T.I64), torch.zeros(5, **T.I64), torch.ones(1, **T.I32), torch.zeros((4, 2), **T.I64)
+kp, vp = (torch.zeros((n_pages, H, P, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+dp, lp = torch.zeros((n_pages, H, P), **T.I32), torch.zeros((n_pages, H, P), device="cuda")
+cp, cl = torch.zeros((n_pages, H, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((n_pages, H), device="cuda")
+pool = b.QuantPool.empty(n_pages, H, P)
+q = torch.randn((4, H * G, 128), generator=g, device="cuda").bfloat16()
+sel, o1, o2 = torch.zeros((4, H, 3), **T.I32), torch.zeros_like(q), torch.zeros_like(q)
+ws = torch.zeros(b.decode_quantized_workspace_bytes(4, H, G, 128, 700), dtype=torch.uint8, device="cuda")
+ko, vo = (torch.zeros((H, 700, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+def step():
+    b.pages_resize(old, new, tables, ring, state, slots, begin, lens_out, state_out, status, P, views)
+    b.pages_write(slots, k, v, kp, vp, dp, lp)
+    b.pages_quantize(slots, k, v, pool)
+    b.pages_summarize(views, kp, dp, cp, cl, 11, old)
+    b.pages_select(views, cp, cl, P, G, q, 0.09, 700, sel, 1, 1)
+    b.decode_attn_selected(views, kp, vp, lp, sel, H, G, q, o1, 0.09)
+    b.decode_attn_quantized(views, pool, H, G, q, o2, 0.09, 700, ws)
+    b.pages_dequantize(tables[0], 700, pool, ko, vo)
+outs = (tables, slots, views, kp, vp, cp, cl, sel, o1, o2, ko, vo)
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    step()
+graph.replay()
+torch.cuda.synchronize()
+first = [x.clone() for x in outs]
+assert status.item() == 0 and o1.abs().sum().item() > 0 and o2.abs().sum().item() > 0
+for x in (kp, vp, cp, cl, sel, o1, o2, ko, vo):
+    x.zero_()
+step()
+torch.cuda.synchronize()
+assert all(torch.equal(x, y) for x, y in zip(first, outs))
+print("captured")
+"""
+    here = os.path.dirname(os.path.abspath(__file__))
+    res = subprocess.run([sys.executable, "-c", code.format(tests=here, root=os.path.dirname(here))], capture_output=True, text=True, timeout=200)
+    assert res.returncode == 0 and "captured" in res.stdout, res.stdout + res.stderr

@@ -58,6 +58,8 @@ def test_write_and_quantize_refusals(b):
     w = lambda slots=5 * A, n=3, k=6 * A, v=7 * A, n_pages=4, page=64: b.lib.ckv_pages_write(C.byref(r), slots, n, k, v, None, None, n_pages, page, None)  # noqa: E731
     assert w(slots=None) == 1 and w(n=-1) == 1 and w(k=None) == 1 and w(v=None) == 1 and w(n_pages=0) == 1
     assert w(k=6 * A + 8) == 2 and w(page=96) == 6 and w(n=1 << 31) == 6
+    assert w(n_pages=1 << 22) == 6                                       # 2^22 pages x 8 heads x 64 rows pass 31 bits
+    assert b.lib.ckv_pages_quantize(C.byref(r), 5 * A, 3, C.byref(p), 1 << 22, 64, None) == 6
     assert w(n=0) == 0 and w(n=0, slots=None) == 0                       # nothing to write: nothing is launched
     for name in ("k_codes", "v_codes", "k_scales", "v_scales"):
         for value, status in ((None, 1), (A + 8, 2)):
@@ -88,6 +90,11 @@ def test_summarize_and_select_refusals(b):
     assert s(dt=b.F32) == 6 and s(G=9) == 6 and s(page=100) == 6 and s(n=64 * 24576 + 1) == 6 and s(q=3 * A + 2) == 2
 
 
+def test_bounds_of_launches(b):
+    v = lambda n: b.lib.ckv_pages_summarize(A, None, 2, 2 * A, None, 64, 8, 128, b.BF16, n, 3 * A, 4 * A, None)  # noqa: E731
+    assert v(2**31) == 6 and v(2**63 - 1) == 6 and v(0) == 0 and v(-1) == 1
+
+
 def test_attention_refusals(b):
     s = lambda views=A, k=2 * A, v=3 * A, page=64, sel=4 * A, n=8, Bz=2, H=8, G=4, D=128, dt=b.BF16, q=5 * A, out=6 * A: b.lib.ckv_decode_attn_selected(  # noqa: E731
         views, k, v, None, page, sel, n, Bz, H, G, D, dt, q, out, 0.1, None)
@@ -99,6 +106,10 @@ def test_attention_refusals(b):
     s = lambda views=A, page=64, Bz=2, H=8, G=4, D=128, dt=b.BF16, q=5 * A, out=6 * A, n=1000, ws=7 * A, nb=need: b.lib.ckv_decode_attn_quantized(  # noqa: E731
         views, C.byref(p), page, Bz, H, G, D, dt, q, out, 0.1, n, ws, nb, None)
     assert s(views=None) == 1 and s(q=None) == 1 and s(out=None) == 1 and s(Bz=0) == 1 and s(n=-1) == 1 and s(dt=4) == 1
+    assert s(Bz=60000, H=60000) == 6
+    big = dict(Bz=1024, H=64, n=2**20 - 31)                              # 1024 * 64 * (max_len + 32) = 2^36 + 2^16
+    assert s(**big, nb=1 << 50) == 6 and s(n=2**63 - 1, nb=1 << 50) == 6
+    assert 0 < b.decode_quantized_workspace_bytes(2, 8, 4, 128, 2**63 - 1) == b.decode_quantized_workspace_bytes(2, 8, 4, 128, 1 << 20)
     assert s(dt=b.F32) == 6 and s(G=9) == 6 and s(page=24) == 6 and s(ws=None) == 4 and s(nb=need - 1) == 4 and s(q=5 * A + 8) == 2
 
 
