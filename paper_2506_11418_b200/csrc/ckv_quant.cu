@@ -28,7 +28,7 @@ constexpr int kCodeBytes = 64, kScaleBytes = 4;  // per row
 // Half a warp per row, eight elements per lane; a group is four lanes.  Shared exponent = floor(log2 of the group's largest
 // magnitude) - 2, so that the largest element lies in [4, 8) steps and codes end at 6; elements round to the nearest code,
 // ties to the even one.  A group with an element that is not finite becomes NaN as a whole (scale 255, codes 0).  32749 tokens
-// x 8 heads: 36 us = 0.73 of the measured bandwidth, and 31 us (0.88) back.
+// x 8 heads of bf16: 32 us = 0.83 of the measured bandwidth, and 30 us (0.87) back; of fp32: 47 us (1.0) and 49 us (0.97).
 
 // a lane's eight elements as they lie in memory
 template <bool F32>
@@ -146,7 +146,9 @@ __device__ __forceinline__ float scale_value(uint32_t byte) {  // 2^(byte - 127)
   return byte == 255 ? __uint_as_float(0x7fffffffu) : byte == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
 }
 
-__device__ __forceinline__ void store8(void* p, int64_t vec, int lane16, bool f32, uint32_t codes, float s) {
+// (all lanes of the warp call; those with ok = false store nothing)
+template <bool F32>
+__device__ __forceinline__ void store8(void* p, int64_t vec, int lane16, bool ok, uint32_t codes, float s) {
   uint32_t h[4];
   ptx::unpack_e2m1x8(codes, h);
   float x[8];
@@ -156,11 +158,19 @@ __device__ __forceinline__ void store8(void* p, int64_t vec, int lane16, bool f3
     x[2 * i] = f.x * s;
     x[2 * i + 1] = f.y * s;
   }
-  if (f32) {
-    float4* f = reinterpret_cast<float4*>(p) + vec + 2 * lane16;
-    f[0] = make_float4(x[0], x[1], x[2], x[3]);
-    f[1] = make_float4(x[4], x[5], x[6], x[7]);
-  } else {
+  if constexpr (F32) {
+    // lanes 2 i and 2 i + 1 write the 32 bytes of the one, then of the other: whole sectors per instruction
+    const bool odd = lane16 & 1;
+    float4 mine = odd ? make_float4(x[0], x[1], x[2], x[3]) : make_float4(x[4], x[5], x[6], x[7]), theirs;
+    theirs.x = __shfl_xor_sync(0xffffffffu, mine.x, 1);
+    theirs.y = __shfl_xor_sync(0xffffffffu, mine.y, 1);
+    theirs.z = __shfl_xor_sync(0xffffffffu, mine.z, 1);
+    theirs.w = __shfl_xor_sync(0xffffffffu, mine.w, 1);
+    if (!ok) return;
+    float4* f = reinterpret_cast<float4*>(p) + vec + 2 * (lane16 & ~1);
+    f[lane16 & 1] = odd ? theirs : make_float4(x[0], x[1], x[2], x[3]);
+    f[2 + (lane16 & 1)] = odd ? make_float4(x[4], x[5], x[6], x[7]) : theirs;
+  } else if (ok) {
     reinterpret_cast<uint4*>(p)[vec + lane16] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
   }
 }
@@ -183,7 +193,7 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
   const int64_t i0 = (int64_t)blockIdx.x * (kRows * U), mask = ((int64_t)1 << a.shift) - 1;
   griddep_wait();
   griddep_launch();
-  uint32_t kc[U], vc[U], ks[U], vs[U];
+  uint32_t kc[U] = {}, vc[U] = {}, ks[U] = {}, vs[U] = {};
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t i = i0 + u * kRows + r0;
@@ -198,10 +208,9 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t i = i0 + u * kRows + r0;
-    if (i >= a.len) continue;
     const int64_t vec = ((int64_t)h * a.cap + i) * kVecs;
-    store8(a.k, vec, lane16, F32, kc[u], scale_value((ks[u] >> (8 * j)) & 255u));
-    store8(a.v, vec, lane16, F32, vc[u], scale_value((vs[u] >> (8 * j)) & 255u));
+    store8<F32>(a.k, vec, lane16, i < a.len, kc[u], scale_value((ks[u] >> (8 * j)) & 255u));
+    store8<F32>(a.v, vec, lane16, i < a.len, vc[u], scale_value((vs[u] >> (8 * j)) & 255u));
   }
   if (a.deg || a.logdeg)
     for (int64_t i = i0 + threadIdx.x; i < min(a.len, i0 + kRows * U); i += blockDim.x) {
@@ -910,8 +919,10 @@ int ckv_pages_quantize(const ckv_token_rows* rows, const int64_t* slots, int64_t
     const dim3 grid((unsigned)((n + rows_per_cta - 1) / rows_per_cta), (unsigned)rows->H);
     return launch_dependent(kernel, grid, dim3(kQuantThreads), 0, stream, r, slots, n, *pool, n_rows, (int32_t)shift);
   };
-  const bool many = n * rows->H >= (int64_t)64 * sm_count();  // four rows per half warp once that fills the SMs
-  const cudaError_t e = rows->dtype == CKV_F32 ? (many ? go(pages_quantize_kernel<true, 4>, 64) : go(pages_quantize_kernel<true, 1>, 16))
+  // a half warp takes several rows once that fills the SMs, four of bf16 (32749 tokens x 8 heads: 32 us, with one row 39) or two
+  // of fp32, which are as many bytes in flight (47 and 49; four rows 49); of 1200 tokens one row each is faster, 3.0 and 3.4
+  const bool many = n * rows->H >= (int64_t)128 * sm_count();
+  const cudaError_t e = rows->dtype == CKV_F32 ? (many ? go(pages_quantize_kernel<true, 2>, 32) : go(pages_quantize_kernel<true, 1>, 16))
                                                : (many ? go(pages_quantize_kernel<false, 4>, 64) : go(pages_quantize_kernel<false, 1>, 16));
   return e == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
@@ -928,15 +939,17 @@ int ckv_pages_dequantize(const int32_t* block_table, int64_t len, const ckv_quan
   if (len == 0) return CKV_OK;
   DequantArgs a{};
   a.table = block_table; a.len = len; a.cap = cap; a.pool = *pool; a.k = k; a.v = v; a.deg = deg; a.logdeg = logdeg; a.H = H; a.shift = shift;
-  const bool many = len * H >= (int64_t)64 * sm_count();
-  const int rows = many ? 64 : 16;
+  // writes are what counts, and one row per half warp gives the shortest chains before them; two of bf16 for many rows (32749
+  // tokens x 8 heads: 30.1 us, one row 31.6, four 33; of 3000 tokens: 4.2, 3.6, 4.1); fp32 by one row always (48.6, by two 49.4)
+  const bool many = dtype == CKV_BF16 && len * H >= (int64_t)512 * sm_count();
+  const int rows = many ? 32 : 16;
   const int64_t ctas = (len + rows - 1) / rows;
   if (ctas > INT32_MAX) return CKV_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)ctas, (unsigned)H);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   auto go = [&](auto kernel) { return launch_dependent(kernel, grid, dim3(kQuantThreads), 0, stream, a); };
-  const cudaError_t e = dtype == CKV_F32 ? (many ? go(pages_dequantize_kernel<true, 4>) : go(pages_dequantize_kernel<true, 1>))
-                                         : (many ? go(pages_dequantize_kernel<false, 4>) : go(pages_dequantize_kernel<false, 1>));
+  const cudaError_t e = dtype == CKV_F32 ? go(pages_dequantize_kernel<true, 1>)
+                                         : (many ? go(pages_dequantize_kernel<false, 2>) : go(pages_dequantize_kernel<false, 1>));
   return e == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 

@@ -526,7 +526,7 @@ def odd_rows(k):
 
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("n,H,P,layout", [(1, 1, 32, "step"), (65, 3, 64, "fused"), (2047, 8, 64, "slab"), (300, 2, 256, "step"), (77, 4, 32, "mixed"),
-                                          (3, 1, 64, "fused")])
+                                          (3, 1, 64, "fused"), (9601, 8, 64, "slab")])
 def test_quantize_and_back(dt, n, H, P, layout):
     b = lib()
     k, v = token_rows(n, H, dt, layout, n)
