@@ -235,18 +235,18 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
 //       the tokens that matter keep 11 bits: weights from 2^-21 of the largest on, and below that 2^-32 of the largest.
 //   m   the softmax's reference and F move only when a tile needs it (an exponent above 6, a weight that would pass 2^15):
 //       after a sequence's first tiles that is rare, and the accumulators are left alone.
-//   e   lanes share tokens: each tile's 256 scales are converted once, one token per lane, and read back as fp32, each twice in
-//       a row, ready to multiply two heads
+//   e   lanes share tokens: each tile's 256 scales are converted once, one token per lane, and read back as fp32 (doubled in
+//       registers; kept doubled in shared memory they cost 73 us below, in place of 71)
 //   V   two tokens' codes are interleaved by nibble before they are unpacked, which gives the operand's pairs of
 //       neighbouring tokens without permuting fp16 values.
-// Batch 32, 4097 .. 16384 tokens, 8 KV heads of 4 query heads: 73 us = 0.75 of the measured bandwidth.  About 530 instructions per
+// Batch 32, 4097 .. 16384 tokens, 8 KV heads of 4 query heads: 71 us = 0.77 of the measured bandwidth.  About 530 instructions per
 // tile at 2.2 per cycle and SM, 128 of them cvt on the half-rate ALU pipe: that pipe is 58 % busy, the tensor pipe 25 %.
 constexpr int kQT = 32;  // tokens per tile
 constexpr int kQShareWarps = 16, kQShareStages = 2;      // the launch by shares: one CTA per SM, 128 registers per thread
 constexpr int kQClusterWarps = 8, kQClusterStages = 3;   // the launch by clusters
 constexpr int kQCodes = kQT * kCodeBytes;
 constexpr int kQStageBytes = 2 * kQCodes + 2 * kQT * kScaleBytes + kQT * 4;  // codes of K, V; scales of K, V; log-degrees
-constexpr int kQScaleOut = 2 * kQT * 32;                                     // a tile's scales of K, V as fp32, twice each
+constexpr int kQScaleOut = 2 * kQT * 16;                                     // a tile's scales of K, V as fp32
 constexpr int quant_warp_bytes(int stages) { return stages * kQStageBytes + kQScaleOut; }
 static_assert(quant_warp_bytes(kQClusterStages) >= 8 * kPartial * 4 + kQClusterWarps * 16 * 4, "cluster_combine's rows and weights take a warp's part or less");
 static_assert(quant_warp_bytes(kQShareStages) >= 8 * kPartial * 4, "a warp's partial takes its ring's place");
@@ -308,7 +308,7 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   return d;
 }
 
-// four scale bytes as fp32, each twice: 2^(byte - 127), 255 NaN (bf16 holds them all exactly)
+// four scale bytes as fp32: 2^(byte - 127), 255 NaN (bf16 holds them all exactly)
 __device__ __forceinline__ void scales_f32(uint32_t w, float4* out) {
   uint32_t lo, hi;
   asm("{\n\t.reg .b16 a, b;\n\t"
@@ -319,8 +319,7 @@ __device__ __forceinline__ void scales_f32(uint32_t w, float4* out) {
       : "r"(w));
   const float s0 = __uint_as_float(lo << 16), s1 = __uint_as_float(lo & 0xffff0000u);
   const float s2 = __uint_as_float(hi << 16), s3 = __uint_as_float(hi & 0xffff0000u);
-  out[0] = make_float4(s0, s0, s1, s1);
-  out[1] = make_float4(s2, s2, s3, s3);
+  *out = make_float4(s0, s1, s2, s3);
 }
 
 // Where row r of a tile of V codes sits, and its 16-byte piece c: even rows first, pieces exchanged every other row pair, so
@@ -377,14 +376,17 @@ __global__ void __launch_bounds__((CL > 0 ? kQClusterWarps : kQShareWarps) * 32,
       return sum;
     };
     ckv_paged_view v;
-    int n, sum = 0, total = 0;  // tiles of one head
+    int n, sum = 0, total = 0, longest = 0;  // tiles of one head; of the longest sequence
     for (int i = 0; i < a.Bz; i += 32) {
       sum = scan(i, v, n);
       if (gw == 0 && i + lane < a.Bz) qa_.plan[i + lane] = total + sum - n;
       total += __shfl_sync(0xffffffffu, sum, 31);
+      longest = max(longest, __reduce_max_sync(0xffffffffu, n));
     }
     const uint32_t all = (uint32_t)total * a.H, warps = gridDim.x * NW;
-    share = max((int)((all + warps - 1) / warps), 1);
+    // (not so small that one pair is cut into many more stretches than its combining warps have in flight: one head of 66000
+    // tokens takes 15.6 us, by single tiles 29.5)
+    share = max(max((int)((all + warps - 1) / warps), (longest + 511) / 512), 1);
     if (gw == 0 && lane == 0) {
       qa_.plan[a.Bz] = total;
       qa_.plan[a.Bz + 1] = share;
@@ -412,7 +414,7 @@ __global__ void __launch_bounds__((CL > 0 ? kQClusterWarps : kQShareWarps) * 32,
   }
   unsigned char* const mine = smem_raw + (size_t)warp * kQWarpBytes;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(mine);
-  float4* const sc_out = reinterpret_cast<float4*>(mine + ST * kQStageBytes);  // [K, V][token][groups 0 0 1 1, 2 2 3 3]
+  float4* const sc_out = reinterpret_cast<float4*>(mine + ST * kQStageBytes);  // [K, V][token][group]
   const float* logdeg = qa_.pool.logdeg_pages;
 
   for (;;) {  // one stretch of tiles of one (sequence, KV head)
@@ -523,8 +525,8 @@ __global__ void __launch_bounds__((CL > 0 ? kQClusterWarps : kQShareWarps) * 32,
     // ---- scales: one token per lane
     {
       const uint32_t* w = reinterpret_cast<const uint32_t*>(st + 2 * kQCodes);
-      scales_f32(w[lane], sc_out + 2 * lane);
-      scales_f32(w[TT + lane], sc_out + 2 * (TT + lane));
+      scales_f32(w[lane], sc_out + lane);
+      scales_f32(w[TT + lane], sc_out + TT + lane);
       __syncwarp();
     }
     // ---- exponents of tokens 8 n + g with this lane's heads, relative to the reference
@@ -534,10 +536,9 @@ __global__ void __launch_bounds__((CL > 0 ? kQClusterWarps : kQShareWarps) * 32,
       const uint4 ka = *reinterpret_cast<const uint4*>(st + (16 * s + g) * kCodeBytes + 16 * t);
       const uint4 kb = *reinterpret_cast<const uint4*>(st + (16 * s + 8 + g) * kCodeBytes + 16 * t);
       const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
-      const float4 a01 = sc_out[2 * (16 * s + g)], a23 = sc_out[2 * (16 * s + g) + 1];
-      const float4 b01 = sc_out[2 * (16 * s + 8 + g)], b23 = sc_out[2 * (16 * s + 8 + g) + 1];
-      const f32x2 sa[4] = {f32x2(a01.x, a01.y), f32x2(a01.z, a01.w), f32x2(a23.x, a23.y), f32x2(a23.z, a23.w)};
-      const f32x2 sb[4] = {f32x2(b01.x, b01.y), f32x2(b01.z, b01.w), f32x2(b23.x, b23.y), f32x2(b23.z, b23.w)};
+      const float4 fa = sc_out[16 * s + g], fb = sc_out[16 * s + 8 + g];
+      const f32x2 sa[4] = {f32x2(fa.x, fa.x), f32x2(fa.y, fa.y), f32x2(fa.z, fa.z), f32x2(fa.w, fa.w)};
+      const f32x2 sb[4] = {f32x2(fb.x, fb.x), f32x2(fb.y, fb.y), f32x2(fb.z, fb.z), f32x2(fb.w, fb.w)};
       f32x2 xa, xb;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -603,7 +604,7 @@ __global__ void __launch_bounds__((CL > 0 ? kQClusterWarps : kQShareWarps) * 32,
     // ---- weights p 2^e of two groups times F in fp16, then their O^T += V^T P
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
-      const float4* const v_scales = sc_out + 2 * (TT + g) + (HALF ? t >> 1 : u);
+      const float2* const v_scales = reinterpret_cast<const float2*>(sc_out + TT + g) + (HALF ? t >> 1 : u);
       uint32_t pk[2][4];  // [group][n]: token 8 n + g, this lane's heads
       bool over = move;
 #pragma unroll 1
@@ -618,7 +619,7 @@ __global__ void __launch_bounds__((CL > 0 ? kQClusterWarps : kQShareWarps) * 32,
             float now[2] = {0.f, 0.f};
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
-              const float v = reinterpret_cast<const float*>(v_scales + 16 * n)[2 * j];
+              const float v = reinterpret_cast<const float*>(v_scales + 16 * n)[j];
               float p0, p1;
               p[n].get(p0, p1);
               now[0] = fmaxf(now[0], p0 * v);
@@ -651,8 +652,8 @@ __global__ void __launch_bounds__((CL > 0 ? kQClusterWarps : kQShareWarps) * 32,
         uint32_t high[2] = {wtop[2 * u], wtop[2 * u + 1]};
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-          const float4 s01 = v_scales[16 * n];
-          const f32x2 vs[2] = {f32x2(s01.x, s01.y), f32x2(s01.z, s01.w)};
+          const float2 s01 = v_scales[16 * n];
+          const f32x2 vs[2] = {f32x2(s01.x, s01.x), f32x2(s01.y, s01.y)};
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             float w0, w1;
@@ -762,9 +763,9 @@ __global__ void __launch_bounds__((CL > 0 ? kQClusterWarps : kQShareWarps) * 32,
 }
 
 // One CTA per (sequence, query head) joins the partials of the stretches that cover its pair: its W warps take every W-th, a
-// lane owns four columns, and the loads of four partials are in flight at once.  Eight warps for few rows (their pairs are
-// spread over many stretches), four for a batch.
-constexpr int kQCombThreads = 256;
+// lane owns four columns, and the loads of four partials are in flight at once.  The host gives each warp four or so: few pairs
+// are spread over many stretches (8 pairs of 131072 tokens over 296 each: 38 us with 32 warps, 50 with eight).
+constexpr int kQCombThreads = 1024;
 
 __global__ void __launch_bounds__(kQCombThreads) quant_combine_kernel(const QuantArgs qa_) {
   const int W = blockDim.x / 32;
@@ -807,7 +808,17 @@ __global__ void __launch_bounds__(kQCombThreads) quant_combine_kernel(const Quan
   if (lane == 0) s_ml[warp] = make_float2(m, l);
   __syncthreads();
   if (warp == 0) {
-    for (int w = 1; w < W; ++w) add(s_ml[w], s_out[w][lane]);
+    const float2 ml = lane < W ? s_ml[lane] : make_float2(-INFINITY, 0.f);
+    m = warp_max(ml.x);
+    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
+    l = warp_sum(f * ml.y);
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int w = 0; w < W; ++w) {
+      const float fw = __shfl_sync(0xffffffffu, f, w);
+      const float4 y = s_out[w][lane];
+      o.x = fmaf(fw, y.x, o.x); o.y = fmaf(fw, y.y, o.y); o.z = fmaf(fw, y.z, o.z); o.w = fmaf(fw, y.w, o.w);
+    }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     store4(reinterpret_cast<__nv_bfloat16*>(a.out) + (int64_t)row * kD + lane * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
   }
@@ -875,17 +886,18 @@ cudaError_t launch_quant(const QuantArgs& a, cudaStream_t st) {
   cfg.numAttrs = CL > 0 ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, decode_quant_kernel<CL, HALF>, a);
   if (e != cudaSuccess || CL > 0) return e;
-  const int64_t rows = (int64_t)a.d.Bz * a.d.H * a.d.G;
-  return launch_dependent(quant_combine_kernel, dim3((unsigned)rows), dim3(rows < 512 ? kQCombThreads : kQCombThreads / 2), 0, st, a);
+  const int64_t pairs = (int64_t)a.d.Bz * a.d.H, each = quant_ctas(a.d.Bz, a.d.H, a.d.max_len) * kQShareWarps / pairs;  // stretches per pair
+  const int warps = each > 64 ? 32 : each > 32 ? 16 : each > 16 ? 8 : 4;
+  return launch_dependent(quant_combine_kernel, dim3((unsigned)(pairs * a.d.G)), dim3(warps * 32), 0, st, a);
 }
 
 template <bool HALF>
 cudaError_t launch_quant_heads(const QuantArgs& a, cudaStream_t st) {
   // Few pairs: one cluster each, the largest of which all are resident at once, unless the sequences are so long that the
-  // SMs a cluster cannot use (all but 80 of 148 for 8 pairs) count for more than the second kernel (about 5 us).  8 pairs
-  // of 16416 tokens: 15.1 us by clusters, 16.9 by shares; of 131072 tokens: 67 and 47.
+  // SMs a cluster cannot use (all but 80 of 148 for 8 pairs) count for more than the second kernel (about 3 us).  8 pairs
+  // of 8000 tokens: 10.7 us by clusters, 11.6 by shares; of 16416: 14.5 both; of 33000: 22.0 and 18.0.
   const int64_t pairs = (int64_t)a.d.Bz * a.d.H, tiles = (a.d.max_len + kQT - 1) / kQT;
-  auto fits = [&](int clusters, int cl) { return clusters >= pairs && tiles <= (int64_t)128 * cl; };
+  auto fits = [&](int clusters, int cl) { return clusters >= pairs && tiles <= (int64_t)64 * cl; };
   if (fits(quant_clusters<16, HALF>(), 16)) return launch_quant<16, HALF>(a, st);
   if (fits(quant_clusters<10, HALF>(), 10)) return launch_quant<10, HALF>(a, st);
   if (fits(quant_clusters<8, HALF>(), 8)) return launch_quant<8, HALF>(a, st);
