@@ -113,8 +113,9 @@ __global__ void __launch_bounds__(kSumThreads) pages_summarize_kernel(const Summ
 //     are scored in 64 bits and ranked.  If they are many (equal pages, or scores that are not finite), all pages are scored
 //     in 64 bits and the k-th is found digit by digit.
 //  4. The chosen blocks are written in ascending order.
-// Bound by the latency of these steps: 13 us for 256 (sequence, head) pairs of up to 1024 pages (23 MB of summaries: 3.6 us),
-// 10 us for 8 pairs of 2048 pages; with all scores in 64 bits the former took 47 us.
+// Bound by the latency of these steps: 12.4 us for 256 (sequence, head) pairs of up to 1024 pages (23 MB of summaries: 3.6 us),
+// 9.0 us for 8 pairs of 2048 pages (scores 2.9, interval 1.6, border 2.5, order 1.3); with all scores in 64 bits the former
+// took 47 us.
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelBins = 1024;
@@ -423,6 +424,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
       if (!(width > 1e-30f) || !(inv > 0.f)) break;
       for (int i = tid; i < kSelBins + 2; i += kSelThreads) sh.hist[i] = 0;
       __syncthreads();
+#pragma unroll 4
       for (int i = f0 + tid; i < f1; i += kSelThreads) {
         const float s = score[i];
         const int bin = s < lo ? 0 : s > hi ? kSelBins + 1 : 1 + min(kSelBins - 1, (int)((s - lo) * inv));
@@ -468,11 +470,11 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
   // ---- 3. the blocks in between
   int above = 0;
   if (need > 0 && fine) {
+#pragma unroll 4
     for (int i = f0 + tid; i < f1; i += kSelThreads) {
       const float s = score[i];
-      if (s > top) {
-        ++above;
-      } else if (s >= bottom) {
+      above += s > top;
+      if (s <= top && s >= bottom) {
         const int at = atomicAdd(&sh.n_near, 1);
         if (at < kSelNear) sh.near_id[at] = i;
       }
@@ -518,6 +520,24 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
 
   // ---- 4. in ascending order: a bit per block, a place per word of 32 blocks, then a lane per block
   const int words = (n + 31) / 32;
+  if (few && words <= 32 * kSelWarps) {  // up to 8192 blocks: each warp has a run of words, one per lane, and nothing goes through memory
+    const int run = (words + kSelWarps - 1) / kSelWarps, first = min(words, warp * run), last = min(words, first + run);
+    uint32_t bits = 0;
+#pragma unroll 4
+    for (int w = first; w < last; ++w) {
+      const int i = 32 * w + lane;
+      const uint32_t m = __ballot_sync(0xffffffffu, i < n && (i < f0 || i >= f1 || (need > 0 && score[i] > top)));
+      if (lane == w - first) bits = m;
+    }
+    int at = sum_before(__popc(bits), sh.gt);
+#pragma unroll 4
+    for (int w = first; w < last; ++w) {
+      const uint32_t m = __shfl_sync(0xffffffffu, bits, w - first);
+      const int to = __shfl_sync(0xffffffffu, at, w - first) + __popc(m & ((1u << lane) - 1u));
+      if ((m >> lane & 1u) && to < a.n_select) out[to] = 32 * w + lane;
+    }
+    return;
+  }
 #pragma unroll 4
   for (int w = warp; w < words; w += kSelWarps) {
     const int i = 32 * w + lane;
