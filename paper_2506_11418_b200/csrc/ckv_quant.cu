@@ -239,8 +239,8 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
 //       registers; kept doubled in shared memory they cost 73 us below, in place of 71)
 //   V   two tokens' codes are interleaved by nibble before they are unpacked, which gives the operand's pairs of
 //       neighbouring tokens without permuting fp16 values.
-// Batch 32, 4097 .. 16384 tokens, 8 KV heads of 4 query heads: 71 us = 0.77 of the measured bandwidth.  About 530 instructions per
-// tile at 2.2 per cycle and SM, 128 of them cvt on the half-rate ALU pipe: that pipe is 58 % busy, the tensor pipe 25 %.
+// Batch 32, 4097 .. 16384 tokens, 8 KV heads of 4 query heads: 71 us = 0.77 of the measured bandwidth.  About 580 instructions per
+// tile at 2.4 per cycle and SM, 128 of them cvt on the half-rate ALU pipe: that pipe is 57 % busy, the tensor pipe 25 %.
 constexpr int kQT = 32;  // tokens per tile
 constexpr int kQShareWarps = 16, kQShareStages = 2;      // the launch by shares: one CTA per SM, 128 registers per thread
 constexpr int kQClusterWarps = 8, kQClusterStages = 3;   // the launch by clusters

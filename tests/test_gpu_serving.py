@@ -329,6 +329,7 @@ def test_select_group_sizes(G):
     ([3000 + 997 * i % 9000 for i in range(20)], 7, 64, 16, 2, 3),   # clusters of two
     ([100 + 1297 * i % 9000 for i in range(50)], 8, 128, 9, 0, 0),   # one CTA per pair
     ([4096], 1, 64, 1, 0, 0), ([4096], 1, 64, 63, 31, 32), ([4096], 3, 64, 64, 0, 0), ([4097], 3, 64, 64, 3, 0), ([65 * 256], 1, 256, 2, 1, 1),
+    ([8192 * 32 - 31, 8193 * 32 - 31, 8191 * 32, 40], 1, 32, 200, 1, 1),   # on both sides of 8192 blocks
     ([24576 * 32], 1, 32, 1000, 1, 1)])                       # the largest number of blocks
 def test_select_shapes(lens, H, P, k, first, last):
     select_case(lens, H, 4, P, k, first, last, seed=k)
