@@ -652,7 +652,9 @@ def test_quantized_attention_group_sizes(G):
 
 @pytest.mark.parametrize("lens,H,G,P,with_logdeg", [
     ([20000], 8, 4, 64, True), ([9000, 8200, 2, 0], 2, 8, 32, True), ([777] * 20, 8, 4, 128, True), ([5000 - 97 * i for i in range(40)], 8, 2, 256, False),
-    ([16416], 1, 1, 64, True), ([1], 1, 1, 32, False), ([300 + 13 * i for i in range(90)], 1, 4, 64, True), ([40000, 5, 12345], 8, 4, 64, True)])
+    ([16416], 1, 1, 64, True), ([1], 1, 1, 32, False), ([300 + 13 * i for i in range(90)], 1, 4, 64, True), ([40000, 5, 12345], 8, 4, 64, True),
+    ([50001], 1, 4, 64, True), ([33, 66001], 1, 8, 32, True), ([70000], 4, 3, 64, False),   # shares of more than one tile, many partials per row
+    ([2000 + 31 * i for i in range(8)], 8, 4, 64, True), ([600 + 37 * i for i in range(16)], 8, 4, 64, True)])   # 16 and 8 combining warps
 def test_quantized_attention_shapes(lens, H, G, P, with_logdeg):
     """Batches on both sides of the launch choice (one cluster per pair, or splits joined by a second kernel)."""
     quant_attention(lens, H, G, P, seed=len(lens), with_logdeg=with_logdeg)
