@@ -466,7 +466,7 @@ def _token_rows(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, deg: torc
     int32 [n, H] with any strides."""
     (n, H, D), (kt, kh, k1), (vt, vh, v1), dt = k.shape, k.stride(), v.stride(), k.dtype
     assert k1 == v1 == 1 and v.dtype is dt and v.shape == (n, H, D) and H == heads, "rows"
-    assert slots.nbytes == 8 * n and slots.is_contiguous(), "slots"
+    assert slots.dtype is _i64 and slots.nbytes == 8 * n and slots.is_contiguous(), "slots"
     ts, hs, dp = 0, 0, 0
     if deg is not None:
         assert deg.dtype is _i32 and deg.shape == (n, H), "degrees"

@@ -1,0 +1,105 @@
+"""What the bindings of the serving calls look at before a pointer reaches the library, on the host: tensors that claim to be on
+the current CUDA device, and a library that only notes which call was made."""
+import types
+
+import pytest
+import torch
+
+BF16, F32, F64, I32, I64, U8 = torch.bfloat16, torch.float32, torch.float64, torch.int32, torch.int64, torch.uint8
+
+
+class OnDevice(torch.Tensor):
+    """A host tensor that says it is on CUDA device `where`."""
+    where = 0
+
+    def get_device(self):
+        return self.where
+
+
+def made(*shape, dt=BF16, where=0):
+    t = torch.zeros(shape, dtype=dt).as_subclass(OnDevice)
+    t.where = where
+    return t
+
+
+@pytest.fixture
+def b(monkeypatch):
+    from paper_2506_11418_b200 import binding
+    binding_calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: binding_calls.append(name) or 0
+    monkeypatch.setattr(binding, "lib", Library())
+    monkeypatch.setattr(binding, "_raw_device", lambda: 0)
+    monkeypatch.setattr(binding, "_raw_stream", lambda dev: 0)
+    return types.SimpleNamespace(calls=binding_calls, **{k: getattr(binding, k) for k in dir(binding) if not k.startswith("__") and k != "calls"})
+
+
+def pool_tensors():
+    n, H, P = 4, 2, 64
+    return dict(k_codes=made(n, H, P, 64, dt=U8), v_codes=made(n, H, P, 64, dt=U8), k_scales=made(n, H, P, 4, dt=U8), v_scales=made(n, H, P, 4, dt=U8),
+                deg_pages=made(n, H, P, dt=I32), logdeg_pages=made(n, H, P, dt=F32))
+
+
+POOL = ("k_codes", "v_codes", "k_scales", "v_scales", "deg_pages", "logdeg_pages")
+
+
+def arguments(name):
+    """A call's arguments, all of them given: 3 tokens or 2 sequences, 2 KV heads, groups of 4, 4 pages of 64 tokens."""
+    kv = lambda n: made(n, 2, 128)  # noqa: E731
+    pages = lambda: made(4, 2, 64, 128)  # noqa: E731
+    views, q = made(2, 2, dt=I64), made(2, 8, 128)
+    if name == "pages_resize":
+        return dict(lens=made(2, dt=I64), new_lens=made(2, dt=I64), block_tables=made(2, 5, dt=I32), ring=made(9, dt=I32), ring_state=made(2, dt=I64),
+                    slots=made(3, dt=I64), slot_begin=made(3, dt=I64), lens_out=made(2, dt=I64), ring_state_out=made(2, dt=I64), status=made(1, dt=I32),
+                    page_tokens=64, views=views)
+    if name == "pages_write":
+        return dict(slots=made(3, dt=I64), k=kv(3), v=kv(3), k_pages=pages(), v_pages=pages(), deg_pages=made(4, 2, 64, dt=I32),
+                    logdeg_pages=made(4, 2, 64, dt=F32), deg=made(3, 2, dt=I32))
+    if name == "pages_summarize":
+        return dict(views=views, k_pages=pages(), deg_pages=made(4, 2, 64, dt=I32), c_pages=made(4, 2, 128), clog_pages=made(4, 2, dt=F32), max_blocks=2,
+                    from_lens=made(2, dt=I64))
+    if name == "pages_select":
+        return dict(views=views, c_pages=made(4, 2, 128), clog_pages=made(4, 2, dt=F32), page_tokens=64, G=4, q=q, scale=0.1, max_len=100,
+                    selected=made(2, 2, 3, dt=I32))
+    if name == "decode_attn_selected":
+        return dict(views=views, k_pages=pages(), v_pages=pages(), logdeg_pages=made(4, 2, 64, dt=F32), selected=made(2, 2, 3, dt=I32), H=2, G=4, q=q,
+                    out=made(2, 8, 128), scale=0.1)
+    if name == "pages_quantize":
+        return dict(slots=made(3, dt=I64), k=kv(3), v=kv(3), deg=made(3, 2, dt=I32), **pool_tensors())
+    if name == "pages_dequantize":
+        return dict(block_table=made(1, dt=I32), length=60, k=made(2, 60, 128), v=made(2, 60, 128), deg=made(2, 60, dt=I32), logdeg=made(2, 60, dt=F32),
+                    **pool_tensors())
+    return dict(views=views, H=2, G=4, q=q, out=made(2, 8, 128), scale=0.1, max_len=100, workspace=made(1 << 16, dt=U8), **pool_tensors())
+
+
+CALLS = ("pages_resize", "pages_write", "pages_summarize", "pages_select", "decode_attn_selected", "pages_quantize", "pages_dequantize",
+         "decode_attn_quantized")
+
+
+def call(b, name, **change):
+    a = {**arguments(name), **change}
+    if "k_codes" in a:
+        a["pool"] = b.QuantPool(*(a.pop(x) for x in POOL))
+    getattr(b, name)(**a)
+
+
+def refused(b, name, error=AssertionError, **change):
+    with pytest.raises(error):
+        call(b, name, **change)
+    assert b.calls == []
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_whole_arguments_reach_the_library(b, name):
+    call(b, name)
+    assert b.calls == ["ckv_" + name]
+
+
+@pytest.mark.parametrize("name", ["pages_write", "pages_quantize"])
+def test_slots_are_64_bit_integers(b, name):
+    """Another type of the same size in bytes is not a slot list: the library would read past its end, or read its bits as slots."""
+    refused(b, name, slots=made(6, dt=I32))
+    refused(b, name, slots=made(3, dt=F64))
+    refused(b, name, slots=made(24, dt=U8))
