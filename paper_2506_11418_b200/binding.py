@@ -433,11 +433,15 @@ _ROWS = struct.Struct("@PPPqqqqqqiii4x")   # ckv_token_rows
 _POOL = struct.Struct("@PPPPPP")           # ckv_quant_pool
 
 
-def _stream_for(t: torch.Tensor):
-    """The current stream, for tensors on the current device (the library launches there; another device's are refused)."""
-    dev = t.get_device()
+def _stream_for(first: torch.Tensor, *others: torch.Tensor | None):
+    """The current stream, for a call whose tensors are all on the current device (the library launches there and takes every
+    pointer for one of that device's: the host's and other devices' are refused)."""
+    dev = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors are on {first.device} and on {t.device}")
     if dev < 0 or dev != _raw_device():
-        raise ValueError(f"tensors are on {t.device}, which is not the current CUDA device")
+        raise ValueError(f"tensors are on {first.device}, which is not the current CUDA device")
     return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
@@ -458,7 +462,8 @@ def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_tables: torch
     assert views is None or views.nbytes == 16 * Bz and views.is_contiguous(), "views"
     _check(lib.ckv_pages_resize(lens.data_ptr(), new_lens.data_ptr(), Bz, page_tokens, block_tables.data_ptr(), row, ring.data_ptr(),
                                 n_pages, ring_state.data_ptr(), slots.data_ptr(), n_slots, slot_begin.data_ptr(),
-                                lens_out.data_ptr(), ring_state_out.data_ptr(), status.data_ptr(), _ptr(views), _stream_for(lens)))
+                                lens_out.data_ptr(), ring_state_out.data_ptr(), status.data_ptr(), _ptr(views),
+                                _stream_for(lens, new_lens, block_tables, ring, ring_state, slots, slot_begin, lens_out, ring_state_out, status, views)))
 
 
 def _token_rows(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, deg: torch.Tensor | None, heads: int) -> bytes:
@@ -484,7 +489,7 @@ def pages_write(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: 
     assert deg_pages is None or deg_pages.nbytes == per_row and deg_pages.is_contiguous(), "degree pages"
     assert logdeg_pages is None or logdeg_pages.nbytes == per_row and logdeg_pages.is_contiguous(), "log-degree pages"
     _check(lib.ckv_pages_write(rows, slots.data_ptr(), slots.numel(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(deg_pages),
-                               _ptr(logdeg_pages), n_pages, P, _stream_for(slots)))
+                               _ptr(logdeg_pages), n_pages, P, _stream_for(slots, k, v, k_pages, v_pages, deg_pages, logdeg_pages, deg)))
 
 
 def pages_summarize(views: torch.Tensor, k_pages: torch.Tensor, deg_pages: torch.Tensor | None, c_pages: torch.Tensor, clog_pages: torch.Tensor,
@@ -498,7 +503,8 @@ def pages_summarize(views: torch.Tensor, k_pages: torch.Tensor, deg_pages: torch
     assert c_pages.dtype is dt and c_pages.numel() == heads * D and c_pages.is_contiguous(), "summaries"
     assert clog_pages.nbytes == 4 * heads and clog_pages.is_contiguous(), "summaries"
     _check(lib.ckv_pages_summarize(views.data_ptr(), _ptr(from_lens), Bz, k_pages.data_ptr(), _ptr(deg_pages), P, H, D, _DTYPE_CODES[dt],
-                                   max_blocks, c_pages.data_ptr(), clog_pages.data_ptr(), _stream_for(views)))
+                                   max_blocks, c_pages.data_ptr(), clog_pages.data_ptr(),
+                                   _stream_for(views, k_pages, deg_pages, c_pages, clog_pages, from_lens)))
 
 
 def pages_select(views: torch.Tensor, c_pages: torch.Tensor, clog_pages: torch.Tensor | None, page_tokens: int, G: int, q: torch.Tensor,
@@ -512,7 +518,8 @@ def pages_select(views: torch.Tensor, c_pages: torch.Tensor, clog_pages: torch.T
     assert clog_pages is None or clog_pages.nbytes == 4 * n_pages * H and clog_pages.is_contiguous(), "summaries"
     assert selected.dtype is _i32 and selected.is_contiguous(), "selected"
     _check(lib.ckv_pages_select(views.data_ptr(), c_pages.data_ptr(), _ptr(clog_pages), page_tokens, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(),
-                                scale, max_len, n_first, n_last, n_select, selected.data_ptr(), _stream_for(views)))
+                                scale, max_len, n_first, n_last, n_select, selected.data_ptr(),
+                                _stream_for(views, c_pages, clog_pages, q, selected)))
 
 
 def decode_attn_selected(views: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, logdeg_pages: torch.Tensor | None,
@@ -527,7 +534,8 @@ def decode_attn_selected(views: torch.Tensor, k_pages: torch.Tensor, v_pages: to
     assert logdeg_pages is None or logdeg_pages.nbytes == 4 * n_pages * H * P and logdeg_pages.is_contiguous(), "log-degree pages"
     assert selected.dtype is _i32 and selected.numel() == Bz * H * n_select and selected.is_contiguous(), "selected"
     _check(lib.ckv_decode_attn_selected(views.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(logdeg_pages), P, selected.data_ptr(),
-                                        n_select, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(), out.data_ptr(), scale, _stream_for(views)))
+                                        n_select, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(), out.data_ptr(), scale,
+                                        _stream_for(views, k_pages, v_pages, logdeg_pages, selected, q, out)))
 
 
 @dataclass
@@ -561,11 +569,15 @@ class QuantPool:
         return _POOL.pack(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), 0 if deg is None else deg.data_ptr(),
                           0 if logdeg is None else logdeg.data_ptr()), n, H, P
 
+    def tensors(self):
+        return self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.deg_pages, self.logdeg_pages
+
 
 def pages_quantize(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pool: QuantPool, deg: torch.Tensor | None = None):
     """ckv_pages_quantize on the current stream: k, v [n, H, D] (bf16 or fp32) to the slots of a four-bit pool."""
     cp, n_pages, H, P = pool.c()
-    _check(lib.ckv_pages_quantize(_token_rows(slots, k, v, deg, H), slots.data_ptr(), slots.numel(), cp, n_pages, P, _stream_for(slots)))
+    _check(lib.ckv_pages_quantize(_token_rows(slots, k, v, deg, H), slots.data_ptr(), slots.numel(), cp, n_pages, P,
+                                  _stream_for(slots, k, v, deg, *pool.tensors())))
 
 
 def pages_dequantize(block_table: torch.Tensor, length: int, pool: QuantPool, k: torch.Tensor, v: torch.Tensor,
@@ -578,7 +590,7 @@ def pages_dequantize(block_table: torch.Tensor, length: int, pool: QuantPool, k:
     assert deg is None or deg.nbytes == 4 * H * cap and deg.is_contiguous(), "degrees"
     assert logdeg is None or logdeg.nbytes == 4 * H * cap and logdeg.is_contiguous(), "log-degrees"
     _check(lib.ckv_pages_dequantize(block_table.data_ptr(), length, cp, P, H, D, _DTYPE_CODES[dt], k.data_ptr(), v.data_ptr(),
-                                    _ptr(deg), _ptr(logdeg), cap, _stream_for(block_table)))
+                                    _ptr(deg), _ptr(logdeg), cap, _stream_for(block_table, k, v, deg, logdeg, *pool.tensors())))
 
 
 def decode_quantized_workspace_bytes(Bz, H, G, D, max_len) -> int:
@@ -594,4 +606,4 @@ def decode_attn_quantized(views: torch.Tensor, pool: QuantPool, H: int, G: int, 
     assert HG == H * G and heads == H and q.is_contiguous() and views.nbytes == 16 * Bz and views.is_contiguous(), "queries"
     assert out.dtype is dt and out.numel() == Bz * HG * D and out.is_contiguous(), "out"
     _check(lib.ckv_decode_attn_quantized(views.data_ptr(), cp, P, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(), out.data_ptr(), scale, max_len,
-                                         workspace.data_ptr(), workspace.nbytes, _stream_for(views)))
+                                         workspace.data_ptr(), workspace.nbytes, _stream_for(views, q, out, workspace, *pool.tensors())))

@@ -103,3 +103,16 @@ def test_slots_are_64_bit_integers(b, name):
     refused(b, name, slots=made(6, dt=I32))
     refused(b, name, slots=made(3, dt=F64))
     refused(b, name, slots=made(24, dt=U8))
+
+
+def tensor_arguments():
+    return [(name, x) for name in CALLS for x, v in arguments(name).items() if isinstance(v, torch.Tensor)]
+
+
+@pytest.mark.parametrize("where", [-1, 1])
+@pytest.mark.parametrize("name,x", tensor_arguments())
+def test_every_tensor_is_on_the_current_device(b, name, x, where):
+    """One tensor on the host or on another device among those of the current one: its pointer would be read or written by the kernel."""
+    t = arguments(name)[x]
+    t.where = where
+    refused(b, name, ValueError, **{x: t})
