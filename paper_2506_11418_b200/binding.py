@@ -428,7 +428,7 @@ def pages_scatter(block_table, length, k, v, deg, k_pages, v_pages, deg_pages, l
 # a wrong read or write could come from, and its type where the library is told one.)
 
 _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-_i32, _i64 = torch.int32, torch.int64
+_i32, _i64, _f32 = torch.int32, torch.int64, torch.float32
 _ROWS = struct.Struct("@PPPqqqqqqiii4x")   # ckv_token_rows
 _POOL = struct.Struct("@PPPPPP")           # ckv_quant_pool
 
@@ -486,8 +486,8 @@ def pages_write(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: 
     rows, per_row = _token_rows(slots, k, v, deg, H), 4 * n_pages * H * P
     assert k_pages.dtype is v_pages.dtype is k.dtype and k_pages.nbytes == v_pages.nbytes and k.shape[2] == D, "pages"
     assert k_pages.is_contiguous() and v_pages.is_contiguous(), "pages"
-    assert deg_pages is None or deg_pages.nbytes == per_row and deg_pages.is_contiguous(), "degree pages"
-    assert logdeg_pages is None or logdeg_pages.nbytes == per_row and logdeg_pages.is_contiguous(), "log-degree pages"
+    assert deg_pages is None or deg_pages.dtype is _i32 and deg_pages.nbytes == per_row and deg_pages.is_contiguous(), "degree pages"
+    assert logdeg_pages is None or logdeg_pages.dtype is _f32 and logdeg_pages.nbytes == per_row and logdeg_pages.is_contiguous(), "log-degree pages"
     _check(lib.ckv_pages_write(rows, slots.data_ptr(), slots.numel(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(deg_pages),
                                _ptr(logdeg_pages), n_pages, P, _stream_for(slots, k, v, k_pages, v_pages, deg_pages, logdeg_pages, deg)))
 
@@ -499,9 +499,10 @@ def pages_summarize(views: torch.Tensor, k_pages: torch.Tensor, deg_pages: torch
     n_pages, H, P, D = k_pages.shape
     Bz, dt, heads = views.numel() // 2, k_pages.dtype, n_pages * H
     assert views.dtype is _i64 and views.is_contiguous() and (from_lens is None or from_lens.nbytes == 8 * Bz and from_lens.is_contiguous()), "views"
-    assert k_pages.is_contiguous() and (deg_pages is None or deg_pages.nbytes == 4 * heads * P and deg_pages.is_contiguous()), "pages"
+    assert k_pages.is_contiguous(), "pages"
+    assert deg_pages is None or deg_pages.dtype is _i32 and deg_pages.nbytes == 4 * heads * P and deg_pages.is_contiguous(), "degree pages"
     assert c_pages.dtype is dt and c_pages.numel() == heads * D and c_pages.is_contiguous(), "summaries"
-    assert clog_pages.nbytes == 4 * heads and clog_pages.is_contiguous(), "summaries"
+    assert clog_pages.dtype is _f32 and clog_pages.nbytes == 4 * heads and clog_pages.is_contiguous(), "summaries"
     _check(lib.ckv_pages_summarize(views.data_ptr(), _ptr(from_lens), Bz, k_pages.data_ptr(), _ptr(deg_pages), P, H, D, _DTYPE_CODES[dt],
                                    max_blocks, c_pages.data_ptr(), clog_pages.data_ptr(),
                                    _stream_for(views, k_pages, deg_pages, c_pages, clog_pages, from_lens)))
@@ -515,7 +516,7 @@ def pages_select(views: torch.Tensor, c_pages: torch.Tensor, clog_pages: torch.T
     dt = q.dtype
     assert heads == H and q.shape == (Bz, H * G, D) and q.is_contiguous() and views.nbytes == 16 * Bz and views.is_contiguous(), "queries"
     assert c_pages.dtype is dt and c_pages.is_contiguous(), "summaries"
-    assert clog_pages is None or clog_pages.nbytes == 4 * n_pages * H and clog_pages.is_contiguous(), "summaries"
+    assert clog_pages is None or clog_pages.dtype is _f32 and clog_pages.nbytes == 4 * n_pages * H and clog_pages.is_contiguous(), "summaries"
     assert selected.dtype is _i32 and selected.is_contiguous(), "selected"
     _check(lib.ckv_pages_select(views.data_ptr(), c_pages.data_ptr(), _ptr(clog_pages), page_tokens, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(),
                                 scale, max_len, n_first, n_last, n_select, selected.data_ptr(),
@@ -531,7 +532,7 @@ def decode_attn_selected(views: torch.Tensor, k_pages: torch.Tensor, v_pages: to
     assert HG == H * G and heads == H and width == D and q.is_contiguous() and views.nbytes == 16 * Bz and views.is_contiguous(), "queries"
     assert out.dtype is dt and out.numel() == Bz * HG * D and out.is_contiguous(), "out"
     assert k_pages.dtype is v_pages.dtype is dt and k_pages.nbytes == v_pages.nbytes and k_pages.is_contiguous() and v_pages.is_contiguous(), "pages"
-    assert logdeg_pages is None or logdeg_pages.nbytes == 4 * n_pages * H * P and logdeg_pages.is_contiguous(), "log-degree pages"
+    assert logdeg_pages is None or logdeg_pages.dtype is _f32 and logdeg_pages.nbytes == 4 * n_pages * H * P and logdeg_pages.is_contiguous(), "log-degree pages"
     assert selected.dtype is _i32 and selected.numel() == Bz * H * n_select and selected.is_contiguous(), "selected"
     _check(lib.ckv_decode_attn_selected(views.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(logdeg_pages), P, selected.data_ptr(),
                                         n_select, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(), out.data_ptr(), scale,
@@ -564,8 +565,8 @@ class QuantPool:
         per_row = 4 * n * H * P
         assert width == 64 and kc.nbytes == vc.nbytes == 16 * per_row and kc.is_contiguous() and vc.is_contiguous(), "codes"
         assert ks.nbytes == vs.nbytes == per_row and ks.is_contiguous() and vs.is_contiguous(), "scales"
-        assert deg is None or deg.nbytes == per_row and deg.is_contiguous(), "degree pages"
-        assert logdeg is None or logdeg.nbytes == per_row and logdeg.is_contiguous(), "log-degree pages"
+        assert deg is None or deg.dtype is _i32 and deg.nbytes == per_row and deg.is_contiguous(), "degree pages"
+        assert logdeg is None or logdeg.dtype is _f32 and logdeg.nbytes == per_row and logdeg.is_contiguous(), "log-degree pages"
         return _POOL.pack(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), 0 if deg is None else deg.data_ptr(),
                           0 if logdeg is None else logdeg.data_ptr()), n, H, P
 
@@ -587,8 +588,8 @@ def pages_dequantize(block_table: torch.Tensor, length: int, pool: QuantPool, k:
     (heads, cap, D), dt = k.shape, k.dtype
     assert block_table.dtype is _i32 and block_table.is_contiguous() and block_table.numel() * P >= length, "block table"
     assert heads == H and v.dtype is dt and v.nbytes == k.nbytes and k.is_contiguous() and v.is_contiguous(), "slab"
-    assert deg is None or deg.nbytes == 4 * H * cap and deg.is_contiguous(), "degrees"
-    assert logdeg is None or logdeg.nbytes == 4 * H * cap and logdeg.is_contiguous(), "log-degrees"
+    assert deg is None or deg.dtype is _i32 and deg.nbytes == 4 * H * cap and deg.is_contiguous(), "degrees"
+    assert logdeg is None or logdeg.dtype is _f32 and logdeg.nbytes == 4 * H * cap and logdeg.is_contiguous(), "log-degrees"
     _check(lib.ckv_pages_dequantize(block_table.data_ptr(), length, cp, P, H, D, _DTYPE_CODES[dt], k.data_ptr(), v.data_ptr(),
                                     _ptr(deg), _ptr(logdeg), cap, _stream_for(block_table, k, v, deg, logdeg, *pool.tensors())))
 

@@ -116,3 +116,21 @@ def test_every_tensor_is_on_the_current_device(b, name, x, where):
     t = arguments(name)[x]
     t.where = where
     refused(b, name, ValueError, **{x: t})
+
+
+@pytest.mark.parametrize("name", ["pages_write", "pages_quantize", "pages_dequantize", "decode_attn_quantized"])
+def test_degrees_and_their_logarithms_are_not_exchanged(b, name):
+    """Both have four bytes per row; exchanged, the attention would read integers as logarithms."""
+    a = arguments(name)
+    for x, y in (("deg_pages", "logdeg_pages"), ("deg", "logdeg")):
+        if x in a and y in a:
+            refused(b, name, **{x: a[y], y: a[x]})
+        for z, dt in ((x, F32), (y, I32)):
+            if z in a:
+                refused(b, name, **{z: made(*a[z].shape, dt=dt)})
+
+
+@pytest.mark.parametrize("name,x,dt", [("pages_summarize", "deg_pages", F32), ("pages_summarize", "clog_pages", I32), ("pages_select", "clog_pages", I32),
+                                       ("decode_attn_selected", "logdeg_pages", I32)])
+def test_degrees_are_integers_and_logarithms_fp32(b, name, x, dt):
+    refused(b, name, **{x: made(*arguments(name)[x].shape, dt=dt)})
