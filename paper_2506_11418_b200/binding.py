@@ -424,8 +424,9 @@ def pages_scatter(block_table, length, k, v, deg, k_pages, v_pages, deg_pages, l
 
 
 # ---- block tables and slot maps, attention over selected pages, four-bit pages
-# (Calls of a few microseconds on the GPU: what is checked of a tensor is its size in bytes and that it is contiguous, which is what
-# a wrong read or write could come from, and its type where the library is told one.)
+# (Calls of a few microseconds on the GPU: what is checked of a tensor is what a wrong read or write could come from: its device,
+# its size in bytes and that it is contiguous, and the type of everything but a pool's codes and scales and the workspace, which
+# are bytes.)
 
 _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _i32, _i64, _f32 = torch.int32, torch.int64, torch.float32
@@ -454,12 +455,14 @@ def pages_resize(lens: torch.Tensor, new_lens: torch.Tensor, block_tables: torch
     views int64 [Bz, 2] (paged_views' layout)."""
     Bz, row = block_tables.shape
     n_pages, n_slots = ring.numel(), slots.numel()
+    assert lens.dtype is new_lens.dtype is lens_out.dtype is slot_begin.dtype is _i64, "lengths"
     assert lens.nbytes == new_lens.nbytes == lens_out.nbytes == slot_begin.nbytes - 8 == 8 * Bz, "lengths"
     assert lens.is_contiguous() and new_lens.is_contiguous() and lens_out.is_contiguous() and slot_begin.is_contiguous(), "lengths"
-    assert ring_state.nbytes == ring_state_out.nbytes == 16 and ring_state.is_contiguous() and ring_state_out.is_contiguous(), "ring"
-    assert ring.dtype is _i32 and ring.is_contiguous() and status.nbytes == 4, "ring"
+    assert ring_state.dtype is ring_state_out.dtype is _i64 and ring_state.nbytes == ring_state_out.nbytes == 16, "ring"
+    assert ring_state.is_contiguous() and ring_state_out.is_contiguous(), "ring"
+    assert ring.dtype is _i32 and ring.is_contiguous() and status.dtype is _i32 and status.nbytes == 4, "ring"
     assert block_tables.dtype is _i32 and block_tables.is_contiguous() and slots.dtype is _i64 and slots.is_contiguous(), "tables"
-    assert views is None or views.nbytes == 16 * Bz and views.is_contiguous(), "views"
+    assert views is None or views.dtype is _i64 and views.nbytes == 16 * Bz and views.is_contiguous(), "views"
     _check(lib.ckv_pages_resize(lens.data_ptr(), new_lens.data_ptr(), Bz, page_tokens, block_tables.data_ptr(), row, ring.data_ptr(),
                                 n_pages, ring_state.data_ptr(), slots.data_ptr(), n_slots, slot_begin.data_ptr(),
                                 lens_out.data_ptr(), ring_state_out.data_ptr(), status.data_ptr(), _ptr(views),
@@ -498,7 +501,8 @@ def pages_summarize(views: torch.Tensor, k_pages: torch.Tensor, deg_pages: torch
     the batch's pages, from the one that holds token from_lens[b] on."""
     n_pages, H, P, D = k_pages.shape
     Bz, dt, heads = views.numel() // 2, k_pages.dtype, n_pages * H
-    assert views.dtype is _i64 and views.is_contiguous() and (from_lens is None or from_lens.nbytes == 8 * Bz and from_lens.is_contiguous()), "views"
+    assert views.dtype is _i64 and views.is_contiguous(), "views"
+    assert from_lens is None or from_lens.dtype is _i64 and from_lens.nbytes == 8 * Bz and from_lens.is_contiguous(), "lengths"
     assert k_pages.is_contiguous(), "pages"
     assert deg_pages is None or deg_pages.dtype is _i32 and deg_pages.nbytes == 4 * heads * P and deg_pages.is_contiguous(), "degree pages"
     assert c_pages.dtype is dt and c_pages.numel() == heads * D and c_pages.is_contiguous(), "summaries"
@@ -514,7 +518,8 @@ def pages_select(views: torch.Tensor, c_pages: torch.Tensor, clog_pages: torch.T
     n_pages, H, D = c_pages.shape
     Bz, heads, n_select = selected.shape
     dt = q.dtype
-    assert heads == H and q.shape == (Bz, H * G, D) and q.is_contiguous() and views.nbytes == 16 * Bz and views.is_contiguous(), "queries"
+    assert heads == H and q.shape == (Bz, H * G, D) and q.is_contiguous(), "queries"
+    assert views.dtype is _i64 and views.nbytes == 16 * Bz and views.is_contiguous(), "views"
     assert c_pages.dtype is dt and c_pages.is_contiguous(), "summaries"
     assert clog_pages is None or clog_pages.dtype is _f32 and clog_pages.nbytes == 4 * n_pages * H and clog_pages.is_contiguous(), "summaries"
     assert selected.dtype is _i32 and selected.is_contiguous(), "selected"
@@ -529,10 +534,12 @@ def decode_attn_selected(views: torch.Tensor, k_pages: torch.Tensor, v_pages: to
     Bz, HG, D = q.shape
     n_pages, heads, P, width = k_pages.shape
     dt, n_select = q.dtype, selected.shape[2]
-    assert HG == H * G and heads == H and width == D and q.is_contiguous() and views.nbytes == 16 * Bz and views.is_contiguous(), "queries"
+    assert HG == H * G and heads == H and width == D and q.is_contiguous(), "queries"
+    assert views.dtype is _i64 and views.nbytes == 16 * Bz and views.is_contiguous(), "views"
     assert out.dtype is dt and out.numel() == Bz * HG * D and out.is_contiguous(), "out"
     assert k_pages.dtype is v_pages.dtype is dt and k_pages.nbytes == v_pages.nbytes and k_pages.is_contiguous() and v_pages.is_contiguous(), "pages"
-    assert logdeg_pages is None or logdeg_pages.dtype is _f32 and logdeg_pages.nbytes == 4 * n_pages * H * P and logdeg_pages.is_contiguous(), "log-degree pages"
+    assert logdeg_pages is None or logdeg_pages.dtype is _f32 and logdeg_pages.nbytes == 4 * n_pages * H * P, "log-degree pages"
+    assert logdeg_pages is None or logdeg_pages.is_contiguous(), "log-degree pages"
     assert selected.dtype is _i32 and selected.numel() == Bz * H * n_select and selected.is_contiguous(), "selected"
     _check(lib.ckv_decode_attn_selected(views.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(logdeg_pages), P, selected.data_ptr(),
                                         n_select, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(), out.data_ptr(), scale,
@@ -604,7 +611,8 @@ def decode_attn_quantized(views: torch.Tensor, pool: QuantPool, H: int, G: int, 
     Bz, HG, D = q.shape
     cp, _, heads, P = pool.c()
     dt = q.dtype
-    assert HG == H * G and heads == H and q.is_contiguous() and views.nbytes == 16 * Bz and views.is_contiguous(), "queries"
+    assert HG == H * G and heads == H and q.is_contiguous(), "queries"
+    assert views.dtype is _i64 and views.nbytes == 16 * Bz and views.is_contiguous(), "views"
     assert out.dtype is dt and out.numel() == Bz * HG * D and out.is_contiguous(), "out"
     _check(lib.ckv_decode_attn_quantized(views.data_ptr(), cp, P, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(), out.data_ptr(), scale, max_len,
                                          workspace.data_ptr(), workspace.nbytes, _stream_for(views, q, out, workspace, *pool.tensors())))

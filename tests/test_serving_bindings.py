@@ -134,3 +134,18 @@ def test_degrees_and_their_logarithms_are_not_exchanged(b, name):
                                        ("decode_attn_selected", "logdeg_pages", I32)])
 def test_degrees_are_integers_and_logarithms_fp32(b, name, x, dt):
     refused(b, name, **{x: made(*arguments(name)[x].shape, dt=dt)})
+
+
+@pytest.mark.parametrize("dt,wrong", [(I64, F64), (I32, F32)])
+@pytest.mark.parametrize("name,x", tensor_arguments())
+def test_lengths_counts_and_views_are_integers(b, name, x, dt, wrong):
+    """Floats of the same size would be read as bits."""
+    t = arguments(name)[x]
+    if t.dtype is dt:
+        refused(b, name, **{x: made(*t.shape, dt=wrong)})
+
+
+@pytest.mark.parametrize("name,x", [(n, x) for n, x in tensor_arguments() if x in ("lens", "new_lens", "lens_out", "from_lens", "views", "ring_state", "ring_state_out")])
+def test_lengths_of_half_the_width_are_refused(b, name, x):
+    t = arguments(name)[x]
+    refused(b, name, **{x: made(t.shape[0], 2 * (t.numel() // t.shape[0]), dt=I32)})
