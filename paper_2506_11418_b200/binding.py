@@ -498,7 +498,7 @@ def pages_write(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: 
 def pages_summarize(views: torch.Tensor, k_pages: torch.Tensor, deg_pages: torch.Tensor | None, c_pages: torch.Tensor, clog_pages: torch.Tensor,
                     max_blocks: int, from_lens: torch.Tensor | None = None):
     """ckv_pages_summarize on the current stream: mean keys c_pages [n_pages, H, D] and log-degrees clog_pages [n_pages, H] of
-    the batch's pages, from the one that holds token from_lens[b] on."""
+    the batch's pages, from the one that holds token from_lens[b] on (of a sequence that is now shorter: its last page)."""
     n_pages, H, P, D = k_pages.shape
     Bz, dt, heads = views.numel() // 2, k_pages.dtype, n_pages * H
     assert views.dtype is _i64 and views.is_contiguous(), "views"

@@ -22,7 +22,7 @@ constexpr int kSumThreads = 256;
 
 struct SummarizeArgs {
   const ckv_paged_view* views;
-  const int64_t* from_lens;  // null: from the first block
+  const int64_t* from_lens;  // null: from the first block; above the length: from the last
   const uint4* k_pages;
   const int32_t* deg_pages;  // null: all ones
   __nv_bfloat16* c_pages;
@@ -42,7 +42,9 @@ __global__ void __launch_bounds__(kSumThreads) pages_summarize_kernel(const Summ
   griddep_wait();
   griddep_launch();
   const ckv_paged_view view = a.views[b];
-  const int64_t blk = (a.from_lens ? max(a.from_lens[b], (int64_t)0) >> a.shift : 0) + x, left = view.len - (blk << a.shift);
+  int64_t from = a.from_lens ? a.from_lens[b] : 0;
+  if (from > view.len) from = view.len - 1;  // (a sequence that shrank: its last block lost tokens)
+  const int64_t blk = (max(from, (int64_t)0) >> a.shift) + x, left = view.len - (blk << a.shift);
   const int rows = x < a.max_blocks && left > 0 ? (int)min(left, (int64_t)1 << a.shift) : 0;
   if (WPH == 1 && rows == 0) return;
   const int64_t ph = rows > 0 ? (int64_t)view.block_table[blk] * a.H + h : 0, row = ph << a.shift;

@@ -1,0 +1,48 @@
+"""The serving calls where a step changes what the calls before it left behind, and at sizes where a launch changes form.
+Tolerances as in test_gpu_serving.py."""
+import numpy as np
+import pytest
+import torch
+
+import parity_util as PU
+from paper_2506_11418_b200 import synth
+from test_gpu_serving import D, DEV, I32, I64, SCALE, blocks, lib, paged_batch, select_plain, summaries_plain
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- summaries of sequences that shrink
+
+@pytest.mark.parametrize("P,H", [(32, 3), (64, 8)])
+@pytest.mark.parametrize("bound", ["tight", "loose"])
+def test_summaries_of_sequences_that_shrink(P, H, bound):
+    """The last block that is left loses the tokens that were dropped, and the selection scores it without them, though it is not
+    always chosen.  Beside them sequences that grow, stay, and start."""
+    b = lib()
+    old = [20 * P + 5, 20 * P + 5, 12 * P, 9 * P + 1, 30 * P, 8 * P - 1, 700, 15 * P + 3, 0, 5 * P]
+    new = [11 * P + 7, 11 * P, 11 * P + 1, 9 * P, 1, 0, 701, 15 * P + 3, 40, 5 * P]
+    s = paged_batch([max(o, n) for o, n in zip(old, new)], H, P, seed=P, deg_top=60)
+    views = lambda lens: b.paged_views([s["tables"][i] for i in range(len(lens))], lens, DEV)  # noqa: E731
+    cp, cl = torch.full((s["n_pages"], H, D), 9.0, dtype=torch.bfloat16, device=DEV), torch.full((s["n_pages"], H), 9.0, device=DEV)
+    b.pages_summarize(views(old), s["kp"], s["dp"], cp, cl, max(blocks(n, P) for n in old))
+    most = 2 if bound == "tight" else 40
+    b.pages_summarize(views(new), s["kp"], s["dp"], cp, cl, most, torch.tensor(old, **I64))
+    got_c, got_l, tables = PU.to_np64(cp), cl.cpu().numpy(), s["tables"].cpu().numpy()
+    s["lens"] = new
+    for i, n in enumerate(new):
+        for blk, (c, lg, mag) in enumerate(summaries_plain(s, i, 0, True)):
+            p = tables[i, blk]
+            assert np.all(np.abs(got_c[p] - c) <= 2.0 ** -8 * np.abs(c) + (P + 2) * 2.0 ** -24 * mag), f"sequence {i}, block {blk}"
+            np.testing.assert_allclose(got_l[p], lg, rtol=1e-6, atol=1e-7)
+        for blk in range(blocks(n, P), blocks(old[i], P)):              # blocks that were given back: nobody's, and left alone
+            assert np.all(np.isfinite(got_l[tables[i, blk]]))
+    G, k = 4, 4
+    q = synth.queries(len(new), H * G, D, seed=3, dtype="bf16", device=DEV)
+    sel = torch.full((len(new), H, k), -9, **I32)
+    b.pages_select(views(new), cp, cl, P, G, q, SCALE, max(new), sel)
+    qn, got = PU.to_np64(q), sel.cpu().numpy()
+    for i, n in enumerate(new):
+        p = tables[i, :blocks(n, P)]
+        for h in range(H):
+            want = select_plain(qn[i, h * G:(h + 1) * G], got_c[p, h], got_l[p, h].astype(np.float64), SCALE, 0, 0, k) if n else []
+            assert got[i, h].tolist() == want + [-1] * (k - len(want)), f"sequence {i}, head {h}"
