@@ -346,8 +346,8 @@ typedef struct ckv_quant_pool {
   uint8_t* v_codes;
   uint8_t* k_scales;
   uint8_t* v_scales;
-  int32_t* deg_pages;  /* [n_pages, H, page_tokens]; NULL = all ones */
-  float* logdeg_pages; /* [n_pages, H, page_tokens]; NULL = all degrees one */
+  int32_t* deg_pages;  /* [n_pages, H, page_tokens]; NULL = not kept (all ones, if logdeg_pages is NULL too) */
+  float* logdeg_pages; /* [n_pages, H, page_tokens], all that the attention reads of the degrees; NULL = it takes all for one */
 } ckv_quant_pool;
 
 /* As ckv_pages_write, into four-bit pages.  A group's power of two is 2^(floor(log2 of its largest magnitude) - 2), no less
@@ -357,7 +357,8 @@ int ckv_pages_quantize(const ckv_token_rows* rows, const int64_t* slots, int64_t
                        void* cuda_stream);
 
 /* As ckv_pages_gather, from four-bit pages: the values that the codes stand for, exactly, as a slab k, v [H, cap, D] of `dtype`
- * (to run ckv_compress_* on it), with deg and logdeg [H, cap] (either may be NULL; all ones where the pool has no degrees). */
+ * (to run ckv_compress_* on it), with deg and logdeg [H, cap] (either may be NULL; all ones where the pool has neither degrees
+ * nor logarithms).  From a pool with logdeg_pages alone logdeg is the stored one, and deg has to be NULL (CKV_ERR_INVALID_ARG). */
 int ckv_pages_dequantize(const int32_t* block_table, int64_t len, const ckv_quant_pool* pool, int32_t page_tokens, int32_t H, int32_t D,
                          int32_t dtype, void* k, void* v, int32_t* deg, float* logdeg, int64_t cap, void* cuda_stream);
 

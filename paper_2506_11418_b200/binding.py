@@ -549,7 +549,8 @@ def decode_attn_selected(views: torch.Tensor, k_pages: torch.Tensor, v_pages: to
 @dataclass
 class QuantPool:
     """One layer's four-bit pool: codes uint8 [n_pages, H, page_tokens, 64], scales uint8 [n_pages, H, page_tokens, 4], degrees
-    int32 and log-degrees fp32 [n_pages, H, page_tokens] (either may be None: all ones)."""
+    int32 and log-degrees fp32 [n_pages, H, page_tokens].  Either may be None: the attention reads the log-degrees (None: all
+    degrees one), pages_dequantize returns what is kept and refuses to return degrees that are kept as logarithms alone."""
     k_codes: torch.Tensor
     v_codes: torch.Tensor
     k_scales: torch.Tensor

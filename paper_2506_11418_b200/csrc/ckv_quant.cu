@@ -214,9 +214,10 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
   }
   if (a.deg || a.logdeg)
     for (int64_t i = i0 + threadIdx.x; i < min(a.len, i0 + kRows * U); i += blockDim.x) {
-      const int dg = a.pool.deg_pages ? a.pool.deg_pages[(((int64_t)a.table[i >> a.shift] * a.H + h) << a.shift) + (i & mask)] : 1;
+      const int64_t row = (((int64_t)a.table[i >> a.shift] * a.H + h) << a.shift) + (i & mask);
+      const int dg = a.pool.deg_pages ? a.pool.deg_pages[row] : 1;
       if (a.deg) a.deg[(int64_t)h * a.cap + i] = dg;
-      if (a.logdeg) a.logdeg[(int64_t)h * a.cap + i] = logf((float)dg);
+      if (a.logdeg) a.logdeg[(int64_t)h * a.cap + i] = a.pool.deg_pages || !a.pool.logdeg_pages ? logf((float)dg) : a.pool.logdeg_pages[row];
     }
 }
 
@@ -946,6 +947,7 @@ int ckv_pages_dequantize(const int32_t* block_table, int64_t len, const ckv_quan
   int st = check_pool(pool);
   if (st != CKV_OK) return st;
   const int shift = page_shift(page_tokens);
+  if (deg && pool->logdeg_pages && !pool->deg_pages) return CKV_ERR_INVALID_ARG;  // (the degrees are known by their logarithms only)
   if (shift < 0 || D != kD || H > 65535) return CKV_ERR_UNSUPPORTED;
   if (!aligned16(k) || !aligned16(v)) return CKV_ERR_ALIGNMENT;
   if (len == 0) return CKV_OK;

@@ -46,3 +46,38 @@ def test_summaries_of_sequences_that_shrink(P, H, bound):
         for h in range(H):
             want = select_plain(qn[i, h * G:(h + 1) * G], got_c[p, h], got_l[p, h].astype(np.float64), SCALE, 0, 0, k) if n else []
             assert got[i, h].tolist() == want + [-1] * (k - len(want)), f"sequence {i}, head {h}"
+
+
+# ---------------------------------------------------------------- degrees of four-bit pools that keep one of their two forms
+
+@pytest.mark.parametrize("with_deg,with_logdeg", [(True, True), (True, False), (False, True), (False, False)])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_degrees_come_back_from_every_kind_of_pool(dt, with_deg, with_logdeg):
+    """What a pool keeps of the degrees comes back, as degrees, as logarithms or both; what it does not keep is refused, not made one."""
+    b = lib()
+    n, H, P = 777, 3, 64
+    g = torch.Generator(DEV).manual_seed(1)
+    k, v = (torch.randn((n, H, D), generator=g, device=DEV).to(dt) for _ in range(2))
+    deg = torch.randint(1, 70000, (n, H), generator=g, **I32)
+    table = torch.randperm(blocks(n, P) + 2, generator=torch.Generator().manual_seed(2)).to(torch.int32).to(DEV)
+    pos = torch.arange(n, device=DEV)
+    slots = table.long()[pos // P] * P + pos % P
+    pool = b.QuantPool.empty(len(table), H, P)
+    pool.deg_pages, pool.logdeg_pages = pool.deg_pages if with_deg else None, pool.logdeg_pages if with_logdeg else None
+    b.pages_quantize(slots, k, v, pool, deg)
+    want = deg.t() if with_deg or with_logdeg else torch.ones((H, n), **I32)
+    for ask_deg in (False, True):
+        ko, vo = (torch.zeros((H, n + 1, D), dtype=dt, device=DEV) for _ in range(2))
+        do, lo = torch.full((H, n + 1), -3, **I32) if ask_deg else None, torch.full((H, n + 1), -3.0, device=DEV)
+        if ask_deg and with_logdeg and not with_deg:
+            with pytest.raises(b.CkvError):
+                b.pages_dequantize(table, n, pool, ko, vo, do, lo)
+            assert torch.all(do == -3) and torch.all(lo == -3) and torch.all(ko == 0)
+            continue
+        b.pages_dequantize(table, n, pool, ko, vo, do, lo)
+        torch.testing.assert_close(lo[:, :n], torch.log(want.double()).float(), rtol=1e-6, atol=1e-7)
+        assert torch.all(lo[:, n:] == -3)
+        if ask_deg:
+            assert torch.equal(do[:, :n], want) and torch.all(do[:, n:] == -3)
+        if with_logdeg and not with_deg:  # as they are stored, bit for bit
+            assert torch.equal(lo[:, :n], pool.logdeg_pages.transpose(0, 1).reshape(H, -1)[:, slots])

@@ -149,3 +149,17 @@ def test_lengths_counts_and_views_are_integers(b, name, x, dt, wrong):
 def test_lengths_of_half_the_width_are_refused(b, name, x):
     t = arguments(name)[x]
     refused(b, name, **{x: made(t.shape[0], 2 * (t.numel() // t.shape[0]), dt=I32)})
+
+
+def test_degrees_kept_as_logarithms_alone_are_not_returned_as_ones():
+    """The library itself, on the host: the refusal comes before a launch."""
+    import ctypes as C
+
+    from paper_2506_11418_b200 import binding as lib
+    A = 0x10000  # sixteen-byte aligned, never read
+
+    def dequantize(deg, logdeg, deg_pages, logdeg_pages, n=0):
+        p = lib.CkvQuantPool(A, 2 * A, 3 * A, 4 * A, deg_pages, logdeg_pages)
+        return lib.lib.ckv_pages_dequantize(5 * A, n, C.byref(p), 64, 8, 128, lib.BF16, 6 * A, 7 * A, deg, logdeg, 3, None)
+    assert dequantize(8 * A, None, None, 9 * A, n=3) == 1 and dequantize(8 * A, 10 * A, None, 9 * A, n=3) == 1 and dequantize(8 * A, None, None, 9 * A) == 1
+    assert dequantize(None, 8 * A, None, 9 * A) == 0 and dequantize(8 * A, 10 * A, 9 * A, None) == 0 and dequantize(8 * A, 10 * A, None, None) == 0
