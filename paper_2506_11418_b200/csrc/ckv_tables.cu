@@ -293,7 +293,8 @@ int ckv_pages_resize(const int64_t* lens, const int64_t* new_lens, int32_t Bz, i
   // one run of 128 slots per warp, but every CTA repeats the sums: at most two CTAs per SM
   const int64_t ctas = std::min<int64_t>(std::max<int64_t>((n_slots + 128 * kResizeWarps - 1) / (128 * kResizeWarps), 1), 2 * sm_count());
   const size_t smem = (size_t)3 * (Bz + 1) * 4;
-  if (smem > 48 * 1024 &&
+  // (48 KB come without asking, but hold the kernel's static arrays too)
+  if (smem > 40 * 1024 &&
       cudaFuncSetAttribute(pages_resize_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * (kResizeMaxSeqs + 1) * 4) != cudaSuccess)
     return CKV_ERR_CUDA;
   return launch_dependent(pages_resize_kernel, dim3((unsigned)ctas), dim3(kResizeThreads), smem, static_cast<cudaStream_t>(cuda_stream), a) == cudaSuccess

@@ -1,5 +1,9 @@
 """The serving calls where a step changes what the calls before it left behind, and at sizes where a launch changes form.
 Tolerances as in test_gpu_serving.py."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -81,3 +85,30 @@ def test_degrees_come_back_from_every_kind_of_pool(dt, with_deg, with_logdeg):
             assert torch.equal(do[:, :n], want) and torch.all(do[:, n:] == -3)
         if with_logdeg and not with_deg:  # as they are stored, bit for bit
             assert torch.equal(lo[:, :n], pool.logdeg_pages.transpose(0, 1).reshape(H, -1)[:, slots])
+
+
+# ---------------------------------------------------------------- batches whose sums fill the shared memory that needs no opt-in
+
+def test_resize_of_every_batch_size_about_the_shared_memory_limit():
+    """In a fresh process, where no larger batch has raised the kernel's limit before."""
+    code = """
+import sys
+sys.path[:0] = [{tests!r}, {root!r}]
+import os
+import subprocess
+import sys
+
+import numpy as np
+import test_gpu_serving as T
+for Bz in (3400, 3412, 3413, 3414, 4076, 4077, 4078, 4090, 4094, 4095):
+    rng = np.random.default_rng(Bz)
+    old, new = rng.integers(0, 70, Bz), rng.integers(0, 70, Bz)
+    need = sum(T.blocks(max(int(o), int(n)), 32) for o, n in zip(old, new))
+    T.check_resize(old.tolist(), new.tolist(), 32, 4, need, 5, Bz)
+for Bz in (4096, 8192, 4095):
+    T.check_resize([1] * Bz, [2] * Bz, 32, 4, Bz, 5, Bz)
+print("resized")
+"""
+    here = os.path.dirname(os.path.abspath(__file__))
+    res = subprocess.run([sys.executable, "-c", code.format(tests=here, root=os.path.dirname(here))], capture_output=True, text=True, timeout=200)
+    assert res.returncode == 0 and "resized" in res.stdout, res.stdout + res.stderr
