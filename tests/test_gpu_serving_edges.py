@@ -10,7 +10,7 @@ import torch
 
 import parity_util as PU
 from paper_2506_11418_b200 import synth
-from test_gpu_serving import D, DEV, I32, I64, SCALE, blocks, lib, paged_batch, select_plain, summaries_plain
+from test_gpu_serving import D, DEV, I32, I64, SCALE, blocks, lib, paged_batch, quant_batch, select_case, select_plain, summaries_plain
 
 pytestmark = pytest.mark.gpu
 
@@ -112,3 +112,72 @@ print("resized")
     here = os.path.dirname(os.path.abspath(__file__))
     res = subprocess.run([sys.executable, "-c", code.format(tests=here, root=os.path.dirname(here))], capture_output=True, text=True, timeout=200)
     assert res.returncode == 0 and "resized" in res.stdout, res.stdout + res.stderr
+
+
+# ---------------------------------------------------------------- selection: the path through 64 bits beyond 8192 blocks
+
+LONG = [([24576 * 32, 9000 * 32 - 7], 64), ([8193 * 32, 16384 * 32, 40], 3000)]
+
+
+@pytest.mark.parametrize("lens,k", LONG)
+def test_select_equal_scores_of_very_long_sequences(lens, k):
+    """All summaries equal, a few different ones, and chosen blocks that straddle a thread's run of words."""
+    def same(cp, cl, q, tables):
+        cp[:], cl[:] = cp[:1], 0.5
+    select_case(lens, 1, 4, 32, k, 1, 2, seed=1, with_clog=True, change=same)
+
+    def few(cp, cl, q, tables):
+        p = torch.arange(cp.shape[0], device=DEV) % 5
+        cp[:], cl[:] = cp[p], cl[p]
+    select_case(lens, 1, 4, 32, k, 0, 1, seed=2, change=few)
+    select_case(lens, 1, 4, 32, k, 2, 0, seed=3, change=few)
+
+
+@pytest.mark.parametrize("lens,k", LONG)
+def test_select_values_that_are_not_finite_in_very_long_sequences(lens, k):
+    def odd(cp, cl, q, tables):
+        cp[::7, 0, 3] = float("nan")
+        cp[3::11, 0, 5] = float("inf")
+        cp[5::13, 0, 9] = float("-inf")
+        cl[2::17] = float("-inf")
+    select_case(lens, 1, 2, 32, k, 1, 2, seed=5, change=odd)
+
+    def nan(cp, cl, q, tables):
+        q[:] = float("nan")
+    select_case(lens, 1, 4, 32, k, 1, 2, seed=7, change=nan)
+
+
+def test_select_products_below_the_normal_range():
+    """Scores whose products are subnormal in 32 bits, brought back by the scale, next to ordinary ones through the log-degree."""
+    def tiny(cp, cl, q, tables):
+        cp.mul_(2.0 ** -66)
+        q.mul_(2.0 ** -66)
+        cl[:] = 0.0
+    for scale in (2.0 ** 6, 2.0 ** 30, 2.0 ** 120, -2.0 ** 100):
+        select_case([64 * 700, 64 * 100], 2, 4, 64, 30, 1, 1, seed=21, scale=scale, change=tiny)
+
+
+# ---------------------------------------------------------------- four-bit attention: NaN through the second kernel
+
+def test_quantized_attention_nan_group_is_seen_across_shares():
+    """As for a batch of one cluster per pair: a NaN scale reaches the heads that read it and no other, whatever part of the
+    sequence holds it and however many partials are joined."""
+    b = lib()
+    lens, H, G, P = [3000, 40, 2000, 1, 777, 4000] * 6, 4, 4, 64
+    pool, views, seqs, tables = quant_batch(lens, H, P, seed=61)
+    q = synth.queries(len(lens), H * G, D, seed=1, dtype="bf16", device=DEV)
+    ws = torch.empty(b.decode_quantized_workspace_bytes(len(lens), H, G, D, 4000), dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(q)
+    b.decode_attn_quantized(views, pool, H, G, q, out, SCALE, 4000, ws)
+    assert torch.all(torch.isfinite(out.float()))
+    want = torch.zeros((len(lens), H, G, D), dtype=torch.bool, device=DEV)
+    for seq, h, pos, group in ((0, 0, 0, 0), (2, 3, 1999, 2), (3, 1, 0, 3), (5, 2, 2222, 1), (35, 3, 3999, 0)):
+        pool.v_scales[tables[seq, pos // P].item(), h, pos % P, group] = 255
+        want[seq, h, :, 32 * group:32 * group + 32] = True
+    b.decode_attn_quantized(views, pool, H, G, q, out, SCALE, 4000, ws)
+    assert torch.equal(torch.isnan(out).view_as(want), want)
+    for seq, h, pos, group in ((6, 0, 2999, 0), (8, 1, 5, 3), (9, 2, 0, 1)):
+        pool.k_scales[tables[seq, pos // P].item(), h, pos % P, group] = 255
+        want[seq, h] = True
+    b.decode_attn_quantized(views, pool, H, G, q, out, SCALE, 4000, ws)
+    assert torch.equal(torch.isnan(out).view_as(want), want)
