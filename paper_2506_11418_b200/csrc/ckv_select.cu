@@ -365,8 +365,9 @@ __global__ void __launch_bounds__(kSelThreads, 2) pages_select_kernel(const Sele
       if (t < 2) {  // lanes 4 g: row g; 4 g + 1: row g + 8
         const int i = base + g + 8 * t;
         const float s = (t ? sb : sa) + (t ? lb : la);
-        // |q| |c| scale 2^-15, and the roundings after the sum
-        const float e = (t ? eb : ea) * fabsf(a.scale) * 0x1p-15f + fabsf(t ? lb : la) * 0x1p-20f + 0x1p-120f;
+        // (|q| |c| + 2^-125) scale 2^-15, and the roundings after the sum; 2^-140 is what 128 subnormal products and additions can
+        // lose, with a factor of two to spare
+        const float e = (t ? eb : ea) * fabsf(a.scale) * 0x1p-15f + fabsf(a.scale) * 0x1p-140f + fabsf(t ? lb : la) * 0x1p-20f + 0x1p-120f;
         if (i < n) {
           err = fmaxf(err, e < 1e30f ? e : INFINITY);  // (NaN becomes infinite)
           if (i >= f0 && i < f1) {

@@ -157,6 +157,17 @@ def test_select_products_below_the_normal_range():
         select_case([64 * 700, 64 * 100], 2, 4, 64, 30, 1, 1, seed=21, scale=scale, change=tiny)
 
 
+@pytest.mark.parametrize("q_exp,c_exp", [(-75, -75), (-20, -124), (-110, -34)])
+def test_select_products_that_32_bits_do_not_hold(q_exp, c_exp):
+    """Products below 2^-149, zeros in 32 bits, that a large scale makes scores of: the bound on the 32-bit scores counts what they lose."""
+    def tiny(cp, cl, q, tables):
+        cp.mul_(2.0 ** c_exp)
+        q.mul_(2.0 ** q_exp)
+        cl[:] = 0.0
+    for scale in (2.0 ** 120, -2.0 ** 127):
+        select_case([64 * 700, 64 * 100], 2, 4, 64, 30, 1, 1, seed=22, scale=scale, change=tiny)
+
+
 # ---------------------------------------------------------------- four-bit attention: NaN through the second kernel
 
 def test_quantized_attention_nan_group_is_seen_across_shares():
