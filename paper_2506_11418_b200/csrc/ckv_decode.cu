@@ -656,7 +656,8 @@ cudaError_t launch_decode_fast(const DecodeArgs& a, cudaStream_t st) {
   }
   const dim3 grid((unsigned)((a.n_splits + kFWarps - 1) / kFWarps), (unsigned)a.H, (unsigned)a.Bz);
   if ((e = launch_dependent(decode_fast_kernel<PAGED, 0, kFT, kFWarps, kFStages>, grid, dim3(kFWarps * 32), kFSmemBytes, st, a)) != cudaSuccess) return e;
-  return launch_decode_combine(a, st);
+  return launch_dependent(decode_combine_kernel<__nv_bfloat16, 128>, dim3((unsigned)(a.Bz * a.H * a.G)), dim3(kCombThreads), 0,
+                          st, a);
 }
 
 }  // namespace
@@ -715,10 +716,6 @@ cudaError_t launch_decode(const DecodeArgs& a, int dtype, int D, cudaStream_t st
 }
 
 cudaError_t launch_decode_paged(const DecodeArgs& a, cudaStream_t st) { return launch_decode_fast<true>(a, st); }
-
-cudaError_t launch_decode_combine(const DecodeArgs& a, cudaStream_t st) {
-  return launch_dependent(decode_combine_kernel<__nv_bfloat16, 128>, dim3((unsigned)(a.Bz * a.H * a.G)), dim3(kCombThreads), 0, st, a);
-}
 
 cudaError_t launch_decode_selected(const DecodeArgs& a, cudaStream_t st) {
   // The most warps per pair of which all pairs are resident at once (an SM holds four warps and their rings), while each has

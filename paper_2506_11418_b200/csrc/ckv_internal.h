@@ -213,7 +213,6 @@ cudaError_t launch_compose_assign(int32_t* total, const int32_t* step, int64_t n
 cudaError_t launch_decode(const DecodeArgs& a, int dtype, int D, cudaStream_t st);
 cudaError_t launch_decode_paged(const DecodeArgs& a, cudaStream_t st);
 cudaError_t launch_decode_selected(const DecodeArgs& a, cudaStream_t st);
-cudaError_t launch_decode_combine(const DecodeArgs& a, cudaStream_t st);  // bf16: partials of a split launch -> out
 void decode_plan(int32_t Bz, int32_t H, int dtype, int64_t max_len, int64_t max_partial_floats, int32_t G, int32_t D,
                  int32_t* n_splits, int64_t* span);
 size_t decode_partial_floats(int32_t Bz, int32_t H, int32_t G, int32_t D, int64_t max_len);
