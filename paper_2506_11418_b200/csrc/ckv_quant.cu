@@ -419,9 +419,9 @@ __global__ void __launch_bounds__((CL > 0 ? kQClusterWarps : kQShareWarps) * 32,
   const float* logdeg = qa_.pool.logdeg_pages;
 
   for (;;) {  // one stretch of tiles of one (sequence, KV head)
-  const int len = (int)view.len, seq_tiles = tiles_of(view.len);
+  const int seq_tiles = tiles_of(view.len);
   const int ntiles = CL > 0 ? (int)((int64_t)seq_tiles * (gw + 1) / (CL * NW)) - tile0 : min(share, seq_tiles - tile0);
-  const int n_tail = len - (seq_tiles - 1) * TT;  // tokens of the sequence's last tile
+  const int n_tail = (int)(view.len - (int64_t)(seq_tiles - 1) * TT);  // tokens of the sequence's last tile
   const int tile_shift = a.page_shift - 5;        // tiles per page
   const int n_blocks = (seq_tiles + (1 << tile_shift) - 1) >> tile_shift;
   int blk0 = tile0 >> tile_shift;

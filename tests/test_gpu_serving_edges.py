@@ -192,3 +192,22 @@ def test_quantized_attention_nan_group_is_seen_across_shares():
         want[seq, h] = True
     b.decode_attn_quantized(views, pool, H, G, q, out, SCALE, 4000, ws)
     assert torch.equal(torch.isnan(out).view_as(want), want)
+
+
+def test_quantized_attention_past_2_to_the_31_tokens():
+    """A block table that names the same pages again and again: the softmax over all of them is that over the pages once, each token
+    weighted by how often it is met."""
+    b = lib()
+    H, G, P, laps, extra = 1, 2, 1 << 15, 1 << 15, (1 << 15) + 4321
+    pool, _, seqs, tables = quant_batch([2 * P], H, P, seed=71)
+    n = 2 * P * laps + extra                                             # past 2^31, its last tile not a whole one
+    assert n > 2 ** 31 and n % 32
+    K, V, deg = seqs[0]
+    table = torch.cat([tables[0].repeat(laps), tables[0]])
+    views = b.paged_views([table], [n], DEV)
+    q = synth.queries(1, H * G, D, seed=2, dtype="bf16", device=DEV)
+    out = torch.empty_like(q)
+    ws = torch.empty(b.decode_quantized_workspace_bytes(1, H, G, D, n), dtype=torch.uint8, device=DEV)
+    b.decode_attn_quantized(views, pool, H, G, q, out, SCALE, n, ws)
+    times = laps + (np.arange(2 * P) < extra)
+    PU.check_attention(PU.to_np64(out[0]), PU.to_np64(q[0]), K, V, deg * times, SCALE, "bf16", "2^31 tokens")
