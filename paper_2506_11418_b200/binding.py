@@ -567,7 +567,7 @@ class QuantPool:
                    torch.zeros((n_pages, H, page_tokens), dtype=torch.float32, device=device))
 
     def c(self):
-        """(ckv_quant_pool, n_pages, H, page_tokens), checked."""
+        """(ckv_quant_pool, n_pages, H, page_tokens), checked; all tensors are on k_codes' device."""
         kc, vc, ks, vs, deg, logdeg = self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.deg_pages, self.logdeg_pages
         n, H, P, width = kc.shape
         per_row = 4 * n * H * P
@@ -575,18 +575,19 @@ class QuantPool:
         assert ks.nbytes == vs.nbytes == per_row and ks.is_contiguous() and vs.is_contiguous(), "scales"
         assert deg is None or deg.dtype is _i32 and deg.nbytes == per_row and deg.is_contiguous(), "degree pages"
         assert logdeg is None or logdeg.dtype is _f32 and logdeg.nbytes == per_row and logdeg.is_contiguous(), "log-degree pages"
+        dev = kc.get_device()
+        if not (dev == vc.get_device() == ks.get_device() == vs.get_device() and (deg is None or deg.get_device() == dev) and
+                (logdeg is None or logdeg.get_device() == dev)):
+            raise ValueError("the pool's tensors are on different devices")
         return _POOL.pack(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), 0 if deg is None else deg.data_ptr(),
                           0 if logdeg is None else logdeg.data_ptr()), n, H, P
-
-    def tensors(self):
-        return self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.deg_pages, self.logdeg_pages
 
 
 def pages_quantize(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pool: QuantPool, deg: torch.Tensor | None = None):
     """ckv_pages_quantize on the current stream: k, v [n, H, D] (bf16 or fp32) to the slots of a four-bit pool."""
     cp, n_pages, H, P = pool.c()
     _check(lib.ckv_pages_quantize(_token_rows(slots, k, v, deg, H), slots.data_ptr(), slots.numel(), cp, n_pages, P,
-                                  _stream_for(slots, k, v, deg, *pool.tensors())))
+                                  _stream_for(slots, k, v, deg, pool.k_codes)))
 
 
 def pages_dequantize(block_table: torch.Tensor, length: int, pool: QuantPool, k: torch.Tensor, v: torch.Tensor,
@@ -599,7 +600,7 @@ def pages_dequantize(block_table: torch.Tensor, length: int, pool: QuantPool, k:
     assert deg is None or deg.dtype is _i32 and deg.nbytes == 4 * H * cap and deg.is_contiguous(), "degrees"
     assert logdeg is None or logdeg.dtype is _f32 and logdeg.nbytes == 4 * H * cap and logdeg.is_contiguous(), "log-degrees"
     _check(lib.ckv_pages_dequantize(block_table.data_ptr(), length, cp, P, H, D, _DTYPE_CODES[dt], k.data_ptr(), v.data_ptr(),
-                                    _ptr(deg), _ptr(logdeg), cap, _stream_for(block_table, k, v, deg, logdeg, *pool.tensors())))
+                                    _ptr(deg), _ptr(logdeg), cap, _stream_for(block_table, k, v, deg, logdeg, pool.k_codes)))
 
 
 def decode_quantized_workspace_bytes(Bz, H, G, D, max_len) -> int:
@@ -616,4 +617,4 @@ def decode_attn_quantized(views: torch.Tensor, pool: QuantPool, H: int, G: int, 
     assert views.dtype is _i64 and views.nbytes == 16 * Bz and views.is_contiguous(), "views"
     assert out.dtype is dt and out.numel() == Bz * HG * D and out.is_contiguous(), "out"
     _check(lib.ckv_decode_attn_quantized(views.data_ptr(), cp, P, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(), out.data_ptr(), scale, max_len,
-                                         workspace.data_ptr(), workspace.nbytes, _stream_for(views, q, out, workspace, *pool.tensors())))
+                                         workspace.data_ptr(), workspace.nbytes, _stream_for(views, q, out, workspace, pool.k_codes)))
