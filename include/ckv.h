@@ -366,6 +366,8 @@ int ckv_pages_dequantize(const int32_t* block_table, int64_t len, const ckv_quan
 size_t ckv_decode_quantized_workspace_bytes(int32_t Bz, int32_t H, int32_t G, int32_t D, int64_t max_len);
 
 /* Eq. 3 over four-bit pages: as ckv_decode_attn_paged with the keys and values that the codes stand for.  q, out: bf16.
+ * Scores and sums are fp32, divided by the softmax's denominator at the end: keys have to stay below 2^104 and values below
+ * 2^121 / len in magnitude.  A query's elements are taken exactly, or within 2^-39 of the largest of their row.
  * Bz * H * (max_len + 32) < 2^36 (CKV_ERR_UNSUPPORTED above). */
 int ckv_decode_attn_quantized(const ckv_paged_view* views_dev, const ckv_quant_pool* pool, int32_t page_tokens, int32_t Bz, int32_t H, int32_t G,
                               int32_t D, int32_t dtype, const void* q, void* out, float scale, int64_t max_len, void* workspace,

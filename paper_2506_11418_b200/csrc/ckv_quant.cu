@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
 // ---- ckv_decode_attn_quantized ----------------------------------------------------------------------------------------
 // As the bf16 kernel: every warp walks its own span of a sequence in tiles of 32 tokens through a ring of cp.async copies,
 // scores and outputs on mma.sync (fp16 inputs: e2m1 levels are exact in fp16, and so are the query's elements after the
-// row is scaled by a power of two), softmax online in the exp2 domain, and partials that are joined in the cluster or by
+// row is scaled by a power of two, down to 2^-31 of its largest; smaller ones are off by 2^-39 of it at most), softmax online in the exp2 domain, and partials that are joined in the cluster or by
 // a second kernel.  With four bits per element the issue slots are what counts (a tile's 4480 bytes take 192 cycles of an
 // SM's share of the measured bandwidth), so unpacking and scaling are arranged to cost as few instructions as they can:
 //   S   S^T = K Q^T: tokens fill the 16 rows of the A operand and up to eight heads the columns of B, so no row is padding.  A
@@ -232,8 +232,9 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
 //       per token, head and group in place of 32 products with the scale), two heads per instruction
 //   O   V's scale belongs to a token and a group, as the weight p belongs to a token: the weight of token t in group j is
 //       p_t 2^e_tj, one B operand per group, turned from S^T's layout by movmatrix.  It goes to fp16 times a power of two F
-//       that is the head's and the group's own and follows the largest such weight so far, so that whatever the scales are
-//       the tokens that matter keep 11 bits: weights from 2^-21 of the largest on, and below that 2^-32 of the largest.
+//       that is the head's and the group's own and follows the largest such weight so far, so that however far the scales lie
+//       apart the tokens that matter keep 11 bits: weights from 2^-21 of the largest on, and below that 2^-32 of the largest.
+//       Sums are fp32 and divided last: p goes up to 2^6, so 2^6 times the tokens times the largest value has to stay in range.
 //   m   the softmax's reference and F move only when a tile needs it (an exponent above 6, a weight that would pass 2^15):
 //       after a sequence's first tiles that is rare, and the accumulators are left alone.
 //   e   lanes share tokens: each tile's 256 scales are converted once, one token per lane, and read back as fp32 (doubled in

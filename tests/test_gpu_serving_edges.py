@@ -10,7 +10,8 @@ import torch
 
 import parity_util as PU
 from paper_2506_11418_b200 import synth
-from test_gpu_serving import D, DEV, I32, I64, SCALE, blocks, lib, paged_batch, quant_batch, select_case, select_plain, summaries_plain
+from test_gpu_serving import (D, DEV, I32, I64, SCALE, blocks, lib, paged_batch, quant_attention, quant_batch, select_case, select_plain,
+                              summaries_plain)
 
 pytestmark = pytest.mark.gpu
 
@@ -211,3 +212,20 @@ def test_quantized_attention_past_2_to_the_31_tokens():
     b.decode_attn_quantized(views, pool, H, G, q, out, SCALE, n, ws)
     times = laps + (np.arange(2 * P) < extra)
     PU.check_attention(PU.to_np64(out[0]), PU.to_np64(q[0]), K, V, deg * times, SCALE, "bf16", "2^31 tokens")
+
+
+@pytest.mark.parametrize("Bz", [1, 12])
+def test_quantized_attention_at_the_ends_of_its_range(Bz):
+    """Values up to 2^121 / len, keys up to 2^104, through one cluster per pair and through shares; log-degrees up to log 7."""
+    H, G, n = 8, 4, 1000
+
+    def largest(x, top):  # the largest magnitude becomes 0.99 top, the others follow
+        x *= 0.99 * top / x.abs().max()
+    quant_attention([n, 37] * Bz, H, G, 64, seed=81, v_change=lambda V: largest(V, 2.0 ** 121 / n))
+
+    def rising(V):
+        V *= torch.exp2(torch.linspace(-60, 0, V.shape[1], device=DEV))[None, :, None]
+        largest(V, 2.0 ** 121 / n)
+    quant_attention([n, 37] * Bz, H, G, 64, seed=82, v_change=rising, deg_top=1)
+    # the keys' largest are 15 or so: within a factor of two or three of 2^104; queries that bring the scores back
+    quant_attention([n, 37] * Bz, H, G, 64, seed=83, k_scale=2.0 ** 99, q_change=lambda q: q.mul_(2.0 ** -99))
