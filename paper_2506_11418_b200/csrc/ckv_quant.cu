@@ -212,13 +212,16 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
     store8<F32>(a.k, vec, lane16, i < a.len, kc[u], scale_value((ks[u] >> (8 * j)) & 255u));
     store8<F32>(a.v, vec, lane16, i < a.len, vc[u], scale_value((vs[u] >> (8 * j)) & 255u));
   }
-  if (a.deg || a.logdeg)
+  if (!a.deg && a.logdeg && a.pool.logdeg_pages && !a.pool.deg_pages) {  // known by their logarithms only
+    for (int64_t i = i0 + threadIdx.x; i < min(a.len, i0 + kRows * U); i += blockDim.x)
+      a.logdeg[(int64_t)h * a.cap + i] = a.pool.logdeg_pages[(((int64_t)a.table[i >> a.shift] * a.H + h) << a.shift) + (i & mask)];
+  } else if (a.deg || a.logdeg) {
     for (int64_t i = i0 + threadIdx.x; i < min(a.len, i0 + kRows * U); i += blockDim.x) {
-      const int64_t row = (((int64_t)a.table[i >> a.shift] * a.H + h) << a.shift) + (i & mask);
-      const int dg = a.pool.deg_pages ? a.pool.deg_pages[row] : 1;
+      const int dg = a.pool.deg_pages ? a.pool.deg_pages[(((int64_t)a.table[i >> a.shift] * a.H + h) << a.shift) + (i & mask)] : 1;
       if (a.deg) a.deg[(int64_t)h * a.cap + i] = dg;
-      if (a.logdeg) a.logdeg[(int64_t)h * a.cap + i] = a.pool.deg_pages || !a.pool.logdeg_pages ? logf((float)dg) : a.pool.logdeg_pages[row];
+      if (a.logdeg) a.logdeg[(int64_t)h * a.cap + i] = logf((float)dg);
     }
+  }
 }
 
 // ---- ckv_decode_attn_quantized ----------------------------------------------------------------------------------------
