@@ -28,7 +28,8 @@ constexpr int kCodeBytes = 64, kScaleBytes = 4;  // per row
 // Half a warp per row, eight elements per lane; a group is four lanes.  Shared exponent = floor(log2 of the group's largest
 // magnitude) - 2, so that the largest element lies in [4, 8) steps and codes end at 6; elements round to the nearest code,
 // ties to the even one.  A group with an element that is not finite becomes NaN as a whole (scale 255, codes 0).  32749 tokens
-// x 8 heads of bf16: 32 us = 0.83 of the measured bandwidth, and 30 us (0.87) back; of fp32: 47 us (1.0) and 49 us (0.97).
+// x 8 heads of bf16, from a graph: 34 us = 0.79 of the measured bandwidth, and 33 us (0.81) back; of fp32: 47 us (1.0) and 50.5
+// us (0.93).
 
 // a lane's eight elements as they lie in memory
 template <bool F32>
@@ -244,8 +245,10 @@ __global__ void __launch_bounds__(kQuantThreads) pages_dequantize_kernel(const D
 //       registers; kept doubled in shared memory they cost 73 us below, in place of 71)
 //   V   two tokens' codes are interleaved by nibble before they are unpacked, which gives the operand's pairs of
 //       neighbouring tokens without permuting fp16 values.
-// Batch 32, 4097 .. 16384 tokens, 8 KV heads of 4 query heads: 71 us = 0.77 of the measured bandwidth.  About 580 instructions per
-// tile at 2.4 per cycle and SM, 128 of them cvt on the half-rate ALU pipe: that pipe is 57 % busy, the tensor pipe 25 %.
+// Batch 32, 4097 .. 16384 tokens, 8 KV heads of 4 query heads: 71 us = 0.77 of the measured bandwidth at an SM clock of 1965 MHz;
+// in a long loop the power limit takes the clock to 1740, and a call 80 us.  With 8 query heads: 77 us.  About 580 instructions per
+// tile at 2.4 per cycle and SM, 128 of them cvt on the half-rate ALU pipe: that pipe is 57 % busy, the tensor pipe 25 %, and four
+// warps per scheduler leave the rest to latency.
 constexpr int kQT = 32;  // tokens per tile
 constexpr int kQShareWarps = 16, kQShareStages = 2;      // the launch by shares: one CTA per SM, 128 registers per thread
 constexpr int kQClusterWarps = 8, kQClusterStages = 3;   // the launch by clusters

@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kSumThreads) pages_summarize_kernel(const Summ
 //     in 64 bits and the k-th is found digit by digit.
 //  4. The chosen blocks are written in ascending order.
 // Bound by the latency of these steps: 12.4 us for 256 (sequence, head) pairs of up to 1024 pages (23 MB of summaries: 3.6 us),
-// 9.0 us for 8 pairs of 2048 pages (scores 2.9, interval 1.6, border 2.5, order 1.3); with all scores in 64 bits the former
+// 16.8 us when the summaries are not in the L2; 9.0 us (11.1) for 8 pairs of 2048 pages (scores 2.9, interval 1.6, border 2.5, order 1.3); with all scores in 64 bits the former
 // took 47 us.
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
