@@ -311,7 +311,7 @@ int ckv_pages_write(const ckv_token_rows* rows, const int64_t* slots, int64_t n,
  * block's tokens that the sequence holds.  A step that appends tokens or drops them from the end passes the lengths before it:
  * of a sequence that is now shorter than from_lens[b] the last block is summarised anew.  A sequence whose rows were
  * rewritten (compressed, clustered) passes 0.  deg_pages NULL = all ones.  max_blocks (host): an upper bound on the blocks
- * that any sequence has from there on; blocks past it are not summarised.  bf16 pages. */
+ * that any sequence has from there on (a shorter one: one); blocks past it are not summarised.  bf16 pages. */
 int ckv_pages_summarize(const ckv_paged_view* views_dev, const int64_t* from_lens, int32_t Bz, const void* k_pages, const int32_t* deg_pages,
                         int32_t page_tokens, int32_t H, int32_t D, int32_t dtype, int64_t max_blocks, void* c_pages, float* clog_pages,
                         void* cuda_stream);
