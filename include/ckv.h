@@ -373,6 +373,34 @@ int ckv_decode_attn_quantized(const ckv_paged_view* views_dev, const ckv_quant_p
                               int32_t D, int32_t dtype, const void* q, void* out, float scale, int64_t max_len, void* workspace,
                               size_t workspace_bytes, void* cuda_stream);
 
+/* ---- Attention of a chunk of new tokens --------------------------------------------------------------------------------
+ * A prompt that is fed in chunks, speculative tokens to be verified, a scheduler's step that mixes chunks with single tokens:
+ * sequence b has n_b >= 0 new tokens, whose queries are the rows q_begin[b] .. q_begin[b + 1] - 1 of q and whose keys and
+ * values are already in its pages, in its last slots (ckv_pages_write, ckv_pages_quantize).  New token i stands at slot
+ * p = views_dev[b].len - n_b + i and attends to slots 0 .. p (Eq. 3, causal among the new tokens):
+ *   out = softmax_{t <= p}(q k_t * scale + log N_t) v_t.
+ * A token that has no slot to attend to (p < 0) gets zeros.  q_begin [Bz + 1] (device) ascends within 0 .. n_rows;
+ * ckv_pages_resize writes it as slot_begin, with the views.  Rows of out that belong to no sequence are left as they were.
+ * Element d of row i and query head j is at q[i * q_row_stride + j * q_head_stride + d] (in elements: a slice of a fused
+ * projection fits; rows 16-byte aligned); out: [n_rows, H*G, D].  Query head j reads KV head j / G; G <= 8, H <= 8192.
+ * The values of slots that a token does not attend to may be anything but count as finite where another new token of the
+ * sequence attends to them (a slot's infinity or NaN times a weight of zero): slots behind a sequence's last are never read
+ * into a sum.  A call's workspace starts with a status word for ckv_workspace_status, as those of the compress calls. */
+
+/* Host-only: workspace bytes of the two calls (partials of rows whose slots several thread blocks share). */
+size_t ckv_extend_workspace_bytes(int64_t n_rows, int32_t H, int32_t G, int32_t D);
+
+/* bf16 pages [n_pages, H, page_tokens, D], logdeg_pages NULL = all degrees one. */
+int ckv_extend_attn_paged(const ckv_paged_view* views_dev, const int64_t* q_begin, int64_t n_rows, const void* k_pages, const void* v_pages,
+                          const float* logdeg_pages, int64_t n_pages, int32_t page_tokens, int32_t Bz, int32_t H, int32_t G, int32_t D,
+                          int32_t dtype, const void* q, int64_t q_row_stride, int64_t q_head_stride, void* out, float scale, void* workspace,
+                          size_t workspace_bytes, void* cuda_stream);
+
+/* Four-bit pages; q, out: bf16. */
+int ckv_extend_attn_quantized(const ckv_paged_view* views_dev, const int64_t* q_begin, int64_t n_rows, const ckv_quant_pool* pool, int64_t n_pages,
+                              int32_t page_tokens, int32_t Bz, int32_t H, int32_t G, int32_t D, int32_t dtype, const void* q, int64_t q_row_stride,
+                              int64_t q_head_stride, void* out, float scale, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* ckv_decode_attn for callers that cannot hand over a workspace because they cannot allocate device
  * memory at the point of the call: code running inside a serving engine's steady-state loop whose memory
  * pool is frozen after start-up, a plug-in that is given only its input and output tensors, or a host

@@ -25,7 +25,7 @@ EXPORTS = ["ckv_compress_plan", "ckv_workspace_bytes", "ckv_compress_prefill", "
            "ckv_pages_scatter", "ckv_pages_plan", "ckv_paged_workspace_bytes", "ckv_compress_paged",
            "ckv_decode_append_attn_paged", "ckv_pages_resize", "ckv_pages_write", "ckv_pages_summarize", "ckv_pages_select",
            "ckv_decode_attn_selected", "ckv_pages_quantize", "ckv_pages_dequantize", "ckv_decode_quantized_workspace_bytes",
-           "ckv_decode_attn_quantized"]
+           "ckv_decode_attn_quantized", "ckv_extend_workspace_bytes", "ckv_extend_attn_paged", "ckv_extend_attn_quantized"]
 
 RESIZE_OK, RESIZE_NO_PAGES, RESIZE_TABLE_FULL, RESIZE_SLOTS_FULL, RESIZE_INCONSISTENT = range(5)   # device status of pages_resize
 
@@ -129,11 +129,15 @@ def _load():
             "ckv_decode_attn_selected": [p, p, p, p, i32, p, i32, i32, i32, i32, i32, i32, p, p, f32, p],
             "ckv_pages_quantize": [p, p, i64, p, i64, i32, p],
             "ckv_pages_dequantize": [p, i64, p, i32, i32, i32, i32, p, p, p, p, i64, p],
-            "ckv_decode_attn_quantized": [p, p, i32, i32, i32, i32, i32, i32, p, p, f32, i64, p, C.c_size_t, p]}.items():
+            "ckv_decode_attn_quantized": [p, p, i32, i32, i32, i32, i32, i32, p, p, f32, i64, p, C.c_size_t, p],
+            "ckv_extend_attn_paged": [p, p, i64, p, p, p, i64, i32, i32, i32, i32, i32, i32, p, i64, i64, p, f32, p, C.c_size_t, p],
+            "ckv_extend_attn_quantized": [p, p, i64, p, i64, i32, i32, i32, i32, i32, i32, p, i64, i64, p, f32, p, C.c_size_t, p]}.items():
         getattr(lib, name).restype = C.c_int
         getattr(lib, name).argtypes = args
     lib.ckv_decode_quantized_workspace_bytes.restype = C.c_size_t
     lib.ckv_decode_quantized_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
+    lib.ckv_extend_workspace_bytes.restype = C.c_size_t
+    lib.ckv_extend_workspace_bytes.argtypes = [i64, i32, i32, i32]
     return lib
 
 
@@ -618,3 +622,46 @@ def decode_attn_quantized(views: torch.Tensor, pool: QuantPool, H: int, G: int, 
     assert out.dtype is dt and out.numel() == Bz * HG * D and out.is_contiguous(), "out"
     _check(lib.ckv_decode_attn_quantized(views.data_ptr(), cp, P, Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(), out.data_ptr(), scale, max_len,
                                          workspace.data_ptr(), workspace.nbytes, _stream_for(views, q, out, workspace, pool.k_codes)))
+
+
+# ---- attention of a chunk of new tokens: queries q [n_rows, H*G, D] (rows of any strides), sequence b's are q_begin[b] .. q_begin[b + 1] - 1
+
+def extend_workspace_bytes(n_rows: int, H: int, G: int, D: int) -> int:
+    return lib.ckv_extend_workspace_bytes(n_rows, H, G, D)
+
+
+def _extend_rows(views, q_begin, H, G, q, out):
+    (n, HG, D), (row, head, one) = q.shape, q.stride()
+    Bz = views.numel() // 2
+    assert HG == H * G and one == 1, "queries"
+    assert views.dtype is _i64 and views.is_contiguous(), "views"
+    assert q_begin.dtype is _i64 and q_begin.nbytes == 8 * (Bz + 1) and q_begin.is_contiguous(), "q_begin"
+    assert out.dtype is q.dtype and out.shape == q.shape and out.is_contiguous(), "out"
+    return n, D, Bz, row, head
+
+
+def extend_attn_paged(views: torch.Tensor, q_begin: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, logdeg_pages: torch.Tensor | None,
+                      H: int, G: int, q: torch.Tensor, out: torch.Tensor, scale: float, workspace: torch.Tensor):
+    """ckv_extend_attn_paged on the current stream: every sequence's new tokens, which are its last ones, attend to its slots up
+    to their own."""
+    n_pages, heads, P, width = k_pages.shape
+    n, D, Bz, row, head = _extend_rows(views, q_begin, H, G, q, out)
+    dt = q.dtype
+    assert heads == H and width == D and k_pages.dtype is v_pages.dtype is dt, "pages"
+    assert k_pages.nbytes == v_pages.nbytes and k_pages.is_contiguous() and v_pages.is_contiguous(), "pages"
+    assert logdeg_pages is None or logdeg_pages.dtype is _f32 and logdeg_pages.nbytes == 4 * n_pages * H * P, "log-degree pages"
+    assert logdeg_pages is None or logdeg_pages.is_contiguous(), "log-degree pages"
+    _check(lib.ckv_extend_attn_paged(views.data_ptr(), q_begin.data_ptr(), n, k_pages.data_ptr(), v_pages.data_ptr(), _ptr(logdeg_pages), n_pages, P,
+                                     Bz, H, G, D, _DTYPE_CODES[dt], q.data_ptr(), row, head, out.data_ptr(), scale, workspace.data_ptr(),
+                                     workspace.nbytes, _stream_for(views, q_begin, k_pages, v_pages, logdeg_pages, q, out, workspace)))
+
+
+def extend_attn_quantized(views: torch.Tensor, q_begin: torch.Tensor, pool: QuantPool, H: int, G: int, q: torch.Tensor, out: torch.Tensor,
+                          scale: float, workspace: torch.Tensor):
+    """ckv_extend_attn_quantized on the current stream: the same over four-bit pages."""
+    cp, n_pages, heads, P = pool.c()
+    n, D, Bz, row, head = _extend_rows(views, q_begin, H, G, q, out)
+    assert heads == H, "pages"
+    _check(lib.ckv_extend_attn_quantized(views.data_ptr(), q_begin.data_ptr(), n, cp, n_pages, P, Bz, H, G, D, _DTYPE_CODES[q.dtype], q.data_ptr(),
+                                         row, head, out.data_ptr(), scale, workspace.data_ptr(), workspace.nbytes,
+                                         _stream_for(views, q_begin, q, out, workspace, pool.k_codes)))
