@@ -1,4 +1,31 @@
 // Attention of a chunk of new tokens over a paged cache (bf16 or four-bit pages): ckv_extend_attn_paged, ckv_extend_attn_quantized.
+//
+// Rows.  The new tokens of a sequence and the G query heads of one KV head are the rows of one problem: row r of a tile is token
+// r / G, head r % G, T = 128 / G tokens in a tile of 128 rows, so every key and value that is fetched serves all of them.  An
+// item is two tiles of consecutive tokens of one (sequence, KV head) and the slots that the last of them sees.
+//
+// One CTA per SM, persistent.  S = Q K^T and O += P V run on tcgen05.mma (128 x 128 x 16, operands in shared memory with the
+// 128-byte swizzle, P read from tensor memory), slots in steps of 128:
+//   warps 0-3, 4-7  softmax of tile 0 and of tile 1, a row per thread: S from tensor memory, y = s * scale + log n, weights
+//                   exp(y - m) to bf16 over S's place, their sum in fp32 registers.  m is the largest y when the tile's rows began,
+//                   and moves (the row of O is then scaled in tensor memory) only when a later y exceeds it by more than
+//                   kSlack, so that O is rarely touched; weights stay below e^kSlack.
+//   warp 8          TMA: the item's queries, and keys, values and log-degrees through a ring of four 32 KB stages
+//   warp 9          issues the MMAs: PV of one tile and the next QK^T of it while the other tile's softmax runs
+// Tensor memory: S0 | S1 | O0 | O1, 128 columns each, all 512.
+// An item with one tile only (single tokens, short chunks) uses the second set for every other step of slots: two softmax
+// states of the same rows, joined at the end.  Otherwise such an item would wait for its softmax at every step.
+//
+// Sharing the work.  All items' lengths (slots + kItemCost each) are laid end to end, in the order (sequence, KV head, tile
+// pair), and every CTA takes an equal stretch, wherever it begins and ends, so a ragged batch, few rows over a long cache and
+// many rows are all balanced to a step.  Each CTA finds its stretch by itself from lengths on the device: the sum over a sequence's
+// items is an arithmetic series.  A piece that is not a whole item leaves (O, m, sum) in the workspace, and extend_join_kernel
+// joins them, in order, so results do not depend on timing.
+//
+// Waits are bounded; one that gives up sets the status word at the start of the workspace, and the other roles follow.
+#include <cuda.h>
+#include <cuda_fp16.h>
+
 #include <algorithm>
 
 #include "../../include/ckv.h"
@@ -7,27 +34,790 @@
 #include "ckv_internal.h"
 #include "ckv_ptx.cuh"
 
-#include <cuda_fp16.h>
-
 namespace ckv {
 namespace {
 
-constexpr int kED = 128;
+using namespace ptx;
+
+constexpr int kED = 128;            // head_dim
+constexpr int kEN = 128;            // slots per step; rows per tile
+constexpr int kEStages = 4;         // K and V tiles in flight
+constexpr int kETile = kEN * kED * 2;
+constexpr int kEHalf = kETile / 2;  // 64 columns of a tile: 128 rows of 128 bytes
+constexpr int kEBiasSlots = 4;
+constexpr int kEWarps = 12;         // (the last two only complete the warpgroup that gives its registers away)
+constexpr int kESoftmaxRegs = 216, kEOtherRegs = 72;  // two warps of the first and one of the second on each quarter of an SM: 3 x 168, as launched
+constexpr int kEThreads = kEWarps * 32;
+constexpr int kItemCost = 128;      // what an item costs beside its slots (queries in, rows out), in slots
+constexpr int kMinShare = 512;      // slots that a CTA takes at least
+constexpr float kSlack = 5.5f;      // weights below e^5.5 = 245
+constexpr int kPartRow = 132;       // floats of a partial row: O, m, sum, pad
+// shared memory, from a 1024-byte boundary
+constexpr int oQ = 0;
+constexpr int oRing = oQ + 2 * kETile;
+constexpr int oBias = oRing + kEStages * kETile;
+constexpr int oState = oBias + kEBiasSlots * kEN * 4;  // float2 [256]: m and sum of every row, exchanged by one-tile items
+constexpr int oBar = oState + 256 * 8;
+constexpr int oMisc = oBar + 256;
+constexpr int kEBytes = oMisc + 256;
 
 struct ExtendArgs {
   const ckv_paged_view* views;
   const int64_t* q_begin;
-  const __nv_bfloat16* q;
   __nv_bfloat16* out;
-  const __nv_bfloat16* k_pages;
-  const __nv_bfloat16* v_pages;
   ckv_quant_pool pool;
   const float* logdeg;
-  int64_t n_rows, q_row, q_head;  // strides in elements
-  int32_t Bz, H, G, shift;
+  int64_t n_rows, max_slots;
+  int32_t Bz, H, G, T, shift;
   float scale;
-  int32_t* status;
+  int32_t* status;      // workspace: status word | pieces [CTAs] | partial rows
+  struct ExtendPiece* pieces;
+  float* partial;       // [2 CTAs][slot_rows][kPartRow]
+  int32_t slot_rows;
 };
+
+// What the joining kernel needs to know of a CTA's stretch.  Slot 1 of a CTA holds a piece of the item that begins in its
+// stretch and does not end there, slot 0 one of the item that began in an earlier CTA's.
+struct ExtendPiece {
+  int64_t row0;      // the item that this CTA ends and did not begin: its first row of q,
+  int32_t h, ntok;   // KV head, tokens (0: there is none),
+  int32_t first;     // and the CTA that began it
+  int32_t held[2];   // whether the slots hold something
+};
+
+// One sequence's part of the work
+struct ExtendSeq {
+  int64_t row0;   // first of its rows of q
+  int32_t n;      // new tokens
+  int32_t len;    // slots
+  __device__ __forceinline__ int items(int T2) const { return (n + T2 - 1) / T2; }
+  // slots that item j's last token sees
+  __device__ __forceinline__ int end(int j, int T2) const { return max(0, len - n + min((j + 1) * T2, n)); }
+  // cost of items 0 .. m - 1 of one head
+  __device__ __forceinline__ int64_t before(int m, int T2) const {
+    const int base = len - n, last = items(T2) - 1;
+    const int j0 = base >= 0 ? 0 : -base / T2, e = max(min(m, last), j0);
+    int64_t c = (int64_t)m * kItemCost + (int64_t)(e - j0) * base + (int64_t)T2 * (((int64_t)e * (e + 1) - (int64_t)j0 * (j0 + 1)) / 2);
+    if (m > last) c += len;
+    return c;
+  }
+};
+
+__device__ __forceinline__ ExtendSeq extend_seq(const ExtendArgs& a, int b) {
+  ExtendSeq s;
+  const int64_t r0 = min(max(a.q_begin[b], (int64_t)0), a.n_rows), r1 = min(max(a.q_begin[b + 1], r0), a.n_rows);
+  s.row0 = r0;
+  s.n = (int32_t)(r1 - r0);
+  s.len = (int32_t)min(max(a.views[b].len, (int64_t)0), a.max_slots);
+  return s;
+}
+
+// A piece of an item: steps lo .. hi - 1 of its slots
+struct Piece {
+  int64_t row0;   // first row of q
+  int b, h, ntok;
+  int base;       // slot at which the item's first token stands
+  int end;        // slots that its last token sees
+  int lo, hi, steps;
+  bool one;       // one tile of rows
+  bool whole;
+  bool first;      // the item begins in this stretch
+};
+
+// A CTA's stretch, piece by piece.  Every warp walks it for itself.
+struct Walk {
+  int64_t left, x;  // what is left of the stretch; offset in the item
+  ExtendSeq s;
+  int b, h, j;
+  __device__ __forceinline__ bool next(const ExtendArgs& a, Piece& p) {
+    const int T2 = 2 * a.T;
+    while (left > 0) {
+      const int end = s.end(j, T2), steps = (end + kEN - 1) / kEN;
+      const int64_t cost = (int64_t)end + kItemCost, to = min(x + left, cost);
+      auto step_of = [&](int64_t y) { return (int)min(max(y - kItemCost + kEN / 2, (int64_t)0) / kEN, (int64_t)steps); };
+      p.lo = step_of(x);
+      const bool ends = to == cost;
+      p.hi = ends ? steps : step_of(to);
+      p.first = x == 0;
+      p.row0 = s.row0 + (int64_t)j * T2;
+      p.b = b; p.h = h;
+      p.ntok = min(T2, s.n - j * T2);
+      p.base = s.len - s.n + j * T2;
+      p.end = end;
+      p.steps = steps;
+      p.one = p.ntok <= a.T;
+      p.whole = p.lo == 0 && p.hi == steps;
+      left -= to - x;
+      x = to;
+      if (ends) {
+        x = 0;
+        if (++j >= s.items(T2)) {
+          j = 0;
+          if (++h == a.H) {
+            h = 0;
+            s.n = 0;
+            while (left > 0 && s.n == 0) {  // (what is left belongs to a later sequence)
+              if (++b < a.Bz)
+                s = extend_seq(a, b);
+              else
+                left = 0;
+            }
+          }
+        }
+      }
+      if (p.lo < p.hi || (steps == 0 && ends)) return true;
+    }
+    return false;
+  }
+};
+
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+// D[tmem] (+)= A[tmem] * B[smem desc]
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+      "%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// 32 columns, and the wait with the registers as operands (so that no use moves above it)
+__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+      "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
+                 "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
+                 "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+struct f32x2 {
+  uint64_t v;
+  __device__ __forceinline__ f32x2() {}
+  __device__ __forceinline__ f32x2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+  return d;
+}
+
+// tcgen05 instruction descriptors: bf16 x bf16 -> fp32, M = N = 128; B K-major (keys) or N-major (values)
+constexpr uint32_t kDescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+constexpr uint32_t kDescPV = kDescQK | (1u << 16);
+
+template <int N>
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// A warp's wait: false if any lane gave up
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); }
+
+__global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                                                              const __grid_constant__ CUtensorMap tm_v, const ExtendArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t s0 = smem_u32(smem);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // barriers: full [stage] | empty [stage] | bias full, empty [slot] | S full [tile] | P full [tile] | O full [tile] | Q full, empty | exchange 2
+  auto bar = [&](int i) { return s0 + oBar + 8u * i; };
+  auto b_full = [&](int i) { return bar(i); };
+  auto b_empty = [&](int i) { return bar(kEStages + i); };
+  auto b_bias = [&](int i) { return bar(2 * kEStages + i); };
+  auto b_bias_free = [&](int i) { return bar(2 * kEStages + kEBiasSlots + i); };
+  constexpr int kRest = 2 * kEStages + 2 * kEBiasSlots;
+  auto b_s = [&](int g) { return bar(kRest + g); };
+  auto b_p = [&](int g) { return bar(kRest + 2 + g); };
+  auto b_o = [&](int g) { return bar(kRest + 4 + g); };
+  const uint32_t b_q = bar(kRest + 6), b_q_free = bar(kRest + 7), b_x = bar(kRest + 8);
+  int64_t* const s_start = reinterpret_cast<int64_t*>(smem + oMisc);            // begin of the stretch in its sequence, left, sequence
+  int64_t* const s_sum = reinterpret_cast<int64_t*>(smem + oState);             // (before the roles begin)
+  volatile uint32_t* const s_tmem = reinterpret_cast<volatile uint32_t*>(smem + oMisc + 64);
+
+  if (tid == 0) {
+    for (int i = 0; i < kEStages; ++i) {
+      mbar_init(b_full(i), 1);
+      mbar_init(b_empty(i), 1);
+    }
+    for (int i = 0; i < kEBiasSlots; ++i) {
+      mbar_init(b_bias(i), 1);
+      mbar_init(b_bias_free(i), 8);
+    }
+    for (int g = 0; g < 2; ++g) {
+      mbar_init(b_s(g), 1);
+      mbar_init(b_p(g), 4);
+      mbar_init(b_o(g), 1);
+    }
+    mbar_init(b_q, 1);
+    mbar_init(b_q_free, 1);
+    mbar_init(b_x, 8);
+    mbar_init_fence();
+    s_start[0] = -1;
+  }
+  griddep_wait();
+  griddep_launch();
+  if (blockIdx.x == 0 && tid == 0) *a.status = 0;
+  const int T2 = 2 * a.T;
+
+  // this CTA's stretch: every thread sums a run of sequences
+  const int per = (a.Bz + kEThreads - 1) / kEThreads, q0 = min(a.Bz, tid * per), q1 = min(a.Bz, q0 + per);
+  int64_t mine = 0;
+  for (int b = q0; b < q1; ++b) {
+    const ExtendSeq s = extend_seq(a, b);
+    if (s.n > 0) mine += s.before(s.items(T2), T2) * a.H;
+  }
+  int64_t upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 31) s_sum[warp] = upto;
+  __syncthreads();
+  int64_t total = 0, at = upto - mine;
+  for (int w = 0; w < kEWarps; ++w) {
+    if (w < warp) at += s_sum[w];
+    total += s_sum[w];
+  }
+  const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kMinShare), begin = share * blockIdx.x;
+  if (begin < total && begin >= at && begin < at + mine) {
+    for (int b = q0; b < q1; ++b) {
+      const ExtendSeq s = extend_seq(a, b);
+      if (s.n == 0) continue;
+      const int64_t c = s.before(s.items(T2), T2) * a.H;
+      if (begin < at + c) {
+        s_start[0] = begin - at;
+        s_start[1] = b;
+        break;
+      }
+      at += c;
+    }
+  }
+  __syncthreads();
+  const int64_t offset = s_start[0];
+  ExtendPiece* const mark = a.pieces + blockIdx.x;
+  if (offset < 0) {  // no work
+    if (tid == 0) *mark = ExtendPiece{0, 0, 0, 0, {0, 0}};
+    return;
+  }
+  Walk walk;
+  walk.b = (int)s_start[1];
+  walk.s = extend_seq(a, walk.b);
+  walk.left = min(share, total - begin);
+  {
+    const int items = walk.s.items(T2);
+    const int64_t head = walk.s.before(items, T2);
+    walk.h = (int)(offset / head);
+    const int64_t in_head = offset - walk.h * head;
+    int lo = 0, hi = items;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (walk.s.before(mid, T2) <= in_head) lo = mid; else hi = mid;
+    }
+    walk.j = lo;
+    walk.x = in_head - walk.s.before(lo, T2);
+  }
+  const int64_t item_begin = begin - walk.x;  // of the item in which the stretch begins, on the line of all items
+
+  if (warp == 9) tmem_alloc(s0 + oMisc + 64, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *s_tmem;
+  bool ok = true;
+  Piece p;
+
+  if (warp >= 8) {
+  give_registers<kEOtherRegs>();
+  if (warp == 8) {
+    // ---------------------------------------------------------------- TMA
+    const int run = min(kEN, 1 << a.shift), runs = kEN / run;  // slots of a step that lie in one page
+    const int rr = (lane >> 1) % runs, half = lane & 1;
+    int n = 0, np = 0;                                         // steps and pieces so far
+    while (ok && walk.next(a, p)) {
+      if (p.lo >= p.hi) continue;
+      const int32_t* const table = a.views[p.b].block_table;
+      const int n_blocks = (p.end + (1 << a.shift) - 1) >> a.shift;
+      int win = -32;
+      int32_t cur = 0, nxt = 0;
+      if (!(ok = warp_wait(b_q_free, (uint32_t)((np & 1) ^ 1)))) break;
+      ++np;
+      if (lane == 0) {
+        mbar_arrive_expect_tx(b_q, (uint32_t)(4 * a.T * a.G * 128));
+        for (int g = 0; g < 2; ++g)
+          for (int f = 0; f < 2; ++f)
+            tma_load_3d(s0 + oQ + g * kETile + f * kEHalf, &tm_q, 64 * f, p.h * a.G, (int)p.row0 + (p.one ? 0 : g * a.T), b_q);
+      }
+      for (int i = p.lo; i < p.hi; ++i, ++n) {
+        const int t0 = i * kEN, blk0 = t0 >> a.shift;
+        if ((blk0 & ~31) != win) {
+          const bool first = win < 0 || (blk0 & ~31) != win + 32;
+          win = blk0 & ~31;
+          cur = first ? (win + lane < n_blocks ? table[win + lane] : 0) : nxt;
+          nxt = win + 32 + lane < n_blocks ? table[win + 32 + lane] : 0;
+        }
+        const int slot = t0 + rr * run;                        // this lane's run of slots
+        const int page = __shfl_sync(0xffffffffu, cur, (slot >> a.shift) & 31);
+        const int row = ((page * a.H + p.h) << a.shift) + (slot & ((1 << a.shift) - 1));
+        const int live = min(runs, (p.end - t0 + run - 1) / run);  // runs that hold something
+        const bool mine_ = lane < 2 * runs && rr < live;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          const int idx = 2 * n + kv, st = idx % kEStages;
+          if (!(ok = warp_wait(b_empty(st), (uint32_t)(((idx / kEStages) & 1) ^ 1)))) break;
+          if (lane == 0) mbar_arrive_expect_tx(b_full(st), (uint32_t)(live * run * 256));
+          __syncwarp();
+          if (mine_) tma_load_2d(s0 + oRing + st * kETile + half * kEHalf + rr * run * 128, kv ? &tm_v : &tm_k, 64 * half, row, b_full(st));
+          if (kv == 0 && a.logdeg) {
+            const int bs = n % kEBiasSlots;
+            if (!(ok = warp_wait(b_bias_free(bs), (uint32_t)(((n / kEBiasSlots) & 1) ^ 1)))) break;
+            if (lane == 0) mbar_arrive_expect_tx(b_bias(bs), (uint32_t)(live * run * 4));
+            __syncwarp();
+            if (mine_ && half == 0) bulk_load(s0 + oBias + (bs * kEN + rr * run) * 4, a.logdeg + row, run * 4, b_bias(bs));
+          }
+        }
+        if (!ok) break;
+      }
+    }
+  } else if (warp == 9) {
+    // ---------------------------------------------------------------- MMA
+    int n = 0, np = 0, nq[2] = {0, 0};   // steps, pieces, P tiles so far
+    auto qk = [&](int g, int i) {        // S of tile g at the piece's step i, and its arrival
+      const uint32_t kt = s0 + oRing + (uint32_t)((2 * (n + i)) % kEStages) * kETile, qt = s0 + oQ + (uint32_t)g * kETile;
+      if (lane == 0) {
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          const uint32_t off = (uint32_t)(ks >> 2) * kEHalf + (uint32_t)(ks & 3) * 32u;
+          umma_bf16(tmem + (uint32_t)g * 128, umma_desc_sw128(qt + off, 16, 1024), umma_desc_sw128(kt + off, 16, 1024), kDescQK, ks ? 1u : 0u);
+        }
+        umma_commit(b_s(g));
+      }
+    };
+    auto pv = [&](int g, int i, bool more) {
+      const uint32_t vt = s0 + oRing + (uint32_t)((2 * (n + i) + 1) % kEStages) * kETile;
+      if (lane == 0) {
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+          umma_bf16_ts(tmem + 256 + (uint32_t)g * 128, tmem + (uint32_t)g * 128 + 8 * ks, umma_desc_sw128(vt + 2048 * ks, kEHalf, 1024), kDescPV,
+                       (more || ks) ? 1u : 0u);
+      }
+    };
+    auto stage_full = [&](int idx) { return warp_wait(b_full(idx % kEStages), (uint32_t)((idx / kEStages) & 1)); };
+    auto release = [&](int idx) { if (lane == 0) umma_commit(b_empty(idx % kEStages)); };
+    auto p_full = [&](int g) { return warp_wait(b_p(g), (uint32_t)(nq[g]++ & 1)); };
+    while (ok && walk.next(a, p)) {
+      const int steps = p.hi - p.lo;
+      if (steps <= 0) continue;
+      if (!(ok = warp_wait(b_q, (uint32_t)(np++ & 1)))) break;
+      // slots behind the last that the item sees: whatever their values are, they must not meet a weight of zero
+      auto values = [&](int i) {
+        if (!stage_full(2 * (n + i) + 1)) return false;
+        const int seen = p.end - (p.lo + i) * kEN;
+        if (seen < kEN) {
+          const uint32_t vt = s0 + oRing + (uint32_t)((2 * (n + i) + 1) % kEStages) * kETile;
+          for (int c = seen * 8 + lane; c < kEN * 8; c += 32) {
+            st_shared_v4(vt + c * 16, make_uint4(0, 0, 0, 0));
+            st_shared_v4(vt + kEHalf + c * 16, make_uint4(0, 0, 0, 0));
+          }
+          fence_async_smem();
+          __syncwarp();
+        }
+        return true;
+      };
+      tc_fence_after();
+      const int ahead = p.one ? 2 : 1;
+      if (!(ok = stage_full(2 * n))) break;
+      tc_fence_after();
+      qk(0, 0);
+      if (p.one) {
+        release(2 * n);
+        if (steps > 1) {
+          if (!(ok = stage_full(2 * (n + 1)))) break;
+          tc_fence_after();
+          qk(1, 1);
+          release(2 * (n + 1));
+        }
+      } else {
+        qk(1, 0);
+        release(2 * n);
+      }
+      if (steps <= ahead && lane == 0) umma_commit(b_q_free);
+      for (int i = 0; i < steps; ++i) {
+        if (!(ok = values(i))) break;
+        const int g0 = p.one ? i & 1 : 0, g1 = p.one ? g0 : 1;
+        const bool more = i + ahead < steps;
+        for (int g = g0; g <= g1; ++g) {
+          if (!(ok = p_full(g))) break;
+          tc_fence_after();
+          pv(g, i, i >= ahead);
+          if (g == g1) release(2 * (n + i) + 1);
+          if (more) {
+            if (g == g0 && !(ok = stage_full(2 * (n + i + ahead)))) break;
+            tc_fence_after();
+            qk(g, i + ahead);
+            if (g == g1) release(2 * (n + i + ahead));
+          } else if (!p.one && lane == 0) {
+            umma_commit(b_o(g));
+          }
+        }
+        if (!ok) break;
+        if (i + ahead == steps - 1 && lane == 0) umma_commit(b_q_free);
+      }
+      if (!ok) break;
+      if (p.one && lane == 0) {
+        umma_commit(b_o(0));
+        umma_commit(b_o(1));
+      }
+      n += steps;
+    }
+  }
+  } else {
+    // ---------------------------------------------------------------- softmax of tile g, one row per thread
+    take_registers<kESoftmaxRegs>();
+    const int g = warp >> 2, r = tid & 127, tok = r / a.G, head = r - tok * a.G;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // (32 lanes of tensor memory per warp, lane number in the upper half word)
+    const uint32_t t_s = tmem + lanes + (uint32_t)g * 128, t_o = t_s + 256;
+    float2* const state = reinterpret_cast<float2*>(smem + oState);
+    const float scale = a.scale;
+    int n = 0, ns = 0, np = 0, nx = 0;  // steps, own steps, pieces, exchanges so far
+    ExtendPiece note{0, 0, 0, 0, {0, 0}};
+    while (ok && walk.next(a, p)) {
+      const int steps = p.hi - p.lo, my_tok = tok + (p.one ? 0 : g * a.T);
+      const bool valid = tok < a.T && my_tok < p.ntok;
+      const bool busy = __any_sync(0xffffffffu, valid);
+      const int lim = valid ? p.base + my_tok + 1 : 0;  // slots that this row sees
+      const int lim_min = __reduce_min_sync(0xffffffffu, valid ? lim : INT32_MAX);
+      float m = -INFINITY;
+      f32x2 l2(0.f, 0.f);
+      for (int i = 0; i < steps; ++i, ++n) {
+        const int bs = n % kEBiasSlots;
+        const bool own = !p.one || (i & 1) == g;
+        if (a.logdeg && !(ok = warp_wait(b_bias(bs), (uint32_t)((n / kEBiasSlots) & 1)))) break;
+        if (own) {
+          if (!(ok = warp_wait(b_s(g), (uint32_t)(ns++ & 1)))) break;
+          tc_fence_after();
+          if (busy) {
+            uint32_t sv[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32_issue(t_s + 32 * c, sv[c]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld_wait(sv[c]);
+            float y[128];
+            const f32x2 sc(scale, scale);
+            if (a.logdeg) {
+              const ulonglong2* const bias = reinterpret_cast<const ulonglong2*>(smem + oBias + bs * kEN * 4);
+#pragma unroll
+              for (int c = 0; c < 32; ++c) {
+                const ulonglong2 b4 = bias[c];
+                f32x2 lo, hi;
+                lo.v = b4.x;
+                hi.v = b4.y;
+                fma2(f32x2(__uint_as_float(sv[c / 8][4 * c % 32]), __uint_as_float(sv[c / 8][4 * c % 32 + 1])), sc, lo).get(y[4 * c], y[4 * c + 1]);
+                fma2(f32x2(__uint_as_float(sv[c / 8][4 * c % 32 + 2]), __uint_as_float(sv[c / 8][4 * c % 32 + 3])), sc, hi).get(y[4 * c + 2], y[4 * c + 3]);
+              }
+            } else {
+#pragma unroll
+              for (int c = 0; c < 64; ++c)
+                mul2(f32x2(__uint_as_float(sv[c / 16][2 * c % 32]), __uint_as_float(sv[c / 16][2 * c % 32 + 1])), sc).get(y[2 * c], y[2 * c + 1]);
+            }
+            const int seen = lim - (p.lo + i) * kEN;
+            if ((p.lo + i + 1) * kEN > lim_min) {  // (some row of the warp does not see all of the step's slots)
+#pragma unroll
+              for (int c = 0; c < 128; ++c) y[c] = c < seen ? y[c] : -INFINITY;
+            }
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int c = 0; c < 128; c += 8) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], y[c + 2 * k], y[c + 2 * k + 1]);
+            }
+            const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+            if (__any_sync(0xffffffffu, top > m + kSlack)) {
+              const bool up = top > m;
+              const float f = up ? ex2((m - top) * kLog2e) : 1.f;
+              if (__any_sync(0xffffffffu, m > -INFINITY)) {  // O holds something (its last product is complete: S came behind it)
+                for (int c = 0; c < 4; ++c) {
+                  uint32_t o[32];
+                  tmem_ld32_issue(t_o + 32 * c, o);
+                  tmem_ld_wait(o);
+#pragma unroll
+                  for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                  tmem_st32(t_o + 32 * c, o);
+                }
+              }
+              l2 = mul2(l2, f32x2(f, f));
+              m = up ? top : m;
+            }
+            const float mz = m == -INFINITY ? 0.f : m, mL = mz * kLog2e;
+            // (y and m next to the type's ends: y log2 e would overflow, y - m does not)
+            if (__any_sync(0xffffffffu, fabsf(mL) == INFINITY && fabsf(mz) != INFINITY)) {
+#pragma unroll
+              for (int c = 0; c < 128; ++c) y[c] = ex2((y[c] - mz) * kLog2e);
+            } else {
+              const f32x2 le(kLog2e, kLog2e), mm(-mL, -mL);
+#pragma unroll
+              for (int c = 0; c < 128; c += 2) {
+                fma2(f32x2(y[c], y[c + 1]), le, mm).get(y[c], y[c + 1]);
+                y[c] = ex2(y[c]);
+                y[c + 1] = ex2(y[c + 1]);
+              }
+            }
+            f32x2 la(0.f, 0.f), lb(0.f, 0.f);
+            uint32_t pk[2][32];
+#pragma unroll
+            for (int c = 0; c < 128; c += 4) {
+              la = add2(la, f32x2(y[c], y[c + 1]));
+              lb = add2(lb, f32x2(y[c + 2], y[c + 3]));
+              pk[c / 64][c % 64 / 2] = pack_bf16x2(y[c], y[c + 1]);
+              pk[c / 64][c % 64 / 2 + 1] = pack_bf16x2(y[c + 2], y[c + 3]);
+            }
+            tmem_st32(t_s, pk[0]);
+            tmem_st32(t_s + 32, pk[1]);
+            l2 = add2(l2, add2(la, lb));
+            tmem_st_wait();
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b_p(g));
+        }
+        if (a.logdeg && lane == 0) mbar_arrive(b_bias_free(bs));
+      }
+      if (!ok) break;
+      float l;
+      {
+        float x, y;
+        l2.get(x, y);
+        l = x + y;
+      }
+      // ------------------------------------------------------------ rows out
+      if (steps > 0) {
+        if (!(ok = warp_wait(b_o(g), (uint32_t)(np++ & 1)))) break;
+        tc_fence_after();
+      }
+      const int64_t row = p.row0 + my_tok;
+      __nv_bfloat16* const out = a.out + (row * a.H * a.G + p.h * a.G + head) * kED;
+      const int slot = p.first ? 1 : 0;
+      float* const part = a.partial + ((int64_t)(2 * blockIdx.x + slot) * a.slot_rows + my_tok * a.G + head) * kPartRow;
+      float f0 = 1.f, f1 = 0.f;
+      if (p.one && steps > 0) {  // two states of the same rows
+        state[tid] = make_float2(m, l);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_x);
+        if (!(ok = warp_wait(b_x, (uint32_t)(nx++ & 1)))) break;
+        const float2 x0 = state[r], x1 = state[128 + r];
+        m = fmaxf(x0.x, x1.x);
+        f0 = x0.x == -INFINITY ? 0.f : ex2((x0.x - m) * kLog2e);
+        f1 = x1.x == -INFINITY ? 0.f : ex2((x1.x - m) * kLog2e);
+        l = x0.y * f0 + x1.y * f1;
+      }
+      if (busy) {
+        const float inv = !p.whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+        // a one-tile item's columns are shared between the two tiles' warps
+        const int c0 = p.one && steps > 0 ? 2 * g : 0, c1 = p.one && steps > 0 ? c0 + 2 : (p.one && g == 1) ? 0 : 4;
+        for (int c = c0; c < c1; ++c) {
+          float o[32];
+          if (steps > 0) {
+            uint32_t u[32];
+            tmem_ld32_issue((p.one ? tmem + lanes + 256 : t_o) + 32 * c, u);
+            tmem_ld_wait(u);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = f0 == 0.f ? 0.f : __uint_as_float(u[k]) * f0;
+            if (p.one && steps > 1) {
+              tmem_ld32_issue(tmem + lanes + 384 + 32 * c, u);
+              tmem_ld_wait(u);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] += f1 == 0.f ? 0.f : __uint_as_float(u[k]) * f1;
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = 0.f;
+          }
+          if (valid && p.whole) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 8)
+              *reinterpret_cast<uint4*>(out + 32 * c + k) = make_uint4(pack_bf16x2(o[k] * inv, o[k + 1] * inv), pack_bf16x2(o[k + 2] * inv, o[k + 3] * inv),
+                                                                       pack_bf16x2(o[k + 4] * inv, o[k + 5] * inv), pack_bf16x2(o[k + 6] * inv, o[k + 7] * inv));
+          } else if (valid) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(part + 32 * c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          }
+        }
+        if (valid && !p.whole && (!p.one || g == 0)) *reinterpret_cast<float2*>(part + kED) = make_float2(m, l);
+      }
+      if (p.one && steps > 0) {  // nobody goes on to the next piece's products before both have read
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_x);
+        if (!(ok = warp_wait(b_x, (uint32_t)(nx++ & 1)))) break;
+      }
+      if (!p.whole) {
+        note.held[slot] = 1;
+        if (p.lo > 0 && p.hi == p.steps) {
+          note.row0 = p.row0;
+          note.h = p.h;
+          note.ntok = p.ntok;
+          note.first = (int32_t)(item_begin / share);
+        }
+      }
+    }
+    if (tid == 0) *mark = note;
+  }
+  if (!ok) {
+    *a.status = 1;
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);  // copies and products that are still under way
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+// Joins the pieces of the items that CTA blockIdx.x of the kernel above ended and did not begin.  Rows are dealt to gridDim.y CTAs: a warp
+// per row where there are few pieces, else a CTA per row, whose warps share them.
+constexpr int kJoinWarps = 8;
+
+__global__ void __launch_bounds__(kJoinWarps * 32) extend_join_kernel(const ExtendArgs a) {
+  __shared__ float2 s_ml[kJoinWarps];
+  __shared__ float4 s_o[kJoinWarps][32];
+  griddep_wait();
+  griddep_launch();
+  const ExtendPiece last = a.pieces[blockIdx.x];
+  if (last.ntok == 0) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rows = last.ntok * a.G, n = (int)blockIdx.x - last.first + 1;
+  const bool together = n > 8;
+  for (int r = together ? (int)blockIdx.y : (int)blockIdx.y * kJoinWarps + warp; r < rows; r += (int)gridDim.y * (together ? 1 : kJoinWarps)) {
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int p0 = together ? warp : 0, dp = together ? kJoinWarps : 1;
+    for (int p = p0; p < n; p += 4 * dp) {
+      float2 ml[4];
+      float4 y[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int c = last.first + p + u * dp, slot = p + u * dp == 0 ? 1 : 0;
+        ml[u] = make_float2(-INFINITY, 0.f);
+        y[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p + u * dp < n && a.pieces[c].held[slot]) {
+          const float* const at = a.partial + ((int64_t)(2 * c + slot) * a.slot_rows + r) * kPartRow;
+          ml[u] = *reinterpret_cast<const float2*>(at + kED);
+          y[u] = *reinterpret_cast<const float4*>(at + 4 * lane);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float mm = fmaxf(m, ml[u].x);
+        if (mm == -INFINITY && !(ml[u].y != 0.f)) continue;  // (no slots, or only such of weight zero)
+        const float c = m == -INFINITY ? 0.f : exp2f((m - mm) * kLog2e), f = ml[u].x == -INFINITY ? 0.f : exp2f((ml[u].x - mm) * kLog2e);
+        o = make_float4(fmaf(f, y[u].x, o.x * c), fmaf(f, y[u].y, o.y * c), fmaf(f, y[u].z, o.z * c), fmaf(f, y[u].w, o.w * c));
+        l = fmaf(f, ml[u].y, l * c);
+        m = mm;
+      }
+    }
+    if (together) {
+      s_o[warp][lane] = o;
+      if (lane == 0) s_ml[warp] = make_float2(m, l);
+      __syncthreads();
+      if (warp == 0) {
+        m = -INFINITY;
+        for (int w = 0; w < kJoinWarps; ++w) m = fmaxf(m, s_ml[w].x);
+        l = 0.f;
+        o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 0; w < kJoinWarps; ++w) {
+          const float f = s_ml[w].x == -INFINITY ? 0.f : exp2f((s_ml[w].x - m) * kLog2e);
+          const float4 y = s_o[w][lane];
+          l = fmaf(f, s_ml[w].y, l);
+          o = make_float4(fmaf(f, y.x, o.x), fmaf(f, y.y, o.y), fmaf(f, y.z, o.z), fmaf(f, y.w, o.w));
+        }
+      }
+      __syncthreads();
+    }
+    if (!together || warp == 0) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int tok = r / a.G, head = r - tok * a.G;
+      store4(a.out + ((last.row0 + tok) * a.H * a.G + last.h * a.G + head) * kED + 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    }
+  }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn extend_encode_fn() {
+  static const EncodeTiledFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess
+               ? reinterpret_cast<EncodeTiledFn>(p)
+               : nullptr;
+  }();
+  return fn;
+}
+
+bool encode(CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+  const cuuint32_t es[3] = {1, 1, 1};
+  return extend_encode_fn() && extend_encode_fn()(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, es,
+                                                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Sets the kernel's shared memory once per device
+bool extend_ready() {
+  constexpr int kMaxDev = 64;
+  static std::atomic<bool> done[kMaxDev];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDev) return false;
+  if (done[dev].load(std::memory_order_relaxed)) return true;
+  if (cudaFuncSetAttribute(extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEBytes + 1024) != cudaSuccess) return false;
+  done[dev].store(true, std::memory_order_relaxed);
+  return true;
+}
+
+int32_t slot_rows(int64_t n_rows, int32_t G) { return (int32_t)std::min<int64_t>(2 * (kEN / G) * G, n_rows * G); }
+size_t pieces_bytes() { return ((size_t)sm_count() * sizeof(ExtendPiece) + 255) / 256 * 256; }
 
 __device__ __forceinline__ float4 level4(uint32_t two_bytes, float s) {
   uint32_t h[4];
@@ -37,8 +827,7 @@ __device__ __forceinline__ float4 level4(uint32_t two_bytes, float s) {
 }
 
 // One warp per (new token, query head), a lane has four columns; online softmax over the token's slots.
-template <bool QUANT>
-__global__ void __launch_bounds__(256) extend_simple_kernel(const ExtendArgs a) {
+__global__ void __launch_bounds__(256) extend_simple_kernel(const ExtendArgs a, const __nv_bfloat16* q_, int64_t q_row, int64_t q_head) {
   griddep_wait();
   griddep_launch();
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
@@ -54,21 +843,18 @@ __global__ void __launch_bounds__(256) extend_simple_kernel(const ExtendArgs a) 
   }
   const ckv_paged_view view = a.views[lo];
   const int64_t end = view.len - (a.q_begin[lo + 1] - row) + 1;
-  const float4 q = load4(a.q + row * a.q_row + j * a.q_head + 4 * lane);
+  const float4 q = load4(q_ + row * q_row + j * q_head + 4 * lane);
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int64_t t = 0; t < end; ++t) {
     const int64_t r = (((int64_t)view.block_table[t >> a.shift] * a.H + h) << a.shift) + (t & (((int64_t)1 << a.shift) - 1));
     float4 k, v;
-    if (QUANT) {
+    {
       const int jj = lane >> 3, u = lane & 7;
       const uint32_t kc = *reinterpret_cast<const uint32_t*>(a.pool.k_codes + r * 64 + 16 * (u >> 1) + 4 * jj) >> (16 * (u & 1));
       const uint32_t vc = *reinterpret_cast<const uint32_t*>(a.pool.v_codes + r * 64 + 8 * u + 4 * (jj >> 1)) >> (16 * (jj & 1));
       k = level4(kc, exp2f((float)a.pool.k_scales[r * 4 + jj] - 127.f));
       v = level4(vc, exp2f((float)a.pool.v_scales[r * 4 + jj] - 127.f));
-    } else {
-      k = load4(a.k_pages + r * kED + 4 * lane);
-      v = load4(a.v_pages + r * kED + 4 * lane);
     }
     const float s = warp_sum(q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w) * a.scale + (a.logdeg ? a.logdeg[r] : 0.f);
     const float mm = fmaxf(m, s), base = mm == -INFINITY ? 0.f : mm;
@@ -92,11 +878,31 @@ int check_extend(const void* views, const void* q_begin, int64_t n_rows, int32_t
   return CKV_OK;
 }
 
-template <bool QUANT>
-int run_extend(ExtendArgs& a, cudaStream_t st) {
+// Fills in what both calls have in common and launches
+int run_extend(ExtendArgs& a, const void* q, int64_t q_row, int64_t q_head, const void* k, const void* v, int64_t n_pages, void* workspace, cudaStream_t st) {
   if (a.n_rows == 0) return CKV_OK;
-  const int64_t ctas = (a.n_rows * a.H * a.G + 7) / 8;
-  return launch_dependent(extend_simple_kernel<QUANT>, dim3((unsigned)ctas), dim3(256), 0, st, a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
+  a.T = kEN / a.G;
+  a.max_slots = n_pages << a.shift;
+  a.status = static_cast<int32_t*>(workspace);
+  a.pieces = reinterpret_cast<ExtendPiece*>(static_cast<unsigned char*>(workspace) + 256);
+  a.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + 256 + pieces_bytes());
+  a.slot_rows = slot_rows(a.n_rows, a.G);
+  CUtensorMap tm[3];
+  const cuuint64_t HG = (cuuint64_t)a.H * a.G, rows = ((cuuint64_t)n_pages * a.H) << a.shift;
+  {  // (the stride of a single head or row is never used)
+    const cuuint64_t dims[3] = {kED, HG, (cuuint64_t)a.n_rows}, strides[2] = {HG > 1 ? (cuuint64_t)q_head * 2 : 256, a.n_rows > 1 ? (cuuint64_t)q_row * 2 : 256};
+    const cuuint32_t box[3] = {64, (cuuint32_t)a.G, (cuuint32_t)a.T};
+    if (!encode(&tm[0], q, 3, dims, strides, box)) return CKV_ERR_UNSUPPORTED;
+  }
+  for (int i = 0; i < 2; ++i) {
+    const cuuint64_t dims[2] = {kED, rows}, strides[1] = {kED * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)std::min(kEN, 1 << a.shift)};
+    if (!encode(&tm[1 + i], i ? v : k, 2, dims, strides, box)) return CKV_ERR_UNSUPPORTED;
+  }
+  if (!extend_ready()) return CKV_ERR_CUDA;
+  const unsigned ctas = (unsigned)sm_count();
+  if (launch_dependent(extend_kernel, dim3(ctas), dim3(kEThreads), kEBytes + 1024, st, tm[0], tm[1], tm[2], a) != cudaSuccess) return CKV_ERR_CUDA;
+  return launch_dependent(extend_join_kernel, dim3(ctas, (unsigned)(a.slot_rows + 31) / 32), dim3(kJoinWarps * 32), 0, st, a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
 }  // namespace
@@ -108,7 +914,7 @@ extern "C" {
 
 size_t ckv_extend_workspace_bytes(int64_t n_rows, int32_t H, int32_t G, int32_t D) {
   if (n_rows < 0 || H <= 0 || G <= 0 || D <= 0) return 0;
-  return 256;
+  return 256 + pieces_bytes() + (size_t)2 * sm_count() * slot_rows(n_rows, G) * kPartRow * sizeof(float);
 }
 
 int ckv_extend_attn_paged(const ckv_paged_view* views_dev, const int64_t* q_begin, int64_t n_rows, const void* k_pages, const void* v_pages,
@@ -123,9 +929,9 @@ int ckv_extend_attn_paged(const ckv_paged_view* views_dev, const int64_t* q_begi
   if (n_pages > (INT32_MAX >> shift) / H) return CKV_ERR_UNSUPPORTED;  // (2^31 rows of a pool: 1 TB)
   ExtendArgs a{};
   a.views = views_dev; a.q_begin = q_begin; a.n_rows = n_rows; a.Bz = Bz; a.H = H; a.G = G; a.shift = shift; a.scale = scale;
-  a.q = static_cast<const __nv_bfloat16*>(q); a.out = static_cast<__nv_bfloat16*>(out); a.q_row = q_row_stride; a.q_head = q_head_stride; a.status = static_cast<int32_t*>(workspace);
-  a.k_pages = static_cast<const __nv_bfloat16*>(k_pages); a.v_pages = static_cast<const __nv_bfloat16*>(v_pages); a.logdeg = logdeg_pages;
-  return run_extend<false>(a, static_cast<cudaStream_t>(cuda_stream));
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.logdeg = logdeg_pages;
+  return run_extend(a, q, q_row_stride, q_head_stride, k_pages, v_pages, n_pages, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int ckv_extend_attn_quantized(const ckv_paged_view* views_dev, const int64_t* q_begin, int64_t n_rows, const ckv_quant_pool* pool, int64_t n_pages,
@@ -141,9 +947,11 @@ int ckv_extend_attn_quantized(const ckv_paged_view* views_dev, const int64_t* q_
   if (n_pages > (INT32_MAX >> shift) / H) return CKV_ERR_UNSUPPORTED;
   ExtendArgs a{};
   a.views = views_dev; a.q_begin = q_begin; a.n_rows = n_rows; a.Bz = Bz; a.H = H; a.G = G; a.shift = shift; a.scale = scale;
-  a.q = static_cast<const __nv_bfloat16*>(q); a.out = static_cast<__nv_bfloat16*>(out); a.q_row = q_row_stride; a.q_head = q_head_stride; a.status = static_cast<int32_t*>(workspace);
+  a.out = static_cast<__nv_bfloat16*>(out);
   a.pool = *pool; a.logdeg = pool->logdeg_pages;
-  return run_extend<true>(a, static_cast<cudaStream_t>(cuda_stream));
+  a.status = static_cast<int32_t*>(workspace);
+  if (n_rows == 0) return CKV_OK;
+  return launch_dependent(extend_simple_kernel, dim3((unsigned)((a.n_rows * a.H * a.G + 7) / 8)), dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), a, static_cast<const __nv_bfloat16*>(q), q_row_stride, q_head_stride) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
 }  // extern "C"
