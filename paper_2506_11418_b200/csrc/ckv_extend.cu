@@ -6,12 +6,13 @@
 //
 // One CTA per SM, persistent.  S = Q K^T and O += P V run on tcgen05.mma (128 x 128 x 16, operands in shared memory with the
 // 128-byte swizzle, P read from tensor memory), slots in steps of 128:
-//   warps 0-3, 4-7  softmax of tile 0 and of tile 1, a row per thread: S from tensor memory, y = s * scale + log n, weights
-//                   exp(y - m) to bf16 over S's place, their sum in fp32 registers.  m is the largest y when the tile's rows began,
+//   warps 0-3, 4-7  softmax of tile 0 and of tile 1, a row per thread: S from tensor memory, y = (s * scale + log n) log2 e,
+//                   weights 2^(y - m) to bf16 over S's place, their sum in fp32 registers.  m is the largest y when the tile's rows began,
 //                   and moves (the row of O is then scaled in tensor memory) only when a later y exceeds it by more than
-//                   kSlack, so that O is rarely touched; weights stay below e^kSlack.
+//                   kSlack, so that O is rarely touched; weights stay below 2^kSlack.
 //   warp 8          TMA: the item's queries, and keys, values and log-degrees through a ring of four 32 KB stages
 //   warp 9          issues the MMAs: PV of one tile and the next QK^T of it while the other tile's softmax runs
+//   warps 10, 11    values behind an item's last slot to zero; log-degrees to base two
 // Tensor memory: S0 | S1 | O0 | O1, 128 columns each, all 512.
 // An item with one tile only (single tokens, short chunks) uses the second set for every other step of slots: two softmax
 // states of the same rows, joined at the end.  Otherwise such an item would wait for its softmax at every step.
@@ -27,6 +28,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <cfloat>
 
 #include "../../include/ckv.h"
 #include "ckv_common.cuh"
@@ -41,16 +43,16 @@ using namespace ptx;
 
 constexpr int kED = 128;            // head_dim
 constexpr int kEN = 128;            // slots per step; rows per tile
-constexpr int kEStages = 4;         // K and V tiles in flight
+constexpr int kEStages = 4;         // tiles in flight: keys in the even ones, values in the odd
 constexpr int kETile = kEN * kED * 2;
 constexpr int kEHalf = kETile / 2;  // 64 columns of a tile: 128 rows of 128 bytes
 constexpr int kEBiasSlots = 4;
-constexpr int kEWarps = 12;         // (the last two only complete the warpgroup that gives its registers away)
+constexpr int kEWarps = 12;
 constexpr int kESoftmaxRegs = 216, kEOtherRegs = 72;  // two warps of the first and one of the second on each quarter of an SM: 3 x 168, as launched
 constexpr int kEThreads = kEWarps * 32;
 constexpr int kItemCost = 128;      // what an item costs beside its slots (queries in, rows out), in slots
 constexpr int kMinShare = 512;      // slots that a CTA takes at least
-constexpr float kSlack = 5.5f;      // weights below e^5.5 = 245
+constexpr float kSlack = 8.f;       // weights below 2^8
 constexpr int kPartRow = 132;       // floats of a partial row: O, m, sum, pad
 // shared memory, from a 1024-byte boundary
 constexpr int oQ = 0;
@@ -58,7 +60,7 @@ constexpr int oRing = oQ + 2 * kETile;
 constexpr int oBias = oRing + kEStages * kETile;
 constexpr int oState = oBias + kEBiasSlots * kEN * 4;  // float2 [256]: m and sum of every row, exchanged by one-tile items
 constexpr int oBar = oState + 256 * 8;
-constexpr int oMisc = oBar + 256;
+constexpr int oMisc = oBar + 384;
 constexpr int kEBytes = oMisc + 256;
 
 struct ExtendArgs {
@@ -192,26 +194,38 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// 32 columns, and the wait with the registers as operands (so that no use moves above it)
-__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32]) {
+// 128 columns of 32 lanes into registers, and the wait in the same statement (no use can move above it)
+__device__ __forceinline__ void tmem_ld128(uint32_t taddr, float (&v)[128]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
-      "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      "{\n\t.reg .b32 t1, t2, t3;\n\t"
+      "add.u32 t1, %128, 32;\n\tadd.u32 t2, %128, 64;\n\tadd.u32 t3, %128, 96;\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%128];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+      "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [t1];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%77,%78,%79,"
+      "%80,%81,%82,%83,%84,%85,%86,%87,%88,%89,%90,%91,%92,%93,%94,%95}, [t2];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%96,%97,%98,%99,%100,%101,%102,%103,%104,%105,%106,%107,%108,%109,%110,%111,"
+      "%112,%113,%114,%115,%116,%117,%118,%119,%120,%121,%122,%123,%124,%125,%126,%127}, [t3];\n\t"
+      "tcgen05.wait::ld.sync.aligned;\n\t}"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+        "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+        "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]),
+        "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]),
+        "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]),
+        "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]),
+        "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63]),
+        "=f"(v[64]), "=f"(v[65]), "=f"(v[66]), "=f"(v[67]), "=f"(v[68]), "=f"(v[69]), "=f"(v[70]), "=f"(v[71]),
+        "=f"(v[72]), "=f"(v[73]), "=f"(v[74]), "=f"(v[75]), "=f"(v[76]), "=f"(v[77]), "=f"(v[78]), "=f"(v[79]),
+        "=f"(v[80]), "=f"(v[81]), "=f"(v[82]), "=f"(v[83]), "=f"(v[84]), "=f"(v[85]), "=f"(v[86]), "=f"(v[87]),
+        "=f"(v[88]), "=f"(v[89]), "=f"(v[90]), "=f"(v[91]), "=f"(v[92]), "=f"(v[93]), "=f"(v[94]), "=f"(v[95]),
+        "=f"(v[96]), "=f"(v[97]), "=f"(v[98]), "=f"(v[99]), "=f"(v[100]), "=f"(v[101]), "=f"(v[102]), "=f"(v[103]),
+        "=f"(v[104]), "=f"(v[105]), "=f"(v[106]), "=f"(v[107]), "=f"(v[108]), "=f"(v[109]), "=f"(v[110]), "=f"(v[111]),
+        "=f"(v[112]), "=f"(v[113]), "=f"(v[114]), "=f"(v[115]), "=f"(v[116]), "=f"(v[117]), "=f"(v[118]), "=f"(v[119]),
+        "=f"(v[120]), "=f"(v[121]), "=f"(v[122]), "=f"(v[123]), "=f"(v[124]), "=f"(v[125]), "=f"(v[126]), "=f"(v[127])
       : "r"(taddr)
       : "memory");
-}
-__device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
-                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
-                 "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
-                 "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-               :
-               : "memory");
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
@@ -254,6 +268,12 @@ __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.
 template <int N>
 __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
+__device__ __forceinline__ bool elect_one() {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+  return ok != 0;
+}
+
 // A warp's wait: false if any lane gave up
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); }
 
@@ -263,17 +283,19 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
   unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t s0 = smem_u32(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // barriers: full [stage] | empty [stage] | bias full, empty [slot] | S full [tile] | P full [tile] | O full [tile] | Q full, empty | exchange 2
+  // barriers: full [stage] | empty [stage] | bias full, free, ready [slot] | S full [tile] | P full [tile, half] | O full [tile] | Q full, empty | exchange | values ready [stage / 2]
   auto bar = [&](int i) { return s0 + oBar + 8u * i; };
   auto b_full = [&](int i) { return bar(i); };
   auto b_empty = [&](int i) { return bar(kEStages + i); };
   auto b_bias = [&](int i) { return bar(2 * kEStages + i); };
   auto b_bias_free = [&](int i) { return bar(2 * kEStages + kEBiasSlots + i); };
-  constexpr int kRest = 2 * kEStages + 2 * kEBiasSlots;
+  auto b_bias_ready = [&](int i) { return bar(2 * kEStages + 2 * kEBiasSlots + i); };
+  constexpr int kRest = 2 * kEStages + 3 * kEBiasSlots;
   auto b_s = [&](int g) { return bar(kRest + g); };
-  auto b_p = [&](int g) { return bar(kRest + 2 + g); };
-  auto b_o = [&](int g) { return bar(kRest + 4 + g); };
-  const uint32_t b_q = bar(kRest + 6), b_q_free = bar(kRest + 7), b_x = bar(kRest + 8);
+  auto b_p = [&](int g, int half) { return bar(kRest + 2 + 2 * g + half); };  // (columns 0-63, 64-127)
+  auto b_o = [&](int g) { return bar(kRest + 6 + g); };
+  const uint32_t b_q = bar(kRest + 8), b_q_free = bar(kRest + 9), b_x = bar(kRest + 10);
+  auto b_v = [&](int i) { return bar(kRest + 11 + i); };
   int64_t* const s_start = reinterpret_cast<int64_t*>(smem + oMisc);            // begin of the stretch in its sequence, left, sequence
   int64_t* const s_sum = reinterpret_cast<int64_t*>(smem + oState);             // (before the roles begin)
   volatile uint32_t* const s_tmem = reinterpret_cast<volatile uint32_t*>(smem + oMisc + 64);
@@ -286,15 +308,18 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     for (int i = 0; i < kEBiasSlots; ++i) {
       mbar_init(b_bias(i), 1);
       mbar_init(b_bias_free(i), 8);
+      mbar_init(b_bias_ready(i), 1);
     }
     for (int g = 0; g < 2; ++g) {
       mbar_init(b_s(g), 1);
-      mbar_init(b_p(g), 4);
+      mbar_init(b_p(g, 0), 4);
+      mbar_init(b_p(g, 1), 4);
       mbar_init(b_o(g), 1);
     }
     mbar_init(b_q, 1);
     mbar_init(b_q_free, 1);
     mbar_init(b_x, 8);
+    for (int i = 0; i < kEStages / 2; ++i) mbar_init(b_v(i), 1);
     mbar_init_fence();
     s_start[0] = -1;
   }
@@ -424,95 +449,126 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
       }
     }
   } else if (warp == 9) {
-    // ---------------------------------------------------------------- MMA
-    int n = 0, np = 0, nq[2] = {0, 0};   // steps, pieces, P tiles so far
-    auto qk = [&](int g, int i) {        // S of tile g at the piece's step i, and its arrival
-      const uint32_t kt = s0 + oRing + (uint32_t)((2 * (n + i)) % kEStages) * kETile, qt = s0 + oQ + (uint32_t)g * kETile;
-      if (lane == 0) {
+    // ---------------------------------------------------------------- MMA: one thread
+    if (elect_one()) {
+      int n = 0, np = 0;                     // steps and pieces so far
+      uint32_t par[2] = {0, 0};              // of P
+      const uint64_t d_q = umma_desc_sw128(s0 + oQ, 16, 1024), d_k = umma_desc_sw128(s0 + oRing, 16, 1024), d_v = umma_desc_sw128(s0 + oRing, kEHalf, 1024);
+      auto qk = [&](int g, int i) {          // S of tile g at the piece's step i, and its arrival
+        const uint64_t dk = d_k + (uint64_t)((2 * (n + i)) % kEStages) * (kETile >> 4), dq = d_q + (uint64_t)g * (kETile >> 4);
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
-          const uint32_t off = (uint32_t)(ks >> 2) * kEHalf + (uint32_t)(ks & 3) * 32u;
-          umma_bf16(tmem + (uint32_t)g * 128, umma_desc_sw128(qt + off, 16, 1024), umma_desc_sw128(kt + off, 16, 1024), kDescQK, ks ? 1u : 0u);
+          const uint64_t off = (uint64_t)((ks >> 2) * (kEHalf >> 4) + (ks & 3) * 2);
+          umma_bf16(tmem + (uint32_t)g * 128, dq + off, dk + off, kDescQK, ks ? 1u : 0u);
         }
         umma_commit(b_s(g));
-      }
-    };
-    auto pv = [&](int g, int i, bool more) {
-      const uint32_t vt = s0 + oRing + (uint32_t)((2 * (n + i) + 1) % kEStages) * kETile;
-      if (lane == 0) {
+      };
+      auto pv = [&](int g, int i, int ks0, bool more) {  // four of the eight steps of 16 slots
+        const uint64_t dv = d_v + (uint64_t)((2 * (n + i) + 1) % kEStages) * (kETile >> 4);
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-          umma_bf16_ts(tmem + 256 + (uint32_t)g * 128, tmem + (uint32_t)g * 128 + 8 * ks, umma_desc_sw128(vt + 2048 * ks, kEHalf, 1024), kDescPV,
-                       (more || ks) ? 1u : 0u);
+        for (int ks = 0; ks < 4; ++ks)
+          umma_bf16_ts(tmem + 256 + (uint32_t)g * 128, tmem + (uint32_t)g * 128 + 8 * (ks0 + ks), dv + (uint64_t)(ks0 + ks) * 128, kDescPV, (more || ks) ? 1u : 0u);
+      };
+      auto stage_full = [&](int idx) { return mbar_wait(b_full(idx % kEStages), (uint32_t)((idx / kEStages) & 1)); };
+      auto release = [&](int idx) { umma_commit(b_empty(idx % kEStages)); };
+      while (ok && walk.next(a, p)) {
+        const int steps = p.hi - p.lo;
+        if (steps <= 0) continue;
+        const int ahead = p.one ? 2 : 1;
+        if (!(ok = mbar_wait(b_q, (uint32_t)(np++ & 1)) && stage_full(2 * n))) break;
+        tc_fence_after();
+        qk(0, 0);
+        if (p.one) {
+          release(2 * n);
+          if (steps > 1) {
+            if (!(ok = stage_full(2 * (n + 1)))) break;
+            tc_fence_after();
+            qk(1, 1);
+            release(2 * (n + 1));
+          }
+        } else {
+          qk(1, 0);
+          release(2 * n);
+        }
+        if (steps <= ahead) umma_commit(b_q_free);
+        for (int i = 0; ok && i < steps; ++i) {
+          const int g0 = p.one ? i & 1 : 0, g1 = p.one ? g0 : 1;
+          const bool more = i + ahead < steps;
+          const int iv = n + i;
+          if (!(ok = mbar_wait(b_v(iv % (kEStages / 2)), (uint32_t)((iv / (kEStages / 2)) & 1)))) break;
+          for (int g = g0; g <= g1; ++g) {
+            if (!(ok = mbar_wait(b_p(g, 0), par[g]))) break;
+            tc_fence_after();
+            pv(g, i, 0, i >= ahead);
+            if (!(ok = mbar_wait(b_p(g, 1), par[g]))) break;
+            par[g] ^= 1;
+            tc_fence_after();
+            pv(g, i, 4, true);
+            if (g == g1) release(2 * (n + i) + 1);
+            if (more) {
+              if (g == g0 && !(ok = stage_full(2 * (n + i + ahead)))) break;
+              tc_fence_after();
+              qk(g, i + ahead);
+              if (g == g1) release(2 * (n + i + ahead));
+            } else if (!p.one) {
+              umma_commit(b_o(g));
+            }
+          }
+          if (i + ahead == steps - 1) umma_commit(b_q_free);
+        }
+        if (ok && p.one) {
+          umma_commit(b_o(0));
+          umma_commit(b_o(1));
+        }
+        n += steps;
       }
-    };
-    auto stage_full = [&](int idx) { return warp_wait(b_full(idx % kEStages), (uint32_t)((idx / kEStages) & 1)); };
-    auto release = [&](int idx) { if (lane == 0) umma_commit(b_empty(idx % kEStages)); };
-    auto p_full = [&](int g) { return warp_wait(b_p(g), (uint32_t)(nq[g]++ & 1)); };
+    }
+  } else if (warp == 10) {
+    // ---------------------------------------------------------------- slots behind the last that an item sees: whatever their values
+    // are, they must not meet a weight of zero
+    int n = 0;
     while (ok && walk.next(a, p)) {
-      const int steps = p.hi - p.lo;
-      if (steps <= 0) continue;
-      if (!(ok = warp_wait(b_q, (uint32_t)(np++ & 1)))) break;
-      // slots behind the last that the item sees: whatever their values are, they must not meet a weight of zero
-      auto values = [&](int i) {
-        if (!stage_full(2 * (n + i) + 1)) return false;
-        const int seen = p.end - (p.lo + i) * kEN;
+      for (int i = p.lo; i < p.hi; ++i, ++n) {
+        const int st = (2 * n + 1) % kEStages, seen = p.end - i * kEN;
+        if (!(ok = warp_wait(b_full(st), (uint32_t)(((2 * n + 1) / kEStages) & 1)))) break;
         if (seen < kEN) {
-          const uint32_t vt = s0 + oRing + (uint32_t)((2 * (n + i) + 1) % kEStages) * kETile;
+          const uint32_t vt = s0 + oRing + (uint32_t)st * kETile;
           for (int c = seen * 8 + lane; c < kEN * 8; c += 32) {
             st_shared_v4(vt + c * 16, make_uint4(0, 0, 0, 0));
             st_shared_v4(vt + kEHalf + c * 16, make_uint4(0, 0, 0, 0));
           }
           fence_async_smem();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_v(st / 2));
+      }
+    }
+  } else if (warp == 11) {
+    // ---------------------------------------------------------------- log-degrees to base two, in place.  The type's largest values stay
+    // finite: where a caller masks slots with them, scores minus their maximum have to be numbers.  (Only log-degrees above
+    // 2^127 ln 2 in magnitude are changed by this.)
+    if (!a.logdeg) {
+      for (int c = lane; c < kEBiasSlots * kEN; c += 32) reinterpret_cast<float*>(smem + oBias)[c] = 0.f;
+      __syncwarp();
+      if (lane == 0)
+        for (int i = 0; i < kEBiasSlots; ++i) mbar_arrive(b_bias_ready(i));
+    } else {
+      int n = 0;
+      while (ok && walk.next(a, p)) {
+        for (int i = p.lo; i < p.hi; ++i, ++n) {
+          const int bs = n % kEBiasSlots;
+          if (!(ok = warp_wait(b_bias(bs), (uint32_t)((n / kEBiasSlots) & 1)))) break;
+          float4* const at = reinterpret_cast<float4*>(smem + oBias + bs * kEN * 4) + lane;
+          float4 b = *at;
+          auto base2 = [](float x) {
+            const float y = x * kLog2e;
+            return fabsf(y) == INFINITY && fabsf(x) != INFINITY ? copysignf(FLT_MAX, x) : y;
+          };
+          *at = make_float4(base2(b.x), base2(b.y), base2(b.z), base2(b.w));
           __syncwarp();
+          if (lane == 0) mbar_arrive(b_bias_ready(bs));
         }
-        return true;
-      };
-      tc_fence_after();
-      const int ahead = p.one ? 2 : 1;
-      if (!(ok = stage_full(2 * n))) break;
-      tc_fence_after();
-      qk(0, 0);
-      if (p.one) {
-        release(2 * n);
-        if (steps > 1) {
-          if (!(ok = stage_full(2 * (n + 1)))) break;
-          tc_fence_after();
-          qk(1, 1);
-          release(2 * (n + 1));
-        }
-      } else {
-        qk(1, 0);
-        release(2 * n);
       }
-      if (steps <= ahead && lane == 0) umma_commit(b_q_free);
-      for (int i = 0; i < steps; ++i) {
-        if (!(ok = values(i))) break;
-        const int g0 = p.one ? i & 1 : 0, g1 = p.one ? g0 : 1;
-        const bool more = i + ahead < steps;
-        for (int g = g0; g <= g1; ++g) {
-          if (!(ok = p_full(g))) break;
-          tc_fence_after();
-          pv(g, i, i >= ahead);
-          if (g == g1) release(2 * (n + i) + 1);
-          if (more) {
-            if (g == g0 && !(ok = stage_full(2 * (n + i + ahead)))) break;
-            tc_fence_after();
-            qk(g, i + ahead);
-            if (g == g1) release(2 * (n + i + ahead));
-          } else if (!p.one && lane == 0) {
-            umma_commit(b_o(g));
-          }
-        }
-        if (!ok) break;
-        if (i + ahead == steps - 1 && lane == 0) umma_commit(b_q_free);
-      }
-      if (!ok) break;
-      if (p.one && lane == 0) {
-        umma_commit(b_o(0));
-        umma_commit(b_o(1));
-      }
-      n += steps;
     }
   }
   } else {
@@ -522,7 +578,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // (32 lanes of tensor memory per warp, lane number in the upper half word)
     const uint32_t t_s = tmem + lanes + (uint32_t)g * 128, t_o = t_s + 256;
     float2* const state = reinterpret_cast<float2*>(smem + oState);
-    const float scale = a.scale;
+    const float scale = a.scale * kLog2e;  // (all in base two)
     int n = 0, ns = 0, np = 0, nx = 0;  // steps, own steps, pieces, exchanges so far
     ExtendPiece note{0, 0, 0, 0, {0, 0}};
     while (ok && walk.next(a, p)) {
@@ -536,38 +592,29 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
       for (int i = 0; i < steps; ++i, ++n) {
         const int bs = n % kEBiasSlots;
         const bool own = !p.one || (i & 1) == g;
-        if (a.logdeg && !(ok = warp_wait(b_bias(bs), (uint32_t)((n / kEBiasSlots) & 1)))) break;
+        if (!(ok = warp_wait(b_bias_ready(bs), a.logdeg ? (uint32_t)((n / kEBiasSlots) & 1) : 0u))) break;
         if (own) {
           if (!(ok = warp_wait(b_s(g), (uint32_t)(ns++ & 1)))) break;
           tc_fence_after();
           if (busy) {
-            uint32_t sv[4][32];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32_issue(t_s + 32 * c, sv[c]);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld_wait(sv[c]);
             float y[128];
+            tmem_ld128(t_s, y);
             const f32x2 sc(scale, scale);
-            if (a.logdeg) {
-              const ulonglong2* const bias = reinterpret_cast<const ulonglong2*>(smem + oBias + bs * kEN * 4);
+            const ulonglong2* const bias = reinterpret_cast<const ulonglong2*>(smem + oBias + bs * kEN * 4);
 #pragma unroll
-              for (int c = 0; c < 32; ++c) {
-                const ulonglong2 b4 = bias[c];
-                f32x2 lo, hi;
-                lo.v = b4.x;
-                hi.v = b4.y;
-                fma2(f32x2(__uint_as_float(sv[c / 8][4 * c % 32]), __uint_as_float(sv[c / 8][4 * c % 32 + 1])), sc, lo).get(y[4 * c], y[4 * c + 1]);
-                fma2(f32x2(__uint_as_float(sv[c / 8][4 * c % 32 + 2]), __uint_as_float(sv[c / 8][4 * c % 32 + 3])), sc, hi).get(y[4 * c + 2], y[4 * c + 3]);
-              }
-            } else {
-#pragma unroll
-              for (int c = 0; c < 64; ++c)
-                mul2(f32x2(__uint_as_float(sv[c / 16][2 * c % 32]), __uint_as_float(sv[c / 16][2 * c % 32 + 1])), sc).get(y[2 * c], y[2 * c + 1]);
+            for (int c = 0; c < 32; ++c) {
+              const ulonglong2 b4 = bias[c];
+              f32x2 lo, hi;
+              lo.v = b4.x;
+              hi.v = b4.y;
+              fma2(f32x2(y[4 * c], y[4 * c + 1]), sc, lo).get(y[4 * c], y[4 * c + 1]);
+              fma2(f32x2(y[4 * c + 2], y[4 * c + 3]), sc, hi).get(y[4 * c + 2], y[4 * c + 3]);
             }
             const int seen = lim - (p.lo + i) * kEN;
             if ((p.lo + i + 1) * kEN > lim_min) {  // (some row of the warp does not see all of the step's slots)
 #pragma unroll
-              for (int c = 0; c < 128; ++c) y[c] = c < seen ? y[c] : -INFINITY;
+              for (int c = 0; c < 128; ++c)
+                asm volatile("{\n\t.reg .pred q;\n\tsetp.le.s32 q, %1, %2;\n\t@q mov.f32 %0, 0fFF800000;\n\t}" : "+f"(y[c]) : "r"(seen), "r"(c));
             }
             float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -578,51 +625,52 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
             const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
             if (__any_sync(0xffffffffu, top > m + kSlack)) {
               const bool up = top > m;
-              const float f = up ? ex2((m - top) * kLog2e) : 1.f;
+              const float f = up ? ex2(m - top) : 1.f;
               if (__any_sync(0xffffffffu, m > -INFINITY)) {  // O holds something (its last product is complete: S came behind it)
                 for (int c = 0; c < 4; ++c) {
-                  uint32_t o[32];
-                  tmem_ld32_issue(t_o + 32 * c, o);
-                  tmem_ld_wait(o);
+                  float o[32];
+                  uint32_t u[32];
+                  tmem_ld32(t_o + 32 * c, o);
 #pragma unroll
-                  for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                  tmem_st32(t_o + 32 * c, o);
+                  for (int k = 0; k < 32; ++k) u[k] = __float_as_uint(o[k] * f);
+                  tmem_st32(t_o + 32 * c, u);
                 }
               }
               l2 = mul2(l2, f32x2(f, f));
               m = up ? top : m;
             }
-            const float mz = m == -INFINITY ? 0.f : m, mL = mz * kLog2e;
-            // (y and m next to the type's ends: y log2 e would overflow, y - m does not)
-            if (__any_sync(0xffffffffu, fabsf(mL) == INFINITY && fabsf(mz) != INFINITY)) {
-#pragma unroll
-              for (int c = 0; c < 128; ++c) y[c] = ex2((y[c] - mz) * kLog2e);
-            } else {
-              const f32x2 le(kLog2e, kLog2e), mm(-mL, -mL);
-#pragma unroll
-              for (int c = 0; c < 128; c += 2) {
-                fma2(f32x2(y[c], y[c + 1]), le, mm).get(y[c], y[c + 1]);
-                y[c] = ex2(y[c]);
-                y[c + 1] = ex2(y[c + 1]);
-              }
-            }
+            const float off = m == -INFINITY ? 0.f : -m;
+            const f32x2 mm(off, off);
             f32x2 la(0.f, 0.f), lb(0.f, 0.f);
-            uint32_t pk[2][32];
 #pragma unroll
-            for (int c = 0; c < 128; c += 4) {
-              la = add2(la, f32x2(y[c], y[c + 1]));
-              lb = add2(lb, f32x2(y[c + 2], y[c + 3]));
-              pk[c / 64][c % 64 / 2] = pack_bf16x2(y[c], y[c + 1]);
-              pk[c / 64][c % 64 / 2 + 1] = pack_bf16x2(y[c + 2], y[c + 3]);
+            for (int half = 0; half < 2; ++half) {
+              uint32_t pk[32];
+#pragma unroll
+              for (int c = 64 * half; c < 64 * half + 64; c += 4) {
+                float e[4];
+                add2(f32x2(y[c], y[c + 1]), mm).get(e[0], e[1]);
+                add2(f32x2(y[c + 2], y[c + 3]), mm).get(e[2], e[3]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) e[k] = ex2(e[k]);
+                la = add2(la, f32x2(e[0], e[1]));
+                lb = add2(lb, f32x2(e[2], e[3]));
+                pk[c % 64 / 2] = pack_bf16x2(e[0], e[1]);
+                pk[c % 64 / 2 + 1] = pack_bf16x2(e[2], e[3]);
+              }
+              tmem_st32(t_s + 32 * half, pk);
+              tmem_st_wait();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(b_p(g, half));
             }
-            tmem_st32(t_s, pk[0]);
-            tmem_st32(t_s + 32, pk[1]);
             l2 = add2(l2, add2(la, lb));
-            tmem_st_wait();
+          } else {
+            tc_fence_before();
+            if (lane == 0) {
+              mbar_arrive(b_p(g, 0));
+              mbar_arrive(b_p(g, 1));
+            }
           }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(b_p(g));
         }
         if (a.logdeg && lane == 0) mbar_arrive(b_bias_free(bs));
       }
@@ -650,8 +698,8 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
         if (!(ok = warp_wait(b_x, (uint32_t)(nx++ & 1)))) break;
         const float2 x0 = state[r], x1 = state[128 + r];
         m = fmaxf(x0.x, x1.x);
-        f0 = x0.x == -INFINITY ? 0.f : ex2((x0.x - m) * kLog2e);
-        f1 = x1.x == -INFINITY ? 0.f : ex2((x1.x - m) * kLog2e);
+        f0 = x0.x == -INFINITY ? 0.f : ex2(x0.x - m);
+        f1 = x1.x == -INFINITY ? 0.f : ex2(x1.x - m);
         l = x0.y * f0 + x1.y * f1;
       }
       if (busy) {
@@ -661,16 +709,14 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
         for (int c = c0; c < c1; ++c) {
           float o[32];
           if (steps > 0) {
-            uint32_t u[32];
-            tmem_ld32_issue((p.one ? tmem + lanes + 256 : t_o) + 32 * c, u);
-            tmem_ld_wait(u);
+            tmem_ld32((p.one ? tmem + lanes + 256 : t_o) + 32 * c, o);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = f0 == 0.f ? 0.f : __uint_as_float(u[k]) * f0;
+            for (int k = 0; k < 32; ++k) o[k] = f0 == 0.f ? 0.f : o[k] * f0;
             if (p.one && steps > 1) {
-              tmem_ld32_issue(tmem + lanes + 384 + 32 * c, u);
-              tmem_ld_wait(u);
+              float u[32];
+              tmem_ld32(tmem + lanes + 384 + 32 * c, u);
 #pragma unroll
-              for (int k = 0; k < 32; ++k) o[k] += f1 == 0.f ? 0.f : __uint_as_float(u[k]) * f1;
+              for (int k = 0; k < 32; ++k) o[k] += f1 == 0.f ? 0.f : u[k] * f1;
             }
           } else {
 #pragma unroll
@@ -718,6 +764,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
 // Joins the pieces of the items that CTA blockIdx.x of the kernel above ended and did not begin.  Rows are dealt to gridDim.y CTAs: a warp
 // per row where there are few pieces, else a CTA per row, whose warps share them.
 constexpr int kJoinWarps = 8;
+constexpr int kJoinTogether = 24;  // pieces from which on a row's are shared by a CTA's warps
 
 __global__ void __launch_bounds__(kJoinWarps * 32) extend_join_kernel(const ExtendArgs a) {
   __shared__ float2 s_ml[kJoinWarps];
@@ -728,16 +775,16 @@ __global__ void __launch_bounds__(kJoinWarps * 32) extend_join_kernel(const Exte
   if (last.ntok == 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rows = last.ntok * a.G, n = (int)blockIdx.x - last.first + 1;
-  const bool together = n > 8;
+  const bool together = n > kJoinTogether;
   for (int r = together ? (int)blockIdx.y : (int)blockIdx.y * kJoinWarps + warp; r < rows; r += (int)gridDim.y * (together ? 1 : kJoinWarps)) {
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     const int p0 = together ? warp : 0, dp = together ? kJoinWarps : 1;
-    for (int p = p0; p < n; p += 4 * dp) {
-      float2 ml[4];
-      float4 y[4];
+    for (int p = p0; p < n; p += 8 * dp) {
+      float2 ml[8];
+      float4 y[8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < 8; ++u) {
         const int c = last.first + p + u * dp, slot = p + u * dp == 0 ? 1 : 0;
         ml[u] = make_float2(-INFINITY, 0.f);
         y[u] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -748,10 +795,10 @@ __global__ void __launch_bounds__(kJoinWarps * 32) extend_join_kernel(const Exte
         }
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < 8; ++u) {
         const float mm = fmaxf(m, ml[u].x);
         if (mm == -INFINITY && !(ml[u].y != 0.f)) continue;  // (no slots, or only such of weight zero)
-        const float c = m == -INFINITY ? 0.f : exp2f((m - mm) * kLog2e), f = ml[u].x == -INFINITY ? 0.f : exp2f((ml[u].x - mm) * kLog2e);
+        const float c = m == -INFINITY ? 0.f : exp2f(m - mm), f = ml[u].x == -INFINITY ? 0.f : exp2f(ml[u].x - mm);
         o = make_float4(fmaf(f, y[u].x, o.x * c), fmaf(f, y[u].y, o.y * c), fmaf(f, y[u].z, o.z * c), fmaf(f, y[u].w, o.w * c));
         l = fmaf(f, ml[u].y, l * c);
         m = mm;
@@ -767,7 +814,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) extend_join_kernel(const Exte
         l = 0.f;
         o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int w = 0; w < kJoinWarps; ++w) {
-          const float f = s_ml[w].x == -INFINITY ? 0.f : exp2f((s_ml[w].x - m) * kLog2e);
+          const float f = s_ml[w].x == -INFINITY ? 0.f : exp2f(s_ml[w].x - m);
           const float4 y = s_o[w][lane];
           l = fmaf(f, s_ml[w].y, l);
           o = make_float4(fmaf(f, y.x, o.x), fmaf(f, y.y, o.y), fmaf(f, y.z, o.z), fmaf(f, y.w, o.w));
@@ -902,7 +949,7 @@ int run_extend(ExtendArgs& a, const void* q, int64_t q_row, int64_t q_head, cons
   if (!extend_ready()) return CKV_ERR_CUDA;
   const unsigned ctas = (unsigned)sm_count();
   if (launch_dependent(extend_kernel, dim3(ctas), dim3(kEThreads), kEBytes + 1024, st, tm[0], tm[1], tm[2], a) != cudaSuccess) return CKV_ERR_CUDA;
-  return launch_dependent(extend_join_kernel, dim3(ctas, (unsigned)(a.slot_rows + 31) / 32), dim3(kJoinWarps * 32), 0, st, a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
+  return launch_dependent(extend_join_kernel, dim3(ctas, (unsigned)std::min(a.slot_rows, 2 * kEN / kJoinWarps)), dim3(kJoinWarps * 32), 0, st, a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
 }  // namespace

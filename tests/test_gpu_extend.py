@@ -250,3 +250,19 @@ def test_pool_past_32_bits():
     c.k, c.v, c.logdeg = k, v, logdeg
     c.table[0] = far
     check(c, [130], 4)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_many_calls_one_after_the_other(kind):
+    """Short items whose pieces have one step each, many times over without a pause: results repeat to the bit."""
+    lens = [1 + 37 * b % 300 for b in range(90)]
+    c, new = Cache(lens, 4, 64, kind), [min(n, 1 + 11 * n % 200) for n in lens]
+    total = sum(new)
+    q, begin, ws = queries(total, 4, 4, 1), torch.tensor(np.concatenate([[0], np.cumsum(new)]), **I64), workspace(total, 4, 4)
+    outs = [torch.zeros_like(q) for _ in range(2)]
+    bad = torch.zeros((), dtype=torch.int64, device=DEV)
+    c.call(begin, 4, q, outs[0], SCALE, ws)
+    for _ in range(300):
+        c.call(begin, 4, q, outs[1], SCALE, ws)
+        bad += (outs[0] != outs[1]).sum() + ws[:4].view(torch.int32)[0].abs()
+    assert bad.item() == 0
