@@ -29,6 +29,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "../../include/ckv.h"
 #include "ckv_common.cuh"
@@ -193,6 +194,20 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
         "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+// eight columns
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+               "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // 128 columns of 32 lanes into registers, and the wait in the same statement (no use can move above it)
 __device__ __forceinline__ void tmem_ld128(uint32_t taddr, float (&v)[128]) {
@@ -274,8 +289,25 @@ __device__ __forceinline__ bool elect_one() {
   return ok != 0;
 }
 
+// Bounded wait.  A poll may sleep for up to a microsecond before it answers, so that the warps that wait (most of the time there
+// are eight) do not take issue slots from those that compute.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+  for (uint32_t i = 0; i < kSpinLimit / 4; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(1000u)
+        : "memory");
+    if (ok) return true;
+  }
+  return false;
+}
+
 // A warp's wait: false if any lane gave up
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); }
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
 
 __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                                                               const __grid_constant__ CUtensorMap tm_v, const ExtendArgs a) {
@@ -469,13 +501,13 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
         for (int ks = 0; ks < 4; ++ks)
           umma_bf16_ts(tmem + 256 + (uint32_t)g * 128, tmem + (uint32_t)g * 128 + 8 * (ks0 + ks), dv + (uint64_t)(ks0 + ks) * 128, kDescPV, (more || ks) ? 1u : 0u);
       };
-      auto stage_full = [&](int idx) { return mbar_wait(b_full(idx % kEStages), (uint32_t)((idx / kEStages) & 1)); };
+      auto stage_full = [&](int idx) { return bar_wait(b_full(idx % kEStages), (uint32_t)((idx / kEStages) & 1)); };
       auto release = [&](int idx) { umma_commit(b_empty(idx % kEStages)); };
       while (ok && walk.next(a, p)) {
         const int steps = p.hi - p.lo;
         if (steps <= 0) continue;
         const int ahead = p.one ? 2 : 1;
-        if (!(ok = mbar_wait(b_q, (uint32_t)(np++ & 1)) && stage_full(2 * n))) break;
+        if (!(ok = bar_wait(b_q, (uint32_t)(np++ & 1)) && stage_full(2 * n))) break;
         tc_fence_after();
         qk(0, 0);
         if (p.one) {
@@ -495,12 +527,12 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
           const int g0 = p.one ? i & 1 : 0, g1 = p.one ? g0 : 1;
           const bool more = i + ahead < steps;
           const int iv = n + i;
-          if (!(ok = mbar_wait(b_v(iv % (kEStages / 2)), (uint32_t)((iv / (kEStages / 2)) & 1)))) break;
+          if (!(ok = bar_wait(b_v(iv % (kEStages / 2)), (uint32_t)((iv / (kEStages / 2)) & 1)))) break;
           for (int g = g0; g <= g1; ++g) {
-            if (!(ok = mbar_wait(b_p(g, 0), par[g]))) break;
+            if (!(ok = bar_wait(b_p(g, 0), par[g]))) break;
             tc_fence_after();
             pv(g, i, 0, i >= ahead);
-            if (!(ok = mbar_wait(b_p(g, 1), par[g]))) break;
+            if (!(ok = bar_wait(b_p(g, 1), par[g]))) break;
             par[g] ^= 1;
             tc_fence_after();
             pv(g, i, 4, true);
@@ -596,7 +628,10 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
         if (own) {
           if (!(ok = warp_wait(b_s(g), (uint32_t)(ns++ & 1)))) break;
           tc_fence_after();
-          if (busy) {
+          // one step of this row; MASK: some row of the warp does not see all of the step's slots.  (Two copies of the code: with
+          // the selection as a branch inside, the compiler moves all 128 registers around it.)
+          auto step = [&](auto mask) {
+            constexpr bool MASK = decltype(mask)::value;
             float y[128];
             tmem_ld128(t_s, y);
             const f32x2 sc(scale, scale);
@@ -610,11 +645,10 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
               fma2(f32x2(y[4 * c], y[4 * c + 1]), sc, lo).get(y[4 * c], y[4 * c + 1]);
               fma2(f32x2(y[4 * c + 2], y[4 * c + 3]), sc, hi).get(y[4 * c + 2], y[4 * c + 3]);
             }
-            const int seen = lim - (p.lo + i) * kEN;
-            if ((p.lo + i + 1) * kEN > lim_min) {  // (some row of the warp does not see all of the step's slots)
+            if constexpr (MASK) {
+              const int seen = lim - (p.lo + i) * kEN;
 #pragma unroll
-              for (int c = 0; c < 128; ++c)
-                asm volatile("{\n\t.reg .pred q;\n\tsetp.le.s32 q, %1, %2;\n\t@q mov.f32 %0, 0fFF800000;\n\t}" : "+f"(y[c]) : "r"(seen), "r"(c));
+              for (int c = 0; c < 128; ++c) y[c] = c < seen ? y[c] : -INFINITY;
             }
             float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -627,13 +661,13 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
               const bool up = top > m;
               const float f = up ? ex2(m - top) : 1.f;
               if (__any_sync(0xffffffffu, m > -INFINITY)) {  // O holds something (its last product is complete: S came behind it)
-                for (int c = 0; c < 4; ++c) {
-                  float o[32];
-                  uint32_t u[32];
-                  tmem_ld32(t_o + 32 * c, o);
+#pragma unroll 1
+                for (int c = 0; c < 128; c += 8) {
+                  float o[8];
+                  tmem_ld8(t_o + c, o);
 #pragma unroll
-                  for (int k = 0; k < 32; ++k) u[k] = __float_as_uint(o[k] * f);
-                  tmem_st32(t_o + 32 * c, u);
+                  for (int k = 0; k < 8; ++k) o[k] *= f;
+                  tmem_st8(t_o + c, o);
                 }
               }
               l2 = mul2(l2, f32x2(f, f));
@@ -644,26 +678,35 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
             f32x2 la(0.f, 0.f), lb(0.f, 0.f);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              uint32_t pk[32];
 #pragma unroll
-              for (int c = 64 * half; c < 64 * half + 64; c += 4) {
-                float e[4];
-                add2(f32x2(y[c], y[c + 1]), mm).get(e[0], e[1]);
-                add2(f32x2(y[c + 2], y[c + 3]), mm).get(e[2], e[3]);
+              for (int c0 = 64 * half; c0 < 64 * half + 64; c0 += 16) {
+                float pk[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) e[k] = ex2(e[k]);
-                la = add2(la, f32x2(e[0], e[1]));
-                lb = add2(lb, f32x2(e[2], e[3]));
-                pk[c % 64 / 2] = pack_bf16x2(e[0], e[1]);
-                pk[c % 64 / 2 + 1] = pack_bf16x2(e[2], e[3]);
+                for (int c = c0; c < c0 + 16; c += 4) {
+                  float e[4];
+                  add2(f32x2(y[c], y[c + 1]), mm).get(e[0], e[1]);
+                  add2(f32x2(y[c + 2], y[c + 3]), mm).get(e[2], e[3]);
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) e[k] = ex2(e[k]);
+                  la = add2(la, f32x2(e[0], e[1]));
+                  lb = add2(lb, f32x2(e[2], e[3]));
+                  pk[(c - c0) / 2] = __uint_as_float(pack_bf16x2(e[0], e[1]));
+                  pk[(c - c0) / 2 + 1] = __uint_as_float(pack_bf16x2(e[2], e[3]));
+                }
+                tmem_st8(t_s + c0 / 2, pk);
               }
-              tmem_st32(t_s + 32 * half, pk);
               tmem_st_wait();
               tc_fence_before();
               __syncwarp();
               if (lane == 0) mbar_arrive(b_p(g, half));
             }
             l2 = add2(l2, add2(la, lb));
+          };
+          if (busy) {
+            if ((p.lo + i + 1) * kEN > lim_min)
+              step(std::true_type{});
+            else
+              step(std::false_type{});
           } else {
             tc_fence_before();
             if (lane == 0) {
