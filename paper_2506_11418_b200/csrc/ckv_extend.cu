@@ -6,13 +6,13 @@
 //
 // One CTA per SM, persistent.  S = Q K^T and O += P V run on tcgen05.mma (128 x 128 x 16, operands in shared memory with the
 // 128-byte swizzle, P read from tensor memory), slots in steps of 128:
-//   warps 0-3, 4-7  softmax of tile 0 and of tile 1, a row per thread: S from tensor memory, y = (s * scale + log n) log2 e,
-//                   weights 2^(y - m) to bf16 over S's place, their sum in fp32 registers.  m is the largest y when the tile's rows began,
-//                   and moves (the row of O is then scaled in tensor memory) only when a later y exceeds it by more than
-//                   kSlack, so that O is rarely touched; weights stay below 2^kSlack.
+//   warps 0-3, 4-7  softmax of tile 0 and of tile 1, a row per thread: S from tensor memory, weights e^(scale (s - m)) to bf16
+//                   over S's place, their sum in fp32 registers.  m is the largest s when the tile's rows began,
+//                   and moves (the row of O is then scaled in tensor memory) only when a later one would weigh
+//                   more than 2^kSlack, so that O is rarely touched.  The log-degree is in s already (warp 11).
 //   warp 8          TMA: the item's queries, and keys, values and log-degrees through a ring of four 32 KB stages
 //   warp 9          issues the MMAs: PV of one tile and the next QK^T of it while the other tile's softmax runs
-//   warps 10, 11    values behind an item's last slot to zero; log-degrees to base two
+//   warps 10, 11    values behind an item's last slot to zero; log-degrees as three more columns of K
 // Tensor memory: S0 | S1 | O0 | O1, 128 columns each, all 512.
 // An item with one tile only (single tokens, short chunks) uses the second set for every other step of slots: two softmax
 // states of the same rows, joined at the end.  Otherwise such an item would wait for its softmax at every step.
@@ -28,7 +28,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
-#include <cfloat>
+#include <cmath>
 #include <type_traits>
 
 #include "../../include/ckv.h"
@@ -59,7 +59,10 @@ constexpr int kPartRow = 132;       // floats of a partial row: O, m, sum, pad
 constexpr int oQ = 0;
 constexpr int oRing = oQ + 2 * kETile;
 constexpr int oBias = oRing + kEStages * kETile;
-constexpr int oState = oBias + kEBiasSlots * kEN * 4;  // float2 [256]: m and sum of every row, exchanged by one-tile items
+constexpr int oAug = oBias + kEBiasSlots * kEN * 4;       // 16 bytes per slot: its log-degree in three bf16, kEBiasSlots steps
+constexpr int oOnes = oAug + kEBiasSlots * kEN * 16;       // 16 bytes per row of Q: three ones
+constexpr int oZero = oOnes + kEN * 16;                    // the other eight columns of both
+constexpr int oState = oZero + kEN * 16;  // float2 [256]: m and sum of every row, exchanged by one-tile items
 constexpr int oBar = oState + 256 * 8;
 constexpr int oMisc = oBar + 384;
 constexpr int kEBytes = oMisc + 256;
@@ -72,7 +75,8 @@ struct ExtendArgs {
   const float* logdeg;
   int64_t n_rows, max_slots;
   int32_t Bz, H, G, T, shift;
-  float scale;
+  float scale;          // above zero
+  uint32_t desc_qk;     // (a negative scale negates Q)
   int32_t* status;      // workspace: status word | pieces [CTAs] | partial rows
   struct ExtendPiece* pieces;
   float* partial;       // [2 CTAs][slot_rows][kPartRow]
@@ -184,16 +188,6 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, u
       ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
-      "%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
 // eight columns
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8]) {
   asm volatile(
@@ -276,6 +270,7 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
 
 // tcgen05 instruction descriptors: bf16 x bf16 -> fp32, M = N = 128; B K-major (keys) or N-major (values)
 constexpr uint32_t kDescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+constexpr uint32_t kNegateA = 1u << 13;
 constexpr uint32_t kDescPV = kDescQK | (1u << 16);
 
 template <int N>
@@ -283,6 +278,10 @@ __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.
 template <int N>
 __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
+// Shared-memory matrix descriptor of an operand without swizzle
+__device__ __forceinline__ uint64_t umma_desc_plain(uint32_t smem_addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
+  return (uint64_t)((smem_addr >> 4) & 0x3fffu) | ((uint64_t)((lbo_bytes >> 4) & 0x3fffu) << 16) | ((uint64_t)((sbo_bytes >> 4) & 0x3fffu) << 32) | (1ull << 46);
+}
 __device__ __forceinline__ bool elect_one() {
   uint32_t ok;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
@@ -315,14 +314,15 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
   unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t s0 = smem_u32(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // barriers: full [stage] | empty [stage] | bias full, free, ready [slot] | S full [tile] | P full [tile, half] | O full [tile] | Q full, empty | exchange | values ready [stage / 2]
+  // barriers: full [stage] | empty [stage] | log-degrees full, free, in bf16, free [slot] | S full [tile] | P full [tile, half] | O full [tile] | Q full, empty | exchange | values ready [stage / 2]
   auto bar = [&](int i) { return s0 + oBar + 8u * i; };
   auto b_full = [&](int i) { return bar(i); };
   auto b_empty = [&](int i) { return bar(kEStages + i); };
   auto b_bias = [&](int i) { return bar(2 * kEStages + i); };
   auto b_bias_free = [&](int i) { return bar(2 * kEStages + kEBiasSlots + i); };
   auto b_bias_ready = [&](int i) { return bar(2 * kEStages + 2 * kEBiasSlots + i); };
-  constexpr int kRest = 2 * kEStages + 3 * kEBiasSlots;
+  auto b_aug_free = [&](int i) { return bar(2 * kEStages + 3 * kEBiasSlots + i); };
+  constexpr int kRest = 2 * kEStages + 4 * kEBiasSlots;
   auto b_s = [&](int g) { return bar(kRest + g); };
   auto b_p = [&](int g, int half) { return bar(kRest + 2 + 2 * g + half); };  // (columns 0-63, 64-127)
   auto b_o = [&](int g) { return bar(kRest + 6 + g); };
@@ -339,8 +339,9 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     }
     for (int i = 0; i < kEBiasSlots; ++i) {
       mbar_init(b_bias(i), 1);
-      mbar_init(b_bias_free(i), 8);
+      mbar_init(b_bias_free(i), 1);
       mbar_init(b_bias_ready(i), 1);
+      mbar_init(b_aug_free(i), 1);
     }
     for (int g = 0; g < 2; ++g) {
       mbar_init(b_s(g), 1);
@@ -420,6 +421,11 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
   }
   const int64_t item_begin = begin - walk.x;  // of the item in which the stretch begins, on the line of all items
 
+  if (tid < kEN) {
+    st_shared_v4(s0 + oOnes + tid * 16, make_uint4(0x3f803f80u, 0x00003f80u, 0, 0));
+    st_shared_v4(s0 + oZero + tid * 16, make_uint4(0, 0, 0, 0));
+    fence_async_smem();
+  }
   if (warp == 9) tmem_alloc(s0 + oMisc + 64, 512);
   tc_fence_before();
   __syncthreads();
@@ -486,13 +492,17 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
       int n = 0, np = 0;                     // steps and pieces so far
       uint32_t par[2] = {0, 0};              // of P
       const uint64_t d_q = umma_desc_sw128(s0 + oQ, 16, 1024), d_k = umma_desc_sw128(s0 + oRing, 16, 1024), d_v = umma_desc_sw128(s0 + oRing, kEHalf, 1024);
+      // (no swizzle: rows of 16 bytes, eight of them in 128; the second eight columns are the zeros, at the leading offset)
+      const uint64_t d_ones = umma_desc_plain(s0 + oOnes, oZero - oOnes, 128), d_aug = umma_desc_plain(s0 + oAug, oZero - oAug, 128);
+      constexpr uint64_t kAugStep = (uint64_t)(kEN * 16 >> 4) - ((uint64_t)(kEN * 16 >> 4) << 16);  // the next slot begins later: its zeros are nearer
       auto qk = [&](int g, int i) {          // S of tile g at the piece's step i, and its arrival
         const uint64_t dk = d_k + (uint64_t)((2 * (n + i)) % kEStages) * (kETile >> 4), dq = d_q + (uint64_t)g * (kETile >> 4);
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
           const uint64_t off = (uint64_t)((ks >> 2) * (kEHalf >> 4) + (ks & 3) * 2);
-          umma_bf16(tmem + (uint32_t)g * 128, dq + off, dk + off, kDescQK, ks ? 1u : 0u);
+          umma_bf16(tmem + (uint32_t)g * 128, dq + off, dk + off, a.desc_qk, ks ? 1u : 0u);
         }
+        if (a.logdeg) umma_bf16(tmem + (uint32_t)g * 128, d_ones, d_aug + (uint64_t)((n + i) % kEBiasSlots) * kAugStep, kDescQK, 1u);
         umma_commit(b_s(g));
       };
       auto pv = [&](int g, int i, int ks0, bool more) {  // four of the eight steps of 16 slots
@@ -502,25 +512,33 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
           umma_bf16_ts(tmem + 256 + (uint32_t)g * 128, tmem + (uint32_t)g * 128 + 8 * (ks0 + ks), dv + (uint64_t)(ks0 + ks) * 128, kDescPV, (more || ks) ? 1u : 0u);
       };
       auto stage_full = [&](int idx) { return bar_wait(b_full(idx % kEStages), (uint32_t)((idx / kEStages) & 1)); };
+      auto keys = [&](int i) {               // of the piece's step i, and its log-degrees
+        return stage_full(2 * (n + i)) &&
+               (!a.logdeg || bar_wait(b_bias_ready((n + i) % kEBiasSlots), (uint32_t)(((n + i) / kEBiasSlots) & 1)));
+      };
+      auto release_keys = [&](int i) {
+        umma_commit(b_empty(2 * (n + i) % kEStages));
+        if (a.logdeg) umma_commit(b_aug_free((n + i) % kEBiasSlots));
+      };
       auto release = [&](int idx) { umma_commit(b_empty(idx % kEStages)); };
       while (ok && walk.next(a, p)) {
         const int steps = p.hi - p.lo;
         if (steps <= 0) continue;
         const int ahead = p.one ? 2 : 1;
-        if (!(ok = bar_wait(b_q, (uint32_t)(np++ & 1)) && stage_full(2 * n))) break;
+        if (!(ok = bar_wait(b_q, (uint32_t)(np++ & 1)) && keys(0))) break;
         tc_fence_after();
         qk(0, 0);
         if (p.one) {
-          release(2 * n);
+          release_keys(0);
           if (steps > 1) {
-            if (!(ok = stage_full(2 * (n + 1)))) break;
+            if (!(ok = keys(1))) break;
             tc_fence_after();
             qk(1, 1);
-            release(2 * (n + 1));
+            release_keys(1);
           }
         } else {
           qk(1, 0);
-          release(2 * n);
+          release_keys(0);
         }
         if (steps <= ahead) umma_commit(b_q_free);
         for (int i = 0; ok && i < steps; ++i) {
@@ -538,10 +556,10 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
             pv(g, i, 4, true);
             if (g == g1) release(2 * (n + i) + 1);
             if (more) {
-              if (g == g0 && !(ok = stage_full(2 * (n + i + ahead)))) break;
+              if (g == g0 && !(ok = keys(i + ahead))) break;
               tc_fence_after();
               qk(g, i + ahead);
-              if (g == g1) release(2 * (n + i + ahead));
+              if (g == g1) release_keys(i + ahead);
             } else if (!p.one) {
               umma_commit(b_o(g));
             }
@@ -575,30 +593,33 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
         if (lane == 0) mbar_arrive(b_v(st / 2));
       }
     }
-  } else if (warp == 11) {
-    // ---------------------------------------------------------------- log-degrees to base two, in place.  The type's largest values stay
-    // finite: where a caller masks slots with them, scores minus their maximum have to be numbers.  (Only log-degrees above
-    // 2^127 ln 2 in magnitude are changed by this.)
-    if (!a.logdeg) {
-      for (int c = lane; c < kEBiasSlots * kEN; c += 32) reinterpret_cast<float*>(smem + oBias)[c] = 0.f;
-      __syncwarp();
-      if (lane == 0)
-        for (int i = 0; i < kEBiasSlots; ++i) mbar_arrive(b_bias_ready(i));
-    } else {
-      int n = 0;
-      while (ok && walk.next(a, p)) {
-        for (int i = p.lo; i < p.hi; ++i, ++n) {
-          const int bs = n % kEBiasSlots;
-          if (!(ok = warp_wait(b_bias(bs), (uint32_t)((n / kEBiasSlots) & 1)))) break;
-          float4* const at = reinterpret_cast<float4*>(smem + oBias + bs * kEN * 4) + lane;
-          float4 b = *at;
-          auto base2 = [](float x) {
-            const float y = x * kLog2e;
-            return fabsf(y) == INFINITY && fabsf(x) != INFINITY ? copysignf(FLT_MAX, x) : y;
-          };
-          *at = make_float4(base2(b.x), base2(b.y), base2(b.z), base2(b.w));
-          __syncwarp();
-          if (lane == 0) mbar_arrive(b_bias_ready(bs));
+  } else if (warp == 11 && a.logdeg) {
+    // ---------------------------------------------------------------- log-degrees: three more columns of K, next to three ones in Q.  log n / |scale|
+    // as the sum of three bf16 holds 24 bits of it.  What the type's largest values become stays finite, here and times
+    // scale * log2 e: where a caller masks slots with them, scores minus their maximum have to be numbers.
+    const float inv = 1.f / a.scale, most = fminf(3.3e38f, 3e38f / (a.scale * kLog2e));
+    int n = 0;
+    while (ok && walk.next(a, p)) {
+      for (int i = p.lo; i < p.hi; ++i, ++n) {
+        const int bs = n % kEBiasSlots;
+        if (!(ok = warp_wait(b_bias(bs), (uint32_t)((n / kEBiasSlots) & 1)) && warp_wait(b_aug_free(bs), (uint32_t)(((n / kEBiasSlots) & 1) ^ 1)))) break;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int t = lane + 32 * k;
+          const float x = reinterpret_cast<const float*>(smem + oBias)[bs * kEN + t];
+          float b = x * inv;
+          if (fabsf(b) > most && fabsf(x) != INFINITY) b = copysignf(most, b);
+          const __nv_bfloat16 hi = __float2bfloat16_rn(b);
+          const float r1 = fabsf(b) < INFINITY ? b - __bfloat162float(hi) : 0.f;
+          const __nv_bfloat16 mid = __float2bfloat16_rn(r1);
+          st_shared_v4(s0 + oAug + (bs * kEN + t) * 16, make_uint4((uint32_t)__bfloat16_as_ushort(hi) | (uint32_t)__bfloat16_as_ushort(mid) << 16,
+                                                                  pack_bf16x2(r1 - __bfloat162float(mid), 0.f), 0, 0));
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(b_bias_free(bs));
+          mbar_arrive(b_bias_ready(bs));
         }
       }
     }
@@ -610,8 +631,8 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // (32 lanes of tensor memory per warp, lane number in the upper half word)
     const uint32_t t_s = tmem + lanes + (uint32_t)g * 128, t_o = t_s + 256;
     float2* const state = reinterpret_cast<float2*>(smem + oState);
-    const float scale = a.scale * kLog2e;  // (all in base two)
-    int n = 0, ns = 0, np = 0, nx = 0;  // steps, own steps, pieces, exchanges so far
+    const float scale = a.scale * kLog2e, slack = kSlack / scale;  // (a.scale is positive)
+    int ns = 0, np = 0, nx = 0;  // own steps, pieces, exchanges so far
     ExtendPiece note{0, 0, 0, 0, {0, 0}};
     while (ok && walk.next(a, p)) {
       const int steps = p.hi - p.lo, my_tok = tok + (p.one ? 0 : g * a.T);
@@ -621,10 +642,8 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
       const int lim_min = __reduce_min_sync(0xffffffffu, valid ? lim : INT32_MAX);
       float m = -INFINITY;
       f32x2 l2(0.f, 0.f);
-      for (int i = 0; i < steps; ++i, ++n) {
-        const int bs = n % kEBiasSlots;
+      for (int i = 0; i < steps; ++i) {
         const bool own = !p.one || (i & 1) == g;
-        if (!(ok = warp_wait(b_bias_ready(bs), a.logdeg ? (uint32_t)((n / kEBiasSlots) & 1) : 0u))) break;
         if (own) {
           if (!(ok = warp_wait(b_s(g), (uint32_t)(ns++ & 1)))) break;
           tc_fence_after();
@@ -634,17 +653,6 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
             constexpr bool MASK = decltype(mask)::value;
             float y[128];
             tmem_ld128(t_s, y);
-            const f32x2 sc(scale, scale);
-            const ulonglong2* const bias = reinterpret_cast<const ulonglong2*>(smem + oBias + bs * kEN * 4);
-#pragma unroll
-            for (int c = 0; c < 32; ++c) {
-              const ulonglong2 b4 = bias[c];
-              f32x2 lo, hi;
-              lo.v = b4.x;
-              hi.v = b4.y;
-              fma2(f32x2(y[4 * c], y[4 * c + 1]), sc, lo).get(y[4 * c], y[4 * c + 1]);
-              fma2(f32x2(y[4 * c + 2], y[4 * c + 3]), sc, hi).get(y[4 * c + 2], y[4 * c + 3]);
-            }
             if constexpr (MASK) {
               const int seen = lim - (p.lo + i) * kEN;
 #pragma unroll
@@ -657,9 +665,9 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
               for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], y[c + 2 * k], y[c + 2 * k + 1]);
             }
             const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
-            if (__any_sync(0xffffffffu, top > m + kSlack)) {
+            if (__any_sync(0xffffffffu, top > m + slack)) {
               const bool up = top > m;
-              const float f = up ? ex2(m - top) : 1.f;
+              const float f = up ? ex2((m - top) * scale) : 1.f;
               if (__any_sync(0xffffffffu, m > -INFINITY)) {  // O holds something (its last product is complete: S came behind it)
 #pragma unroll 1
                 for (int c = 0; c < 128; c += 8) {
@@ -673,8 +681,15 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
               l2 = mul2(l2, f32x2(f, f));
               m = up ? top : m;
             }
-            const float off = m == -INFINITY ? 0.f : -m;
-            const f32x2 mm(off, off);
+            float off = m == -INFINITY ? 0.f : -m * scale;
+            // (what the rounding of m * scale leaves is the same factor for all of a row's weights, unless m is a mask of the type's
+            // largest values)
+            if (__any_sync(0xffffffffu, fabsf(fmaf(m, scale, off)) > 0x1p-12f && m > -INFINITY)) {
+#pragma unroll
+              for (int c = 0; c < 128; ++c) y[c] -= m > -INFINITY ? m : 0.f;
+              off = 0.f;
+            }
+            const f32x2 sc(scale, scale), mm(off, off);
             f32x2 la(0.f, 0.f), lb(0.f, 0.f);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -684,8 +699,8 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
 #pragma unroll
                 for (int c = c0; c < c0 + 16; c += 4) {
                   float e[4];
-                  add2(f32x2(y[c], y[c + 1]), mm).get(e[0], e[1]);
-                  add2(f32x2(y[c + 2], y[c + 3]), mm).get(e[2], e[3]);
+                  fma2(f32x2(y[c], y[c + 1]), sc, mm).get(e[0], e[1]);
+                  fma2(f32x2(y[c + 2], y[c + 3]), sc, mm).get(e[2], e[3]);
 #pragma unroll
                   for (int k = 0; k < 4; ++k) e[k] = ex2(e[k]);
                   la = add2(la, f32x2(e[0], e[1]));
@@ -715,9 +730,9 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
             }
           }
         }
-        if (a.logdeg && lane == 0) mbar_arrive(b_bias_free(bs));
       }
       if (!ok) break;
+      m *= scale;  // (in base two from here on)
       float l;
       {
         float x, y;
@@ -972,6 +987,9 @@ int check_extend(const void* views, const void* q_begin, int64_t n_rows, int32_t
 int run_extend(ExtendArgs& a, const void* q, int64_t q_row, int64_t q_head, const void* k, const void* v, int64_t n_pages, void* workspace, cudaStream_t st) {
   if (a.n_rows == 0) return CKV_OK;
   a.T = kEN / a.G;
+  // log-degrees are divided by the scale: next to 1e-30 products vanish as they do next to zero
+  a.desc_qk = kDescQK | (a.scale < 0 ? kNegateA : 0u);
+  a.scale = std::max(std::fabs(a.scale), 1e-30f);
   a.max_slots = n_pages << a.shift;
   a.status = static_cast<int32_t*>(workspace);
   a.pieces = reinterpret_cast<ExtendPiece*>(static_cast<unsigned char*>(workspace) + 256);
