@@ -54,7 +54,7 @@ constexpr int kEThreads = kEWarps * 32;
 constexpr int kItemCost = 128;      // what an item costs beside its slots (queries in, rows out), in slots
 constexpr int kMinShare = 512;      // slots that a CTA takes at least
 constexpr float kSlack = 8.f;       // weights below 2^8
-constexpr int kPartRow = 132;       // floats of a partial row: O, m, sum, pad
+constexpr int kPartRow = 132;       // floats of a partial row: O, m, sum, pad; a piece's rows lie side by side, four floats of each
 // shared memory, from a 1024-byte boundary
 constexpr int oQ = 0;
 constexpr int oRing = oQ + 2 * kETile;
@@ -63,9 +63,11 @@ constexpr int oAug = oBias + kEBiasSlots * kEN * 4;       // 16 bytes per slot: 
 constexpr int oOnes = oAug + kEBiasSlots * kEN * 16;       // 16 bytes per row of Q: three ones
 constexpr int oZero = oOnes + kEN * 16;                    // the other eight columns of both
 constexpr int oState = oZero + kEN * 16;  // float2 [256]: m and sum of every row, exchanged by one-tile items
-constexpr int oBar = oState + 256 * 8;
-constexpr int oMisc = oBar + 384;
-constexpr int kEBytes = oMisc + 256;
+constexpr int oStage = oState + 256 * 8;                   // 2 KB per softmax warp: 32 columns of its rows on their way out
+constexpr int oBar = oStage + 8 * 2048;
+constexpr int oPieces = oBar + 512;
+constexpr int oMisc = oPieces + 256;
+constexpr int kEBytes = oMisc + 128;
 
 struct ExtendArgs {
   const ckv_paged_view* views;
@@ -119,41 +121,40 @@ __device__ __forceinline__ ExtendSeq extend_seq(const ExtendArgs& a, int b) {
   return s;
 }
 
-// A piece of an item: steps lo .. hi - 1 of its slots
-struct Piece {
+// A piece of an item: steps lo .. hi - 1 of its slots.  The TMA warp walks the CTA's stretch and passes its pieces to the other warps
+// through a ring in shared memory.
+constexpr int kEPieces = 4;
+enum : int { kOneTile = 1, kWhole = 2, kFirst = 4, kStop = 8 };
+struct __align__(16) Piece {
   int64_t row0;   // first row of q
-  int b, h, ntok;
-  int base;       // slot at which the item's first token stands
-  int end;        // slots that its last token sees
-  int lo, hi, steps;
-  bool one;       // one tile of rows
-  bool whole;
-  bool first;      // the item begins in this stretch
+  int h, ntok;    // KV head, tokens
+  int base, end;  // slot at which the item's first token stands, slots that its last token sees
+  int lo, hi;
+  int flags;      // one tile of rows; the whole item; the item begins in this stretch; there is no piece any more
+  int pad[3];
 };
 
-// A CTA's stretch, piece by piece.  Every warp walks it for itself.
 struct Walk {
   int64_t left, x;  // what is left of the stretch; offset in the item
   ExtendSeq s;
   int b, h, j;
-  __device__ __forceinline__ bool next(const ExtendArgs& a, Piece& p) {
+  // the next piece that has something to do, and its sequence
+  __device__ __forceinline__ bool next(const ExtendArgs& a, Piece& p, int& seq) {
     const int T2 = 2 * a.T;
     while (left > 0) {
       const int end = s.end(j, T2), steps = (end + kEN - 1) / kEN;
       const int64_t cost = (int64_t)end + kItemCost, to = min(x + left, cost);
       auto step_of = [&](int64_t y) { return (int)min(max(y - kItemCost + kEN / 2, (int64_t)0) / kEN, (int64_t)steps); };
-      p.lo = step_of(x);
       const bool ends = to == cost;
+      p.lo = step_of(x);
       p.hi = ends ? steps : step_of(to);
-      p.first = x == 0;
       p.row0 = s.row0 + (int64_t)j * T2;
-      p.b = b; p.h = h;
+      p.h = h;
       p.ntok = min(T2, s.n - j * T2);
       p.base = s.len - s.n + j * T2;
       p.end = end;
-      p.steps = steps;
-      p.one = p.ntok <= a.T;
-      p.whole = p.lo == 0 && p.hi == steps;
+      p.flags = (p.ntok <= a.T ? kOneTile : 0) | (p.lo == 0 && p.hi == steps ? kWhole : 0) | (x == 0 ? kFirst : 0);
+      seq = b;
       left -= to - x;
       x = to;
       if (ends) {
@@ -282,6 +283,7 @@ __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.
 __device__ __forceinline__ uint64_t umma_desc_plain(uint32_t smem_addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
   return (uint64_t)((smem_addr >> 4) & 0x3fffu) | ((uint64_t)((lbo_bytes >> 4) & 0x3fffu) << 16) | ((uint64_t)((sbo_bytes >> 4) & 0x3fffu) << 32) | (1ull << 46);
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); }
 __device__ __forceinline__ bool elect_one() {
   uint32_t ok;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
@@ -314,7 +316,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
   unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t s0 = smem_u32(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // barriers: full [stage] | empty [stage] | log-degrees full, free, in bf16, free [slot] | S full [tile] | P full [tile, half] | O full [tile] | Q full, empty | exchange | values ready [stage / 2]
+  // barriers: full [stage] | empty [stage] | log-degrees full, free, in bf16, free [slot] | S full [tile] | P full [tile, half] | O full [tile] | Q full, empty | exchange | values ready [stage / 2] | piece, free [slot]
   auto bar = [&](int i) { return s0 + oBar + 8u * i; };
   auto b_full = [&](int i) { return bar(i); };
   auto b_empty = [&](int i) { return bar(kEStages + i); };
@@ -328,7 +330,10 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
   auto b_o = [&](int g) { return bar(kRest + 6 + g); };
   const uint32_t b_q = bar(kRest + 8), b_q_free = bar(kRest + 9), b_x = bar(kRest + 10);
   auto b_v = [&](int i) { return bar(kRest + 11 + i); };
-  int64_t* const s_start = reinterpret_cast<int64_t*>(smem + oMisc);            // begin of the stretch in its sequence, left, sequence
+  auto b_piece = [&](int i) { return bar(kRest + 11 + kEStages / 2 + i); };
+  auto b_piece_free = [&](int i) { return bar(kRest + 11 + kEStages / 2 + kEPieces + i); };
+  Piece* const pieces = reinterpret_cast<Piece*>(smem + oPieces);
+  int64_t* const s_start = reinterpret_cast<int64_t*>(smem + oMisc);            // the stretch's offset in its sequence, sequence
   int64_t* const s_sum = reinterpret_cast<int64_t*>(smem + oState);             // (before the roles begin)
   volatile uint32_t* const s_tmem = reinterpret_cast<volatile uint32_t*>(smem + oMisc + 64);
 
@@ -353,9 +358,22 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     mbar_init(b_q_free, 1);
     mbar_init(b_x, 8);
     for (int i = 0; i < kEStages / 2; ++i) mbar_init(b_v(i), 1);
+    for (int i = 0; i < kEPieces; ++i) {
+      mbar_init(b_piece(i), 1);
+      mbar_init(b_piece_free(i), 10 + (a.logdeg ? 1 : 0));  // softmax warps, MMA, warps 10 and 11
+    }
     mbar_init_fence();
     s_start[0] = -1;
+    prefetch_map(&tm_q);
+    prefetch_map(&tm_k);
+    prefetch_map(&tm_v);
   }
+  if (tid < kEN) {
+    st_shared_v4(s0 + oOnes + tid * 16, make_uint4(0x3f803f80u, 0x00003f80u, 0, 0));
+    st_shared_v4(s0 + oZero + tid * 16, make_uint4(0, 0, 0, 0));
+    fence_async_smem();
+  }
+  if (warp == 9) tmem_alloc(s0 + oMisc + 64, 512);
   griddep_wait();
   griddep_launch();
   if (blockIdx.x == 0 && tid == 0) *a.status = 0;
@@ -375,6 +393,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     if (lane >= o) upto += y;
   }
   if (lane == 31) s_sum[warp] = upto;
+  tc_fence_before();
   __syncthreads();
   int64_t total = 0, at = upto - mine;
   for (int w = 0; w < kEWarps; ++w) {
@@ -400,61 +419,71 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
   ExtendPiece* const mark = a.pieces + blockIdx.x;
   if (offset < 0) {  // no work
     if (tid == 0) *mark = ExtendPiece{0, 0, 0, 0, {0, 0}};
+    if (warp == 9) tmem_dealloc(*s_tmem, 512);
     return;
   }
-  Walk walk;
-  walk.b = (int)s_start[1];
-  walk.s = extend_seq(a, walk.b);
-  walk.left = min(share, total - begin);
-  {
-    const int items = walk.s.items(T2);
-    const int64_t head = walk.s.before(items, T2);
-    walk.h = (int)(offset / head);
-    const int64_t in_head = offset - walk.h * head;
-    int lo = 0, hi = items;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (walk.s.before(mid, T2) <= in_head) lo = mid; else hi = mid;
-    }
-    walk.j = lo;
-    walk.x = in_head - walk.s.before(lo, T2);
-  }
-  const int64_t item_begin = begin - walk.x;  // of the item in which the stretch begins, on the line of all items
-
-  if (tid < kEN) {
-    st_shared_v4(s0 + oOnes + tid * 16, make_uint4(0x3f803f80u, 0x00003f80u, 0, 0));
-    st_shared_v4(s0 + oZero + tid * 16, make_uint4(0, 0, 0, 0));
-    fence_async_smem();
-  }
-  if (warp == 9) tmem_alloc(s0 + oMisc + 64, 512);
-  tc_fence_before();
-  __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
   bool ok = true;
-  Piece p;
+  // the other warps' side of the ring of pieces: the next one, or none; one arrival per warp gives a slot back
+  int np = 0;
+  auto next_piece = [&](auto wait) {
+    if (!(ok = wait(b_piece(np % kEPieces), (uint32_t)((np / kEPieces) & 1)))) return false;
+    return !(pieces[np % kEPieces].flags & kStop);
+  };
+  auto piece_done = [&] {
+    mbar_arrive(b_piece_free(np % kEPieces));
+    ++np;
+  };
 
   if (warp >= 8) {
   give_registers<kEOtherRegs>();
   if (warp == 8) {
-    // ---------------------------------------------------------------- TMA
+    // ---------------------------------------------------------------- TMA, and the walk along the stretch
+    Walk walk;
+    walk.b = (int)s_start[1];
+    walk.s = extend_seq(a, walk.b);
+    walk.left = min(share, total - begin);
+    {
+      const int items = walk.s.items(T2);
+      const int64_t head = walk.s.before(items, T2);
+      walk.h = (int)(offset / head);
+      const int64_t in_head = offset - walk.h * head;
+      int lo = 0, hi = items;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (walk.s.before(mid, T2) <= in_head) lo = mid; else hi = mid;
+      }
+      walk.j = lo;
+      walk.x = in_head - walk.s.before(lo, T2);
+    }
+    ExtendPiece note{0, 0, 0, (int32_t)((begin - walk.x) / share), {0, 0}};  // (the CTA in which the first item begins)
     const int run = min(kEN, 1 << a.shift), runs = kEN / run;  // slots of a step that lie in one page
     const int rr = (lane >> 1) % runs, half = lane & 1;
-    int n = 0, np = 0;                                         // steps and pieces so far
-    while (ok && walk.next(a, p)) {
-      if (p.lo >= p.hi) continue;
-      const int32_t* const table = a.views[p.b].block_table;
+    int n = 0, nq = 0, seq = 0;                                // steps so far, pieces with steps, sequence
+    Piece p;
+    while (true) {
+      const bool more = walk.next(a, p, seq);
+      if (!more) p.flags = kStop;
+      if (!(ok = warp_wait(b_piece_free(np % kEPieces), (uint32_t)(((np / kEPieces) & 1) ^ 1)))) break;
+      if (lane == 0) {
+        pieces[np % kEPieces] = p;
+        mbar_arrive(b_piece(np % kEPieces));
+      }
+      ++np;
+      if (!more) break;
+      if (!(p.flags & kWhole)) {
+        note.held[p.flags & kFirst ? 1 : 0] = 1;
+        if (p.lo > 0 && p.hi * kEN >= p.end) {  // it ends an item that it did not begin
+          note.row0 = p.row0;
+          note.h = p.h;
+          note.ntok = p.ntok;
+        }
+      }
+      const int32_t* const table = a.views[seq].block_table;
       const int n_blocks = (p.end + (1 << a.shift) - 1) >> a.shift;
       int win = -32;
       int32_t cur = 0, nxt = 0;
-      if (!(ok = warp_wait(b_q_free, (uint32_t)((np & 1) ^ 1)))) break;
-      ++np;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(b_q, (uint32_t)(4 * a.T * a.G * 128));
-        for (int g = 0; g < 2; ++g)
-          for (int f = 0; f < 2; ++f)
-            tma_load_3d(s0 + oQ + g * kETile + f * kEHalf, &tm_q, 64 * f, p.h * a.G, (int)p.row0 + (p.one ? 0 : g * a.T), b_q);
-      }
       for (int i = p.lo; i < p.hi; ++i, ++n) {
         const int t0 = i * kEN, blk0 = t0 >> a.shift;
         if ((blk0 & ~31) != win) {
@@ -483,13 +512,24 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
             if (mine_ && half == 0) bulk_load(s0 + oBias + (bs * kEN + rr * run) * 4, a.logdeg + row, run * 4, b_bias(bs));
           }
         }
+        if (ok && i == p.lo) {  // the queries' place is free only when the last item's products are done: its first keys come before
+          if (!(ok = warp_wait(b_q_free, (uint32_t)((nq++ & 1) ^ 1)))) break;
+          if (lane == 0) {
+            mbar_arrive_expect_tx(b_q, (uint32_t)(4 * a.T * a.G * 128));
+            for (int g = 0; g < 2; ++g)
+              for (int f = 0; f < 2; ++f)
+                tma_load_3d(s0 + oQ + g * kETile + f * kEHalf, &tm_q, 64 * f, p.h * a.G, (int)p.row0 + (p.flags & kOneTile ? 0 : g * a.T), b_q);
+          }
+        }
         if (!ok) break;
       }
+      if (!ok) break;
     }
+    if (lane == 0) *mark = note;
   } else if (warp == 9) {
     // ---------------------------------------------------------------- MMA: one thread
     if (elect_one()) {
-      int n = 0, np = 0;                     // steps and pieces so far
+      int n = 0, nq = 0;                     // steps, pieces with steps so far
       uint32_t par[2] = {0, 0};              // of P
       const uint64_t d_q = umma_desc_sw128(s0 + oQ, 16, 1024), d_k = umma_desc_sw128(s0 + oRing, 16, 1024), d_v = umma_desc_sw128(s0 + oRing, kEHalf, 1024);
       // (no swizzle: rows of 16 bytes, eight of them in 128; the second eight columns are the zeros, at the leading offset)
@@ -521,14 +561,16 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
         if (a.logdeg) umma_commit(b_aug_free((n + i) % kEBiasSlots));
       };
       auto release = [&](int idx) { umma_commit(b_empty(idx % kEStages)); };
-      while (ok && walk.next(a, p)) {
-        const int steps = p.hi - p.lo;
+      while (next_piece(bar_wait)) {
+        const int steps = pieces[np % kEPieces].hi - pieces[np % kEPieces].lo;
+        const bool one = pieces[np % kEPieces].flags & kOneTile;
+        piece_done();
         if (steps <= 0) continue;
-        const int ahead = p.one ? 2 : 1;
-        if (!(ok = bar_wait(b_q, (uint32_t)(np++ & 1)) && keys(0))) break;
+        const int ahead = one ? 2 : 1;
+        if (!(ok = bar_wait(b_q, (uint32_t)(nq++ & 1)) && keys(0))) break;
         tc_fence_after();
         qk(0, 0);
-        if (p.one) {
+        if (one) {
           release_keys(0);
           if (steps > 1) {
             if (!(ok = keys(1))) break;
@@ -542,7 +584,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
         }
         if (steps <= ahead) umma_commit(b_q_free);
         for (int i = 0; ok && i < steps; ++i) {
-          const int g0 = p.one ? i & 1 : 0, g1 = p.one ? g0 : 1;
+          const int g0 = one ? i & 1 : 0, g1 = one ? g0 : 1;
           const bool more = i + ahead < steps;
           const int iv = n + i;
           if (!(ok = bar_wait(b_v(iv % (kEStages / 2)), (uint32_t)((iv / (kEStages / 2)) & 1)))) break;
@@ -560,13 +602,14 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
               tc_fence_after();
               qk(g, i + ahead);
               if (g == g1) release_keys(i + ahead);
-            } else if (!p.one) {
+            } else if (!one) {
               umma_commit(b_o(g));
             }
           }
           if (i + ahead == steps - 1) umma_commit(b_q_free);
         }
-        if (ok && p.one) {
+        if (!ok) break;
+        if (one) {
           umma_commit(b_o(0));
           umma_commit(b_o(1));
         }
@@ -577,9 +620,12 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     // ---------------------------------------------------------------- slots behind the last that an item sees: whatever their values
     // are, they must not meet a weight of zero
     int n = 0;
-    while (ok && walk.next(a, p)) {
-      for (int i = p.lo; i < p.hi; ++i, ++n) {
-        const int st = (2 * n + 1) % kEStages, seen = p.end - i * kEN;
+    while (next_piece(warp_wait)) {
+      const int end = pieces[np % kEPieces].end, lo = pieces[np % kEPieces].lo, hi = pieces[np % kEPieces].hi;
+      __syncwarp();
+      if (lane == 0) piece_done(); else ++np;
+      for (int i = lo; i < hi; ++i, ++n) {
+        const int st = (2 * n + 1) % kEStages, seen = end - i * kEN;
         if (!(ok = warp_wait(b_full(st), (uint32_t)(((2 * n + 1) / kEStages) & 1)))) break;
         if (seen < kEN) {
           const uint32_t vt = s0 + oRing + (uint32_t)st * kETile;
@@ -592,6 +638,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
         __syncwarp();
         if (lane == 0) mbar_arrive(b_v(st / 2));
       }
+      if (!ok) break;
     }
   } else if (warp == 11 && a.logdeg) {
     // ---------------------------------------------------------------- log-degrees: three more columns of K, next to three ones in Q.  log n / |scale|
@@ -599,8 +646,11 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     // scale * log2 e: where a caller masks slots with them, scores minus their maximum have to be numbers.
     const float inv = 1.f / a.scale, most = fminf(3.3e38f, 3e38f / (a.scale * kLog2e));
     int n = 0;
-    while (ok && walk.next(a, p)) {
-      for (int i = p.lo; i < p.hi; ++i, ++n) {
+    while (next_piece(warp_wait)) {
+      const int steps = pieces[np % kEPieces].hi - pieces[np % kEPieces].lo;
+      __syncwarp();
+      if (lane == 0) piece_done(); else ++np;
+      for (int i = 0; i < steps; ++i, ++n) {
         const int bs = n % kEBiasSlots;
         if (!(ok = warp_wait(b_bias(bs), (uint32_t)((n / kEBiasSlots) & 1)) && warp_wait(b_aug_free(bs), (uint32_t)(((n / kEBiasSlots) & 1) ^ 1)))) break;
 #pragma unroll
@@ -622,6 +672,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
           mbar_arrive(b_bias_ready(bs));
         }
       }
+      if (!ok) break;
     }
   }
   } else {
@@ -632,18 +683,20 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     const uint32_t t_s = tmem + lanes + (uint32_t)g * 128, t_o = t_s + 256;
     float2* const state = reinterpret_cast<float2*>(smem + oState);
     const float scale = a.scale * kLog2e, slack = kSlack / scale;  // (a.scale is positive)
-    int ns = 0, np = 0, nx = 0;  // own steps, pieces, exchanges so far
-    ExtendPiece note{0, 0, 0, 0, {0, 0}};
-    while (ok && walk.next(a, p)) {
-      const int steps = p.hi - p.lo, my_tok = tok + (p.one ? 0 : g * a.T);
+    int ns = 0, no = 0, nx = 0;  // own steps, pieces with steps, exchanges so far
+    while (next_piece(warp_wait)) {
+      const Piece& p = pieces[np % kEPieces];
+      const int lo = p.lo, steps = p.hi - lo;
+      const bool one = p.flags & kOneTile;
+      const int my_tok = tok + (one ? 0 : g * a.T);
       const bool valid = tok < a.T && my_tok < p.ntok;
       const bool busy = __any_sync(0xffffffffu, valid);
-      const int lim = valid ? p.base + my_tok + 1 : 0;  // slots that this row sees
+      const int lim = valid ? p.base + my_tok + 1 - lo * kEN : 0;  // slots of the piece that this row sees
       const int lim_min = __reduce_min_sync(0xffffffffu, valid ? lim : INT32_MAX);
       float m = -INFINITY;
       f32x2 l2(0.f, 0.f);
       for (int i = 0; i < steps; ++i) {
-        const bool own = !p.one || (i & 1) == g;
+        const bool own = !one || (i & 1) == g;
         if (own) {
           if (!(ok = warp_wait(b_s(g), (uint32_t)(ns++ & 1)))) break;
           tc_fence_after();
@@ -654,7 +707,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
             float y[128];
             tmem_ld128(t_s, y);
             if constexpr (MASK) {
-              const int seen = lim - (p.lo + i) * kEN;
+              const int seen = lim - i * kEN;
 #pragma unroll
               for (int c = 0; c < 128; ++c) y[c] = c < seen ? y[c] : -INFINITY;
             }
@@ -718,7 +771,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
             l2 = add2(l2, add2(la, lb));
           };
           if (busy) {
-            if ((p.lo + i + 1) * kEN > lim_min)
+            if ((i + 1) * kEN > lim_min)
               step(std::true_type{});
             else
               step(std::false_type{});
@@ -741,15 +794,14 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
       }
       // ------------------------------------------------------------ rows out
       if (steps > 0) {
-        if (!(ok = warp_wait(b_o(g), (uint32_t)(np++ & 1)))) break;
+        if (!(ok = warp_wait(b_o(g), (uint32_t)(no++ & 1)))) break;
         tc_fence_after();
       }
-      const int64_t row = p.row0 + my_tok;
-      __nv_bfloat16* const out = a.out + (row * a.H * a.G + p.h * a.G + head) * kED;
-      const int slot = p.first ? 1 : 0;
-      float* const part = a.partial + ((int64_t)(2 * blockIdx.x + slot) * a.slot_rows + my_tok * a.G + head) * kPartRow;
+      const bool whole = p.flags & kWhole;
+      const int slot = p.flags & kFirst ? 1 : 0;
+      float4* const part = reinterpret_cast<float4*>(a.partial + (int64_t)(2 * blockIdx.x + slot) * a.slot_rows * kPartRow) + my_tok * a.G + head;
       float f0 = 1.f, f1 = 0.f;
-      if (p.one && steps > 0) {  // two states of the same rows
+      if (one && steps > 0) {  // two states of the same rows
         state[tid] = make_float2(m, l);
         __syncwarp();
         if (lane == 0) mbar_arrive(b_x);
@@ -761,16 +813,18 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
         l = x0.y * f0 + x1.y * f1;
       }
       if (busy) {
-        const float inv = !p.whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+        __nv_bfloat16* const out = a.out + (p.row0 * a.H * a.G + p.h * a.G) * kED;
+        const uint32_t stage = s0 + oStage + warp * 2048;
+        const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
         // a one-tile item's columns are shared between the two tiles' warps
-        const int c0 = p.one && steps > 0 ? 2 * g : 0, c1 = p.one && steps > 0 ? c0 + 2 : (p.one && g == 1) ? 0 : 4;
+        const int c0 = one && steps > 0 ? 2 * g : 0, c1 = one && steps > 0 ? c0 + 2 : (one && g == 1) ? 0 : 4;
         for (int c = c0; c < c1; ++c) {
           float o[32];
           if (steps > 0) {
-            tmem_ld32((p.one ? tmem + lanes + 256 : t_o) + 32 * c, o);
+            tmem_ld32((one ? tmem + lanes + 256 : t_o) + 32 * c, o);
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = f0 == 0.f ? 0.f : o[k] * f0;
-            if (p.one && steps > 1) {
+            if (one && steps > 1) {
               float u[32];
               tmem_ld32(tmem + lanes + 384 + 32 * c, u);
 #pragma unroll
@@ -780,35 +834,39 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = 0.f;
           }
-          if (valid && p.whole) {
+          if (whole) {
+            // A row per thread would be 32 lines per store: the warp's 32 columns are turned in shared memory, four lanes to a row.
 #pragma unroll
-            for (int k = 0; k < 32; k += 8)
-              *reinterpret_cast<uint4*>(out + 32 * c + k) = make_uint4(pack_bf16x2(o[k] * inv, o[k + 1] * inv), pack_bf16x2(o[k + 2] * inv, o[k + 3] * inv),
-                                                                       pack_bf16x2(o[k + 4] * inv, o[k + 5] * inv), pack_bf16x2(o[k + 6] * inv, o[k + 7] * inv));
+            for (int k = 0; k < 4; ++k)
+              st_shared_v4(stage + lane * 64 + ((k ^ (lane >> 1)) & 3) * 16,
+                           make_uint4(pack_bf16x2(o[8 * k] * inv, o[8 * k + 1] * inv), pack_bf16x2(o[8 * k + 2] * inv, o[8 * k + 3] * inv),
+                                      pack_bf16x2(o[8 * k + 4] * inv, o[8 * k + 5] * inv), pack_bf16x2(o[8 * k + 6] * inv, o[8 * k + 7] * inv)));
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int from = 8 * k + (lane >> 2);
+              const int to = __shfl_sync(0xffffffffu, valid ? (my_tok * a.H * a.G + head) * kED : -1, from);
+              uint4 v;
+              ld_shared_v4(stage + from * 64 + ((lane ^ (from >> 1)) & 3) * 16, v);
+              if (to >= 0) *reinterpret_cast<uint4*>(out + to + 32 * c + (lane & 3) * 8) = v;
+            }
+            __syncwarp();
           } else if (valid) {
 #pragma unroll
-            for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(part + 32 * c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+            for (int k = 0; k < 8; ++k) part[(8 * c + k) * a.slot_rows] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
           }
         }
-        if (valid && !p.whole && (!p.one || g == 0)) *reinterpret_cast<float2*>(part + kED) = make_float2(m, l);
+        if (valid && !whole && (!one || g == 0)) part[32 * a.slot_rows] = make_float4(m, l, 0.f, 0.f);
       }
-      if (p.one && steps > 0) {  // nobody goes on to the next piece's products before both have read
+      if (one && steps > 0) {  // nobody goes on to the next piece's products before both have read
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(b_x);
         if (!(ok = warp_wait(b_x, (uint32_t)(nx++ & 1)))) break;
       }
-      if (!p.whole) {
-        note.held[slot] = 1;
-        if (p.lo > 0 && p.hi == p.steps) {
-          note.row0 = p.row0;
-          note.h = p.h;
-          note.ntok = p.ntok;
-          note.first = (int32_t)(item_begin / share);
-        }
-      }
+      __syncwarp();
+      if (lane == 0) piece_done(); else ++np;
     }
-    if (tid == 0) *mark = note;
   }
   if (!ok) {
     *a.status = 1;
@@ -839,18 +897,21 @@ __global__ void __launch_bounds__(kJoinWarps * 32) extend_join_kernel(const Exte
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     const int p0 = together ? warp : 0, dp = together ? kJoinWarps : 1;
     for (int p = p0; p < n; p += 8 * dp) {
-      float2 ml[8];
-      float4 y[8];
+      float4 ml[8], y[8];
+      int held[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {  // (every address is in the workspace, whether something was left there or not)
+        const int q = min(p + u * dp, n - 1), c = last.first + q, slot = q == 0 ? 1 : 0;
+        const float4* const at = reinterpret_cast<const float4*>(a.partial + (int64_t)(2 * c + slot) * a.slot_rows * kPartRow) + r;
+        held[u] = a.pieces[c].held[slot];
+        ml[u] = at[32 * a.slot_rows];
+        y[u] = at[lane * a.slot_rows];
+      }
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int c = last.first + p + u * dp, slot = p + u * dp == 0 ? 1 : 0;
-        ml[u] = make_float2(-INFINITY, 0.f);
+        if (p + u * dp < n && held[u]) continue;
+        ml[u] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
         y[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (p + u * dp < n && a.pieces[c].held[slot]) {
-          const float* const at = a.partial + ((int64_t)(2 * c + slot) * a.slot_rows + r) * kPartRow;
-          ml[u] = *reinterpret_cast<const float2*>(at + kED);
-          y[u] = *reinterpret_cast<const float4*>(at + 4 * lane);
-        }
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
@@ -1010,7 +1071,7 @@ int run_extend(ExtendArgs& a, const void* q, int64_t q_row, int64_t q_head, cons
   if (!extend_ready()) return CKV_ERR_CUDA;
   const unsigned ctas = (unsigned)sm_count();
   if (launch_dependent(extend_kernel, dim3(ctas), dim3(kEThreads), kEBytes + 1024, st, tm[0], tm[1], tm[2], a) != cudaSuccess) return CKV_ERR_CUDA;
-  return launch_dependent(extend_join_kernel, dim3(ctas, (unsigned)std::min(a.slot_rows, 2 * kEN / kJoinWarps)), dim3(kJoinWarps * 32), 0, st, a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
+  return launch_dependent(extend_join_kernel, dim3(ctas, (unsigned)std::max((a.slot_rows + kJoinWarps - 1) / kJoinWarps, std::min(a.slot_rows, 8))), dim3(kJoinWarps * 32), 0, st, a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
 }  // namespace
