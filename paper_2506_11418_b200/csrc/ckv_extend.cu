@@ -877,76 +877,70 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
   if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
-// Joins the pieces of the items that CTA blockIdx.x of the kernel above ended and did not begin.  Rows are dealt to gridDim.y CTAs: a warp
-// per row where there are few pieces, else a CTA per row, whose warps share them.
+// Joins the pieces of the item that CTA blockIdx.x of the kernel above ended and did not begin, 32 rows per CTA, 16 columns per warp.  A
+// lane has a row, so that loads are whole lines and a store is a sector; where there are few rows (single tokens over a long cache, and
+// then many pieces), the lanes that are left share a row's pieces.
 constexpr int kJoinWarps = 8;
-constexpr int kJoinTogether = 24;  // pieces from which on a row's are shared by a CTA's warps
+constexpr int kJoinRows = 32;
 
 __global__ void __launch_bounds__(kJoinWarps * 32) extend_join_kernel(const ExtendArgs a) {
-  __shared__ float2 s_ml[kJoinWarps];
-  __shared__ float4 s_o[kJoinWarps][32];
   griddep_wait();
   griddep_launch();
   const ExtendPiece last = a.pieces[blockIdx.x];
-  if (last.ntok == 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int rows = last.ntok * a.G, n = (int)blockIdx.x - last.first + 1;
-  const bool together = n > kJoinTogether;
-  for (int r = together ? (int)blockIdx.y : (int)blockIdx.y * kJoinWarps + warp; r < rows; r += (int)gridDim.y * (together ? 1 : kJoinWarps)) {
-    float m = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int p0 = together ? warp : 0, dp = together ? kJoinWarps : 1;
-    for (int p = p0; p < n; p += 8 * dp) {
-      float4 ml[8], y[8];
-      int held[8];
+  const int n = (int)blockIdx.x - last.first + 1, row0 = (int)blockIdx.y * kJoinRows, rows = min(last.ntok * a.G - row0, kJoinRows);
+  if (rows <= 0) return;
+  const int RB = rows > 16 ? 32 : rows > 8 ? 16 : rows > 4 ? 8 : 4, S = 32 / RB;  // lanes with a row each, times lanes that share its pieces
+  const int r = row0 + min(lane % RB, rows - 1);
+  float m = -INFINITY, l = 0.f;
+  float o[16];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {  // (every address is in the workspace, whether something was left there or not)
-        const int q = min(p + u * dp, n - 1), c = last.first + q, slot = q == 0 ? 1 : 0;
-        const float4* const at = reinterpret_cast<const float4*>(a.partial + (int64_t)(2 * c + slot) * a.slot_rows * kPartRow) + r;
-        held[u] = a.pieces[c].held[slot];
-        ml[u] = at[32 * a.slot_rows];
-        y[u] = at[lane * a.slot_rows];
-      }
+  for (int k = 0; k < 16; ++k) o[k] = 0.f;
+  auto add = [&](float pm, float pl, const float (&y)[16]) {
+    const float mm = fmaxf(m, pm);
+    if (mm == -INFINITY && !(pl != 0.f)) return;  // (no slots, or only such of weight zero)
+    const float c = m == -INFINITY ? 0.f : exp2f(m - mm), f = pm == -INFINITY ? 0.f : exp2f(pm - mm);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        if (p + u * dp < n && held[u]) continue;
-        ml[u] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-        y[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-      }
+    for (int k = 0; k < 16; ++k) o[k] = fmaf(f, y[k], o[k] * c);
+    l = fmaf(f, pl, l * c);
+    m = mm;
+  };
+  constexpr int U = 4;
+  for (int p = lane / RB; p < n; p += U * S) {
+    float4 ml[U], y[U][4];
+    int held[U];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const float mm = fmaxf(m, ml[u].x);
-        if (mm == -INFINITY && !(ml[u].y != 0.f)) continue;  // (no slots, or only such of weight zero)
-        const float c = m == -INFINITY ? 0.f : exp2f(m - mm), f = ml[u].x == -INFINITY ? 0.f : exp2f(ml[u].x - mm);
-        o = make_float4(fmaf(f, y[u].x, o.x * c), fmaf(f, y[u].y, o.y * c), fmaf(f, y[u].z, o.z * c), fmaf(f, y[u].w, o.w * c));
-        l = fmaf(f, ml[u].y, l * c);
-        m = mm;
-      }
+    for (int u = 0; u < U; ++u) {  // (every address is in the workspace, whether something was left there or not)
+      const int q = min(p + u * S, n - 1), c = last.first + q, slot = q == 0 ? 1 : 0;
+      const float4* const at = reinterpret_cast<const float4*>(a.partial + (int64_t)(2 * c + slot) * a.slot_rows * kPartRow) + r;
+      held[u] = a.pieces[c].held[slot];
+      ml[u] = at[32 * a.slot_rows];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[u][k] = at[(4 * warp + k) * a.slot_rows];
     }
-    if (together) {
-      s_o[warp][lane] = o;
-      if (lane == 0) s_ml[warp] = make_float2(m, l);
-      __syncthreads();
-      if (warp == 0) {
-        m = -INFINITY;
-        for (int w = 0; w < kJoinWarps; ++w) m = fmaxf(m, s_ml[w].x);
-        l = 0.f;
-        o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int w = 0; w < kJoinWarps; ++w) {
-          const float f = s_ml[w].x == -INFINITY ? 0.f : exp2f(s_ml[w].x - m);
-          const float4 y = s_o[w][lane];
-          l = fmaf(f, s_ml[w].y, l);
-          o = make_float4(fmaf(f, y.x, o.x), fmaf(f, y.y, o.y), fmaf(f, y.z, o.z), fmaf(f, y.w, o.w));
-        }
-      }
-      __syncthreads();
-    }
-    if (!together || warp == 0) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int tok = r / a.G, head = r - tok * a.G;
-      store4(a.out + ((last.row0 + tok) * a.H * a.G + last.h * a.G + head) * kED + 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (p + u * S >= n || !held[u]) continue;
+      const float x[16] = {y[u][0].x, y[u][0].y, y[u][0].z, y[u][0].w, y[u][1].x, y[u][1].y, y[u][1].z, y[u][1].w,
+                           y[u][2].x, y[u][2].y, y[u][2].z, y[u][2].w, y[u][3].x, y[u][3].y, y[u][3].z, y[u][3].w};
+      add(ml[u].x, ml[u].y, x);
     }
   }
+  for (int d = RB; d < 32; d <<= 1) {
+    const float pm = __shfl_xor_sync(0xffffffffu, m, d), pl = __shfl_xor_sync(0xffffffffu, l, d);
+    float x[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) x[k] = __shfl_xor_sync(0xffffffffu, o[k], d);
+    add(pm, pl, x);
+  }
+  if (lane >= rows) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int tok = r / a.G, head = r - tok * a.G;
+  uint4* const out = reinterpret_cast<uint4*>(a.out + ((last.row0 + tok) * a.H * a.G + last.h * a.G + head) * kED + 16 * warp);
+#pragma unroll
+  for (int k = 0; k < 16; k += 8)
+    out[k / 8] = make_uint4(pack_bf16x2(o[k] * inv, o[k + 1] * inv), pack_bf16x2(o[k + 2] * inv, o[k + 3] * inv), pack_bf16x2(o[k + 4] * inv, o[k + 5] * inv),
+                            pack_bf16x2(o[k + 6] * inv, o[k + 7] * inv));
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -1071,7 +1065,7 @@ int run_extend(ExtendArgs& a, const void* q, int64_t q_row, int64_t q_head, cons
   if (!extend_ready()) return CKV_ERR_CUDA;
   const unsigned ctas = (unsigned)sm_count();
   if (launch_dependent(extend_kernel, dim3(ctas), dim3(kEThreads), kEBytes + 1024, st, tm[0], tm[1], tm[2], a) != cudaSuccess) return CKV_ERR_CUDA;
-  return launch_dependent(extend_join_kernel, dim3(ctas, (unsigned)std::max((a.slot_rows + kJoinWarps - 1) / kJoinWarps, std::min(a.slot_rows, 8))), dim3(kJoinWarps * 32), 0, st, a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
+  return launch_dependent(extend_join_kernel, dim3(ctas, (unsigned)(a.slot_rows + kJoinRows - 1) / kJoinRows), dim3(kJoinWarps * 32), 0, st, a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
 }  // namespace
