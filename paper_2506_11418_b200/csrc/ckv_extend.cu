@@ -12,6 +12,7 @@
 //                   more than 2^kSlack, so that O is rarely touched.  The log-degree is in s already (warp 11).
 //   warp 8          TMA: the item's queries, and keys, values and log-degrees through a ring of four 32 KB stages
 //   warp 9          issues the MMAs: PV of one tile and the next QK^T of it while the other tile's softmax runs
+//   warps 12-15     over four-bit pages only: codes and scales to bf16 tiles, in place of the TMA warp's keys and values
 //   warps 10, 11    values behind an item's last slot to zero; log-degrees as three more columns of K
 // Tensor memory: S0 | S1 | O0 | O1, 128 columns each, all 512.
 // An item with one tile only (single tokens, short chunks) uses the second set for every other step of slots: two softmax
@@ -48,9 +49,12 @@ constexpr int kEStages = 4;         // tiles in flight: keys in the even ones, v
 constexpr int kETile = kEN * kED * 2;
 constexpr int kEHalf = kETile / 2;  // 64 columns of a tile: 128 rows of 128 bytes
 constexpr int kEBiasSlots = 4;
-constexpr int kEWarps = 12;
-constexpr int kESoftmaxRegs = 216, kEOtherRegs = 72;  // two warps of the first and one of the second on each quarter of an SM: 3 x 168, as launched
-constexpr int kEThreads = kEWarps * 32;
+// Threads and registers: two softmax warps, one of warps 8-11 and, over four-bit pages, one that unpacks on each quarter of an SM;
+// their shares add up to what the block is launched with (3 x 168, 4 x 128).
+template <bool QUANT> constexpr int kEWarps = QUANT ? 16 : 12;
+template <bool QUANT> constexpr int kESoftmaxRegs = QUANT ? 176 : 216;
+constexpr int kEOtherRegs = 72;
+constexpr int kEUnpackRegs = 88;
 constexpr int kItemCost = 128;      // what an item costs beside its slots (queries in, rows out), in slots
 constexpr int kMinShare = 512;      // slots that a CTA takes at least
 constexpr float kSlack = 8.f;       // weights below 2^8
@@ -131,15 +135,15 @@ struct __align__(16) Piece {
   int base, end;  // slot at which the item's first token stands, slots that its last token sees
   int lo, hi;
   int flags;      // one tile of rows; the whole item; the item begins in this stretch; there is no piece any more
-  int pad[3];
+  int seq;
 };
 
 struct Walk {
   int64_t left, x;  // what is left of the stretch; offset in the item
   ExtendSeq s;
   int b, h, j;
-  // the next piece that has something to do, and its sequence
-  __device__ __forceinline__ bool next(const ExtendArgs& a, Piece& p, int& seq) {
+  // the next piece that has something to do
+  __device__ __forceinline__ bool next(const ExtendArgs& a, Piece& p) {
     const int T2 = 2 * a.T;
     while (left > 0) {
       const int end = s.end(j, T2), steps = (end + kEN - 1) / kEN;
@@ -154,7 +158,7 @@ struct Walk {
       p.base = s.len - s.n + j * T2;
       p.end = end;
       p.flags = (p.ntok <= a.T ? kOneTile : 0) | (p.lo == 0 && p.hi == steps ? kWhole : 0) | (x == 0 ? kFirst : 0);
-      seq = b;
+      p.seq = b;
       left -= to - x;
       x = to;
       if (ends) {
@@ -307,10 +311,39 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
   return false;
 }
 
+// Four scale bytes as pairs of equal bf16: 2^(byte - 127), 255 NaN
+__device__ __forceinline__ void scales_bf16x2(uint32_t w, uint32_t (&out)[4]) {
+  uint32_t lo, hi;
+  asm("{\n\t.reg .b16 a, b;\n\t"
+      "mov.b32 {a, b}, %2;\n\t"
+      "cvt.rn.bf16x2.ue8m0x2 %0, a;\n\t"
+      "cvt.rn.bf16x2.ue8m0x2 %1, b;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
+  out[0] = __byte_perm(lo, lo, 0x1010); out[1] = __byte_perm(lo, lo, 0x3232);
+  out[2] = __byte_perm(hi, hi, 0x1010); out[3] = __byte_perm(hi, hi, 0x3232);
+}
+// Eight e2m1 codes, lowest four bits first, times a power of two: bf16, exactly.  The eight levels' bytes are looked up four codes at a time
+// (__byte_perm takes three bits of a code as an index); signs are moved beside them.
+__device__ __forceinline__ void unpack8_bf16(uint32_t w, uint32_t scale, uint32_t (&out)[4]) {
+  constexpr uint32_t lo0 = 0xc0800000u, lo1 = 0xc0804000u;  // 0, 0.5, 1, 1.5 and 2, 3, 4, 6: low bytes of 0000 3f00 3f80 3fc0, 4000 4040 4080 40c0
+  constexpr uint32_t hi0 = 0x3f3f3f00u, hi1 = 0x40404040u;  // and high ones
+  const uint32_t even = (w << 4) & 0x80808080u, odd = w & 0x80808080u;  // signs of codes 0 2 4 6, 1 3 5 7, one per byte
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint32_t sel = (w >> (16 * k)) & 0x7777u;
+    const uint32_t lo = __byte_perm(lo0, lo1, sel), hi = __byte_perm(hi0, hi1, sel) | __byte_perm(even, odd, k ? 0x7362 : 0x5140);
+    const uint32_t a = __byte_perm(lo, hi, 0x5140), b = __byte_perm(lo, hi, 0x7362);
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(out[2 * k]) : "r"(a), "r"(scale));
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(out[2 * k + 1]) : "r"(b), "r"(scale));
+  }
+}
+
 // A warp's wait: false if any lane gave up
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
 
-__global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+template <bool QUANT>
+__global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                                                               const __grid_constant__ CUtensorMap tm_v, const ExtendArgs a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -339,7 +372,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
 
   if (tid == 0) {
     for (int i = 0; i < kEStages; ++i) {
-      mbar_init(b_full(i), 1);
+      mbar_init(b_full(i), QUANT ? 4 : 1);
       mbar_init(b_empty(i), 1);
     }
     for (int i = 0; i < kEBiasSlots; ++i) {
@@ -360,13 +393,15 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     for (int i = 0; i < kEStages / 2; ++i) mbar_init(b_v(i), 1);
     for (int i = 0; i < kEPieces; ++i) {
       mbar_init(b_piece(i), 1);
-      mbar_init(b_piece_free(i), 10 + (a.logdeg ? 1 : 0));  // softmax warps, MMA, warps 10 and 11
+      mbar_init(b_piece_free(i), 9 + (QUANT ? 4 : 1) + (a.logdeg ? 1 : 0));  // softmax warps, MMA, unpacking warps or warp 10, warp 11
     }
     mbar_init_fence();
     s_start[0] = -1;
     prefetch_map(&tm_q);
-    prefetch_map(&tm_k);
-    prefetch_map(&tm_v);
+    if (!QUANT) {
+      prefetch_map(&tm_k);
+      prefetch_map(&tm_v);
+    }
   }
   if (tid < kEN) {
     st_shared_v4(s0 + oOnes + tid * 16, make_uint4(0x3f803f80u, 0x00003f80u, 0, 0));
@@ -380,7 +415,8 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
   const int T2 = 2 * a.T;
 
   // this CTA's stretch: every thread sums a run of sequences
-  const int per = (a.Bz + kEThreads - 1) / kEThreads, q0 = min(a.Bz, tid * per), q1 = min(a.Bz, q0 + per);
+  constexpr int kThreads = kEWarps<QUANT> * 32;
+  const int per = (a.Bz + kThreads - 1) / kThreads, q0 = min(a.Bz, tid * per), q1 = min(a.Bz, q0 + per);
   int64_t mine = 0;
   for (int b = q0; b < q1; ++b) {
     const ExtendSeq s = extend_seq(a, b);
@@ -396,7 +432,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
   tc_fence_before();
   __syncthreads();
   int64_t total = 0, at = upto - mine;
-  for (int w = 0; w < kEWarps; ++w) {
+  for (int w = 0; w < kEWarps<QUANT>; ++w) {
     if (w < warp) at += s_sum[w];
     total += s_sum[w];
   }
@@ -436,7 +472,91 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     ++np;
   };
 
-  if (warp >= 8) {
+  if (QUANT && warp >= 12) {
+    // ---------------------------------------------------------------- four-bit pages: codes and scales to bf16 tiles, exactly
+    give_registers<kEUnpackRegs>();
+    const int w = warp - 12;
+    // Lane l of a group of rows has its 16-byte piece l % 4.  Of keys and values alike such a piece holds, for each of the row's four groups j,
+    // elements 32 j + 8 (l % 4) .. + 7: 16 bytes of the tile.  The two rows that a store's eight lanes write differ in bit 2, which the
+    // swizzle turns into the other half of the banks.
+    const int piece = lane & 3, in8 = (lane >> 3) + 4 * ((lane >> 2) & 1);
+    struct Tile {
+      uint4 codes[4];     // rows 32 w + 8 k + in8
+      uint32_t scales[4];
+      int kv;             // 0: keys, 1: values, 2: there is none any more
+    };
+    int lo = 0, hi = 0, end = 0, h = 0;
+    const int32_t* table = nullptr;
+    int kv = 0;
+    bool open = false;
+    auto fetch = [&](Tile& t) {  // the next tile's rows, begun
+      while (ok && !(open && lo < hi)) {
+        if (open) {
+          __syncwarp();
+          if (lane == 0) piece_done(); else ++np;
+          open = false;
+        }
+        if (!next_piece(warp_wait)) {
+          t.kv = 2;
+          return;
+        }
+        const Piece& p = pieces[np % kEPieces];
+        lo = p.lo; hi = p.hi; end = p.end; h = p.h;
+        table = a.views[p.seq].block_table;
+        open = true;
+      }
+      t.kv = kv;
+      const int slot = lo * kEN + 32 * w, seen = end - slot;  // (32 slots lie in one page)
+      const int64_t row = seen > 0 ? (((int64_t)table[slot >> a.shift] * a.H + h) << a.shift) + (slot & ((1 << a.shift) - 1)) : 0;
+      const uint4* const codes = reinterpret_cast<const uint4*>((kv ? a.pool.v_codes : a.pool.k_codes) + row * 64);
+      const uint32_t* const scales = reinterpret_cast<const uint32_t*>(kv ? a.pool.v_scales : a.pool.k_scales) + row;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {  // (slots behind the last: zeros)
+        const int r = 8 * k + in8;
+        t.codes[k] = r < seen ? codes[r * 4 + piece] : make_uint4(0, 0, 0, 0);
+        t.scales[k] = r < seen ? scales[r] : 0u;
+      }
+      if (kv) ++lo;
+      kv ^= 1;
+    };
+    int idx = 0;
+    auto store = [&](const Tile& t) {
+      const int st = idx % kEStages;
+      if (!(ok = warp_wait(b_empty(st), (uint32_t)(((idx / kEStages) & 1) ^ 1)))) return;
+      ++idx;
+      const uint32_t tile = s0 + oRing + (uint32_t)st * kETile;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = 32 * w + 8 * k + in8;
+        uint32_t sc[4];
+        scales_bf16x2(t.scales[k], sc);
+        const uint4 c = t.codes[k];
+        uint32_t word[4] = {c.x, c.y, c.z, c.w};  // keys: word j has group j's eight codes
+        if (t.kv) {                               // values: half words j and j + 4
+          word[0] = __byte_perm(c.x, c.z, 0x5410); word[1] = __byte_perm(c.x, c.z, 0x7632);
+          word[2] = __byte_perm(c.y, c.w, 0x5410); word[3] = __byte_perm(c.y, c.w, 0x7632);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t v[4];
+          unpack8_bf16(word[j], sc[j], v);
+          st_shared_v4(tile + (j >> 1) * kEHalf + r * 128 + ((((j & 1) * 4 + piece) ^ (r & 7)) << 4), make_uint4(v[0], v[1], v[2], v[3]));
+        }
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(b_full(st));
+    };
+    // two tiles ahead, which is one step: the walk passes a piece on only when the last but one's products are done
+    Tile t0, t1;
+    fetch(t0);
+    if (ok && t0.kv < 2) fetch(t1);
+    while (ok && t0.kv < 2) {
+      store(t0);
+      t0 = t1;
+      if (ok && t1.kv < 2) fetch(t1);
+    }
+  } else if (warp >= 8) {
   give_registers<kEOtherRegs>();
   if (warp == 8) {
     // ---------------------------------------------------------------- TMA, and the walk along the stretch
@@ -460,10 +580,10 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
     ExtendPiece note{0, 0, 0, (int32_t)((begin - walk.x) / share), {0, 0}};  // (the CTA in which the first item begins)
     const int run = min(kEN, 1 << a.shift), runs = kEN / run;  // slots of a step that lie in one page
     const int rr = (lane >> 1) % runs, half = lane & 1;
-    int n = 0, nq = 0, seq = 0;                                // steps so far, pieces with steps, sequence
+    int n = 0, nq = 0;                                         // steps so far, pieces with steps
     Piece p;
     while (true) {
-      const bool more = walk.next(a, p, seq);
+      const bool more = walk.next(a, p);
       if (!more) p.flags = kStop;
       if (!(ok = warp_wait(b_piece_free(np % kEPieces), (uint32_t)(((np / kEPieces) & 1) ^ 1)))) break;
       if (lane == 0) {
@@ -480,7 +600,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
           note.ntok = p.ntok;
         }
       }
-      const int32_t* const table = a.views[seq].block_table;
+      const int32_t* const table = a.views[p.seq].block_table;
       const int n_blocks = (p.end + (1 << a.shift) - 1) >> a.shift;
       int win = -32;
       int32_t cur = 0, nxt = 0;
@@ -499,11 +619,13 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
         const bool mine_ = lane < 2 * runs && rr < live;
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
-          const int idx = 2 * n + kv, st = idx % kEStages;
-          if (!(ok = warp_wait(b_empty(st), (uint32_t)(((idx / kEStages) & 1) ^ 1)))) break;
-          if (lane == 0) mbar_arrive_expect_tx(b_full(st), (uint32_t)(live * run * 256));
-          __syncwarp();
-          if (mine_) tma_load_2d(s0 + oRing + st * kETile + half * kEHalf + rr * run * 128, kv ? &tm_v : &tm_k, 64 * half, row, b_full(st));
+          if constexpr (!QUANT) {
+            const int idx = 2 * n + kv, st = idx % kEStages;
+            if (!(ok = warp_wait(b_empty(st), (uint32_t)(((idx / kEStages) & 1) ^ 1)))) break;
+            if (lane == 0) mbar_arrive_expect_tx(b_full(st), (uint32_t)(live * run * 256));
+            __syncwarp();
+            if (mine_) tma_load_2d(s0 + oRing + st * kETile + half * kEHalf + rr * run * 128, kv ? &tm_v : &tm_k, 64 * half, row, b_full(st));
+          }
           if (kv == 0 && a.logdeg) {
             const int bs = n % kEBiasSlots;
             if (!(ok = warp_wait(b_bias_free(bs), (uint32_t)(((n / kEBiasSlots) & 1) ^ 1)))) break;
@@ -587,7 +709,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
           const int g0 = one ? i & 1 : 0, g1 = one ? g0 : 1;
           const bool more = i + ahead < steps;
           const int iv = n + i;
-          if (!(ok = bar_wait(b_v(iv % (kEStages / 2)), (uint32_t)((iv / (kEStages / 2)) & 1)))) break;
+          if (!(ok = bar_wait(QUANT ? b_full((2 * iv + 1) % kEStages) : b_v(iv % (kEStages / 2)), (uint32_t)((iv / (kEStages / 2)) & 1)))) break;
           for (int g = g0; g <= g1; ++g) {
             if (!(ok = bar_wait(b_p(g, 0), par[g]))) break;
             tc_fence_after();
@@ -616,7 +738,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
         n += steps;
       }
     }
-  } else if (warp == 10) {
+  } else if (warp == 10 && !QUANT) {
     // ---------------------------------------------------------------- slots behind the last that an item sees: whatever their values
     // are, they must not meet a weight of zero
     int n = 0;
@@ -677,7 +799,7 @@ __global__ void __launch_bounds__(kEThreads, 1) extend_kernel(const __grid_const
   }
   } else {
     // ---------------------------------------------------------------- softmax of tile g, one row per thread
-    take_registers<kESoftmaxRegs>();
+    take_registers<kESoftmaxRegs<QUANT>>();
     const int g = warp >> 2, r = tid & 127, tok = r / a.G, head = r - tok * a.G;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // (32 lanes of tensor memory per warp, lane number in the upper half word)
     const uint32_t t_s = tmem + lanes + (uint32_t)g * 128, t_o = t_s + 256;
@@ -965,67 +1087,20 @@ bool encode(CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims,
 }
 
 // Sets the kernel's shared memory once per device
+template <bool QUANT>
 bool extend_ready() {
   constexpr int kMaxDev = 64;
   static std::atomic<bool> done[kMaxDev];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDev) return false;
   if (done[dev].load(std::memory_order_relaxed)) return true;
-  if (cudaFuncSetAttribute(extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEBytes + 1024) != cudaSuccess) return false;
+  if (cudaFuncSetAttribute(extend_kernel<QUANT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEBytes + 1024) != cudaSuccess) return false;
   done[dev].store(true, std::memory_order_relaxed);
   return true;
 }
 
 int32_t slot_rows(int64_t n_rows, int32_t G) { return (int32_t)std::min<int64_t>(2 * (kEN / G) * G, n_rows * G); }
 size_t pieces_bytes() { return ((size_t)sm_count() * sizeof(ExtendPiece) + 255) / 256 * 256; }
-
-__device__ __forceinline__ float4 level4(uint32_t two_bytes, float s) {
-  uint32_t h[4];
-  ptx::unpack_e2m1x8(two_bytes, h);
-  auto f = [](uint32_t x) { return __half2float(__ushort_as_half((unsigned short)x)); };
-  return make_float4(f(h[0]) * s, f(h[0] >> 16) * s, f(h[1]) * s, f(h[1] >> 16) * s);
-}
-
-// One warp per (new token, query head), a lane has four columns; online softmax over the token's slots.
-__global__ void __launch_bounds__(256) extend_simple_kernel(const ExtendArgs a, const __nv_bfloat16* q_, int64_t q_row, int64_t q_head) {
-  griddep_wait();
-  griddep_launch();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
-  const int lane = threadIdx.x & 31, HG = a.H * a.G;
-  const int64_t at = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)), row = at / HG;
-  const int j = (int)(at - row * HG), h = j / a.G;
-  if (row >= a.n_rows) return;
-  int lo = 0, hi = a.Bz;
-  if (row >= a.q_begin[a.Bz] || row < a.q_begin[0]) return;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.q_begin[mid] <= row) lo = mid; else hi = mid;
-  }
-  const ckv_paged_view view = a.views[lo];
-  const int64_t end = view.len - (a.q_begin[lo + 1] - row) + 1;
-  const float4 q = load4(q_ + row * q_row + j * q_head + 4 * lane);
-  float m = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int64_t t = 0; t < end; ++t) {
-    const int64_t r = (((int64_t)view.block_table[t >> a.shift] * a.H + h) << a.shift) + (t & (((int64_t)1 << a.shift) - 1));
-    float4 k, v;
-    {
-      const int jj = lane >> 3, u = lane & 7;
-      const uint32_t kc = *reinterpret_cast<const uint32_t*>(a.pool.k_codes + r * 64 + 16 * (u >> 1) + 4 * jj) >> (16 * (u & 1));
-      const uint32_t vc = *reinterpret_cast<const uint32_t*>(a.pool.v_codes + r * 64 + 8 * u + 4 * (jj >> 1)) >> (16 * (jj & 1));
-      k = level4(kc, exp2f((float)a.pool.k_scales[r * 4 + jj] - 127.f));
-      v = level4(vc, exp2f((float)a.pool.v_scales[r * 4 + jj] - 127.f));
-    }
-    const float s = warp_sum(q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w) * a.scale + (a.logdeg ? a.logdeg[r] : 0.f);
-    const float mm = fmaxf(m, s), base = mm == -INFINITY ? 0.f : mm;
-    const float c = exp2f((m - base) * kLog2e), p = exp2f((s - base) * kLog2e);
-    o = make_float4(o.x * c + p * v.x, o.y * c + p * v.y, o.z * c + p * v.z, o.w * c + p * v.w);
-    l = l * c + p;
-    m = mm;
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  store4(a.out + (row * HG + j) * kED + 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-}
 
 int check_extend(const void* views, const void* q_begin, int64_t n_rows, int32_t page_tokens, int32_t Bz, int32_t H, int32_t G, int32_t D, int32_t dtype,
                  const void* q, int64_t q_row, int64_t q_head, const void* out, const void* workspace, size_t workspace_bytes) {
@@ -1039,6 +1114,7 @@ int check_extend(const void* views, const void* q_begin, int64_t n_rows, int32_t
 }
 
 // Fills in what both calls have in common and launches
+template <bool QUANT>
 int run_extend(ExtendArgs& a, const void* q, int64_t q_row, int64_t q_head, const void* k, const void* v, int64_t n_pages, void* workspace, cudaStream_t st) {
   if (a.n_rows == 0) return CKV_OK;
   a.T = kEN / a.G;
@@ -1050,21 +1126,21 @@ int run_extend(ExtendArgs& a, const void* q, int64_t q_row, int64_t q_head, cons
   a.pieces = reinterpret_cast<ExtendPiece*>(static_cast<unsigned char*>(workspace) + 256);
   a.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + 256 + pieces_bytes());
   a.slot_rows = slot_rows(a.n_rows, a.G);
-  CUtensorMap tm[3];
+  CUtensorMap tm[3] = {};
   const cuuint64_t HG = (cuuint64_t)a.H * a.G, rows = ((cuuint64_t)n_pages * a.H) << a.shift;
   {  // (the stride of a single head or row is never used)
     const cuuint64_t dims[3] = {kED, HG, (cuuint64_t)a.n_rows}, strides[2] = {HG > 1 ? (cuuint64_t)q_head * 2 : 256, a.n_rows > 1 ? (cuuint64_t)q_row * 2 : 256};
     const cuuint32_t box[3] = {64, (cuuint32_t)a.G, (cuuint32_t)a.T};
     if (!encode(&tm[0], q, 3, dims, strides, box)) return CKV_ERR_UNSUPPORTED;
   }
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < (QUANT ? 0 : 2); ++i) {
     const cuuint64_t dims[2] = {kED, rows}, strides[1] = {kED * 2};
     const cuuint32_t box[2] = {64, (cuuint32_t)std::min(kEN, 1 << a.shift)};
     if (!encode(&tm[1 + i], i ? v : k, 2, dims, strides, box)) return CKV_ERR_UNSUPPORTED;
   }
-  if (!extend_ready()) return CKV_ERR_CUDA;
+  if (!extend_ready<QUANT>()) return CKV_ERR_CUDA;
   const unsigned ctas = (unsigned)sm_count();
-  if (launch_dependent(extend_kernel, dim3(ctas), dim3(kEThreads), kEBytes + 1024, st, tm[0], tm[1], tm[2], a) != cudaSuccess) return CKV_ERR_CUDA;
+  if (launch_dependent(extend_kernel<QUANT>, dim3(ctas), dim3(kEWarps<QUANT> * 32), kEBytes + 1024, st, tm[0], tm[1], tm[2], a) != cudaSuccess) return CKV_ERR_CUDA;
   return launch_dependent(extend_join_kernel, dim3(ctas, (unsigned)(a.slot_rows + kJoinRows - 1) / kJoinRows), dim3(kJoinWarps * 32), 0, st, a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
@@ -1094,7 +1170,7 @@ int ckv_extend_attn_paged(const ckv_paged_view* views_dev, const int64_t* q_begi
   a.views = views_dev; a.q_begin = q_begin; a.n_rows = n_rows; a.Bz = Bz; a.H = H; a.G = G; a.shift = shift; a.scale = scale;
   a.out = static_cast<__nv_bfloat16*>(out);
   a.logdeg = logdeg_pages;
-  return run_extend(a, q, q_row_stride, q_head_stride, k_pages, v_pages, n_pages, workspace, static_cast<cudaStream_t>(cuda_stream));
+  return run_extend<false>(a, q, q_row_stride, q_head_stride, k_pages, v_pages, n_pages, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int ckv_extend_attn_quantized(const ckv_paged_view* views_dev, const int64_t* q_begin, int64_t n_rows, const ckv_quant_pool* pool, int64_t n_pages,
@@ -1112,9 +1188,7 @@ int ckv_extend_attn_quantized(const ckv_paged_view* views_dev, const int64_t* q_
   a.views = views_dev; a.q_begin = q_begin; a.n_rows = n_rows; a.Bz = Bz; a.H = H; a.G = G; a.shift = shift; a.scale = scale;
   a.out = static_cast<__nv_bfloat16*>(out);
   a.pool = *pool; a.logdeg = pool->logdeg_pages;
-  a.status = static_cast<int32_t*>(workspace);
-  if (n_rows == 0) return CKV_OK;
-  return launch_dependent(extend_simple_kernel, dim3((unsigned)((a.n_rows * a.H * a.G + 7) / 8)), dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), a, static_cast<const __nv_bfloat16*>(q), q_row_stride, q_head_stride) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
+  return run_extend<true>(a, q, q_row_stride, q_head_stride, nullptr, nullptr, n_pages, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 
 }  // extern "C"
