@@ -301,6 +301,59 @@ typedef struct ckv_token_rows {
 int ckv_pages_write(const ckv_token_rows* rows, const int64_t* slots, int64_t n, void* k_pages, void* v_pages, int32_t* deg_pages,
                     float* logdeg_pages, int64_t n_pages, int32_t page_tokens, void* cuda_stream);
 
+/* ---- Sequences that share pages -------------------------------------------------------------------------------------------
+ * Parallel samples of one prompt, beams, a prefix that several requests begin with: rows of a block table may list the same
+ * page.  shared [n_pages] (device) counts a page's holders beyond the first: 0 for a page that is free or held once, so that pages
+ * which ckv_pages_resize gives out need nothing.  The page into which a sequence writes its next token is never shared (a fork copies it),
+ * so sequences that share pages grow by ckv_pages_resize as others do; they end, and drop tokens of shared pages, by ckv_pages_fork
+ * (ckv_pages_resize takes every page that a sequence gives for free).
+ *
+ * ckv_pages_fork makes a new table from an old one in one launch.  Row b of block_tables_out [n_out, table_stride] is the first keep[b] tokens
+ * (keep NULL: all) of row parents[b] of block_tables [n_in, table_stride]; parents[b] = -1: an empty row.  Old rows that are
+ * nobody's parent end.  A page that keep[b] fills is shared.  The page that it fills in part becomes row b's own: the
+ * first row (lowest b) that goes on writing to it takes it over if nobody holds it whole, in or outside the call; for every other one a page is taken from the
+ * front of the queue, and copies lists (source page, taken page, tokens).  Pages that nobody holds any more are appended to the back of the
+ * queue in the order of their numbers (as with ckv_pages_resize they may be taken in the same call, last).  copies [n_out, 3]: in the order of
+ * the rows, -1 behind the last; ckv_pages_copy carries them out.  Written too: shared_out [n_pages], lens_out [n_out], ring_state_out [2], status
+ * (CKV_RESIZE_OK) and, if views_dev is not NULL, the views [n_out] of the new table.
+ * If it cannot be done, *status is CKV_RESIZE_NO_PAGES or CKV_RESIZE_INCONSISTENT (a length that its row cannot hold, a parent, page or
+ * number of kept tokens that does not exist, more rows of a page than holders, a queue outside its ring), copies are -1, shared_out and ring_state_out repeat the state before
+ * the call, and queue, table, lengths and views are not written.
+ * Outputs must not overlap inputs, ring apart, which only changes behind its last page: repeating a call repeats its results.
+ * Rows of a table behind a sequence's last page are neither read nor written.  n_in, n_out <= 8192. */
+size_t ckv_pages_fork_workspace_bytes(int64_t n_pages); /* host-only */
+
+int ckv_pages_fork(const int64_t* lens, int32_t n_in, const int32_t* parents, const int64_t* keep, int32_t n_out, int32_t page_tokens,
+                   const int32_t* block_tables, int32_t* block_tables_out, int64_t table_stride, const int32_t* shared, int32_t* shared_out,
+                   int32_t* ring, int64_t n_pages, const int64_t* ring_state, int32_t* copies, int64_t* lens_out, int64_t* ring_state_out,
+                   int32_t* status, ckv_paged_view* views_dev, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Moves all held pages to the front of the pool, so that what is behind them can be given back or saved apart: with U pages held by the
+ * batch's rows (all sequences of the pool; every other page counts as free), the k-th held page from U on moves to the k-th free page before
+ * U.  block_tables_out lists the new places, copies [n_copies, 3] the moves (source, target, page_tokens; -1 behind the last),
+ * shared_out the counts, the queue becomes the pages U .. n_pages - 1 from the start of the ring, ring_state_out [2] = 0, n_pages - U.
+ * *status: CKV_RESIZE_OK; CKV_RESIZE_SLOTS_FULL: more moves than n_copies; CKV_RESIZE_INCONSISTENT.  Then copies are -1 and nothing else
+ * is written.  Bz <= 8192. */
+size_t ckv_pages_compact_workspace_bytes(int64_t n_pages); /* host-only */
+
+int ckv_pages_compact(const int64_t* lens, int32_t Bz, int32_t page_tokens, const int32_t* block_tables, int32_t* block_tables_out, int64_t table_stride,
+                      const int32_t* shared, int32_t* shared_out, int32_t* ring, int64_t n_pages, int32_t* copies, int64_t n_copies,
+                      int64_t* ring_state_out, int32_t* status, ckv_paged_view* views_dev, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* One array that has pages, in every layer: page p of layer l is [H, rows, row_bytes] at base + l * layer_bytes + p * H * rows * row_bytes.
+ * Keys, values, codes, scales, degrees, log-degrees: rows = page_tokens, row_bytes a token's.  What a page has once (summaries): rows = 1.
+ * base, row_bytes and layer_bytes are multiples of four; of sixteen where copies are to be fast. */
+typedef struct ckv_page_array {
+  void* base;
+  int64_t layer_bytes;
+  int32_t layers, rows, row_bytes;
+} ckv_page_array;
+
+/* For every entry (source, target, tokens) of copies [n, 3] (device), up to the first with a source below 0: the first min(tokens, rows) rows of every head of
+ * the source page to the target page, in all arrays (HOST array [n_arrays]) and layers.  A target must not be listed twice or be a source.
+ * Entries with a page outside 0 .. n_pages - 1 are skipped. */
+int ckv_pages_copy(const ckv_page_array* arrays, int32_t n_arrays, int32_t H, const int32_t* copies, int64_t n, int64_t n_pages, void* cuda_stream);
+
 /* ---- Attention over selected pages -----------------------------------------------------------------------------------
  * For a long cache each query reads only the pages that matter to it.  A page is summarised as one cluster in the sense of
  * Eq. 5: its degree-weighted mean key and its tokens' degrees summed; log N + q c * scale is then, by Jensen's inequality, a

@@ -25,7 +25,8 @@ EXPORTS = ["ckv_compress_plan", "ckv_workspace_bytes", "ckv_compress_prefill", "
            "ckv_pages_scatter", "ckv_pages_plan", "ckv_paged_workspace_bytes", "ckv_compress_paged",
            "ckv_decode_append_attn_paged", "ckv_pages_resize", "ckv_pages_write", "ckv_pages_summarize", "ckv_pages_select",
            "ckv_decode_attn_selected", "ckv_pages_quantize", "ckv_pages_dequantize", "ckv_decode_quantized_workspace_bytes",
-           "ckv_decode_attn_quantized", "ckv_extend_workspace_bytes", "ckv_extend_attn_paged", "ckv_extend_attn_quantized"]
+           "ckv_decode_attn_quantized", "ckv_extend_workspace_bytes", "ckv_extend_attn_paged", "ckv_extend_attn_quantized",
+           "ckv_pages_fork", "ckv_pages_fork_workspace_bytes", "ckv_pages_compact", "ckv_pages_compact_workspace_bytes", "ckv_pages_copy"]
 
 RESIZE_OK, RESIZE_NO_PAGES, RESIZE_TABLE_FULL, RESIZE_SLOTS_FULL, RESIZE_INCONSISTENT = range(5)   # device status of pages_resize
 
@@ -56,6 +57,10 @@ class CkvTokenRows(C.Structure):
 class CkvQuantPool(C.Structure):
     _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
                 ("deg_pages", C.c_void_p), ("logdeg_pages", C.c_void_p)]
+
+
+class CkvPageArray(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("layer_bytes", C.c_int64), ("layers", C.c_int32), ("rows", C.c_int32), ("row_bytes", C.c_int32)]
 
 
 class CkvLayerView(C.Structure):
@@ -130,12 +135,18 @@ def _load():
             "ckv_pages_quantize": [p, p, i64, p, i64, i32, p],
             "ckv_pages_dequantize": [p, i64, p, i32, i32, i32, i32, p, p, p, p, i64, p],
             "ckv_decode_attn_quantized": [p, p, i32, i32, i32, i32, i32, i32, p, p, f32, i64, p, C.c_size_t, p],
+            "ckv_pages_fork": [p, i32, p, p, i32, i32, p, p, i64, p, p, p, i64, p, p, p, p, p, p, p, C.c_size_t, p],
+            "ckv_pages_compact": [p, i32, i32, p, p, i64, p, p, p, i64, p, i64, p, p, p, p, C.c_size_t, p],
+            "ckv_pages_copy": [p, i32, i32, p, i64, i64, p],
             "ckv_extend_attn_paged": [p, p, i64, p, p, p, i64, i32, i32, i32, i32, i32, i32, p, i64, i64, p, f32, p, C.c_size_t, p],
             "ckv_extend_attn_quantized": [p, p, i64, p, i64, i32, i32, i32, i32, i32, i32, p, i64, i64, p, f32, p, C.c_size_t, p]}.items():
         getattr(lib, name).restype = C.c_int
         getattr(lib, name).argtypes = args
     lib.ckv_decode_quantized_workspace_bytes.restype = C.c_size_t
     lib.ckv_decode_quantized_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
+    for name in ("ckv_pages_fork_workspace_bytes", "ckv_pages_compact_workspace_bytes"):
+        getattr(lib, name).restype = C.c_size_t
+        getattr(lib, name).argtypes = [i64]
     lib.ckv_extend_workspace_bytes.restype = C.c_size_t
     lib.ckv_extend_workspace_bytes.argtypes = [i64, i32, i32, i32]
     return lib
@@ -436,6 +447,7 @@ _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_d
 _i32, _i64, _f32 = torch.int32, torch.int64, torch.float32
 _ROWS = struct.Struct("@PPPqqqqqqiii4x")   # ckv_token_rows
 _POOL = struct.Struct("@PPPPPP")           # ckv_quant_pool
+_ARRAY = struct.Struct("@Pqiii4x")         # ckv_page_array
 
 
 def _stream_for(first: torch.Tensor, *others: torch.Tensor | None):
@@ -497,6 +509,76 @@ def pages_write(slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: 
     assert logdeg_pages is None or logdeg_pages.dtype is _f32 and logdeg_pages.nbytes == per_row and logdeg_pages.is_contiguous(), "log-degree pages"
     _check(lib.ckv_pages_write(rows, slots.data_ptr(), slots.numel(), k_pages.data_ptr(), v_pages.data_ptr(), _ptr(deg_pages),
                                _ptr(logdeg_pages), n_pages, P, _stream_for(slots, k, v, k_pages, v_pages, deg_pages, logdeg_pages, deg)))
+
+
+def pages_fork_workspace_bytes(n_pages: int) -> int:
+    return lib.ckv_pages_fork_workspace_bytes(n_pages)
+
+
+def pages_compact_workspace_bytes(n_pages: int) -> int:
+    return lib.ckv_pages_compact_workspace_bytes(n_pages)
+
+
+def _check_pool_state(n_pages: int, block_tables, block_tables_out, shared, shared_out, ring, copies, ring_state_out, status, views, rows_out: int):
+    assert block_tables.dtype is block_tables_out.dtype is _i32 and block_tables.is_contiguous() and block_tables_out.is_contiguous(), "tables"
+    assert block_tables_out.shape == (rows_out, block_tables.shape[1]), "tables"
+    assert shared.dtype is shared_out.dtype is _i32 and shared.nbytes == shared_out.nbytes == 4 * n_pages, "shared"
+    assert shared.is_contiguous() and shared_out.is_contiguous() and ring.dtype is _i32 and ring.is_contiguous(), "ring"
+    assert copies.dtype is _i32 and copies.dim() == 2 and copies.shape[1] == 3 and copies.is_contiguous(), "copies"
+    assert ring_state_out.dtype is _i64 and ring_state_out.nbytes == 16 and ring_state_out.is_contiguous(), "ring"
+    assert status.dtype is _i32 and status.nbytes == 4, "status"
+    assert views is None or views.dtype is _i64 and views.nbytes == 16 * rows_out and views.is_contiguous(), "views"
+
+
+def pages_fork(lens: torch.Tensor, parents: torch.Tensor, keep: torch.Tensor | None, block_tables: torch.Tensor, block_tables_out: torch.Tensor,
+               shared: torch.Tensor, shared_out: torch.Tensor, ring: torch.Tensor, ring_state: torch.Tensor, copies: torch.Tensor,
+               lens_out: torch.Tensor, ring_state_out: torch.Tensor, status: torch.Tensor, page_tokens: int, workspace: torch.Tensor,
+               views: torch.Tensor | None = None):
+    """ckv_pages_fork on the current stream: row b of block_tables_out [n_out, row] is the first keep[b] tokens of row parents[b] of block_tables
+    [n_in, row].  lens int64 [n_in]; parents int32, keep int64 (None: all), lens_out int64 [n_out]; shared, shared_out, ring int32 [n_pages];
+    copies int32 [n_out, 3]; the rest as for pages_resize."""
+    (n_in, row), n_out, n_pages = block_tables.shape, parents.numel(), ring.numel()
+    _check_pool_state(n_pages, block_tables, block_tables_out, shared, shared_out, ring, copies, ring_state_out, status, views, n_out)
+    assert lens.dtype is lens_out.dtype is _i64 and lens.nbytes == 8 * n_in and lens_out.nbytes == 8 * n_out, "lengths"
+    assert lens.is_contiguous() and lens_out.is_contiguous() and copies.shape[0] == n_out, "lengths"
+    assert parents.dtype is _i32 and parents.is_contiguous(), "parents"
+    assert keep is None or keep.dtype is _i64 and keep.nbytes == 8 * n_out and keep.is_contiguous(), "kept tokens"
+    assert ring_state.dtype is _i64 and ring_state.nbytes == 16 and ring_state.is_contiguous(), "ring"
+    _check(lib.ckv_pages_fork(lens.data_ptr(), n_in, parents.data_ptr(), _ptr(keep), n_out, page_tokens, block_tables.data_ptr(),
+                              block_tables_out.data_ptr(), row, shared.data_ptr(), shared_out.data_ptr(), ring.data_ptr(), n_pages,
+                              ring_state.data_ptr(), copies.data_ptr(), lens_out.data_ptr(), ring_state_out.data_ptr(), status.data_ptr(),
+                              _ptr(views), workspace.data_ptr(), workspace.nbytes,
+                              _stream_for(lens, parents, keep, block_tables, block_tables_out, shared, shared_out, ring, ring_state, copies, lens_out,
+                                          ring_state_out, status, views, workspace)))
+
+
+def pages_compact(lens: torch.Tensor, block_tables: torch.Tensor, block_tables_out: torch.Tensor, shared: torch.Tensor, shared_out: torch.Tensor,
+                  ring: torch.Tensor, copies: torch.Tensor, ring_state_out: torch.Tensor, status: torch.Tensor, page_tokens: int,
+                  workspace: torch.Tensor, views: torch.Tensor | None = None):
+    """ckv_pages_compact on the current stream: all pages that the rows hold to the front of the pool; copies int32 [n, 3] lists the moves."""
+    (Bz, row), n_pages = block_tables.shape, ring.numel()
+    _check_pool_state(n_pages, block_tables, block_tables_out, shared, shared_out, ring, copies, ring_state_out, status, views, Bz)
+    assert lens.dtype is _i64 and lens.nbytes == 8 * Bz and lens.is_contiguous(), "lengths"
+    _check(lib.ckv_pages_compact(lens.data_ptr(), Bz, page_tokens, block_tables.data_ptr(), block_tables_out.data_ptr(), row, shared.data_ptr(),
+                                 shared_out.data_ptr(), ring.data_ptr(), n_pages, copies.data_ptr(), copies.shape[0], ring_state_out.data_ptr(),
+                                 status.data_ptr(), _ptr(views), workspace.data_ptr(), workspace.nbytes,
+                                 _stream_for(lens, block_tables, block_tables_out, shared, shared_out, ring, copies, ring_state_out, status, views,
+                                             workspace)))
+
+
+def pages_copy(copies: torch.Tensor, arrays, page_arrays=(), stacked: bool = False):
+    """ckv_pages_copy on the current stream.  arrays: tensors [n_pages, H, page_tokens, ...], whose rows are tokens; page_arrays:
+    [n_pages, H, ...], which a page has once (summaries).  stacked: all of them with the layers in front ([L, n_pages, H, ...])."""
+    s = 1 if stacked else 0
+    n_pages, H, P = arrays[0].shape[s:s + 3]
+    packed = []
+    for i, t in enumerate((*arrays, *page_arrays)):
+        by_token = i < len(arrays)
+        assert t.shape[s:s + 2] == (n_pages, H) and (not by_token or t.shape[s + 2] == P) and t.is_contiguous(), "arrays"
+        layers, rows = t.shape[0] if stacked else 1, P if by_token else 1
+        packed.append(_ARRAY.pack(t.data_ptr(), t.nbytes // layers, layers, rows, t.nbytes // (layers * n_pages * H * rows)))
+    assert copies.dtype is _i32 and copies.dim() == 2 and copies.shape[1] == 3 and copies.is_contiguous(), "copies"
+    _check(lib.ckv_pages_copy(b"".join(packed), len(packed), H, copies.data_ptr(), copies.shape[0], n_pages, _stream_for(copies, *arrays, *page_arrays)))
 
 
 def pages_summarize(views: torch.Tensor, k_pages: torch.Tensor, deg_pages: torch.Tensor | None, c_pages: torch.Tensor, clog_pages: torch.Tensor,

@@ -1103,8 +1103,10 @@ int32_t slot_rows(int64_t n_rows, int32_t G) { return (int32_t)std::min<int64_t>
 size_t pieces_bytes() { return ((size_t)sm_count() * sizeof(ExtendPiece) + 255) / 256 * 256; }
 
 int check_extend(const void* views, const void* q_begin, int64_t n_rows, int32_t page_tokens, int32_t Bz, int32_t H, int32_t G, int32_t D, int32_t dtype,
-                 const void* q, int64_t q_row, int64_t q_head, const void* out, const void* workspace, size_t workspace_bytes) {
-  if (!views || !q_begin || !q || !out || n_rows < 0 || Bz <= 0 || H <= 0 || G <= 0 || q_row < 0 || q_head < 0) return CKV_ERR_INVALID_ARG;
+                 const void* q, int64_t q_row, int64_t q_head, const void* out, float scale, const void* workspace, size_t workspace_bytes) {
+  if (!views || !q_begin || !q || !out || n_rows < 0 || Bz <= 0 || H <= 0 || G <= 0 || q_row < 0 || q_head < 0 ||
+      !std::isfinite(scale))
+    return CKV_ERR_INVALID_ARG;
   if (dtype != CKV_F32 && dtype != CKV_BF16) return CKV_ERR_INVALID_ARG;
   if (dtype != CKV_BF16 || page_shift(page_tokens) < 0 || D != kED || G > 8 || H > 8192 || Bz > 65535 || n_rows > INT32_MAX / (H * G))
     return CKV_ERR_UNSUPPORTED;
@@ -1162,7 +1164,8 @@ int ckv_extend_attn_paged(const ckv_paged_view* views_dev, const int64_t* q_begi
                           size_t workspace_bytes, void* cuda_stream) {
   if (!k_pages || !v_pages || n_pages <= 0) return CKV_ERR_INVALID_ARG;
   if (!aligned16(k_pages) || !aligned16(v_pages) || (logdeg_pages && !aligned16(logdeg_pages))) return CKV_ERR_ALIGNMENT;
-  const int st = check_extend(views_dev, q_begin, n_rows, page_tokens, Bz, H, G, D, dtype, q, q_row_stride, q_head_stride, out, workspace, workspace_bytes);
+  const int st = check_extend(views_dev, q_begin, n_rows, page_tokens, Bz, H, G, D, dtype, q, q_row_stride, q_head_stride, out, scale, workspace,
+                              workspace_bytes);
   if (st != CKV_OK) return st;
   const int shift = page_shift(page_tokens);
   if (n_pages > (INT32_MAX >> shift) / H) return CKV_ERR_UNSUPPORTED;  // (2^31 rows of a pool: 1 TB)
@@ -1180,7 +1183,8 @@ int ckv_extend_attn_quantized(const ckv_paged_view* views_dev, const int64_t* q_
   if (!aligned16(pool->k_codes) || !aligned16(pool->v_codes) || !aligned16(pool->k_scales) || !aligned16(pool->v_scales) ||
       (pool->logdeg_pages && !aligned16(pool->logdeg_pages)))
     return CKV_ERR_ALIGNMENT;
-  const int st = check_extend(views_dev, q_begin, n_rows, page_tokens, Bz, H, G, D, dtype, q, q_row_stride, q_head_stride, out, workspace, workspace_bytes);
+  const int st = check_extend(views_dev, q_begin, n_rows, page_tokens, Bz, H, G, D, dtype, q, q_row_stride, q_head_stride, out, scale, workspace,
+                              workspace_bytes);
   if (st != CKV_OK) return st;
   const int shift = page_shift(page_tokens);
   if (n_pages > (INT32_MAX >> shift) / H) return CKV_ERR_UNSUPPORTED;
