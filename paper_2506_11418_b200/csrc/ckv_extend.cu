@@ -67,8 +67,9 @@ constexpr int oAug = oBias + kEBiasSlots * kEN * 4;       // 16 bytes per slot: 
 constexpr int oOnes = oAug + kEBiasSlots * kEN * 16;       // 16 bytes per row of Q: three ones
 constexpr int oZero = oOnes + kEN * 16;                    // the other eight columns of both
 constexpr int oState = oZero + kEN * 16;  // float2 [256]: m and sum of every row, exchanged by one-tile items
-constexpr int oStage = oState + 256 * 8;                   // 2 KB per softmax warp: 32 columns of its rows on their way out
-constexpr int oBar = oStage + 8 * 2048;
+constexpr int kERaw = 32 * 64 + 32 * 4;                     // four-bit pages: codes and scales of one unpacking warp's 32 slots
+constexpr int oRaw = oState + 256 * 8;                     // two tiles of them per warp
+constexpr int oBar = oRaw + 4 * 2 * kERaw;
 constexpr int oPieces = oBar + 512;
 constexpr int oMisc = oPieces + 256;
 constexpr int kEBytes = oMisc + 128;
@@ -287,6 +288,10 @@ __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.
 __device__ __forceinline__ uint64_t umma_desc_plain(uint32_t smem_addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
   return (uint64_t)((smem_addr >> 4) & 0x3fffu) | ((uint64_t)((lbo_bytes >> 4) & 0x3fffu) << 16) | ((uint64_t)((sbo_bytes >> 4) & 0x3fffu) << 32) | (1ull << 46);
 }
+// 32 bytes, a whole sector
+__device__ __forceinline__ void st_global_v8(void* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
+}
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); }
 __device__ __forceinline__ bool elect_one() {
   uint32_t ok;
@@ -311,6 +316,11 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
   return false;
 }
 
+__device__ __forceinline__ uint32_t ld_shared_u32(uint32_t addr) {
+  uint32_t x;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
+  return x;
+}
 // Four scale bytes as pairs of equal bf16: 2^(byte - 127), 255 NaN
 __device__ __forceinline__ void scales_bf16x2(uint32_t w, uint32_t (&out)[4]) {
   uint32_t lo, hi;
@@ -476,63 +486,76 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
     // ---------------------------------------------------------------- four-bit pages: codes and scales to bf16 tiles, exactly
     give_registers<kEUnpackRegs>();
     const int w = warp - 12;
+    const uint32_t raw = s0 + oRaw + (uint32_t)w * 2 * kERaw;
     // Lane l of a group of rows has its 16-byte piece l % 4.  Of keys and values alike such a piece holds, for each of the row's four groups j,
     // elements 32 j + 8 (l % 4) .. + 7: 16 bytes of the tile.  The two rows that a store's eight lanes write differ in bit 2, which the
-    // swizzle turns into the other half of the banks.
+    // swizzle turns into the other half of the banks; the codes of such rows lie 64 bytes apart for the same reason.
     const int piece = lane & 3, in8 = (lane >> 3) + 4 * ((lane >> 2) & 1);
-    struct Tile {
-      uint4 codes[4];     // rows 32 w + 8 k + in8
-      uint32_t scales[4];
-      int kv;             // 0: keys, 1: values, 2: there is none any more
-    };
-    int lo = 0, hi = 0, end = 0, h = 0;
+    auto at = [](int r) { return (uint32_t)(r * 64) ^ (uint32_t)((r >> 2) & 1) * 64u; };
+    int lo = 0, hi = 0, end = 0, h = 0, kv = 0, fetched = 0, stored = 0;
     const int32_t* table = nullptr;
-    int kv = 0;
-    bool open = false;
-    auto fetch = [&](Tile& t) {  // the next tile's rows, begun
-      while (ok && !(open && lo < hi)) {
+    int page = 0, page_next = 0;  // of this warp's 32 slots, which lie in one; the next step's is on its way a step before
+    bool open = false, last = false;
+    auto fetch = [&] {            // the next tile's rows, begun (slots behind the last: zeros)
+      while (!last && !(open && lo < hi)) {
         if (open) {
           __syncwarp();
           if (lane == 0) piece_done(); else ++np;
           open = false;
         }
         if (!next_piece(warp_wait)) {
-          t.kv = 2;
-          return;
+          last = true;
+        } else {
+          const Piece& p = pieces[np % kEPieces];
+          lo = p.lo; hi = p.hi; end = p.end; h = p.h;
+          table = a.views[p.seq].block_table;
+          page_next = lo * kEN + 32 * w < end ? table[(lo * kEN + 32 * w) >> a.shift] : 0;
+          open = true;
         }
-        const Piece& p = pieces[np % kEPieces];
-        lo = p.lo; hi = p.hi; end = p.end; h = p.h;
-        table = a.views[p.seq].block_table;
-        open = true;
       }
-      t.kv = kv;
-      const int slot = lo * kEN + 32 * w, seen = end - slot;  // (32 slots lie in one page)
-      const int64_t row = seen > 0 ? (((int64_t)table[slot >> a.shift] * a.H + h) << a.shift) + (slot & ((1 << a.shift) - 1)) : 0;
-      const uint4* const codes = reinterpret_cast<const uint4*>((kv ? a.pool.v_codes : a.pool.k_codes) + row * 64);
-      const uint32_t* const scales = reinterpret_cast<const uint32_t*>(kv ? a.pool.v_scales : a.pool.k_scales) + row;
+      if (!last) {
+        const int slot = lo * kEN + 32 * w, seen = end - slot;
+        if (kv == 0) {
+          page = page_next;
+          page_next = seen > kEN && lo + 1 < hi ? table[(slot + kEN) >> a.shift] : 0;
+        }
+        const int64_t row = (((int64_t)page * a.H + h) << a.shift) + (slot & ((1 << a.shift) - 1));
+        const uint8_t* const codes = (kv ? a.pool.v_codes : a.pool.k_codes) + row * 64;
+        const uint8_t* const scales = (kv ? a.pool.v_scales : a.pool.k_scales) + row * 4;
+        const uint32_t to = raw + (uint32_t)(fetched & 1) * kERaw;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {  // (slots behind the last: zeros)
-        const int r = 8 * k + in8;
-        t.codes[k] = r < seen ? codes[r * 4 + piece] : make_uint4(0, 0, 0, 0);
-        t.scales[k] = r < seen ? scales[r] : 0u;
+        for (int k = 0; k < 4; ++k) {
+          const int r = 8 * k + (lane >> 2);
+          cp_async16(to + at(r) + piece * 16, codes + (r < seen ? r * 64 + piece * 16 : 0), r < seen ? 16u : 0u);
+        }
+        if (lane < 8) {
+          const int left = max(0, min(16, (seen - 4 * lane) * 4));
+          cp_async16(to + 2048 + lane * 16, scales + (left ? lane * 16 : 0), (uint32_t)left);
+        }
+        if (kv) ++lo;
+        kv ^= 1;
+        ++fetched;
       }
-      if (kv) ++lo;
-      kv ^= 1;
+      cp_async_commit();
     };
-    int idx = 0;
-    auto store = [&](const Tile& t) {
-      const int st = idx % kEStages;
-      if (!(ok = warp_wait(b_empty(st), (uint32_t)(((idx / kEStages) & 1) ^ 1)))) return;
-      ++idx;
-      const uint32_t tile = s0 + oRing + (uint32_t)st * kETile;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int r = 32 * w + 8 * k + in8;
+    fetch();
+    fetch();
+    // Two tiles on their way, which is one step: the walk passes a piece on only when the last but one's products are done.
+    while (ok && stored < fetched) {
+      const int st = stored % kEStages;
+      cp_async_wait<1>();
+      __syncwarp();
+      if (!(ok = warp_wait(b_empty(st), (uint32_t)(((stored / kEStages) & 1) ^ 1)))) break;
+      const uint32_t tile = s0 + oRing + (uint32_t)st * kETile + (32 * w + in8) * 128, from = raw + (uint32_t)(stored & 1) * kERaw;
+#pragma unroll 1
+      for (int k = 0; k < 4; ++k) {  // (not unrolled: the warps' code together would not stay in the instruction caches)
+        const int r = 8 * k + in8;
+        uint4 c;
+        ld_shared_v4(from + at(r) + piece * 16, c);
         uint32_t sc[4];
-        scales_bf16x2(t.scales[k], sc);
-        const uint4 c = t.codes[k];
-        uint32_t word[4] = {c.x, c.y, c.z, c.w};  // keys: word j has group j's eight codes
-        if (t.kv) {                               // values: half words j and j + 4
+        scales_bf16x2(ld_shared_u32(from + 2048 + r * 4), sc);
+        uint32_t word[4] = {c.x, c.y, c.z, c.w};  // keys: word j has group j's eight codes; values: half words j and j + 4
+        if (stored & 1) {
           word[0] = __byte_perm(c.x, c.z, 0x5410); word[1] = __byte_perm(c.x, c.z, 0x7632);
           word[2] = __byte_perm(c.y, c.w, 0x5410); word[3] = __byte_perm(c.y, c.w, 0x7632);
         }
@@ -540,22 +563,16 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
         for (int j = 0; j < 4; ++j) {
           uint32_t v[4];
           unpack8_bf16(word[j], sc[j], v);
-          st_shared_v4(tile + (j >> 1) * kEHalf + r * 128 + ((((j & 1) * 4 + piece) ^ (r & 7)) << 4), make_uint4(v[0], v[1], v[2], v[3]));
+          st_shared_v4(tile + k * 1024 + (j >> 1) * kEHalf + ((((j & 1) * 4 + piece) ^ in8) << 4), make_uint4(v[0], v[1], v[2], v[3]));
         }
       }
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(b_full(st));
-    };
-    // two tiles ahead, which is one step: the walk passes a piece on only when the last but one's products are done
-    Tile t0, t1;
-    fetch(t0);
-    if (ok && t0.kv < 2) fetch(t1);
-    while (ok && t0.kv < 2) {
-      store(t0);
-      t0 = t1;
-      if (ok && t1.kv < 2) fetch(t1);
+      ++stored;
+      fetch();
     }
+    cp_async_wait<0>();
   } else if (warp >= 8) {
   give_registers<kEOtherRegs>();
   if (warp == 8) {
@@ -935,8 +952,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
         l = x0.y * f0 + x1.y * f1;
       }
       if (busy) {
-        __nv_bfloat16* const out = a.out + (p.row0 * a.H * a.G + p.h * a.G) * kED;
-        const uint32_t stage = s0 + oStage + warp * 2048;
+        __nv_bfloat16* const out = a.out + ((p.row0 + my_tok) * a.H * a.G + p.h * a.G + head) * kED;
         const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
         // a one-tile item's columns are shared between the two tiles' warps
         const int c0 = one && steps > 0 ? 2 * g : 0, c1 = one && steps > 0 ? c0 + 2 : (one && g == 1) ? 0 : 4;
@@ -956,23 +972,13 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = 0.f;
           }
-          if (whole) {
-            // A row per thread would be 32 lines per store: the warp's 32 columns are turned in shared memory, four lanes to a row.
+          if (valid && whole) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              st_shared_v4(stage + lane * 64 + ((k ^ (lane >> 1)) & 3) * 16,
-                           make_uint4(pack_bf16x2(o[8 * k] * inv, o[8 * k + 1] * inv), pack_bf16x2(o[8 * k + 2] * inv, o[8 * k + 3] * inv),
-                                      pack_bf16x2(o[8 * k + 4] * inv, o[8 * k + 5] * inv), pack_bf16x2(o[8 * k + 6] * inv, o[8 * k + 7] * inv)));
-            __syncwarp();
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int from = 8 * k + (lane >> 2);
-              const int to = __shfl_sync(0xffffffffu, valid ? (my_tok * a.H * a.G + head) * kED : -1, from);
-              uint4 v;
-              ld_shared_v4(stage + from * 64 + ((lane ^ (from >> 1)) & 3) * 16, v);
-              if (to >= 0) *reinterpret_cast<uint4*>(out + to + 32 * c + (lane & 3) * 8) = v;
-            }
-            __syncwarp();
+            for (int k = 0; k < 32; k += 16)
+              st_global_v8(out + 32 * c + k, pack_bf16x2(o[k] * inv, o[k + 1] * inv), pack_bf16x2(o[k + 2] * inv, o[k + 3] * inv),
+                           pack_bf16x2(o[k + 4] * inv, o[k + 5] * inv), pack_bf16x2(o[k + 6] * inv, o[k + 7] * inv),
+                           pack_bf16x2(o[k + 8] * inv, o[k + 9] * inv), pack_bf16x2(o[k + 10] * inv, o[k + 11] * inv),
+                           pack_bf16x2(o[k + 12] * inv, o[k + 13] * inv), pack_bf16x2(o[k + 14] * inv, o[k + 15] * inv));
           } else if (valid) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) part[(8 * c + k) * a.slot_rows] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
