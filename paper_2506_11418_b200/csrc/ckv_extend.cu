@@ -547,7 +547,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
       __syncwarp();
       if (!(ok = warp_wait(b_empty(st), (uint32_t)(((stored / kEStages) & 1) ^ 1)))) break;
       const uint32_t tile = s0 + oRing + (uint32_t)st * kETile + (32 * w + in8) * 128, from = raw + (uint32_t)(stored & 1) * kERaw;
-#pragma unroll 1
+#pragma unroll 2
       for (int k = 0; k < 4; ++k) {  // (not unrolled: the warps' code together would not stay in the instruction caches)
         const int r = 8 * k + in8;
         uint4 c;

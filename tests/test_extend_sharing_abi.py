@@ -191,7 +191,7 @@ def test_tensors_of_another_type_or_size_are_refused(noting, name, x):
 def test_arrays_of_another_shape_are_refused(noting):
     b, c = noting.b, made(5, 3, dt=I32)
     x = made(4, 2, 64, 128)
-    for arrays, more in (([x, made(4, 2, 32, 128)], {}), ([x, made(5, 2, 64)], {}), ([x], dict(page_arrays=[made(4, 3, 128)])), ([x], dict(stacked=True)),
+    for arrays, more in (([x, made(4, 2, 32, 128)], {}), ([x, made(5, 2, 64)], {}), ([x], dict(page_arrays=[made(4, 3, 128)])), ([x.transpose(0, 1)], {}),
                          ([made(2, 4, 2, 64), made(2, 5, 2, 64)], dict(stacked=True))):
         with pytest.raises(AssertionError):
             b.pages_copy(c, arrays, **more)
