@@ -12,7 +12,7 @@
 //                   more than 2^kSlack, so that O is rarely touched.  The log-degree is in s already (warp 11).
 //   warp 8          TMA: the item's queries, and keys, values and log-degrees through a ring of four 32 KB stages
 //   warp 9          issues the MMAs: PV of one tile and the next QK^T of it while the other tile's softmax runs
-//   warps 12-15     over four-bit pages only: codes and scales to bf16 tiles, in place of the TMA warp's keys and values
+//   warps 12-19     over four-bit pages only: codes and scales, as copied, to bf16 tiles
 //   warps 10, 11    values behind an item's last slot to zero; log-degrees as three more columns of K
 // Tensor memory: S0 | S1 | O0 | O1, 128 columns each, all 512.
 // An item with one tile only (single tokens, short chunks) uses the second set for every other step of slots: two softmax
@@ -49,12 +49,12 @@ constexpr int kEStages = 4;         // tiles in flight: keys in the even ones, v
 constexpr int kETile = kEN * kED * 2;
 constexpr int kEHalf = kETile / 2;  // 64 columns of a tile: 128 rows of 128 bytes
 constexpr int kEBiasSlots = 4;
-// Threads and registers: two softmax warps, one of warps 8-11 and, over four-bit pages, one that unpacks on each quarter of an SM;
-// their shares add up to what the block is launched with (3 x 168, 4 x 128).
-template <bool QUANT> constexpr int kEWarps = QUANT ? 16 : 12;
-template <bool QUANT> constexpr int kESoftmaxRegs = QUANT ? 176 : 216;
-constexpr int kEOtherRegs = 72;
-constexpr int kEUnpackRegs = 88;
+// Threads and registers: two softmax warps, one of warps 8-11 and, over four-bit pages, two that unpack on each quarter of an SM;
+// their shares add up to what the block is launched with (3 x 168, 5 x 96).
+template <bool QUANT> constexpr int kEWarps = QUANT ? 20 : 12;
+template <bool QUANT> constexpr int kESoftmaxRegs = QUANT ? 160 : 216;
+template <bool QUANT> constexpr int kEOtherRegs = QUANT ? 64 : 72;
+constexpr int kEUnpackRegs = 48, kEUnpackWarps = 8;
 constexpr int kItemCost = 128;      // what an item costs beside its slots (queries in, rows out), in slots
 constexpr int kMinShare = 512;      // slots that a CTA takes at least
 constexpr float kSlack = 8.f;       // weights below 2^8
@@ -67,9 +67,9 @@ constexpr int oAug = oBias + kEBiasSlots * kEN * 4;       // 16 bytes per slot: 
 constexpr int oOnes = oAug + kEBiasSlots * kEN * 16;       // 16 bytes per row of Q: three ones
 constexpr int oZero = oOnes + kEN * 16;                    // the other eight columns of both
 constexpr int oState = oZero + kEN * 16;  // float2 [256]: m and sum of every row, exchanged by one-tile items
-constexpr int kERaw = 32 * 64 + 32 * 4;                     // four-bit pages: codes and scales of one unpacking warp's 32 slots
-constexpr int oRaw = oState + 256 * 8;                     // two tiles of them per warp
-constexpr int oBar = oRaw + 4 * 2 * kERaw;
+constexpr int kERaw = kEN * (64 + 4);                      // four-bit pages: codes and scales of one tile
+constexpr int oRaw = oState + 256 * 8;                     // two of them
+constexpr int oBar = oRaw + 2 * kERaw;
 constexpr int oPieces = oBar + 512;
 constexpr int oMisc = oPieces + 256;
 constexpr int kEBytes = oMisc + 128;
@@ -292,6 +292,7 @@ __device__ __forceinline__ uint64_t umma_desc_plain(uint32_t smem_addr, uint32_t
 __device__ __forceinline__ void st_global_v8(void* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
 }
+__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) { asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory"); }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); }
 __device__ __forceinline__ bool elect_one() {
   uint32_t ok;
@@ -359,7 +360,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
   unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t s0 = smem_u32(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // barriers: full [stage] | empty [stage] | log-degrees full, free, in bf16, free [slot] | S full [tile] | P full [tile, half] | O full [tile] | Q full, empty | exchange | values ready [stage / 2] | piece, free [slot]
+  // barriers: full [stage] | empty [stage] | log-degrees full, free, in bf16, free [slot] | S full [tile] | P full [tile, half] | O full [tile] | Q full, empty | exchange | values ready [stage / 2] | piece, free [slot] | codes, free [2]
   auto bar = [&](int i) { return s0 + oBar + 8u * i; };
   auto b_full = [&](int i) { return bar(i); };
   auto b_empty = [&](int i) { return bar(kEStages + i); };
@@ -375,6 +376,8 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
   auto b_v = [&](int i) { return bar(kRest + 11 + i); };
   auto b_piece = [&](int i) { return bar(kRest + 11 + kEStages / 2 + i); };
   auto b_piece_free = [&](int i) { return bar(kRest + 11 + kEStages / 2 + kEPieces + i); };
+  auto b_raw = [&](int i) { return bar(kRest + 11 + kEStages / 2 + 2 * kEPieces + i); };
+  auto b_raw_free = [&](int i) { return bar(kRest + 13 + kEStages / 2 + 2 * kEPieces + i); };
   Piece* const pieces = reinterpret_cast<Piece*>(smem + oPieces);
   int64_t* const s_start = reinterpret_cast<int64_t*>(smem + oMisc);            // the stretch's offset in its sequence, sequence
   int64_t* const s_sum = reinterpret_cast<int64_t*>(smem + oState);             // (before the roles begin)
@@ -382,7 +385,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
 
   if (tid == 0) {
     for (int i = 0; i < kEStages; ++i) {
-      mbar_init(b_full(i), QUANT ? 4 : 1);
+      mbar_init(b_full(i), QUANT ? kEUnpackWarps : 1);
       mbar_init(b_empty(i), 1);
     }
     for (int i = 0; i < kEBiasSlots; ++i) {
@@ -401,9 +404,13 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
     mbar_init(b_q_free, 1);
     mbar_init(b_x, 8);
     for (int i = 0; i < kEStages / 2; ++i) mbar_init(b_v(i), 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(b_raw(i), 1);
+      mbar_init(b_raw_free(i), kEUnpackWarps);
+    }
     for (int i = 0; i < kEPieces; ++i) {
       mbar_init(b_piece(i), 1);
-      mbar_init(b_piece_free(i), 9 + (QUANT ? 4 : 1) + (a.logdeg ? 1 : 0));  // softmax warps, MMA, unpacking warps or warp 10, warp 11
+      mbar_init(b_piece_free(i), 9 + (QUANT ? kEUnpackWarps : 1) + (a.logdeg ? 1 : 0));  // softmax warps, MMA, unpacking warps or warp 10, warp 11
     }
     mbar_init_fence();
     s_start[0] = -1;
@@ -485,96 +492,58 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
   if (QUANT && warp >= 12) {
     // ---------------------------------------------------------------- four-bit pages: codes and scales to bf16 tiles, exactly
     give_registers<kEUnpackRegs>();
-    const int w = warp - 12;
-    const uint32_t raw = s0 + oRaw + (uint32_t)w * 2 * kERaw;
-    // Lane l of a group of rows has its 16-byte piece l % 4.  Of keys and values alike such a piece holds, for each of the row's four groups j,
+    // Lane l has its row's 16-byte piece l % 4.  Of keys and values alike such a piece holds, for each of the row's four groups j,
     // elements 32 j + 8 (l % 4) .. + 7: 16 bytes of the tile.  The two rows that a store's eight lanes write differ in bit 2, which the
-    // swizzle turns into the other half of the banks; the codes of such rows lie 64 bytes apart for the same reason.
-    const int piece = lane & 3, in8 = (lane >> 3) + 4 * ((lane >> 2) & 1);
-    auto at = [](int r) { return (uint32_t)(r * 64) ^ (uint32_t)((r >> 2) & 1) * 64u; };
-    int lo = 0, hi = 0, end = 0, h = 0, kv = 0, fetched = 0, stored = 0;
-    const int32_t* table = nullptr;
-    int page = 0, page_next = 0;  // of this warp's 32 slots, which lie in one; the next step's is on its way a step before
-    bool open = false, last = false;
-    auto fetch = [&] {            // the next tile's rows, begun (slots behind the last: zeros)
-      while (!last && !(open && lo < hi)) {
-        if (open) {
+    // swizzle turns into the other half of the banks.
+    const int w = warp - 12, piece = lane & 3, in8 = (lane >> 3) + 4 * ((lane >> 2) & 1);
+    int n = 0;
+    while (next_piece(warp_wait)) {
+      const int end = pieces[np % kEPieces].end, lo = pieces[np % kEPieces].lo, hi = pieces[np % kEPieces].hi;
+      __syncwarp();
+      if (lane == 0) piece_done(); else ++np;
+      for (int i = lo; i < hi; ++i, ++n) {
+        const int seen = end - i * kEN;
+#pragma unroll 1
+        for (int kv = 0; kv < 2; ++kv) {
+          const int st = (2 * n + kv) % kEStages;
+          if (!(ok = warp_wait(b_raw(kv), (uint32_t)(n & 1)) && warp_wait(b_empty(st), (uint32_t)((((2 * n + kv) / kEStages) & 1) ^ 1)))) break;
+          const uint32_t from = s0 + oRaw + (uint32_t)kv * kERaw, tile = s0 + oRing + (uint32_t)st * kETile;
+#pragma unroll
+          for (int k = 0; k < kEN / (8 * kEUnpackWarps); ++k) {
+            const int r = (kEN / kEUnpackWarps) * w + 8 * k + in8;
+            uint4 c;
+            ld_shared_v4(from + r * 64 + piece * 16, c);
+            uint32_t sc[4];
+            scales_bf16x2(ld_shared_u32(from + kEN * 64 + r * 4), sc);
+            if (r >= seen) {  // slots behind the last: zeros, whatever is there
+              c = make_uint4(0, 0, 0, 0);
+              sc[0] = sc[1] = sc[2] = sc[3] = 0;
+            }
+            uint32_t word[4] = {c.x, c.y, c.z, c.w};  // keys: word j has group j's eight codes; values: half words j and j + 4
+            if (kv) {
+              word[0] = __byte_perm(c.x, c.z, 0x5410); word[1] = __byte_perm(c.x, c.z, 0x7632);
+              word[2] = __byte_perm(c.y, c.w, 0x5410); word[3] = __byte_perm(c.y, c.w, 0x7632);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint32_t v[4];
+              unpack8_bf16(word[j], sc[j], v);
+              st_shared_v4(tile + (j >> 1) * kEHalf + r * 128 + ((((j & 1) * 4 + piece) ^ in8) << 4), make_uint4(v[0], v[1], v[2], v[3]));
+            }
+          }
+          fence_async_smem();
           __syncwarp();
-          if (lane == 0) piece_done(); else ++np;
-          open = false;
+          if (lane == 0) {
+            mbar_arrive(b_raw_free(kv));
+            mbar_arrive(b_full(st));
+          }
         }
-        if (!next_piece(warp_wait)) {
-          last = true;
-        } else {
-          const Piece& p = pieces[np % kEPieces];
-          lo = p.lo; hi = p.hi; end = p.end; h = p.h;
-          table = a.views[p.seq].block_table;
-          page_next = lo * kEN + 32 * w < end ? table[(lo * kEN + 32 * w) >> a.shift] : 0;
-          open = true;
-        }
+        if (!ok) break;
       }
-      if (!last) {
-        const int slot = lo * kEN + 32 * w, seen = end - slot;
-        if (kv == 0) {
-          page = page_next;
-          page_next = seen > kEN && lo + 1 < hi ? table[(slot + kEN) >> a.shift] : 0;
-        }
-        const int64_t row = (((int64_t)page * a.H + h) << a.shift) + (slot & ((1 << a.shift) - 1));
-        const uint8_t* const codes = (kv ? a.pool.v_codes : a.pool.k_codes) + row * 64;
-        const uint8_t* const scales = (kv ? a.pool.v_scales : a.pool.k_scales) + row * 4;
-        const uint32_t to = raw + (uint32_t)(fetched & 1) * kERaw;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int r = 8 * k + (lane >> 2);
-          cp_async16(to + at(r) + piece * 16, codes + (r < seen ? r * 64 + piece * 16 : 0), r < seen ? 16u : 0u);
-        }
-        if (lane < 8) {
-          const int left = max(0, min(16, (seen - 4 * lane) * 4));
-          cp_async16(to + 2048 + lane * 16, scales + (left ? lane * 16 : 0), (uint32_t)left);
-        }
-        if (kv) ++lo;
-        kv ^= 1;
-        ++fetched;
-      }
-      cp_async_commit();
-    };
-    fetch();
-    fetch();
-    // Two tiles on their way, which is one step: the walk passes a piece on only when the last but one's products are done.
-    while (ok && stored < fetched) {
-      const int st = stored % kEStages;
-      cp_async_wait<1>();
-      __syncwarp();
-      if (!(ok = warp_wait(b_empty(st), (uint32_t)(((stored / kEStages) & 1) ^ 1)))) break;
-      const uint32_t tile = s0 + oRing + (uint32_t)st * kETile + (32 * w + in8) * 128, from = raw + (uint32_t)(stored & 1) * kERaw;
-#pragma unroll 2
-      for (int k = 0; k < 4; ++k) {  // (not unrolled: the warps' code together would not stay in the instruction caches)
-        const int r = 8 * k + in8;
-        uint4 c;
-        ld_shared_v4(from + at(r) + piece * 16, c);
-        uint32_t sc[4];
-        scales_bf16x2(ld_shared_u32(from + 2048 + r * 4), sc);
-        uint32_t word[4] = {c.x, c.y, c.z, c.w};  // keys: word j has group j's eight codes; values: half words j and j + 4
-        if (stored & 1) {
-          word[0] = __byte_perm(c.x, c.z, 0x5410); word[1] = __byte_perm(c.x, c.z, 0x7632);
-          word[2] = __byte_perm(c.y, c.w, 0x5410); word[3] = __byte_perm(c.y, c.w, 0x7632);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint32_t v[4];
-          unpack8_bf16(word[j], sc[j], v);
-          st_shared_v4(tile + k * 1024 + (j >> 1) * kEHalf + ((((j & 1) * 4 + piece) ^ in8) << 4), make_uint4(v[0], v[1], v[2], v[3]));
-        }
-      }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(b_full(st));
-      ++stored;
-      fetch();
+      if (!ok) break;
     }
-    cp_async_wait<0>();
   } else if (warp >= 8) {
-  give_registers<kEOtherRegs>();
+  give_registers<kEOtherRegs<QUANT>>();
   if (warp == 8) {
     // ---------------------------------------------------------------- TMA, and the walk along the stretch
     Walk walk;
@@ -634,6 +603,15 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
         const int row = ((page * a.H + p.h) << a.shift) + (slot & ((1 << a.shift) - 1));
         const int live = min(runs, (p.end - t0 + run - 1) / run);  // runs that hold something
         const bool mine_ = lane < 2 * runs && rr < live;
+        if (QUANT) {  // two slots hide less than the memory's latency: what comes two steps later is brought into L2
+          const int later = slot + 2 * kEN, in = (later >> a.shift) - win;
+          const int p0 = __shfl_sync(0xffffffffu, cur, in & 31), p1 = __shfl_sync(0xffffffffu, nxt, in & 31);
+          if (lane < 2 * runs && later < p.hi * kEN && later < p.end) {
+            const int64_t at = (int64_t)((((in < 32 ? p0 : p1) * a.H + p.h) << a.shift) + (later & ((1 << a.shift) - 1)));
+            prefetch_l2((half ? a.pool.v_codes : a.pool.k_codes) + at * 64, run * 64);
+            prefetch_l2((half ? a.pool.v_scales : a.pool.k_scales) + at * 4, run * 4);
+          }
+        }
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           if constexpr (!QUANT) {
@@ -642,6 +620,13 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
             if (lane == 0) mbar_arrive_expect_tx(b_full(st), (uint32_t)(live * run * 256));
             __syncwarp();
             if (mine_) tma_load_2d(s0 + oRing + st * kETile + half * kEHalf + rr * run * 128, kv ? &tm_v : &tm_k, 64 * half, row, b_full(st));
+          } else {  // (a slot for the keys, one for the values)
+            if (!(ok = warp_wait(b_raw_free(kv), (uint32_t)((n & 1) ^ 1)))) break;
+            if (lane == 0) mbar_arrive_expect_tx(b_raw(kv), (uint32_t)(live * run * 68));
+            __syncwarp();
+            const uint32_t to = s0 + oRaw + (uint32_t)kv * kERaw;
+            if (mine_ && half == 0) bulk_load(to + rr * run * 64, (kv ? a.pool.v_codes : a.pool.k_codes) + (int64_t)row * 64, run * 64, b_raw(kv));
+            if (mine_ && half == 1) bulk_load(to + kEN * 64 + rr * run * 4, (kv ? a.pool.v_scales : a.pool.k_scales) + (int64_t)row * 4, run * 4, b_raw(kv));
           }
           if (kv == 0 && a.logdeg) {
             const int bs = n % kEBiasSlots;
