@@ -12,7 +12,7 @@
 //                   more than 2^kSlack, so that O is rarely touched.  The log-degree is in s already (warp 11).
 //   warp 8          TMA: the item's queries, and keys, values and log-degrees through a ring of four 32 KB stages
 //   warp 9          issues the MMAs: PV of one tile and the next QK^T of it while the other tile's softmax runs
-//   warps 12-19     over four-bit pages only: codes and scales, as copied, to bf16 tiles
+//   warps 12-19     over four-bit pages only: codes and scales, which warp 10 copies, to bf16 tiles
 //   warps 10, 11    values behind an item's last slot to zero; log-degrees as three more columns of K
 // Tensor memory: S0 | S1 | O0 | O1, 128 columns each, all 512.
 // An item with one tile only (single tokens, short chunks) uses the second set for every other step of slots: two softmax
@@ -45,7 +45,8 @@ using namespace ptx;
 
 constexpr int kED = 128;            // head_dim
 constexpr int kEN = 128;            // slots per step; rows per tile
-constexpr int kEStages = 4;         // tiles in flight: keys in the even ones, values in the odd
+constexpr int kEStages = 4;         // bf16 tiles in flight: keys in the even ones, values in the odd
+constexpr int kERawSlots = 2;       // four-bit pages: tiles as they are, keys and values in turn
 constexpr int kETile = kEN * kED * 2;
 constexpr int kEHalf = kETile / 2;  // 64 columns of a tile: 128 rows of 128 bytes
 constexpr int kEBiasSlots = 4;
@@ -67,9 +68,9 @@ constexpr int oAug = oBias + kEBiasSlots * kEN * 4;       // 16 bytes per slot: 
 constexpr int oOnes = oAug + kEBiasSlots * kEN * 16;       // 16 bytes per row of Q: three ones
 constexpr int oZero = oOnes + kEN * 16;                    // the other eight columns of both
 constexpr int oState = oZero + kEN * 16;  // float2 [256]: m and sum of every row, exchanged by one-tile items
-constexpr int kERaw = kEN * (64 + 4);                      // four-bit pages: codes and scales of one tile
-constexpr int oRaw = oState + 256 * 8;                     // two of them
-constexpr int oBar = oRaw + 2 * kERaw;
+constexpr int kERaw = kEN * (64 + 4);                      // codes and scales of one tile
+constexpr int oRaw = oState + 256 * 8;
+constexpr int oBar = oRaw + kERawSlots * kERaw;
 constexpr int oPieces = oBar + 512;
 constexpr int oMisc = oPieces + 256;
 constexpr int kEBytes = oMisc + 128;
@@ -292,7 +293,10 @@ __device__ __forceinline__ uint64_t umma_desc_plain(uint32_t smem_addr, uint32_t
 __device__ __forceinline__ void st_global_v8(void* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
 }
-__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) { asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory"); }
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// one arrival of every lane once its copies so far are there
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); }
 __device__ __forceinline__ bool elect_one() {
   uint32_t ok;
@@ -360,7 +364,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
   unsigned char* const smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t s0 = smem_u32(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // barriers: full [stage] | empty [stage] | log-degrees full, free, in bf16, free [slot] | S full [tile] | P full [tile, half] | O full [tile] | Q full, empty | exchange | values ready [stage / 2] | piece, free [slot] | codes, free [2]
+  // barriers: full [stage] | empty [stage] | log-degrees full, free, in bf16, free [slot] | S full [tile] | P full [tile, half] | O full [tile] | Q full, empty | exchange | values ready [stage / 2] | piece, free [slot] | codes, free [slot]
   auto bar = [&](int i) { return s0 + oBar + 8u * i; };
   auto b_full = [&](int i) { return bar(i); };
   auto b_empty = [&](int i) { return bar(kEStages + i); };
@@ -377,7 +381,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
   auto b_piece = [&](int i) { return bar(kRest + 11 + kEStages / 2 + i); };
   auto b_piece_free = [&](int i) { return bar(kRest + 11 + kEStages / 2 + kEPieces + i); };
   auto b_raw = [&](int i) { return bar(kRest + 11 + kEStages / 2 + 2 * kEPieces + i); };
-  auto b_raw_free = [&](int i) { return bar(kRest + 13 + kEStages / 2 + 2 * kEPieces + i); };
+  auto b_raw_free = [&](int i) { return bar(kRest + 11 + kEStages / 2 + 2 * kEPieces + kERawSlots + i); };
   Piece* const pieces = reinterpret_cast<Piece*>(smem + oPieces);
   int64_t* const s_start = reinterpret_cast<int64_t*>(smem + oMisc);            // the stretch's offset in its sequence, sequence
   int64_t* const s_sum = reinterpret_cast<int64_t*>(smem + oState);             // (before the roles begin)
@@ -404,13 +408,13 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
     mbar_init(b_q_free, 1);
     mbar_init(b_x, 8);
     for (int i = 0; i < kEStages / 2; ++i) mbar_init(b_v(i), 1);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(b_raw(i), 1);
+    for (int i = 0; i < kERawSlots; ++i) {
+      mbar_init(b_raw(i), 32);
       mbar_init(b_raw_free(i), kEUnpackWarps);
     }
     for (int i = 0; i < kEPieces; ++i) {
       mbar_init(b_piece(i), 1);
-      mbar_init(b_piece_free(i), 9 + (QUANT ? kEUnpackWarps : 1) + (a.logdeg ? 1 : 0));  // softmax warps, MMA, unpacking warps or warp 10, warp 11
+      mbar_init(b_piece_free(i), 10 + (QUANT ? kEUnpackWarps : 0) + (a.logdeg ? 1 : 0));  // softmax warps, MMA, unpacking warps, warps 10 and 11
     }
     mbar_init_fence();
     s_start[0] = -1;
@@ -496,49 +500,44 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
     // elements 32 j + 8 (l % 4) .. + 7: 16 bytes of the tile.  The two rows that a store's eight lanes write differ in bit 2, which the
     // swizzle turns into the other half of the banks.
     const int w = warp - 12, piece = lane & 3, in8 = (lane >> 3) + 4 * ((lane >> 2) & 1);
-    int n = 0;
+    int idx = 0;
     while (next_piece(warp_wait)) {
       const int end = pieces[np % kEPieces].end, lo = pieces[np % kEPieces].lo, hi = pieces[np % kEPieces].hi;
       __syncwarp();
       if (lane == 0) piece_done(); else ++np;
-      for (int i = lo; i < hi; ++i, ++n) {
-        const int seen = end - i * kEN;
+      for (int i = 2 * lo; i < 2 * hi; ++i, ++idx) {  // keys, values, keys, ...
+        const int seen = end - (i >> 1) * kEN, st = idx % kEStages, slot = idx % kERawSlots;
+        const uint32_t from = s0 + oRaw + slot * kERaw, tile = s0 + oRing + (uint32_t)st * kETile;
+        if (!(ok = warp_wait(b_raw(slot), (uint32_t)((idx / kERawSlots) & 1)) && warp_wait(b_empty(st), (uint32_t)(((idx / kEStages) & 1) ^ 1)))) break;
 #pragma unroll 1
-        for (int kv = 0; kv < 2; ++kv) {
-          const int st = (2 * n + kv) % kEStages;
-          if (!(ok = warp_wait(b_raw(kv), (uint32_t)(n & 1)) && warp_wait(b_empty(st), (uint32_t)((((2 * n + kv) / kEStages) & 1) ^ 1)))) break;
-          const uint32_t from = s0 + oRaw + (uint32_t)kv * kERaw, tile = s0 + oRing + (uint32_t)st * kETile;
-#pragma unroll
-          for (int k = 0; k < kEN / (8 * kEUnpackWarps); ++k) {
-            const int r = (kEN / kEUnpackWarps) * w + 8 * k + in8;
-            uint4 c;
-            ld_shared_v4(from + r * 64 + piece * 16, c);
-            uint32_t sc[4];
-            scales_bf16x2(ld_shared_u32(from + kEN * 64 + r * 4), sc);
-            if (r >= seen) {  // slots behind the last: zeros, whatever is there
-              c = make_uint4(0, 0, 0, 0);
-              sc[0] = sc[1] = sc[2] = sc[3] = 0;
-            }
-            uint32_t word[4] = {c.x, c.y, c.z, c.w};  // keys: word j has group j's eight codes; values: half words j and j + 4
-            if (kv) {
-              word[0] = __byte_perm(c.x, c.z, 0x5410); word[1] = __byte_perm(c.x, c.z, 0x7632);
-              word[2] = __byte_perm(c.y, c.w, 0x5410); word[3] = __byte_perm(c.y, c.w, 0x7632);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              uint32_t v[4];
-              unpack8_bf16(word[j], sc[j], v);
-              st_shared_v4(tile + (j >> 1) * kEHalf + r * 128 + ((((j & 1) * 4 + piece) ^ in8) << 4), make_uint4(v[0], v[1], v[2], v[3]));
-            }
+        for (int k = 0; k < kEN / (8 * kEUnpackWarps); ++k) {  // (not unrolled: the roles' code together would not stay in the instruction cache)
+          const int r = (kEN / kEUnpackWarps) * w + 8 * k + in8;
+          uint4 c;
+          ld_shared_v4(from + r * 64 + piece * 16, c);
+          uint32_t sc[4];
+          scales_bf16x2(ld_shared_u32(from + kEN * 64 + r * 4), sc);
+          if (r >= seen) {  // slots behind the last: zeros, whatever is there
+            c = make_uint4(0, 0, 0, 0);
+            sc[0] = sc[1] = sc[2] = sc[3] = 0;
           }
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(b_raw_free(kv));
-            mbar_arrive(b_full(st));
+          uint32_t word[4] = {c.x, c.y, c.z, c.w};  // keys: word j has group j's eight codes; values: half words j and j + 4
+          if (i & 1) {
+            word[0] = __byte_perm(c.x, c.z, 0x5410); word[1] = __byte_perm(c.x, c.z, 0x7632);
+            word[2] = __byte_perm(c.y, c.w, 0x5410); word[3] = __byte_perm(c.y, c.w, 0x7632);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t v[4];
+            unpack8_bf16(word[j], sc[j], v);
+            st_shared_v4(tile + (j >> 1) * kEHalf + r * 128 + ((((j & 1) * 4 + piece) ^ in8) << 4), make_uint4(v[0], v[1], v[2], v[3]));
           }
         }
-        if (!ok) break;
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(b_raw_free(slot));
+          mbar_arrive(b_full(st));
+        }
       }
       if (!ok) break;
     }
@@ -603,15 +602,6 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
         const int row = ((page * a.H + p.h) << a.shift) + (slot & ((1 << a.shift) - 1));
         const int live = min(runs, (p.end - t0 + run - 1) / run);  // runs that hold something
         const bool mine_ = lane < 2 * runs && rr < live;
-        if (QUANT) {  // two slots hide less than the memory's latency: what comes two steps later is brought into L2
-          const int later = slot + 2 * kEN, in = (later >> a.shift) - win;
-          const int p0 = __shfl_sync(0xffffffffu, cur, in & 31), p1 = __shfl_sync(0xffffffffu, nxt, in & 31);
-          if (lane < 2 * runs && later < p.hi * kEN && later < p.end) {
-            const int64_t at = (int64_t)((((in < 32 ? p0 : p1) * a.H + p.h) << a.shift) + (later & ((1 << a.shift) - 1)));
-            prefetch_l2((half ? a.pool.v_codes : a.pool.k_codes) + at * 64, run * 64);
-            prefetch_l2((half ? a.pool.v_scales : a.pool.k_scales) + at * 4, run * 4);
-          }
-        }
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           if constexpr (!QUANT) {
@@ -620,13 +610,6 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
             if (lane == 0) mbar_arrive_expect_tx(b_full(st), (uint32_t)(live * run * 256));
             __syncwarp();
             if (mine_) tma_load_2d(s0 + oRing + st * kETile + half * kEHalf + rr * run * 128, kv ? &tm_v : &tm_k, 64 * half, row, b_full(st));
-          } else {  // (a slot for the keys, one for the values)
-            if (!(ok = warp_wait(b_raw_free(kv), (uint32_t)((n & 1) ^ 1)))) break;
-            if (lane == 0) mbar_arrive_expect_tx(b_raw(kv), (uint32_t)(live * run * 68));
-            __syncwarp();
-            const uint32_t to = s0 + oRaw + (uint32_t)kv * kERaw;
-            if (mine_ && half == 0) bulk_load(to + rr * run * 64, (kv ? a.pool.v_codes : a.pool.k_codes) + (int64_t)row * 64, run * 64, b_raw(kv));
-            if (mine_ && half == 1) bulk_load(to + kEN * 64 + rr * run * 4, (kv ? a.pool.v_scales : a.pool.k_scales) + (int64_t)row * 4, run * 4, b_raw(kv));
           }
           if (kv == 0 && a.logdeg) {
             const int bs = n % kEBiasSlots;
@@ -669,68 +652,58 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
         if (a.logdeg) umma_bf16(tmem + (uint32_t)g * 128, d_ones, d_aug + (uint64_t)((n + i) % kEBiasSlots) * kAugStep, kDescQK, 1u);
         umma_commit(b_s(g));
       };
-      auto pv = [&](int g, int i, int ks0, bool more) {  // four of the eight steps of 16 slots
+      auto pv = [&](int g, int i, bool more) {
         const uint64_t dv = d_v + (uint64_t)((2 * (n + i) + 1) % kEStages) * (kETile >> 4);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {  // as the weights arrive
+          if (!(ok = bar_wait(b_p(g, half), par[g]))) return;
+          tc_fence_after();
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-          umma_bf16_ts(tmem + 256 + (uint32_t)g * 128, tmem + (uint32_t)g * 128 + 8 * (ks0 + ks), dv + (uint64_t)(ks0 + ks) * 128, kDescPV, (more || ks) ? 1u : 0u);
+          for (int ks = 0; ks < 4; ++ks)
+            umma_bf16_ts(tmem + 256 + (uint32_t)g * 128, tmem + (uint32_t)g * 128 + 32 * half + 8 * ks, dv + (uint64_t)(4 * half + ks) * 128, kDescPV,
+                         (more || half || ks) ? 1u : 0u);
+        }
+        par[g] ^= 1;
       };
       auto stage_full = [&](int idx) { return bar_wait(b_full(idx % kEStages), (uint32_t)((idx / kEStages) & 1)); };
       auto keys = [&](int i) {               // of the piece's step i, and its log-degrees
         return stage_full(2 * (n + i)) &&
                (!a.logdeg || bar_wait(b_bias_ready((n + i) % kEBiasSlots), (uint32_t)(((n + i) / kEBiasSlots) & 1)));
       };
-      auto release_keys = [&](int i) {
-        umma_commit(b_empty(2 * (n + i) % kEStages));
-        if (a.logdeg) umma_commit(b_aug_free((n + i) % kEBiasSlots));
+      auto values = [&](int i) {
+        return QUANT ? stage_full(2 * (n + i) + 1) : bar_wait(b_v((n + i) % (kEStages / 2)), (uint32_t)(((n + i) / (kEStages / 2)) & 1));
       };
-      auto release = [&](int idx) { umma_commit(b_empty(idx % kEStages)); };
       while (next_piece(bar_wait)) {
         const int steps = pieces[np % kEPieces].hi - pieces[np % kEPieces].lo;
         const bool one = pieces[np % kEPieces].flags & kOneTile;
         piece_done();
         if (steps <= 0) continue;
-        const int ahead = one ? 2 : 1;
-        if (!(ok = bar_wait(b_q, (uint32_t)(nq++ & 1)) && keys(0))) break;
-        tc_fence_after();
-        qk(0, 0);
-        if (one) {
-          release_keys(0);
-          if (steps > 1) {
-            if (!(ok = keys(1))) break;
-            tc_fence_after();
-            qk(1, 1);
-            release_keys(1);
+        // Tiles of scores in the order of their products: of a pair's two tiles in turn, of a single one's steps in turn.  PV of tile j is
+        // followed by QK^T of tile j + 2, which takes its place.
+        const int tiles = one ? steps : 2 * steps;
+        if (!(ok = bar_wait(b_q, (uint32_t)(nq++ & 1)))) break;
+#pragma unroll 1
+        for (int j = -2; j < tiles; ++j) {
+          const int g = j & 1;
+          if (j >= 0) {
+            const int i = one ? j : j >> 1;
+            if ((one || g == 0) && !(ok = values(i))) break;
+            pv(g, i, j >= 2);
+            if (!ok) break;
+            if (one || g == 1) umma_commit(b_empty((2 * (n + i) + 1) % kEStages));
+            if (!one && j >= tiles - 2) umma_commit(b_o(g));
           }
-        } else {
-          qk(1, 0);
-          release_keys(0);
-        }
-        if (steps <= ahead) umma_commit(b_q_free);
-        for (int i = 0; ok && i < steps; ++i) {
-          const int g0 = one ? i & 1 : 0, g1 = one ? g0 : 1;
-          const bool more = i + ahead < steps;
-          const int iv = n + i;
-          if (!(ok = bar_wait(QUANT ? b_full((2 * iv + 1) % kEStages) : b_v(iv % (kEStages / 2)), (uint32_t)((iv / (kEStages / 2)) & 1)))) break;
-          for (int g = g0; g <= g1; ++g) {
-            if (!(ok = bar_wait(b_p(g, 0), par[g]))) break;
+          if (j + 2 < tiles) {
+            const int i = one ? j + 2 : (j + 2) >> 1;
+            if ((one || g == 0) && !(ok = keys(i))) break;
             tc_fence_after();
-            pv(g, i, 0, i >= ahead);
-            if (!(ok = bar_wait(b_p(g, 1), par[g]))) break;
-            par[g] ^= 1;
-            tc_fence_after();
-            pv(g, i, 4, true);
-            if (g == g1) release(2 * (n + i) + 1);
-            if (more) {
-              if (g == g0 && !(ok = keys(i + ahead))) break;
-              tc_fence_after();
-              qk(g, i + ahead);
-              if (g == g1) release_keys(i + ahead);
-            } else if (!one) {
-              umma_commit(b_o(g));
+            qk(g, i);
+            if (one || g == 1) {
+              umma_commit(b_empty(2 * (n + i) % kEStages));
+              if (a.logdeg) umma_commit(b_aug_free((n + i) % kEBiasSlots));
             }
+            if (j + 3 == tiles) umma_commit(b_q_free);
           }
-          if (i + ahead == steps - 1) umma_commit(b_q_free);
         }
         if (!ok) break;
         if (one) {
@@ -740,7 +713,61 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
         n += steps;
       }
     }
-  } else if (warp == 10 && !QUANT) {
+  } else if (QUANT && warp == 10) {
+    // ---------------------------------------------------------------- four-bit pages: codes and scales of a tile, as they are.  (Bulk copies of
+    // a page's few KB each take about 50 ns to issue; these are 17 instructions per tile.)  What comes two steps later is
+    // brought into L2.
+    int n = 0;
+    while (next_piece(warp_wait)) {
+      const Piece& p = pieces[np % kEPieces];
+      const int end = p.end, lo = p.lo, hi = p.hi, h = p.h;
+      const int32_t* const table = a.views[p.seq].block_table;
+      __syncwarp();
+      if (lane == 0) piece_done(); else ++np;
+      // rows of the pool at which the 32 slots of quarter lane / 8 of step i begin; none behind the last slot
+      auto row_of = [&](int i) -> int {
+        const int slot = i * kEN + 32 * (lane >> 3);
+        return i < hi && slot < end ? ((table[slot >> a.shift] * a.H + h) << a.shift) + (slot & ((1 << a.shift) - 1)) : -1;
+      };
+      auto fetch_l2 = [&](int row) {
+        if (row < 0) return;
+        const int c = lane & 7;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          const uint8_t* const codes = (kv ? a.pool.v_codes : a.pool.k_codes) + (int64_t)row * 64;
+          prefetch_l2(codes + c * 128);
+          prefetch_l2(codes + (c + 8) * 128);
+          if (c == 0) prefetch_l2((kv ? a.pool.v_scales : a.pool.k_scales) + (int64_t)row * 4);
+        }
+      };
+      int r0 = row_of(lo), r1 = row_of(lo + 1), r2 = row_of(lo + 2);
+      fetch_l2(r1);
+      for (int i = lo; i < hi; ++i, ++n) {
+        fetch_l2(r2);
+        const int r3 = row_of(i + 3);
+#pragma unroll 1
+        for (int kv = 0; kv < 2; ++kv) {
+          const int slot = (2 * n + kv) % kERawSlots;
+          if (!(ok = warp_wait(b_raw_free(slot), (uint32_t)((((2 * n + kv) / kERawSlots) & 1) ^ 1)))) break;
+          const uint32_t to = s0 + oRaw + slot * kERaw + (lane >> 3) * 2048 + (lane & 7) * 16;
+          const uint8_t* const codes = (kv ? a.pool.v_codes : a.pool.k_codes);
+          const uint8_t* const from = codes + (r0 < 0 ? 0 : (int64_t)r0 * 64 + (lane & 7) * 16);
+          const uint32_t bytes = r0 < 0 ? 0 : 16;
+#pragma unroll
+          for (int k = 0; k < 16; ++k) cp_async16(to + k * 128, from + (r0 < 0 ? 0 : k * 128), bytes);
+          const uint8_t* const scales = kv ? a.pool.v_scales : a.pool.k_scales;
+          cp_async16(s0 + oRaw + slot * kERaw + kEN * 64 + lane * 16, scales + (r0 < 0 ? 0 : (int64_t)r0 * 4 + (lane & 7) * 16), bytes);
+          cp_async_arrive(b_raw(slot));
+        }
+        if (!ok) break;
+        r0 = r1;
+        r1 = r2;
+        r2 = r3;
+      }
+      if (!ok) break;
+    }
+    cp_async_wait_all();
+  } else if (warp == 10) {
     // ---------------------------------------------------------------- slots behind the last that an item sees: whatever their values
     // are, they must not meet a weight of zero
     int n = 0;
