@@ -11,10 +11,27 @@
 namespace ckv {
 namespace {
 
-// Both table kernels are one cluster of kCtas thread blocks: their phases hand counts of pages over to one another (a few
+// Both table kernels are one cluster of eight thread blocks: their phases hand counts of pages over to one another (a few
 // hundred KB, in L2), and a barrier of the cluster (about a microsecond) is cheaper than a launch.  Bound by latency: a phase
-// is a chain of two or three loads.
+// is a chain of two or three loads.  A small pool takes one block and has the counts in shared memory.
 constexpr int kCtas = 8;
+constexpr int64_t kSmallPool = 16384;  // pages
+constexpr int kSmallRows = 1024;
+template <int CL>
+__device__ __forceinline__ void sync_all() {
+  if constexpr (CL > 1)
+    cluster_sync_all();
+  else
+    __syncthreads();
+}
+// a count that other threads have changed
+template <int CL>
+__device__ __forceinline__ int32_t count_of(const int32_t* p) {
+  if constexpr (CL > 1)
+    return __ldcg(p);
+  else
+    return *p;
+}
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxRows = 8192;
@@ -90,19 +107,26 @@ __device__ __forceinline__ ForkRow fork_row(const ForkArgs& a, int b) {
   return r;
 }
 
-__global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_fork_kernel(const ForkArgs a) {
-  extern __shared__ int32_t rows[];  // [n_in] first child of every old row, [n_out] takes before every new row
+template <int CL>
+__global__ void __launch_bounds__(kThreads) pages_fork_kernel(const ForkArgs a) {
+  // [n_out] tokens kept, parent, the page that is filled in part (-1: none), takes before; [n_in] first child; one block: the pages' counts
+  extern __shared__ int64_t rows[];
   __shared__ int s_warp[kWarps];
-  int32_t* const child = rows;
-  int32_t* const before = rows + a.n_in;
+  int64_t* const kept = rows;
+  int32_t* const parent = reinterpret_cast<int32_t*>(kept + a.n_out);
+  int32_t* const tail = parent + a.n_out;
+  int32_t* const before = tail + a.n_out;
+  int32_t* const child = before + a.n_out;
+  int32_t* const delta = CL > 1 ? a.delta : child + a.n_in;
+  int32_t* const first = CL > 1 ? a.first : delta + a.n_pages;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
-  const int gwarp = cta * kWarps + warp, n_warps = kCtas * kWarps;
-  const int64_t gid = (int64_t)cta * kThreads + tid, gsize = kCtas * kThreads, mask = ((int64_t)1 << a.shift) - 1;
+  const int gwarp = cta * kWarps + warp, n_warps = CL * kWarps;
+  const int64_t gid = (int64_t)cta * kThreads + tid, gsize = CL * kThreads, mask = ((int64_t)1 << a.shift) - 1;
   griddep_wait();
   griddep_launch();
   for (int64_t p = gid; p < a.n_pages; p += gsize) {
-    a.delta[p] = 0;
-    a.first[p] = INT_MAX;
+    delta[p] = 0;
+    first[p] = INT_MAX;
   }
   if (gid == 0) a.head->flags = 0;
   for (int b = tid; b < a.n_in; b += kThreads) child[b] = INT_MAX;
@@ -111,11 +135,24 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_
   for (int b = tid; b < a.n_out; b += kThreads) {
     const ForkRow r = fork_row(a, b);
     bad |= !r.ok;
-    if (r.p >= 0) atomicMin(&child[r.p], b);
+    kept[b] = r.n;
+    parent[b] = r.p;
+    int32_t page = -1;
+    if (r.p >= 0) {
+      atomicMin(&child[r.p], b);
+      if (r.n & mask) {
+        page = a.tables[r.p * a.stride + (r.n >> a.shift)];
+        if ((uint32_t)page >= (uint32_t)a.n_pages) {
+          bad = true;
+          page = -1;
+        }
+      }
+    }
+    tail[b] = page;
   }
   const int64_t head = a.ring_state[0], count = a.ring_state[1];
   bad |= head < 0 || head >= a.n_pages || count < 0 || count > a.n_pages;
-  cluster_sync_all();
+  sync_all<CL>();
 
   // a warp per row: blocks that an old row lists and its first child does not hold whole; blocks that further children hold whole
   for (int b = gwarp; b < a.n_in; b += n_warps) {
@@ -124,57 +161,46 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_
       bad = true;
       continue;
     }
-    const int64_t have = (len + mask) >> a.shift, from = child[b] == INT_MAX ? 0 : fork_row(a, child[b]).n >> a.shift;
+    const int64_t have = (len + mask) >> a.shift, from = child[b] == INT_MAX ? 0 : kept[child[b]] >> a.shift;
     for (int64_t i = lane; i < have; i += 32) {
       const int32_t page = a.tables[b * a.stride + i];
       if ((uint32_t)page >= (uint32_t)a.n_pages)
         bad = true;
       else if (i >= from)
-        atomicSub(&a.delta[page], 1);
+        atomicSub(&delta[page], 1);
     }
   }
   for (int b = gwarp; b < a.n_out; b += n_warps) {
-    const ForkRow r = fork_row(a, b);
-    if (r.p < 0) continue;
-    const int64_t whole = r.n >> a.shift;
-    const int32_t* const row = a.tables + r.p * a.stride;
-    if (child[r.p] != b)
-      for (int64_t i = lane; i < whole; i += 32) {
-        const int32_t page = row[i];
-        if ((uint32_t)page < (uint32_t)a.n_pages) atomicAdd(&a.delta[page], 1);
-      }
-    if (lane == 0 && (r.n & mask)) {
-      const int32_t page = row[whole];
-      if ((uint32_t)page < (uint32_t)a.n_pages) atomicMin(&a.first[page], b);
+    if (parent[b] < 0 || child[parent[b]] == b) continue;
+    const int32_t* const row = a.tables + parent[b] * a.stride;
+    for (int64_t i = lane; i < kept[b] >> a.shift; i += 32) {
+      const int32_t page = row[i];
+      if ((uint32_t)page < (uint32_t)a.n_pages) atomicAdd(&delta[page], 1);
     }
   }
+  for (int b = (int)gid; b < a.n_out; b += (int)gsize)
+    if (tail[b] >= 0) atomicMin(&first[tail[b]], b);
   if (bad) atomicOr(&a.head->flags, 1);
-  cluster_sync_all();
+  sync_all<CL>();
 
   // new rows that need a page of their own, in order (every CTA for itself); pages nobody holds any more, a run of pages per CTA
   int taken = 0;
   bad = false;
   for (int b0 = 0; b0 < a.n_out; b0 += kThreads) {
     const int b = b0 + tid;
-    int take = 0;
-    if (b < a.n_out) {
-      const ForkRow r = fork_row(a, b);
-      if (r.p >= 0 && (r.n & mask)) {
-        const int32_t page = a.tables[r.p * a.stride + (r.n >> a.shift)];
-        if ((uint32_t)page < (uint32_t)a.n_pages) take = !(a.shared[page] + 1 + __ldcg(&a.delta[page]) == 0 && __ldcg(&a.first[page]) == b);
-      }
-    }
+    const int32_t page = b < a.n_out ? tail[b] : -1;
+    const int take = page >= 0 && !(a.shared[page] + 1 + count_of<CL>(&delta[page]) == 0 && count_of<CL>(&first[page]) == b);
     int total;
     const int x = block_scan(take, s_warp, total);
     if (b < a.n_out) before[b] = take ? taken + x : -1 - (taken + x);  // (negative: it takes none)
     taken += total;
   }
-  const int64_t per = (a.n_pages + kCtas - 1) / kCtas, p0 = min(a.n_pages, cta * per), p1 = min(a.n_pages, p0 + per);
+  const int64_t per = (a.n_pages + CL - 1) / CL, p0 = min(a.n_pages, cta * per), p1 = min(a.n_pages, p0 + per);
   auto is_freed = [&](int64_t p, int32_t& left) {
-    const int32_t d = __ldcg(&a.delta[p]);
+    const int32_t d = count_of<CL>(&delta[p]);
     left = a.shared[p] + d;
     bad |= left < -1 || a.shared[p] < 0;
-    return d < 0 && left == -1 && __ldcg(&a.first[p]) == INT_MAX;
+    return d < 0 && left == -1 && count_of<CL>(&first[p]) == INT_MAX;
   };
   int freed = 0;
   for (int64_t p = p0 + tid; p < p1; p += kThreads) {
@@ -185,10 +211,10 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_
   block_scan(freed, s_warp, total);
   if (bad) atomicOr(&a.head->flags, 1);
   if (tid == 0) a.head->count[cta] = total;
-  cluster_sync_all();
+  sync_all<CL>();
 
   int64_t freed_before = 0, freed_all = 0;
-  for (int c = 0; c < kCtas; ++c) {
+  for (int c = 0; c < CL; ++c) {
     const int x = __ldcg(&a.head->count[c]);
     freed_before += c < cta ? x : 0;
     freed_all += x;
@@ -225,12 +251,11 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_
   for (int b = (int)gid; b < a.n_out; b += (int)gsize) {
     if (status || b >= taken) a.copies[3 * b] = a.copies[3 * b + 1] = a.copies[3 * b + 2] = -1;
   }
-  cluster_sync_all();
+  sync_all<CL>();
   if (status) return;
   for (int b = gwarp; b < a.n_out; b += n_warps) {
-    const ForkRow r = fork_row(a, b);
-    const int64_t whole = r.n >> a.shift, blocks = (r.n + mask) >> a.shift;
-    const int32_t* const from = a.tables + max(r.p, 0) * a.stride;
+    const int64_t n = kept[b], whole = n >> a.shift, blocks = (n + mask) >> a.shift;
+    const int32_t* const from = a.tables + max(parent[b], 0) * a.stride;
     int32_t* const to = a.tables_out + b * a.stride;
     for (int64_t i = lane; i < blocks; i += 32) {
       int32_t page = from[i];
@@ -239,14 +264,14 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_
         if (at >= a.n_pages) at -= a.n_pages;
         const int32_t mine = __ldcg(&a.ring[at]);
         int32_t* const c = a.copies + 3 * before[b];
-        c[0] = page; c[1] = mine; c[2] = (int32_t)(r.n & mask);
+        c[0] = page; c[1] = mine; c[2] = (int32_t)(n & mask);
         page = mine;
       }
       to[i] = page;
     }
     if (lane == 0) {
-      a.lens_out[b] = r.n;
-      if (a.views) a.views[b] = ckv_paged_view{to, r.n};
+      a.lens_out[b] = n;
+      if (a.views) a.views[b] = ckv_paged_view{to, n};
     }
   }
 }
@@ -270,19 +295,22 @@ struct CompactArgs {
   int32_t Bz, shift;
 };
 
-__global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_compact_kernel(const CompactArgs a) {
+template <int CL>
+__global__ void __launch_bounds__(kThreads) pages_compact_kernel(const CompactArgs a) {
+  extern __shared__ int32_t s_mark[];  // one block: the pages' marks
   __shared__ int s_warp[kWarps];
+  int32_t* const mark = CL > 1 ? a.mark : s_mark;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
-  const int gwarp = cta * kWarps + warp, n_warps = kCtas * kWarps;
-  const int64_t gid = (int64_t)cta * kThreads + tid, gsize = kCtas * kThreads, mask = ((int64_t)1 << a.shift) - 1;
+  const int gwarp = cta * kWarps + warp, n_warps = CL * kWarps;
+  const int64_t gid = (int64_t)cta * kThreads + tid, gsize = CL * kThreads, mask = ((int64_t)1 << a.shift) - 1;
   griddep_wait();
   griddep_launch();
-  for (int64_t p = gid; p < a.n_pages; p += gsize) a.mark[p] = 0;
+  for (int64_t p = gid; p < a.n_pages; p += gsize) mark[p] = 0;
   if (gid == 0) {
     a.head->flags = 0;
     a.head->front = 0;
   }
-  cluster_sync_all();
+  sync_all<CL>();
   bool bad = false;
   for (int b = gwarp; b < a.Bz; b += n_warps) {
     const int64_t len = a.lens[b];
@@ -295,28 +323,28 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_
       if ((uint32_t)page >= (uint32_t)a.n_pages)
         bad = true;
       else
-        a.mark[page] = 1;
+        mark[page] = 1;
     }
   }
   if (bad) atomicOr(&a.head->flags, 1);
-  cluster_sync_all();
-  const int64_t per = (a.n_pages + kCtas - 1) / kCtas, p0 = min(a.n_pages, cta * per), p1 = min(a.n_pages, p0 + per);
+  sync_all<CL>();
+  const int64_t per = (a.n_pages + CL - 1) / CL, p0 = min(a.n_pages, cta * per), p1 = min(a.n_pages, p0 + per);
   int held = 0, total;
-  for (int64_t p = p0 + tid; p < p1; p += kThreads) held += __ldcg(&a.mark[p]);
+  for (int64_t p = p0 + tid; p < p1; p += kThreads) held += count_of<CL>(&mark[p]);
   block_scan(held, s_warp, total);
   if (tid == 0) a.head->count[cta] = total;
-  cluster_sync_all();
+  sync_all<CL>();
   int64_t held_before = 0, U = 0;
-  for (int c = 0; c < kCtas; ++c) {
+  for (int c = 0; c < CL; ++c) {
     const int x = __ldcg(&a.head->count[c]);
     held_before += c < cta ? x : 0;
     U += x;
   }
   const int64_t first_before = held_before;
   held = 0;
-  for (int64_t p = p0 + tid; p < min(p1, U); p += kThreads) held += __ldcg(&a.mark[p]);
+  for (int64_t p = p0 + tid; p < min(p1, U); p += kThreads) held += count_of<CL>(&mark[p]);
   if (held) atomicAdd(&a.head->front, held);
-  cluster_sync_all();
+  sync_all<CL>();
   const int64_t front = __ldcg(&a.head->front), moves = U - front;
   const int status = (__ldcg(&a.head->flags) & 1) ? CKV_RESIZE_INCONSISTENT : moves > a.n_copies ? CKV_RESIZE_SLOTS_FULL : CKV_RESIZE_OK;
   if (status == 0) {
@@ -325,7 +353,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_
       int h[4], n = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        h[k] = q + k < p1 ? __ldcg(&a.mark[q + k]) : 0;
+        h[k] = q + k < p1 ? count_of<CL>(&mark[q + k]) : 0;
         n += h[k];
       }
       int64_t at = held_before + block_scan(n, s_warp, total);  // held pages in front of q
@@ -337,7 +365,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_
         if (p >= U && h[k]) {
           a.copies[3 * (at - front)] = (int32_t)p;
           a.copies[3 * (at - front) + 2] = (int32_t)mask + 1;
-          a.mark[p] = (int32_t)(at - front) + 1;
+          mark[p] = (int32_t)(at - front) + 1;
         } else if (p < U && !h[k]) {
           a.copies[3 * (p - at) + 1] = (int32_t)p;
         }
@@ -354,7 +382,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_
       a.ring_state_out[1] = a.n_pages - U;
     }
   }
-  cluster_sync_all();
+  sync_all<CL>();
   if (status) return;
   held_before = first_before;
   for (int64_t q0 = p0; q0 < p1; q0 += 4 * kThreads) {  // (pages in front of U keep their mark: 0 or 1)
@@ -362,7 +390,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_
     int h[4], n = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      h[k] = q + k < p1 && __ldcg(&a.mark[q + k]) != 0;
+      h[k] = q + k < p1 && count_of<CL>(&mark[q + k]) != 0;
       n += h[k];
     }
     int64_t at = held_before + block_scan(n, s_warp, total);
@@ -381,7 +409,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) pages_
     int32_t* const to = a.tables_out + b * a.stride;
     for (int64_t i = lane; i < (len + mask) >> a.shift; i += 32) {
       const int32_t page = a.tables[b * a.stride + i];
-      to[i] = page < U ? page : __ldcg(&a.copies[3 * (__ldcg(&a.mark[page]) - 1) + 1]);
+      to[i] = page < U ? page : __ldcg(&a.copies[3 * (count_of<CL>(&mark[page]) - 1) + 1]);
     }
     if (lane == 0 && a.views) a.views[b] = ckv_paged_view{to, len};
   }
@@ -400,37 +428,46 @@ struct CopyPagesArgs {
   int32_t n_arrays, H, layers;
 };
 
+// The same run of two arrays, all loads of a round before its first store (one array after the other would wait twice).
 template <typename T>
-__device__ __forceinline__ void copy_run(unsigned char* to, const unsigned char* from, int64_t bytes) {
+__device__ __forceinline__ void copy_runs(unsigned char* to0, const unsigned char* from0, unsigned char* to1, const unsigned char* from1, int64_t bytes) {
   const int64_t n = bytes / (int64_t)sizeof(T);
   constexpr int U = 4;
   for (int64_t i = threadIdx.x; i < n; i += U * kCopyThreads) {
-    T x[U];
+    T x[U], y[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * kCopyThreads < n) x[u] = reinterpret_cast<const T*>(from)[i + u * kCopyThreads];
+    for (int u = 0; u < U; ++u) {
+      if (i + u * kCopyThreads >= n) break;
+      x[u] = reinterpret_cast<const T*>(from0)[i + u * kCopyThreads];
+      if (to1) y[u] = reinterpret_cast<const T*>(from1)[i + u * kCopyThreads];
+    }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * kCopyThreads < n) reinterpret_cast<T*>(to)[i + u * kCopyThreads] = x[u];
+    for (int u = 0; u < U; ++u) {
+      if (i + u * kCopyThreads >= n) break;
+      reinterpret_cast<T*>(to0)[i + u * kCopyThreads] = x[u];
+      if (to1) reinterpret_cast<T*>(to1)[i + u * kCopyThreads] = y[u];
+    }
   }
 }
 
+template <bool COUNT>
 __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_constant__ CopyPagesArgs a) {
   griddep_wait();
   griddep_launch();
-  // the list ends at its first entry without a source: found in two strides
   int64_t lo = 0, n = a.n;
-  while (n > lo) {
-    const int64_t step = (n - lo + kCopyThreads - 1) / kCopyThreads, i = lo + threadIdx.x * step;
-    const int some = __syncthreads_count(i < n && a.copies[3 * i] >= 0);  // entries lo, lo + step, ... that list something
-    if (some == 0) {
-      n = lo;
-    } else if (step == 1) {
-      lo = n = lo + some;
-    } else {
-      const int64_t last = lo + (some - 1) * step;
-      n = min(n, last + step);
-      lo = last + 1;
+  if (COUNT) {  // the list ends at its first entry without a source: found in two strides
+    while (n > lo) {
+      const int64_t step = (n - lo + kCopyThreads - 1) / kCopyThreads, i = lo + threadIdx.x * step;
+      const int some = __syncthreads_count(i < n && a.copies[3 * i] >= 0);  // entries lo, lo + step, ... that list something
+      if (some == 0) {
+        n = lo;
+      } else if (step == 1) {
+        lo = n = lo + some;
+      } else {
+        const int64_t last = lo + (some - 1) * step;
+        n = min(n, last + step);
+        lo = last + 1;
+      }
     }
   }
   const int64_t per = (int64_t)a.layers * a.H, units = n * per;
@@ -439,20 +476,57 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_c
     const int rest = (int)(u - c * per), layer = rest / a.H, h = rest - layer * a.H;
     const int64_t src = a.copies[3 * c], dst = a.copies[3 * c + 1];
     const int tokens = a.copies[3 * c + 2];
-    if (src >= a.n_pages || dst < 0 || dst >= a.n_pages || src == dst || tokens <= 0) continue;
+    if (src < 0 || src >= a.n_pages || dst < 0 || dst >= a.n_pages || src == dst || tokens <= 0) continue;
     for (int k = 0; k < a.n_arrays; ++k) {
-      const ckv_page_array& r = a.arrays[k];
-      if (layer >= r.layers) continue;
-      unsigned char* const base = static_cast<unsigned char*>(r.base) + layer * r.layer_bytes;
-      const int64_t head_bytes = (int64_t)r.rows * r.row_bytes, bytes = (int64_t)min(tokens, r.rows) * r.row_bytes;
-      unsigned char* const to = base + (dst * a.H + h) * head_bytes;
-      const unsigned char* const from = base + (src * a.H + h) * head_bytes;
-      if (((reinterpret_cast<uintptr_t>(to) | reinterpret_cast<uintptr_t>(from) | (uintptr_t)bytes) & 15) == 0)
-        copy_run<uint4>(to, from, bytes);
+      auto run = [&](int k, unsigned char*& to, const unsigned char*& from, int64_t& bytes) {
+        const ckv_page_array& r = a.arrays[k];
+        unsigned char* const base = static_cast<unsigned char*>(r.base) + layer * r.layer_bytes;
+        const int64_t head_bytes = (int64_t)r.rows * r.row_bytes;
+        bytes = layer < r.layers ? (int64_t)min(tokens, r.rows) * r.row_bytes : 0;
+        to = base + (dst * a.H + h) * head_bytes;
+        from = base + (src * a.H + h) * head_bytes;
+      };
+      unsigned char *to0, *to1 = nullptr;
+      const unsigned char *from0, *from1 = nullptr;
+      int64_t bytes, more = 0;
+      run(k, to0, from0, bytes);
+      if (k + 1 < a.n_arrays) run(k + 1, to1, from1, more);
+      if (more != bytes) {
+        to1 = nullptr;
+        from1 = nullptr;
+      } else {
+        ++k;
+      }
+      if (((reinterpret_cast<uintptr_t>(to0) | reinterpret_cast<uintptr_t>(from0) | reinterpret_cast<uintptr_t>(to1) | reinterpret_cast<uintptr_t>(from1) |
+            (uintptr_t)bytes) & 15) == 0)
+        copy_runs<uint4>(to0, from0, to1, from1, bytes);
       else
-        copy_run<uint32_t>(to, from, bytes);
+        copy_runs<uint32_t>(to0, from0, to1, from1, bytes);
     }
   }
+}
+
+template <typename Args>
+cudaError_t launch_cluster(void (*kernel)(Args), int ctas, size_t smem, cudaStream_t st, const Args& a) {
+  if (smem > 40 * 1024) {  // (48 KB come without asking, but hold the kernel's static arrays too)
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)ctas;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = ctas > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 size_t fork_bytes(int64_t n_pages) { return kHead + (size_t)n_pages * 8; }
@@ -488,9 +562,11 @@ int ckv_pages_fork(const int64_t* lens, int32_t n_in, const int32_t* parents, co
   a.delta = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + kHead);
   a.first = a.delta + n_pages;
   a.stride = table_stride; a.n_pages = n_pages; a.n_in = n_in; a.n_out = n_out; a.shift = shift;
-  const size_t smem = ((size_t)n_in + n_out) * 4;
-  if (smem > 40 * 1024 && cudaFuncSetAttribute(pages_fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kMaxRows * 4) != cudaSuccess) return CKV_ERR_CUDA;
-  return launch_dependent(pages_fork_kernel, dim3(kCtas), dim3(kThreads), smem, static_cast<cudaStream_t>(cuda_stream), a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
+  const bool small = n_pages <= kSmallPool && n_in <= kSmallRows && n_out <= kSmallRows;
+  const size_t smem = (size_t)n_out * 20 + (size_t)n_in * 4 + (small ? (size_t)n_pages * 8 : 0);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = small ? launch_cluster(pages_fork_kernel<1>, 1, smem, st, a) : launch_cluster(pages_fork_kernel<kCtas>, kCtas, smem, st, a);
+  return e == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
 size_t ckv_pages_compact_workspace_bytes(int64_t n_pages) { return n_pages <= 0 || n_pages > INT32_MAX ? 0 : kHead + (size_t)n_pages * 4; }
@@ -513,7 +589,10 @@ int ckv_pages_compact(const int64_t* lens, int32_t Bz, int32_t page_tokens, cons
   a.head = static_cast<Shared*>(workspace);
   a.mark = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + kHead);
   a.stride = table_stride; a.n_pages = n_pages; a.n_copies = n_copies; a.Bz = Bz; a.shift = shift;
-  return launch_dependent(pages_compact_kernel, dim3(kCtas), dim3(kThreads), 0, static_cast<cudaStream_t>(cuda_stream), a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = n_pages <= kSmallPool && Bz <= kSmallRows ? launch_cluster(pages_compact_kernel<1>, 1, (size_t)n_pages * 4, st, a)
+                                                                  : launch_cluster(pages_compact_kernel<kCtas>, kCtas, 0, st, a);
+  return e == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
 int ckv_pages_copy(const ckv_page_array* arrays, int32_t n_arrays, int32_t H, const int32_t* copies, int64_t n, int64_t n_pages, void* cuda_stream) {
@@ -523,6 +602,7 @@ int ckv_pages_copy(const ckv_page_array* arrays, int32_t n_arrays, int32_t H, co
     const ckv_page_array& r = arrays[i];
     if (!r.base || r.layers <= 0 || r.row_bytes <= 0 || r.rows <= 0 || r.layer_bytes < 0) return CKV_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(r.base) | (uintptr_t)r.row_bytes | (uintptr_t)r.layer_bytes) & 3) return CKV_ERR_ALIGNMENT;
+    if (r.layers > 65535) return CKV_ERR_UNSUPPORTED;
   }
   if (n > INT32_MAX || n_pages > INT32_MAX || H > 65535) return CKV_ERR_UNSUPPORTED;
   if (n == 0) return CKV_OK;
@@ -534,9 +614,12 @@ int ckv_pages_copy(const ckv_page_array* arrays, int32_t n_arrays, int32_t H, co
       a.arrays[i] = arrays[at + i];
       a.layers = std::max(a.layers, arrays[at + i].layers);
     }
-    const int64_t ctas = std::min<int64_t>((int64_t)8 * sm_count(), n * std::min<int64_t>((int64_t)a.layers * H, INT32_MAX));
-    if (launch_dependent(pages_copy_kernel, dim3((unsigned)ctas), dim3(kCopyThreads), 0, static_cast<cudaStream_t>(cuda_stream), a) != cudaSuccess)
-      return CKV_ERR_CUDA;
+    // a block per unit, where one that has nothing to do costs less than finding the end of the list first, else blocks that go round
+    const int64_t units = n * (int64_t)a.layers * H;  // (both at most 2^31)
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = units <= 64 * sm_count() ? launch_dependent(pages_copy_kernel<false>, dim3((unsigned)units), dim3(kCopyThreads), 0, st, a)
+                                                   : launch_dependent(pages_copy_kernel<true>, dim3((unsigned)(8 * sm_count())), dim3(kCopyThreads), 0, st, a);
+    if (e != cudaSuccess) return CKV_ERR_CUDA;
   }
   return CKV_OK;
 }
