@@ -436,9 +436,8 @@ int ckv_decode_attn_quantized(const ckv_paged_view* views_dev, const ckv_quant_p
  * ckv_pages_resize writes it as slot_begin, with the views.  Rows of out that belong to no sequence are left as they were.
  * Element d of row i and query head j is at q[i * q_row_stride + j * q_head_stride + d] (in elements: a slice of a fused
  * projection fits; rows 16-byte aligned); out: [n_rows, H*G, D].  Query head j reads KV head j / G; G <= 8, H <= 8192.
- * The values of slots that a token does not attend to may be anything but count as finite where another new token of the
- * sequence attends to them (a slot's infinity or NaN times a weight of zero): slots behind a sequence's last are never read
- * into a sum.  A call's workspace starts with a status word for ckv_workspace_status, as those of the compress calls. */
+ * What is in slots that a token does not attend to, behind a sequence's last ones among them, does not matter to it, NaN included.  out
+ * must not overlap q.  A call's workspace starts with a status word for ckv_workspace_status, as those of the compress calls. */
 
 /* Host-only: workspace bytes of the two calls (partials of rows whose slots several thread blocks share). */
 size_t ckv_extend_workspace_bytes(int64_t n_rows, int32_t H, int32_t G, int32_t D);

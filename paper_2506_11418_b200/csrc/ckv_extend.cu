@@ -78,10 +78,13 @@ constexpr int kEBytes = oMisc + 128;
 struct ExtendArgs {
   const ckv_paged_view* views;
   const int64_t* q_begin;
+  const __nv_bfloat16* q;
   __nv_bfloat16* out;
+  const __nv_bfloat16* k_pages;
+  const __nv_bfloat16* v_pages;
   ckv_quant_pool pool;
   const float* logdeg;
-  int64_t n_rows, max_slots;
+  int64_t n_rows, max_slots, q_row, q_head;  // (strides in elements)
   int32_t Bz, H, G, T, shift;
   float scale;          // above zero
   uint32_t desc_qk;     // (a negative scale negates Q)
@@ -307,7 +310,7 @@ __device__ __forceinline__ bool elect_one() {
 // Bounded wait.  A poll may sleep for up to a microsecond before it answers, so that the warps that wait (most of the time there
 // are eight) do not take issue slots from those that compute.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
-  for (uint32_t i = 0; i < kSpinLimit / 4; ++i) {
+  for (uint32_t i = 0; i < kSpinLimit / 2; ++i) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -356,6 +359,23 @@ __device__ __forceinline__ void unpack8_bf16(uint32_t w, uint32_t scale, uint32_
 
 // A warp's wait: false if any lane gave up
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
+
+// Elements 4 lane .. 4 lane + 3 of a row of keys or values
+template <bool QUANT>
+__device__ __forceinline__ float4 row4(const ExtendArgs& a, int64_t row, bool value, int lane) {
+  if constexpr (!QUANT) {
+    return load4((value ? a.v_pages : a.k_pages) + row * kED + 4 * lane);
+  } else {
+    const int j = lane >> 3, u = lane & 7;
+    const uint32_t* const codes = reinterpret_cast<const uint32_t*>((value ? a.pool.v_codes : a.pool.k_codes) + row * 64);
+    const uint32_t w = value ? codes[2 * u + (j >> 1)] >> (16 * (j & 1)) : codes[4 * (u >> 1) + j] >> (16 * (u & 1));
+    const uint32_t s = (value ? a.pool.v_scales : a.pool.k_scales)[row * 4 + j];
+    uint32_t scale[4], x[4];
+    scales_bf16x2(s, scale);
+    unpack8_bf16(w & 0xffffu, scale[0], x);
+    return make_float4(__uint_as_float(x[0] << 16), __uint_as_float(x[0] & 0xffff0000u), __uint_as_float(x[1] << 16), __uint_as_float(x[1] & 0xffff0000u));
+  }
+}
 
 template <bool QUANT>
 __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -951,7 +971,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
       const bool whole = p.flags & kWhole;
       const int slot = p.flags & kFirst ? 1 : 0;
       float4* const part = reinterpret_cast<float4*>(a.partial + (int64_t)(2 * blockIdx.x + slot) * a.slot_rows * kPartRow) + my_tok * a.G + head;
-      float f0 = 1.f, f1 = 0.f;
+      float f0 = l == 0.f ? 0.f : 1.f, f1 = 0.f;  // (a row that sees nothing: zeros, whatever the values are)
       if (one && steps > 0) {  // two states of the same rows
         state[tid] = make_float2(m, l);
         __syncwarp();
@@ -968,6 +988,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
         const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
         // a one-tile item's columns are shared between the two tiles' warps
         const int c0 = one && steps > 0 ? 2 * g : 0, c1 = one && steps > 0 ? c0 + 2 : (one && g == 1) ? 0 : 4;
+        float finite = 0.f;  // or NaN
         for (int c = c0; c < c1; ++c) {
           float o[32];
           if (steps > 0) {
@@ -984,6 +1005,8 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = 0.f;
           }
+#pragma unroll
+          for (int k = 0; k < 32; ++k) finite = fmaf(o[k], 0.f, finite);
           if (valid && whole) {
 #pragma unroll
             for (int k = 0; k < 32; k += 16)
@@ -994,6 +1017,40 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
           } else if (valid) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) part[(8 * c + k) * a.slot_rows] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+          }
+        }
+        // An infinity or NaN among the values of later new tokens has met weights of zero in the rows that do not see them.  Such rows'
+        // products are formed anew over what they see, a row at a time; m and l are right.
+        __syncwarp();
+        for (uint32_t again = __ballot_sync(0xffffffffu, valid && finite != 0.f && fabsf(l) < INFINITY && fabsf(m) < INFINITY); again; again &= again - 1) {
+          const int from = __ffs((int)again) - 1;
+          const int r_tok = __shfl_sync(0xffffffffu, my_tok, from), r_head = __shfl_sync(0xffffffffu, head, from);
+          const float r_m = __shfl_sync(0xffffffffu, m, from), r_inv = __shfl_sync(0xffffffffu, inv, from);
+          const int begin = lo * kEN, upto = min(p.end, (lo + steps) * kEN), see = min(upto, p.base + r_tok + 1);
+          const int32_t* const table = a.views[p.seq].block_table;
+          auto value_row = [&](int t) { return (((int64_t)table[t >> a.shift] * a.H + p.h) << a.shift) + (t & ((1 << a.shift) - 1)); };
+          bool hit = false;
+          for (int t = max(see, begin); t < upto; ++t) {
+            const float4 v = row4<QUANT>(a, value_row(t), true, lane);
+            hit |= !(fmaf(v.x, 0.f, fmaf(v.y, 0.f, fmaf(v.z, 0.f, v.w * 0.f))) == 0.f);
+          }
+          if (!__any_sync(0xffffffffu, hit)) continue;  // (what is not finite is what the row sees)
+          const float4 q = load4(a.q + (p.row0 + r_tok) * a.q_row + (p.h * a.G + r_head) * a.q_head + 4 * lane);
+          const float sign = a.desc_qk & kNegateA ? -a.scale : a.scale;
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int t = begin; t < see; ++t) {
+            const int64_t row = value_row(t);
+            const float4 k = row4<QUANT>(a, row, false, lane), v = row4<QUANT>(a, row, true, lane);
+            const float y = warp_sum(q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w) * sign + (a.logdeg ? a.logdeg[row] : 0.f);
+            const float w = ex2(fmaf(y, kLog2e, -r_m));
+            o = make_float4(fmaf(w, v.x, o.x), fmaf(w, v.y, o.y), fmaf(w, v.z, o.z), fmaf(w, v.w, o.w));
+          }
+          if (lane >= 8 * c0 && lane < 8 * c1) {
+            const int64_t at = (p.row0 + r_tok) * a.H * a.G + p.h * a.G + r_head;
+            if (whole)
+              store4(a.out + at * kED + 4 * lane, make_float4(o.x * r_inv, o.y * r_inv, o.z * r_inv, o.w * r_inv));
+            else
+              reinterpret_cast<float4*>(a.partial + (int64_t)(2 * blockIdx.x + slot) * a.slot_rows * kPartRow)[lane * a.slot_rows + r_tok * a.G + r_head] = o;
           }
         }
         if (valid && !whole && (!one || g == 0)) part[32 * a.slot_rows] = make_float4(m, l, 0.f, 0.f);
@@ -1137,6 +1194,8 @@ int check_extend(const void* views, const void* q_begin, int64_t n_rows, int32_t
 template <bool QUANT>
 int run_extend(ExtendArgs& a, const void* q, int64_t q_row, int64_t q_head, const void* k, const void* v, int64_t n_pages, void* workspace, cudaStream_t st) {
   if (a.n_rows == 0) return CKV_OK;
+  a.q = static_cast<const __nv_bfloat16*>(q); a.q_row = q_row; a.q_head = q_head;
+  a.k_pages = static_cast<const __nv_bfloat16*>(k); a.v_pages = static_cast<const __nv_bfloat16*>(v);
   a.T = kEN / a.G;
   // log-degrees are divided by the scale: next to 1e-30 products vanish as they do next to zero
   a.desc_qk = kDescQK | (a.scale < 0 ? kNegateA : 0u);

@@ -121,7 +121,9 @@ def expected(cache, new, G, q, scale, rows=None, exact_scores=False):
                     w = w / w.sum(1, keepdim=True).clamp(min=1e-300)
                     e = 2.0**-20 * size.masked_fill(w == 0, 0).amax(1, keepdim=True)  # (slots without weight have no part in it)
                     e = torch.zeros_like(e) if exact_scores else e
-                    o[at + pick, j] = w @ v
+                    v_ = torch.where(torch.isfinite(v), v, 0.0)           # (infinities and NaN where they have a weight alone)
+                    o[at + pick, j] = torch.where((w > 0).double() @ (~torch.isfinite(v)).double() > 0, math.nan, w @ v_)
+                    v = v_
                     bound[at + pick, j] = 2.0**-8 * (w @ v).abs() + (2.0**-8 + 2 * e + (2.0**-25 + 2.0**-27) * n) * (w @ v.abs())
         at += m
     return o, bound
@@ -230,6 +232,39 @@ def test_masked_by_log_degrees(kind):
     c.logdeg[at(slice(800, 900))] = 0
     out = check(c, [200], 4)
     assert (out[:100] == 0).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("lens,new,G", [([700], [300], 4), ([40], [40], 4), ([3000], [20], 4), ([5], [9], 4), ([90], [70], 3), ([5000], [130], 8)])
+def test_values_that_are_not_finite(kind, lens, new, G):
+    """Infinities and NaN in a new token's value: the tokens before it do not see them, the others do."""
+    c = Cache(lens, 2, 64, kind, seed=4)
+    n, m = lens[0], new[0]
+    at = lambda t: (c.table[0, t // 64].long(), slice(None), t % 64)  # noqa: E731
+    bad = sorted({n - 1, n - 2, max(n - m, 0) + min(m, n) // 2} & set(range(n)))
+    for i, t in enumerate(bad):
+        if kind == "bf16":
+            c.v[at(t)[0], 0, t % 64, 5 + 40 * i] = [math.inf, math.nan, -math.inf][i]
+        else:
+            c.scales[1][at(t)[0], 0, t % 64, i] = 255                     # a group of NaN
+    total = m + 2
+    q = queries(total, 2, G, 4)
+    out = torch.full((total, 2 * G, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    ws = workspace(total, 2, G)
+    c.call(torch.tensor([0, m], **I64), G, q, out, SCALE, ws)
+    assert lib().workspace_status(ws) == 0
+    o, bound = expected(c, new, G, q, SCALE)
+    seen = torch.arange(m, device=DEV) + n - m                            # each token's last slot
+    clean = seen < bad[0]
+    got = out[:m].double()
+    assert torch.isfinite(got[clean]).all() and ((got - o).abs() <= bound)[clean].all()
+    assert torch.isfinite(got[:, G:]).all() and ((got - o).abs() <= bound)[:, G:].all()  # the other KV head's
+    for i, t in enumerate(bad):                                           # who sees one has it in its columns, and nowhere else
+        cols = slice(5 + 40 * i, 6 + 40 * i) if kind == "bf16" else slice(32 * i, 32 * i + 32)
+        rows = seen >= t
+        assert not torch.isfinite(got[rows][:, :G, cols]).any() or not rows.any()
+        ok = seen < t
+        assert torch.isfinite(got[ok][:, :G, cols]).all() and ((got - o).abs() <= bound)[ok][:, :G, cols].all()
 
 
 def test_a_long_sequence():
