@@ -56,8 +56,8 @@ template <bool QUANT> constexpr int kEWarps = QUANT ? 20 : 12;
 template <bool QUANT> constexpr int kESoftmaxRegs = QUANT ? 160 : 216;
 template <bool QUANT> constexpr int kEOtherRegs = QUANT ? 64 : 72;
 constexpr int kEUnpackRegs = 48, kEUnpackWarps = 8;
-constexpr int kItemCost = 128;      // what an item costs beside its slots (queries in, rows out), in slots
-constexpr int kMinShare = 512;      // slots that a CTA takes at least
+constexpr int kItemCost = 320;      // what an item costs beside its slots (queries in, rows out), in slots (eight prompts: 124 us, with 128 142)
+constexpr int kMinShare = 256;      // slots that a CTA takes at least (17 tokens over 4113 slots: 19.8 us, with 512 21.1, with 1024 25.2)
 constexpr float kSlack = 8.f;       // weights below 2^8
 constexpr int kPartRow = 132;       // floats of a partial row: O, m, sum, pad; a piece's rows lie side by side, four floats of each
 // shared memory, from a 1024-byte boundary
