@@ -20,7 +20,7 @@
 //
 // Sharing the work.  All items' lengths (slots + kItemCost each) are laid end to end, in the order (sequence, KV head, tile
 // pair), and every CTA takes an equal stretch, wherever it begins and ends, so a ragged batch, few rows over a long cache and
-// many rows are all balanced to a step.  Each CTA finds its stretch by itself from lengths on the device: the sum over a sequence's
+// many rows are all balanced to a step.  (Of one large chunk, whole items are dealt first: see there.)  Each CTA finds its stretch by itself from lengths on the device: the sum over a sequence's
 // items is an arithmetic series.  A piece that is not a whole item leaves (O, m, sum) in the workspace, and extend_join_kernel
 // joins them, in order, so results do not depend on timing.
 //
@@ -59,6 +59,7 @@ constexpr int kEUnpackRegs = 48, kEUnpackWarps = 8;
 constexpr int kItemCost = 320;      // what an item costs beside its slots (queries in, rows out), in slots (eight prompts: 124 us, with 128 142)
 constexpr int kMinShare = 256;      // slots that a CTA takes at least (17 tokens over 4113 slots: 19.8 us, with 512 21.1, with 1024 25.2)
 constexpr float kSlack = 8.f;       // weights below 2^8
+constexpr int kMaxStarts = 220;     // CTAs whose stretches' begins fit beside the sums
 constexpr int kPartRow = 132;       // floats of a partial row: O, m, sum, pad; a piece's rows lie side by side, four floats of each
 // shared memory, from a 1024-byte boundary
 constexpr int oQ = 0;
@@ -143,41 +144,50 @@ struct __align__(16) Piece {
   int seq;
 };
 
+template <bool DEAL>
 struct Walk {
   int64_t left, x;  // what is left of the stretch; offset in the item
   ExtendSeq s;
   int b, h, j;
+  int dealt, item;  // whole items that come before the stretch (one sequence only), and the next of them
   // the next piece that has something to do
   __device__ __forceinline__ bool next(const ExtendArgs& a, Piece& p) {
     const int T2 = 2 * a.T;
-    while (left > 0) {
-      const int end = s.end(j, T2), steps = (end + kEN - 1) / kEN;
-      const int64_t cost = (int64_t)end + kItemCost, to = min(x + left, cost);
+    while ((DEAL && dealt > 0) || left > 0) {
+      const bool deal = DEAL && dealt > 0;
+      const int items = s.items(T2), at_h = deal ? item / items : h, at_j = deal ? item - at_h * items : j;
+      const int end = s.end(at_j, T2), steps = (end + kEN - 1) / kEN;
+      const int64_t cost = (int64_t)end + kItemCost, from = deal ? 0 : x, to = deal ? cost : min(x + left, cost);
       auto step_of = [&](int64_t y) { return (int)min(max(y - kItemCost + kEN / 2, (int64_t)0) / kEN, (int64_t)steps); };
       const bool ends = to == cost;
-      p.lo = step_of(x);
+      p.lo = step_of(from);
       p.hi = ends ? steps : step_of(to);
-      p.row0 = s.row0 + (int64_t)j * T2;
-      p.h = h;
-      p.ntok = min(T2, s.n - j * T2);
-      p.base = s.len - s.n + j * T2;
+      p.row0 = s.row0 + (int64_t)at_j * T2;
+      p.h = at_h;
+      p.ntok = min(T2, s.n - at_j * T2);
+      p.base = s.len - s.n + at_j * T2;
       p.end = end;
-      p.flags = (p.ntok <= a.T ? kOneTile : 0) | (p.lo == 0 && p.hi == steps ? kWhole : 0) | (x == 0 ? kFirst : 0);
+      p.flags = (p.ntok <= a.T ? kOneTile : 0) | (p.lo == 0 && p.hi == steps ? kWhole : 0) | (from == 0 ? kFirst : 0);
       p.seq = b;
-      left -= to - x;
-      x = to;
-      if (ends) {
-        x = 0;
-        if (++j >= s.items(T2)) {
-          j = 0;
-          if (++h == a.H) {
-            h = 0;
-            s.n = 0;
-            while (left > 0 && s.n == 0) {  // (what is left belongs to a later sequence)
-              if (++b < a.Bz)
-                s = extend_seq(a, b);
-              else
-                left = 0;
+      if (deal) {
+        --dealt;
+        item += gridDim.x;
+      } else {
+        left -= to - x;
+        x = to;
+        if (ends) {
+          x = 0;
+          if (++j >= items) {
+            j = 0;
+            if (++h == a.H) {
+              h = 0;
+              s.n = 0;
+              while (left > 0 && s.n == 0) {  // (what is left belongs to a later sequence)
+                if (++b < a.Bz)
+                  s = extend_seq(a, b);
+                else
+                  left = 0;
+              }
             }
           }
         }
@@ -377,7 +387,8 @@ __device__ __forceinline__ float4 row4(const ExtendArgs& a, int64_t row, bool va
   }
 }
 
-template <bool QUANT>
+// DEAL: one sequence, and rows enough for an item per CTA
+template <bool QUANT, bool DEAL>
 __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                                                               const __grid_constant__ CUtensorMap tm_v, const ExtendArgs a) {
   extern __shared__ unsigned char smem_raw[];
@@ -405,6 +416,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
   Piece* const pieces = reinterpret_cast<Piece*>(smem + oPieces);
   int64_t* const s_start = reinterpret_cast<int64_t*>(smem + oMisc);            // the stretch's offset in its sequence, sequence
   int64_t* const s_sum = reinterpret_cast<int64_t*>(smem + oState);             // (before the roles begin)
+  int64_t* const s_starts = s_sum + 32;
   volatile uint32_t* const s_tmem = reinterpret_cast<volatile uint32_t*>(smem + oMisc + 64);
 
   if (tid == 0) {
@@ -477,8 +489,48 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
     if (w < warp) at += s_sum[w];
     total += s_sum[w];
   }
-  const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kMinShare), begin = share * blockIdx.x;
-  if (begin < total && begin >= at && begin < at + mine) {
+  const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kMinShare);
+  int64_t begin = min(share * blockIdx.x, total), left = min(share, total - begin);
+  // One sequence with more items than CTAs (a large chunk): as many items as an even share holds are dealt to the CTAs whole, in
+  // turn, and only the rest is laid out in stretches.  CTAs then go through the same keys at the same time, and L2 has them (2048 tokens over
+  // 32768 slots: 0.4 GB from memory in place of 1.9).
+  int dealt = 0;
+  if (DEAL && total > 0) {
+    const ExtendSeq s = extend_seq(a, 0);
+    const int items = s.items(T2), n = (int)gridDim.x;
+    const int64_t of_head = s.before(items, T2);
+    dealt = (int)min(total / n / (of_head - s.before(items - 1, T2)), (int64_t)items * a.H / n);  // (the last item of a head is the longest)
+    if (dealt > 0) {
+      int64_t whole = 0;
+      if (tid < n)
+        for (int w = 0; w < dealt; ++w) {
+          const int j = (tid + w * n) % items;
+          whole += s.before(j + 1, T2) - s.before(j, T2);
+        }
+      int64_t upto = whole;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+      }
+      __syncthreads();
+      if (lane == 31) s_sum[warp] = upto;
+      __syncthreads();
+      upto -= whole;
+      for (int w = 0; w < warp; ++w) upto += s_sum[w];
+      // where every CTA's stretch begins: behind the dealt items, after what is left of the even shares of the CTAs before
+      const int64_t behind = (int64_t)(dealt * n / items) * of_head + s.before(dealt * n % items, T2);
+      if (tid <= n) s_starts[tid] = behind + tid * total / n - upto;
+      __syncthreads();
+      begin = s_starts[blockIdx.x];
+      left = s_starts[blockIdx.x + 1] - begin;
+      if (tid == 0) {
+        s_start[0] = begin;
+        s_start[1] = 0;
+      }
+    }
+  }
+  if ((!DEAL || dealt == 0) && left > 0 && begin >= at && begin < at + mine) {
     for (int b = q0; b < q1; ++b) {
       const ExtendSeq s = extend_seq(a, b);
       if (s.n == 0) continue;
@@ -565,15 +617,20 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
   give_registers<kEOtherRegs<QUANT>>();
   if (warp == 8) {
     // ---------------------------------------------------------------- TMA, and the walk along the stretch
-    Walk walk;
+    Walk<DEAL> walk;
     walk.b = (int)s_start[1];
     walk.s = extend_seq(a, walk.b);
-    walk.left = min(share, total - begin);
-    {
+    walk.left = left;
+    walk.dealt = dealt;
+    walk.item = (int)blockIdx.x;
+    walk.h = walk.j = 0;
+    walk.x = 0;
+    ExtendPiece note{0, 0, 0, 0, {0, 0}};
+    if (left > 0) {
       const int items = walk.s.items(T2);
-      const int64_t head = walk.s.before(items, T2);
-      walk.h = (int)(offset / head);
-      const int64_t in_head = offset - walk.h * head;
+      const int64_t of_head = walk.s.before(items, T2);
+      walk.h = (int)(offset / of_head);
+      const int64_t in_head = offset - walk.h * of_head;
       int lo = 0, hi = items;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -581,8 +638,16 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
       }
       walk.j = lo;
       walk.x = in_head - walk.s.before(lo, T2);
+      // the CTA in whose stretch this item begins: the last that does not begin behind it
+      const int64_t item_begin = begin - walk.x;
+      if (DEAL && dealt > 0) {
+        note.first = -1;
+        for (int c = 0; c < (int)gridDim.x; c += 32)
+          note.first += __popc(__ballot_sync(0xffffffffu, c + lane < (int)gridDim.x && s_starts[c + lane] <= item_begin));
+      } else {
+        note.first = (int32_t)(item_begin / share);
+      }
     }
-    ExtendPiece note{0, 0, 0, (int32_t)((begin - walk.x) / share), {0, 0}};  // (the CTA in which the first item begins)
     const int run = min(kEN, 1 << a.shift), runs = kEN / run;  // slots of a step that lie in one page
     const int rr = (lane >> 1) % runs, half = lane & 1;
     int n = 0, nq = 0;                                         // steps so far, pieces with steps
@@ -1162,14 +1227,14 @@ bool encode(CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims,
 }
 
 // Sets the kernel's shared memory once per device
-template <bool QUANT>
+template <bool QUANT, bool DEAL>
 bool extend_ready() {
   constexpr int kMaxDev = 64;
   static std::atomic<bool> done[kMaxDev];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDev) return false;
   if (done[dev].load(std::memory_order_relaxed)) return true;
-  if (cudaFuncSetAttribute(extend_kernel<QUANT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEBytes + 1024) != cudaSuccess) return false;
+  if (cudaFuncSetAttribute(extend_kernel<QUANT, DEAL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEBytes + 1024) != cudaSuccess) return false;
   done[dev].store(true, std::memory_order_relaxed);
   return true;
 }
@@ -1217,9 +1282,16 @@ int run_extend(ExtendArgs& a, const void* q, int64_t q_row, int64_t q_head, cons
     const cuuint32_t box[2] = {64, (cuuint32_t)std::min(kEN, 1 << a.shift)};
     if (!encode(&tm[1 + i], i ? v : k, 2, dims, strides, box)) return CKV_ERR_UNSUPPORTED;
   }
-  if (!extend_ready<QUANT>()) return CKV_ERR_CUDA;
   const unsigned ctas = (unsigned)sm_count();
-  if (launch_dependent(extend_kernel<QUANT>, dim3(ctas), dim3(kEWarps<QUANT> * 32), kEBytes + 1024, st, tm[0], tm[1], tm[2], a) != cudaSuccess) return CKV_ERR_CUDA;
+  cudaStream_t stream = st;
+  auto go = [&](auto deal) {
+    constexpr bool DEAL = decltype(deal)::value;
+    return extend_ready<QUANT, DEAL>() && launch_dependent(extend_kernel<QUANT, DEAL>, dim3(ctas), dim3(kEWarps<QUANT> * 32), kEBytes + 1024, stream, tm[0], tm[1],
+                                                           tm[2], a) == cudaSuccess;
+  };
+  // (a kernel of its own: what it does at its start would cost small calls 2 to 6 us)
+  const bool deal = a.Bz == 1 && (a.n_rows + 2 * a.T - 1) / (2 * a.T) * a.H >= ctas && ctas < kMaxStarts;
+  if (!(deal ? go(std::true_type{}) : go(std::false_type{}))) return CKV_ERR_CUDA;
   return launch_dependent(extend_join_kernel, dim3(ctas, (unsigned)(a.slot_rows + kJoinRows - 1) / kJoinRows), dim3(kJoinWarps * 32), 0, st, a) == cudaSuccess ? CKV_OK : CKV_ERR_CUDA;
 }
 
