@@ -181,6 +181,15 @@ def test_how_the_work_is_shared(kind, lens, new, H, G):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,m,H,G,pad", [
+    (5000, 4000, 8, 4, 2), (3000, 3000, 4, 8, 0), (2500, 2600, 8, 8, 1), (1200, 1184, 8, 4, 0), (9000, 1185, 8, 4, 0), (700, 600, 2, 4, 9000), (4000, 3777, 3, 7, 0),
+    (20000, 1184, 8, 4, 0), (300, 300, 64, 8, 0)])
+def test_one_large_chunk(kind, n, m, H, G, pad):
+    """One sequence with more items than SMs (or rows for them): items are dealt whole, the rest in stretches."""
+    check(Cache([n], H, 64, kind, seed=m), [m], G, pad=pad, rows=sorted({0, 1, 31, 32, 63, 64, 500, m // 2, m - 65, m - 64, m - 2, m - 1} & set(range(m))))
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_sequences_without_tokens_or_slots(kind):
     """No new tokens, no slots at all, and more new tokens than slots: the first of them have nothing to attend to."""
     check(Cache([0, 100, 0, 5, 200, 3], 2, 32, kind), [0, 0, 4, 9, 50, 3], 4)
