@@ -7,6 +7,7 @@ if libckv.so is missing or cannot be loaded the import of this module fails.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import struct
 from dataclasses import dataclass
@@ -447,7 +448,7 @@ _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_d
 _i32, _i64, _f32 = torch.int32, torch.int64, torch.float32
 _ROWS = struct.Struct("@PPPqqqqqqiii4x")   # ckv_token_rows
 _POOL = struct.Struct("@PPPPPP")           # ckv_quant_pool
-_ARRAY = struct.Struct("@Pqiii4x")         # ckv_page_array
+_arrays = functools.lru_cache(lambda n: struct.Struct("@" + "Pqiii4x" * n))  # ckv_page_array [n]
 
 
 def _stream_for(first: torch.Tensor, *others: torch.Tensor | None):
@@ -569,16 +570,17 @@ def pages_compact(lens: torch.Tensor, block_tables: torch.Tensor, block_tables_o
 def pages_copy(copies: torch.Tensor, arrays, page_arrays=(), stacked: bool = False):
     """ckv_pages_copy on the current stream.  arrays: tensors [n_pages, H, page_tokens, ...], whose rows are tokens; page_arrays:
     [n_pages, H, ...], which a page has once (summaries).  stacked: all of them with the layers in front ([L, n_pages, H, ...])."""
-    s = 1 if stacked else 0
-    n_pages, H, P = arrays[0].shape[s:s + 3]
-    packed = []
+    s, k, values = int(stacked), len(arrays), []
+    shape = arrays[0].shape
+    n_pages, H, P = shape[s], shape[s + 1], shape[s + 2]
     for i, t in enumerate((*arrays, *page_arrays)):
-        by_token = i < len(arrays)
-        assert t.shape[s:s + 2] == (n_pages, H) and (not by_token or t.shape[s + 2] == P) and t.is_contiguous(), "arrays"
-        layers, rows = t.shape[0] if stacked else 1, P if by_token else 1
-        packed.append(_ARRAY.pack(t.data_ptr(), t.nbytes // layers, layers, rows, t.nbytes // (layers * n_pages * H * rows)))
+        shape = t.shape
+        assert shape[s] == n_pages and shape[s + 1] == H and (i >= k or shape[s + 2] == P) and t.is_contiguous(), "arrays"
+        layers, rows, nbytes = shape[0] if stacked else 1, P if i < k else 1, t.nbytes
+        values += (t.data_ptr(), nbytes // layers, layers, rows, nbytes // (layers * n_pages * H * rows))
+    n_arrays = len(values) // 5
     assert copies.dtype is _i32 and copies.dim() == 2 and copies.shape[1] == 3 and copies.is_contiguous(), "copies"
-    _check(lib.ckv_pages_copy(b"".join(packed), len(packed), H, copies.data_ptr(), copies.shape[0], n_pages, _stream_for(copies, *arrays, *page_arrays)))
+    _check(lib.ckv_pages_copy(_arrays(n_arrays).pack(*values), n_arrays, H, copies.data_ptr(), copies.shape[0], n_pages, _stream_for(copies, *arrays, *page_arrays)))
 
 
 def pages_summarize(views: torch.Tensor, k_pages: torch.Tensor, deg_pages: torch.Tensor | None, c_pages: torch.Tensor, clog_pages: torch.Tensor,

@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(kThreads) pages_compact_kernel(const CompactAr
 // ---- ckv_pages_copy --------------------------------------------------------------------------------------------------
 // A unit of work is the rows of one head of one page in one layer, in all arrays; CTAs go round the units.  Bound by the bytes of the
 // rows, read once and written once.
-constexpr int kCopyThreads = 256;
+constexpr int kCopyThreads = 128;  // (256: a compacted pool of 2.8 GB takes 541 us, so 486)
 constexpr int kMaxArrays = 64;
 
 struct CopyPagesArgs {
@@ -428,24 +428,32 @@ struct CopyPagesArgs {
   int32_t n_arrays, H, layers;
 };
 
-// The same run of two arrays, all loads of a round before its first store (one array after the other would wait twice).
-template <typename T>
+// The same run of two arrays, all loads of a round before its first store (one array after the other would wait twice).  STREAM: past the
+// caches, which a short list's few pages gain from (64 beams: 24.7 -> 23.0 us) and a pool's do not (486 -> 507).
+template <typename T, bool STREAM>
 __device__ __forceinline__ void copy_runs(unsigned char* to0, const unsigned char* from0, unsigned char* to1, const unsigned char* from1, int64_t bytes) {
   const int64_t n = bytes / (int64_t)sizeof(T);
   constexpr int U = 4;
+  auto load = [](const unsigned char* p, int64_t i) { return STREAM ? __ldcs(reinterpret_cast<const T*>(p) + i) : reinterpret_cast<const T*>(p)[i]; };
+  auto store = [](unsigned char* p, int64_t i, T x) {
+    if (STREAM)
+      __stcs(reinterpret_cast<T*>(p) + i, x);
+    else
+      reinterpret_cast<T*>(p)[i] = x;
+  };
   for (int64_t i = threadIdx.x; i < n; i += U * kCopyThreads) {
     T x[U], y[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i + u * kCopyThreads >= n) break;
-      x[u] = reinterpret_cast<const T*>(from0)[i + u * kCopyThreads];
-      if (to1) y[u] = reinterpret_cast<const T*>(from1)[i + u * kCopyThreads];
+      x[u] = load(from0, i + u * kCopyThreads);
+      if (to1) y[u] = load(from1, i + u * kCopyThreads);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i + u * kCopyThreads >= n) break;
-      reinterpret_cast<T*>(to0)[i + u * kCopyThreads] = x[u];
-      if (to1) reinterpret_cast<T*>(to1)[i + u * kCopyThreads] = y[u];
+      store(to0, i + u * kCopyThreads, x[u]);
+      if (to1) store(to1, i + u * kCopyThreads, y[u]);
     }
   }
 }
@@ -499,9 +507,9 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_c
       }
       if (((reinterpret_cast<uintptr_t>(to0) | reinterpret_cast<uintptr_t>(from0) | reinterpret_cast<uintptr_t>(to1) | reinterpret_cast<uintptr_t>(from1) |
             (uintptr_t)bytes) & 15) == 0)
-        copy_runs<uint4>(to0, from0, to1, from1, bytes);
+        copy_runs<uint4, !COUNT>(to0, from0, to1, from1, bytes);
       else
-        copy_runs<uint32_t>(to0, from0, to1, from1, bytes);
+        copy_runs<uint32_t, !COUNT>(to0, from0, to1, from1, bytes);
     }
   }
 }
@@ -618,7 +626,7 @@ int ckv_pages_copy(const ckv_page_array* arrays, int32_t n_arrays, int32_t H, co
     const int64_t units = n * (int64_t)a.layers * H;  // (both at most 2^31)
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const cudaError_t e = units <= 64 * sm_count() ? launch_dependent(pages_copy_kernel<false>, dim3((unsigned)units), dim3(kCopyThreads), 0, st, a)
-                                                   : launch_dependent(pages_copy_kernel<true>, dim3((unsigned)(8 * sm_count())), dim3(kCopyThreads), 0, st, a);
+                                                   : launch_dependent(pages_copy_kernel<true>, dim3((unsigned)(16 * sm_count())), dim3(kCopyThreads), 0, st, a);
     if (e != cudaSuccess) return CKV_ERR_CUDA;
   }
   return CKV_OK;
