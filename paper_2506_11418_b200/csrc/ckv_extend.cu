@@ -1053,37 +1053,47 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
         const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
         // a one-tile item's columns are shared between the two tiles' warps
         const int c0 = one && steps > 0 ? 2 * g : 0, c1 = one && steps > 0 ? c0 + 2 : (one && g == 1) ? 0 : 4;
-        float finite = 0.f;  // or NaN
+        const float a0 = f0 * inv, a1 = f1 * inv;
+        const bool plain = !one && !__any_sync(0xffffffffu, f0 == 0.f);
+        f32x2 finite2(0.f, 0.f);  // or NaN
+#pragma unroll 1
         for (int c = c0; c < c1; ++c) {
           float o[32];
           if (steps > 0) {
             tmem_ld32((one ? tmem + lanes + 256 : t_o) + 32 * c, o);
+            if (plain) {
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = f0 == 0.f ? 0.f : o[k] * f0;
+              for (int k = 0; k < 32; k += 2) mul2(f32x2(o[k], o[k + 1]), f32x2(a0, a0)).get(o[k], o[k + 1]);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] = f0 == 0.f ? 0.f : o[k] * a0;
+            }
             if (one && steps > 1) {
               float u[32];
               tmem_ld32(tmem + lanes + 384 + 32 * c, u);
 #pragma unroll
-              for (int k = 0; k < 32; ++k) o[k] += f1 == 0.f ? 0.f : u[k] * f1;
+              for (int k = 0; k < 32; ++k) o[k] += f1 == 0.f ? 0.f : u[k] * a1;
             }
           } else {
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = 0.f;
           }
 #pragma unroll
-          for (int k = 0; k < 32; ++k) finite = fmaf(o[k], 0.f, finite);
+          for (int k = 0; k < 32; k += 2) finite2 = fma2(f32x2(o[k], o[k + 1]), f32x2(0.f, 0.f), finite2);
           if (valid && whole) {
 #pragma unroll
             for (int k = 0; k < 32; k += 16)
-              st_global_v8(out + 32 * c + k, pack_bf16x2(o[k] * inv, o[k + 1] * inv), pack_bf16x2(o[k + 2] * inv, o[k + 3] * inv),
-                           pack_bf16x2(o[k + 4] * inv, o[k + 5] * inv), pack_bf16x2(o[k + 6] * inv, o[k + 7] * inv),
-                           pack_bf16x2(o[k + 8] * inv, o[k + 9] * inv), pack_bf16x2(o[k + 10] * inv, o[k + 11] * inv),
-                           pack_bf16x2(o[k + 12] * inv, o[k + 13] * inv), pack_bf16x2(o[k + 14] * inv, o[k + 15] * inv));
+              st_global_v8(out + 32 * c + k, pack_bf16x2(o[k], o[k + 1]), pack_bf16x2(o[k + 2], o[k + 3]), pack_bf16x2(o[k + 4], o[k + 5]),
+                           pack_bf16x2(o[k + 6], o[k + 7]), pack_bf16x2(o[k + 8], o[k + 9]), pack_bf16x2(o[k + 10], o[k + 11]),
+                           pack_bf16x2(o[k + 12], o[k + 13]), pack_bf16x2(o[k + 14], o[k + 15]));
           } else if (valid) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) part[(8 * c + k) * a.slot_rows] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
           }
         }
+        float finite, other;
+        finite2.get(finite, other);
+        finite += other;
         // An infinity or NaN among the values of later new tokens has met weights of zero in the rows that do not see them.  Such rows'
         // products are formed anew over what they see, a row at a time; m and l are right.
         __syncwarp();
