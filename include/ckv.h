@@ -50,9 +50,9 @@ typedef enum {
   CKV_ERR_UNSUPPORTED = 6, /* head_dim, chunk size or group size outside this version's range */
   CKV_ERR_CUDA = 7         /* a CUDA runtime call failed (launch configuration, invalid stream ...) */
   /* There is no "timeout" status.  The calls return before their kernels run, so a bounded wait inside a kernel that
-   * gives up cannot be reported here: the compress kernels (the only ones that wait on asynchronous copies, tensor-core
-   * completions or each other) record it in a status word at the start of their workspace, which ckv_workspace_status
-   * reads.  The decode kernels contain no such wait and have no status word. */
+   * gives up cannot be reported here: the kernels that wait on asynchronous copies, tensor-core completions or each other (the
+   * compress calls', and those of the attention for chunks of new tokens) record it in a status word at the start of their
+   * workspace, which ckv_workspace_status reads.  The decode kernels contain no such wait and have no status word. */
 } ckv_status;
 
 /* One sequence's KV cache over all layers and KV heads, with the cluster degrees N of Sec. 3
@@ -147,7 +147,7 @@ int ckv_compress_append_recluster(ckv_cache* cache, ckv_cache* spare, const void
 /* The kernels wait on asynchronous copies with a bounded number of polls; a wait that gives up sets a
  * status word at the start of the workspace instead of hanging.  This call copies that word to
  * *status_host (host pointer) and synchronises the stream: 0 = every wait completed, nonzero = some
- * output of the last ckv_compress_* call on this workspace is incomplete.  The paper has no counterpart. */
+ * output of the last ckv_compress_* or ckv_extend_* call on this workspace is incomplete.  The paper has no counterpart. */
 int ckv_workspace_status(const void* workspace, void* cuda_stream, int32_t* status_host);
 
 /* One layer of one sequence for decode attention: k, v: [H, cap, D]; logdeg: [H, cap] or NULL
@@ -437,7 +437,9 @@ int ckv_decode_attn_quantized(const ckv_paged_view* views_dev, const ckv_quant_p
  * Element d of row i and query head j is at q[i * q_row_stride + j * q_head_stride + d] (in elements: a slice of a fused
  * projection fits; rows 16-byte aligned); out: [n_rows, H*G, D].  Query head j reads KV head j / G; G <= 8, H <= 8192.
  * What is in slots that a token does not attend to, behind a sequence's last ones among them, does not matter to it, NaN included.  out
- * must not overlap q.  A call's workspace starts with a status word for ckv_workspace_status, as those of the compress calls. */
+ * must not overlap q.  Weights enter the products as bf16; scores, sums and outputs before their rounding are fp32.  scale is finite; a
+ * magnitude below 1e-30 counts as that.  Log-degrees may be minus infinity (the slot is left out); finite ones beyond 3.3e38 |scale| or 2e38 in
+ * magnitude count as that.  A call's workspace starts with a status word for ckv_workspace_status, as those of the compress calls. */
 
 /* Host-only: workspace bytes of the two calls (partials of rows whose slots several thread blocks share). */
 size_t ckv_extend_workspace_bytes(int64_t n_rows, int32_t H, int32_t G, int32_t D);
