@@ -349,9 +349,9 @@ typedef struct ckv_page_array {
   int32_t layers, rows, row_bytes;
 } ckv_page_array;
 
-/* For every entry (source, target, tokens) of copies [n, 3] (device), up to the first with a source below 0: the first min(tokens, rows) rows of every head of
- * the source page to the target page, in all arrays (HOST array [n_arrays]) and layers.  A target must not be listed twice or be a source.
- * Entries with a page outside 0 .. n_pages - 1 are skipped. */
+/* For every entry (source, target, tokens) of copies [n, 3] (device): the first min(tokens, rows) rows of every head of the source page to
+ * the target page, in all arrays (HOST array [n_arrays]) and layers.  The list ends at its first entry with a source below 0; all behind
+ * it have to be such.  A target must not be listed twice or be a source.  Entries with a page outside 0 .. n_pages - 1 are skipped. */
 int ckv_pages_copy(const ckv_page_array* arrays, int32_t n_arrays, int32_t H, const int32_t* copies, int64_t n, int64_t n_pages, void* cuda_stream);
 
 /* ---- Attention over selected pages -----------------------------------------------------------------------------------
@@ -437,7 +437,8 @@ int ckv_decode_attn_quantized(const ckv_paged_view* views_dev, const ckv_quant_p
  * Element d of row i and query head j is at q[i * q_row_stride + j * q_head_stride + d] (in elements: a slice of a fused
  * projection fits; rows 16-byte aligned); out: [n_rows, H*G, D].  Query head j reads KV head j / G; G <= 8, H <= 8192.
  * What is in slots that a token does not attend to, behind a sequence's last ones among them, does not matter to it, NaN included.  out
- * must not overlap q.  Weights enter the products as bf16; scores, sums and outputs before their rounding are fp32.  scale is finite; a
+ * must not overlap q.  Weights enter the products as bf16; scores, sums and outputs before their rounding are fp32 (a product of a
+ * weight and a value below 2^-126 may count as zero; scores have to stay below 2^128).  scale is finite; a
  * magnitude below 1e-30 counts as that.  Log-degrees may be minus infinity (the slot is left out); finite ones beyond 3.3e38 |scale| or 2e38 in
  * magnitude count as that.  A call's workspace starts with a status word for ckv_workspace_status, as those of the compress calls. */
 

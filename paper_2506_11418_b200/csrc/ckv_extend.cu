@@ -325,10 +325,11 @@ __device__ __forceinline__ bool elect_one() {
   return ok != 0;
 }
 
-// Bounded wait.  A poll may sleep for up to a microsecond before it answers, so that the warps that wait (most of the time there
-// are eight) do not take issue slots from those that compute.
+// Bounded wait.  A poll sleeps until the barrier's phase ends or some time has passed (4 us were measured), so that the warps that wait
+// (most of the time there are eight) do not take issue slots from those that compute.  The limit is about four seconds: a warp that
+// forms rows anew (values that are not finite) may take long.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
-  for (uint32_t i = 0; i < kSpinLimit / 2; ++i) {
+  for (uint32_t i = 0; i < kSpinLimit / 4; ++i) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -1121,12 +1122,24 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
           const float4 q = load4(a.q + (p.row0 + r_tok) * a.q_row + (p.h * a.G + r_head) * a.q_head + 4 * lane);
           const float sign = a.desc_qk & kNegateA ? -a.scale : a.scale;
           float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int t = begin; t < see; ++t) {
-            const int64_t row = value_row(t);
-            const float4 k = row4<QUANT>(a, row, false, lane), v = row4<QUANT>(a, row, true, lane);
-            const float y = warp_sum(q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w) * sign + (a.logdeg ? a.logdeg[row] : 0.f);
-            const float w = ex2(fmaf(y, kLog2e, -r_m));
-            o = make_float4(fmaf(w, v.x, o.x), fmaf(w, v.y, o.y), fmaf(w, v.z, o.z), fmaf(w, v.w, o.w));
+          for (int t = begin; t < see; t += 4) {  // (four slots' loads on their way at once)
+            float4 k[4], v[4];
+            float y[4], bias[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int64_t row = value_row(min(t + x, see - 1));
+              k[x] = row4<QUANT>(a, row, false, lane);
+              v[x] = row4<QUANT>(a, row, true, lane);
+              bias[x] = a.logdeg ? a.logdeg[row] : 0.f;
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) y[x] = warp_sum(q.x * k[x].x + q.y * k[x].y + q.z * k[x].z + q.w * k[x].w) * sign + bias[x];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              if (t + x >= see) break;
+              const float w = ex2(fmaf(y[x], kLog2e, -r_m));
+              o = make_float4(fmaf(w, v[x].x, o.x), fmaf(w, v[x].y, o.y), fmaf(w, v[x].z, o.z), fmaf(w, v[x].w, o.w));
+            }
           }
           if (lane >= 8 * c0 && lane < 8 * c1) {
             const int64_t at = (p.row0 + r_tok) * a.H * a.G + p.h * a.G + r_head;

@@ -8,6 +8,8 @@ Tolerance (half a step of bf16: 2^-8 relative), for an output o = sum w v with t
                                  the arguments' rounding in base two)
   sums over n slots in fp32      (2^-25 n + 2^-27 n) sum w |v|: the weights' sum, two accumulators of n / 2 additions of half a step,
                                  and n / 16 steps of the products' (2^-23 each, truncated)
+  products below 2^-126          may count as zero (the tensor cores' subnormal products): n 2^-126, since a row's largest weight is one or
+                                 more and so is the sum that divides them; and the output's rounding there, 2^-134
 """
 import math
 
@@ -124,7 +126,7 @@ def expected(cache, new, G, q, scale, rows=None, exact_scores=False):
                     v_ = torch.where(torch.isfinite(v), v, 0.0)           # (infinities and NaN where they have a weight alone)
                     o[at + pick, j] = torch.where((w > 0).double() @ (~torch.isfinite(v)).double() > 0, math.nan, w @ v_)
                     v = v_
-                    bound[at + pick, j] = 2.0**-8 * (w @ v).abs() + (2.0**-8 + 2 * e + (2.0**-25 + 2.0**-27) * n) * (w @ v.abs())
+                    bound[at + pick, j] = 2.0**-8 * (w @ v).abs() + (2.0**-8 + 2 * e + (2.0**-25 + 2.0**-27) * n) * (w @ v.abs()) + n * 2.0**-126 + 2.0**-134
         at += m
     return o, bound
 
@@ -241,6 +243,17 @@ def test_masked_by_log_degrees(kind):
     c.logdeg[at(slice(800, 900))] = 0
     out = check(c, [200], 4)
     assert (out[:100] == 0).all()
+
+
+@pytest.mark.parametrize("keys,values", [((60, 126), (127, 250)), ((0, 3), (20, 60)), ((120, 128), (2, 240)), ((127, 129), (1, 9))])
+def test_scales_far_apart(keys, values):
+    """Groups' powers of two over all of their range; unpacking is exact."""
+    c = Cache([700], 2, 64, "quantized", seed=keys[1])
+    g = torch.Generator(DEV).manual_seed(values[0])
+    for x, (a, b) in zip(c.scales, (keys, values)):
+        x.copy_(torch.where(c.held[..., None], torch.randint(a, b, x.shape, generator=g, device=DEV), 255))
+    c.logdeg = c.logdeg.clamp(max=2.0)                                    # (sums of weights times 2^125 stay numbers)
+    check(c, [90], 4)
 
 
 @pytest.mark.parametrize("kind", KINDS)
