@@ -20,7 +20,7 @@
 // An item with one tile only (single tokens, short chunks) uses the second set for every other step of slots: two softmax
 // states of the same rows, joined at the end.  Otherwise such an item would wait for its softmax at every step.
 //
-// Sharing the work.  All items' lengths (slots + kItemCost each) are laid end to end, in the order (sequence, KV head, tile
+// Sharing the work.  All items' lengths (slots, three quarters of them where there is one tile, + kItemCost each) are laid end to end, in the order (sequence, KV head, tile
 // pair), and every CTA takes an equal stretch, wherever it begins and ends, so a ragged batch, few rows over a long cache and
 // many rows are all balanced to a step.  (Of one large chunk, whole items are dealt first: see there.)  Each CTA finds its stretch
 // by itself from lengths on the device: the sum over a sequence's items is an arithmetic series.  A piece that is not a whole item leaves (O, m, sum) in the workspace, and extend_join_kernel
@@ -65,7 +65,7 @@ template <bool QUANT> constexpr int kESoftmaxRegs = QUANT ? 160 : 216;
 template <bool QUANT> constexpr int kEOtherRegs = QUANT ? 64 : 72;
 constexpr int kEUnpackRegs = 48, kEUnpackWarps = 8;
 constexpr int kItemCost = 320;      // what an item costs beside its slots (queries in, rows out), in slots (eight prompts: 124 us, with 128 142)
-constexpr int kMinShare = 256;      // slots that a CTA takes at least (17 tokens over 4113 slots: 19.8 us, with 512 21.1, with 1024 25.2)
+constexpr int kMinShare = 256;      // slots that a CTA takes at least (17 tokens over 4113 slots: 20.4 us, with 192 21.7, with 512 22.1)
 constexpr float kSlack = 8.f;       // weights below 2^8
 constexpr int kMaxStarts = 220;     // CTAs whose stretches' begins fit beside the sums
 constexpr int kPartRow = 132;       // floats of a partial row: O, m, sum, pad; a piece's rows lie side by side, four floats of each
@@ -113,6 +113,7 @@ struct ExtendPiece {
 };
 
 // One sequence's part of the work
+template <bool DEAL>
 struct ExtendSeq {
   int64_t row0;   // first of its rows of q
   int32_t n;      // new tokens
@@ -120,18 +121,24 @@ struct ExtendSeq {
   __device__ __forceinline__ int items(int T2) const { return (n + T2 - 1) / T2; }
   // slots that item j's last token sees
   __device__ __forceinline__ int end(int j, int T2) const { return max(0, len - n + min((j + 1) * T2, n)); }
+  // Whether item j has one tile of rows (only a sequence's last may), and what its slots then count: a step of it takes 1.4 us next to 2.0,
+  // over four-bit pages 1.7 next to 2.3 (four chunks among twelve single tokens: 380 us, counted alike 395).
+  // A sequence whose items are dealt has too few of them to matter.
+  __device__ __forceinline__ bool one(int j, int T2) const { return n - j * T2 <= T2 / 2; }
+  __host__ __device__ __forceinline__ static constexpr int weigh(int slots, bool one) { return one && !DEAL ? slots - slots / 4 : slots; }
   // cost of items 0 .. m - 1 of one head
   __device__ __forceinline__ int64_t before(int m, int T2) const {
     const int base = len - n, last = items(T2) - 1;
     const int j0 = base >= 0 ? 0 : -base / T2, e = max(min(m, last), j0);
     int64_t c = (int64_t)m * kItemCost + (int64_t)(e - j0) * base + (int64_t)T2 * (((int64_t)e * (e + 1) - (int64_t)j0 * (j0 + 1)) / 2);
-    if (m > last) c += len;
+    if (m > last) c += weigh(len, one(last, T2));
     return c;
   }
 };
 
-__device__ __forceinline__ ExtendSeq extend_seq(const ExtendArgs& a, int b) {
-  ExtendSeq s;
+template <bool DEAL>
+__device__ __forceinline__ ExtendSeq<DEAL> extend_seq(const ExtendArgs& a, int b) {
+  ExtendSeq<DEAL> s;
   const int64_t r0 = min(max(a.q_begin[b], (int64_t)0), a.n_rows), r1 = min(max(a.q_begin[b + 1], r0), a.n_rows);
   s.row0 = r0;
   s.n = (int32_t)(r1 - r0);
@@ -155,7 +162,7 @@ struct __align__(16) Piece {
 template <bool DEAL>
 struct Walk {
   int64_t left, x;  // what is left of the stretch; offset in the item
-  ExtendSeq s;
+  ExtendSeq<DEAL> s;
   int b, h, j;
   int dealt, item;  // whole items that come before the stretch (one sequence only), and the next of them
   // the next piece that has something to do
@@ -165,8 +172,13 @@ struct Walk {
       const bool deal = DEAL && dealt > 0;
       const int items = s.items(T2), at_h = deal ? item / items : h, at_j = deal ? item - at_h * items : j;
       const int end = s.end(at_j, T2), steps = (end + kEN - 1) / kEN;
-      const int64_t cost = (int64_t)end + kItemCost, from = deal ? 0 : x, to = deal ? cost : min(x + left, cost);
-      auto step_of = [&](int64_t y) { return (int)min(max(y - kItemCost + kEN / 2, (int64_t)0) / kEN, (int64_t)steps); };
+      const bool one = s.one(at_j, T2);
+      const int64_t cost = (int64_t)s.weigh(end, one) + kItemCost, from = deal ? 0 : x, to = deal ? cost : min(x + left, cost);
+      auto step_of = [&](int64_t y) {
+        const uint32_t z = (uint32_t)max(y - kItemCost, (int64_t)0);
+        constexpr uint32_t S2 = kEN, S1 = ExtendSeq<DEAL>::weigh(kEN, true);
+        return (int)min(one ? (z + S1 / 2) / S1 : (z + S2 / 2) / S2, (uint32_t)steps);
+      };
       const bool ends = to == cost;
       p.lo = step_of(from);
       p.hi = ends ? steps : step_of(to);
@@ -175,7 +187,7 @@ struct Walk {
       p.ntok = min(T2, s.n - at_j * T2);
       p.base = s.len - s.n + at_j * T2;
       p.end = end;
-      p.flags = (p.ntok <= a.T ? kOneTile : 0) | (p.lo == 0 && p.hi == steps ? kWhole : 0) | (from == 0 ? kFirst : 0);
+      p.flags = (one ? kOneTile : 0) | (p.lo == 0 && p.hi == steps ? kWhole : 0) | (from == 0 ? kFirst : 0);
       p.seq = b;
       if (deal) {
         --dealt;
@@ -192,7 +204,7 @@ struct Walk {
               s.n = 0;
               while (left > 0 && s.n == 0) {  // (what is left belongs to a later sequence)
                 if (++b < a.Bz)
-                  s = extend_seq(a, b);
+                  s = extend_seq<DEAL>(a, b);
                 else
                   left = 0;
               }
@@ -481,7 +493,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
   const int per = (a.Bz + kThreads - 1) / kThreads, q0 = min(a.Bz, tid * per), q1 = min(a.Bz, q0 + per);
   int64_t mine = 0;
   for (int b = q0; b < q1; ++b) {
-    const ExtendSeq s = extend_seq(a, b);
+    const ExtendSeq<DEAL> s = extend_seq<DEAL>(a, b);
     if (s.n > 0) mine += s.before(s.items(T2), T2) * a.H;
   }
   int64_t upto = mine;
@@ -505,7 +517,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
   // 32768 slots: 0.4 GB from memory in place of 1.9).
   int dealt = 0;
   if (DEAL && total > 0) {
-    const ExtendSeq s = extend_seq(a, 0);
+    const ExtendSeq<DEAL> s = extend_seq<DEAL>(a, 0);
     const int items = s.items(T2), n = (int)gridDim.x;
     const int64_t of_head = s.before(items, T2);
     dealt = (int)min(total / n / (of_head - s.before(items - 1, T2)), (int64_t)items * a.H / n);  // (the last item of a head is the longest)
@@ -541,7 +553,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
   }
   if ((!DEAL || dealt == 0) && left > 0 && begin >= at && begin < at + mine) {
     for (int b = q0; b < q1; ++b) {
-      const ExtendSeq s = extend_seq(a, b);
+      const ExtendSeq<DEAL> s = extend_seq<DEAL>(a, b);
       if (s.n == 0) continue;
       const int64_t c = s.before(s.items(T2), T2) * a.H;
       if (begin < at + c) {
@@ -628,7 +640,7 @@ __global__ void __launch_bounds__(kEWarps<QUANT> * 32, 1) extend_kernel(const __
     // ---------------------------------------------------------------- TMA, and the walk along the stretch
     Walk<DEAL> walk;
     walk.b = (int)s_start[1];
-    walk.s = extend_seq(a, walk.b);
+    walk.s = extend_seq<DEAL>(a, walk.b);
     walk.left = left;
     walk.dealt = dealt;
     walk.item = (int)blockIdx.x;
